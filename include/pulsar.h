@@ -416,6 +416,156 @@ int pulsar_phase2_query_noalloc(const void* q, const void* Kg, const void* Vg, i
                                 void* stream);
 
 /*
+ * Visibility of a tree of T drafted tokens (several continuations tried at
+ * once, as in speculative decoding), for pulsar_phase2_tree and
+ * pulsar_phase2_sparse.  One call serves every layer of a step.
+ *
+ * parent  int32 [T]: parent[t] < t is the draft that token t follows, -1 the
+ *         last token before the drafts.  Any other value says that t is no
+ *         token, and so is every t whose parent is none (a draft padded to a
+ *         fixed size): nothing reads beyond the array because of it.
+ * mask    out uint32 [T, ceil(T / 32)]: bit j % 32 of word j / 32 of row t is
+ *         set where token t sees draft j, that is for t and its ancestors; no
+ *         bit of a row that is no token.
+ * depth   out int32 [T], nullable: the number of ancestors of t, so that its
+ *         position is that of the last token before the drafts + 1 + depth;
+ *         -1 for a row that is no token.
+ * EINVAL: T < 0, NULL parent or mask when T > 0.  EUNSUPPORTED: T > 16384.
+ */
+int pulsar_tree_mask(const int32_t* parent, int T, uint32_t* mask, int32_t* depth, void* stream);
+
+/*
+ * Phase-2 attention of a tree of drafted tokens.  As pulsar_phase2_query, but
+ * new token t attends to all retained shards, to the G earlier appended rows
+ * and to those of the Tq new tokens' rows whose bit of mask[t] is set (its own
+ * only if its bit is).  A token that sees no key at all gives o = 0 and
+ * lse = -inf.  Rows of the new tokens that t does not see are not read for it:
+ * what they hold, NaN and infinities included, cannot reach its output.
+ *
+ * The partials of the shards and the G rows are those of pulsar_phase2_query;
+ * the merge folds each token's own branch in, in fp32.
+ *
+ * q, Kg, Vg, G, K, V, lse  as for pulsar_phase2_query (row G + t of Kg and Vg
+ *           is token t's own); K and V 16-byte aligned.
+ * mask      uint32 [Tq, ceil(Tq / 32)] as written by pulsar_tree_mask, or any
+ *           other visibility; bits from Tq on are ignored.
+ * o         out [Tq, Hq, d], float32 or bf16 (the fp32 result rounded once)
+ *           per o_dtype.
+ * workspace device buffer of at least pulsar_phase2_tree_workspace_bytes bytes,
+ *           16-byte aligned; contents on entry do not matter; may be NULL where
+ *           there is neither a shard's key nor an appended row.  As for
+ *           pulsar_phase2_query the size never drops when n_shards, Tq, S or G
+ *           grows.
+ * Errors: as pulsar_phase2_query, plus EINVAL for an unknown o_dtype or a NULL
+ *         mask when Tq > 0.
+ */
+size_t pulsar_phase2_tree_workspace_bytes(int n_shards, int Tq, int64_t S, int64_t G, int Hq,
+                                          int Hkv, int d);
+int pulsar_phase2_tree(const void* q, const void* Kg, const void* Vg, int64_t G,
+                       const uint32_t* mask, const void* K, const void* V, int n_shards, int Tq,
+                       int64_t S, int Hq, int Hkv, int d, float softmax_scale, void* o, int o_dtype,
+                       float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Rows of a generation shard that are kept (the accepted path of a draft, or the
+ * rows that a policy keeps), moved to its front, in place, in K and V of every
+ * layer: row G + keep[j] becomes row G + j.  All other rows stay as they are.
+ *
+ * K, V    bf16 [layers, capacity, Hkv, d], 16-byte aligned; not the same memory.
+ * keep    int32 [n], rising, each in [0, capacity - G).  The list ends at the
+ *         first entry that is negative, not above the one before it, or past
+ *         the cache: the number of rows that a step accepts may stay on the
+ *         device, in a list filled up with -1.
+ * EINVAL: negative sizes, Hkv < 1 or d < 1, G > capacity, n > capacity - G, NULL
+ *         or misaligned pointers when there is work.  EUNSUPPORTED: Hkv * d not
+ *         a multiple of 8, or a row or a layer set beyond 32-bit counts.
+ */
+int pulsar_kv_compact(void* K, void* V, int layers, int64_t capacity, int Hkv, int d, int64_t G,
+                      const int32_t* keep, int n, void* stream);
+
+/*
+ * Channel bounds of every block of a retained shard's keys, from which
+ * pulsar_block_select scores the blocks.  Block b of a shard is its rows
+ * [b * block, min((b + 1) * block, S)).
+ *
+ * K       bf16 [n_shards, S, Hkv, d], 16-byte aligned.
+ * block   16, 32, 64, 128 or 256 keys.
+ * bounds  out bf16 [n_shards, Hkv, ceil(S / block), 2, d], 16-byte aligned: the
+ *         smallest (0) and the largest (1) value of each channel over the
+ *         block's keys; NaN where a key's is NaN.
+ * EINVAL: negative sizes, Hkv < 1, d < 1, block < 1, NULL or misaligned pointers
+ *         when there is work.
+ * EUNSUPPORTED: d not in {64, 128}, another block, S >= 2^31.
+ */
+int pulsar_key_bounds(const void* K, int n_shards, int64_t S, int Hkv, int d, int block,
+                      void* bounds, void* stream);
+
+/*
+ * The topk blocks of each shard that a token may profit most from, for every
+ * token and KV head.  The score of block b for token t and KV head g is the
+ * largest q . k that a key within the block's bounds can have for any of the
+ * heads that read g:
+ *   max over h of sum_i max(q_thi lo_bi, q_thi hi_bi),
+ * formed in fp64 and rounded once to fp32.  Blocks rank by the fp32 score, then
+ * by the lower index; a score that is not a number, as a bound that is not
+ * finite gives, counts as +inf.
+ *
+ * q         bf16 [Tq, Hq, d], 16-byte aligned.
+ * bounds    bf16 [n_shards, Hkv, blocks, 2, d] as written by pulsar_key_bounds.
+ * sel       out int32 [n_shards, Tq, Hkv, topk]: block indices, ascending.
+ * scores    out float [n_shards, Tq, Hkv, blocks], nullable.
+ * workspace device buffer of at least pulsar_block_select_workspace_bytes
+ *           bytes, 16-byte aligned (may be NULL when scores is given); contents
+ *           on entry do not matter.
+ * EINVAL: negative sizes, Hq % Hkv != 0, topk > blocks, NULL or misaligned
+ *         pointers when there is work.  EWORKSPACE: workspace too small.
+ * EUNSUPPORTED: d not in {64, 128}; blocks > 32768; n_shards * Hkv > 65535;
+ *         Tq > 524280 or n_shards * Tq * Hkv >= 2^31.
+ */
+size_t pulsar_block_select_workspace_bytes(int n_shards, int Tq, int blocks, int Hkv);
+int pulsar_block_select(const void* q, const void* bounds, int n_shards, int Tq, int blocks, int Hq,
+                        int Hkv, int d, int topk, int32_t* sel, float* scores, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/*
+ * Phase-2 attention of new tokens over selected blocks of the retained shards:
+ * as pulsar_phase2_query, but of each shard token t reads, for KV head g, the
+ * topk blocks listed in sel alone.  With every block listed it computes what
+ * pulsar_phase2_query does.
+ *
+ * q         bf16 [Tq, Hq, d].
+ * K, V      bf16 [n_shards, S, Hkv, d] (nullable when n_shards, S or topk is 0);
+ *           a shard may exceed 2 GiB.
+ * sel       int32 [n_shards, Tq, Hkv, topk], as written by pulsar_block_select,
+ *           in any order.  An entry outside [0, ceil(S / block)) lists no block
+ *           (a list filled up with -1); a block that is listed twice counts
+ *           twice.
+ * block     as for pulsar_key_bounds.
+ * Kg, Vg, G the generation shard, as for pulsar_phase2_query; both NULL (and
+ *           G = 0) where another host has it: then the result is the partial
+ *           (o, lse) of these shards, for pulsar_lse_merge.
+ * mask      NULL: token t sees the appended rows up to G + t, its own.  Else as
+ *           for pulsar_phase2_tree.
+ * o, lse    as for pulsar_phase2_tree; a token that sees no key gives 0, -inf.
+ *           Rows that a token does not see cannot reach its output.
+ * workspace device buffer of at least pulsar_phase2_sparse_workspace_bytes
+ *           bytes, 16-byte aligned (may be NULL when that is 0); contents on
+ *           entry do not matter.  The size holds for any number of tokens up to
+ *           Tq and for any shards, lists and appended rows.
+ * EINVAL: negative sizes, Hq % Hkv != 0, NULL or misaligned pointers when there
+ *         is work, only one of Kg and Vg, a mask or G > 0 without them, scale
+ *         not finite and > 0, unknown o_dtype.  EWORKSPACE: workspace too small.
+ * EUNSUPPORTED: d not in {64, 128}; another block; S >= 2^31; G + Tq >= 2^24;
+ *         2^30 listed keys or more; a row of K of 16 MiB or more.
+ */
+size_t pulsar_phase2_sparse_workspace_bytes(int Tq, int Hq, int Hkv, int d);
+int pulsar_phase2_sparse(const void* q, const void* K, const void* V, const int32_t* sel,
+                         int n_shards, int Tq, int64_t S, int block, int topk, const void* Kg,
+                         const void* Vg, int64_t G, const uint32_t* mask, int Hq, int Hkv, int d,
+                         float softmax_scale, void* o, int o_dtype, float* lse, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/*
  * Rotary position embedding of query or key rows at given positions
  * (Appendix "RoPE Position ID Assignment").  In the paper's sparse mode every
  * token keeps its global position id, so rotating a layer's Q and K of the

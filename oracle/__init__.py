@@ -32,7 +32,11 @@ Modules, each following the paper's definitions in its own notation:
                    exact scores rounded once to fp32, and the Even-Spaced
                    token offsets (Appendix "Scoring Heuristic Details").
 
+* ``blocks``    -- drafted tokens and block-sparse reads in Phase 2: visibility of a
+                   tree, attention with key multiplicities, block bounds,
+                   scores and selection, compaction of kept rows.
+
 Readings of points the paper leaves open are listed in each function's
 docstring.
 """
-from . import assembly, attention, cost, maxidf, rope, scorers  # noqa: F401
+from . import assembly, attention, blocks, cost, maxidf, rope, scorers  # noqa: F401

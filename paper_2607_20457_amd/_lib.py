@@ -44,6 +44,22 @@ SIGNATURES = {
     "pulsar_phase2_query_noalloc": (_c_int, [_vp, _vp, _vp, _c_i64, _vp, _vp, _c_int, _c_int,
                                              _c_i64, _c_int, _c_int, _c_int, _c_float, _vp, _vp,
                                              _vp]),
+    "pulsar_tree_mask": (_c_int, [_vp, _c_int, _vp, _vp, _vp]),
+    "pulsar_phase2_tree_workspace_bytes": (_c_size, [_c_int, _c_int, _c_i64, _c_i64, _c_int,
+                                                      _c_int, _c_int]),
+    "pulsar_phase2_tree": (_c_int, [_vp, _vp, _vp, _c_i64, _vp, _vp, _vp, _c_int, _c_int, _c_i64,
+                                    _c_int, _c_int, _c_int, _c_float, _vp, _c_int, _vp, _vp,
+                                    _c_size, _vp]),
+    "pulsar_kv_compact": (_c_int, [_vp, _vp, _c_int, _c_i64, _c_int, _c_int, _c_i64, _vp, _c_int,
+                                   _vp]),
+    "pulsar_key_bounds": (_c_int, [_vp, _c_int, _c_i64, _c_int, _c_int, _c_int, _vp, _vp]),
+    "pulsar_block_select_workspace_bytes": (_c_size, [_c_int, _c_int, _c_int, _c_int]),
+    "pulsar_block_select": (_c_int, [_vp, _vp, _c_int, _c_int, _c_int, _c_int, _c_int, _c_int,
+                                     _c_int, _vp, _vp, _vp, _c_size, _vp]),
+    "pulsar_phase2_sparse_workspace_bytes": (_c_size, [_c_int, _c_int, _c_int, _c_int]),
+    "pulsar_phase2_sparse": (_c_int, [_vp, _vp, _vp, _vp, _c_int, _c_int, _c_i64, _c_int, _c_int,
+                                      _vp, _vp, _c_i64, _vp, _c_int, _c_int, _c_int, _c_float,
+                                      _vp, _c_int, _vp, _vp, _c_size, _vp]),
     "pulsar_rope": (_c_int, [_vp, _c_int, _c_i64, _c_int, _c_int, _vp, _c_i64, _vp,
                              ctypes.c_double, _vp]),
 }

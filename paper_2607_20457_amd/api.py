@@ -328,3 +328,200 @@ def phase2_query_noalloc(q, Kg, Vg, G: int, K=None, V=None, softmax_scale: float
                                                 _ptr(lse), _stream())
     _lib.check(st, "pulsar_phase2_query_noalloc")
     return o, lse
+
+
+def _here(*tensors):
+    """The tensors lie on the current device, whose current stream the call uses."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("tensors must be on the current device")
+
+
+def _generation(Kg, Vg, G, Tq, Hkv, d):
+    _need(Kg, torch.bfloat16, "Kg")
+    _need(Vg, torch.bfloat16, "Vg")
+    if G < 0 or Kg.shape != (G + Tq, Hkv, d) or Vg.shape != Kg.shape:
+        raise ValueError("Kg/Vg must be [G + Tq, Hkv, d]")
+
+
+def _need_mask(mask, Tq):
+    _need(mask, torch.int32, "mask")
+    if mask.shape != (Tq, (Tq + 31) // 32):
+        raise ValueError("mask must be [Tq, ceil(Tq / 32)]")
+
+
+def _out(q, o_dtype):
+    if o_dtype not in (OUT_F32, OUT_BF16):
+        raise ValueError("o_dtype must be OUT_F32 or OUT_BF16")
+    return q.new_empty(q.shape, dtype=torch.bfloat16 if o_dtype == OUT_BF16 else torch.float32)
+
+
+def _scratch(workspace, need, like):
+    """The caller's workspace where it is large enough, else a new one."""
+    if workspace is not None:
+        _need(workspace, workspace.dtype, "workspace")
+        if workspace.numel() * workspace.element_size() >= need:
+            return workspace
+    return like.new_empty(need, dtype=torch.uint8) if need else None
+
+
+def tree_mask(parent):
+    """Visibility of a tree of drafted tokens.  parent int32 [T]: the earlier
+    draft that each follows, -1 for the last token before them (any other value:
+    no token) -> (mask int32 [T, ceil(T / 32)], each token's bits set for itself
+    and its ancestors; depth int32 [T], its number of ancestors, -1 for none)."""
+    _need(parent, torch.int32, "parent")
+    if parent.dim() != 1:
+        raise ValueError("parent must be [T]")
+    _here(parent)
+    T = parent.shape[0]
+    mask = parent.new_empty((T, (T + 31) // 32))
+    depth = parent.new_empty((T,))
+    st = _lib.lib().pulsar_tree_mask(_ptr(parent), T, _ptr(mask), _ptr(depth), _stream())
+    _lib.check(st, "pulsar_tree_mask")
+    return mask, depth
+
+
+def phase2_tree_workspace_bytes(n_shards: int, Tq: int, S: int, G: int, Hq: int, Hkv: int,
+                                d: int) -> int:
+    return int(_lib.lib().pulsar_phase2_tree_workspace_bytes(n_shards, Tq, S, G, Hq, Hkv, d))
+
+
+def phase2_tree(q, Kg, Vg, G: int, mask, K=None, V=None, softmax_scale: float | None = None,
+                o_dtype: int = OUT_F32, workspace=None):
+    """Attention of a tree of Tq drafted tokens: q bf16 [Tq, Hq, d] over the
+    retained shards K/V bf16 [n_shards, S, Hkv, d] (or None), the G earlier rows
+    of the generation shard Kg/Vg bf16 [G + Tq, Hkv, d], and those of the drafts'
+    own rows that mask int32 [Tq, ceil(Tq / 32)] (``tree_mask``) sets for each
+    -> (o [Tq, Hq, d] per o_dtype, lse f32 [Hq, Tq])."""
+    _need(q, torch.bfloat16, "q")
+    Tq, Hq, d = q.shape
+    Hkv = Kg.shape[1]
+    _generation(Kg, Vg, G, Tq, Hkv, d)
+    _need_mask(mask, Tq)
+    n_shards, S = 0, 0
+    if K is not None:
+        _need(K, torch.bfloat16, "K")
+        _need(V, torch.bfloat16, "V")
+        n_shards, S = K.shape[0], K.shape[1]
+        if K.shape != (n_shards, S, Hkv, d) or V.shape != K.shape:
+            raise ValueError("K/V must be [n_shards, S, Hkv, d]")
+    scale = 1.0 / math.sqrt(d) if softmax_scale is None else softmax_scale
+    o = _out(q, o_dtype)
+    lse = q.new_empty((Hq, Tq), dtype=torch.float32)
+    lib = _lib.lib()
+    need = lib.pulsar_phase2_tree_workspace_bytes(n_shards, Tq, S, G, Hq, Hkv, d)
+    workspace = _scratch(workspace, need, q)
+    _here(q, Kg, Vg, mask, K, V, workspace)
+    st = lib.pulsar_phase2_tree(_ptr(q), _ptr(Kg), _ptr(Vg), G, _ptr(mask), _ptr(K), _ptr(V),
+                                n_shards, Tq, S, Hq, Hkv, d, scale, _ptr(o), o_dtype, _ptr(lse),
+                                _ptr(workspace), need, _stream())
+    _lib.check(st, "pulsar_phase2_tree")
+    return o, lse
+
+
+def kv_compact_(K, V, G: int, keep):
+    """Rows G + keep[j] of every layer of K/V bf16 [layers, capacity, Hkv, d]
+    moved to row G + j, in place.  keep int32 [n], rising; it ends at the first
+    entry that is negative, does not rise or lies past the cache.  Returns K, V."""
+    _need(K, torch.bfloat16, "K")
+    _need(V, torch.bfloat16, "V")
+    _need(keep, torch.int32, "keep")
+    if K.dim() != 4 or V.shape != K.shape or keep.dim() != 1:
+        raise ValueError("K/V must be [layers, capacity, Hkv, d], keep [n]")
+    if K.data_ptr() == V.data_ptr() and K.numel() > 0:
+        raise ValueError("K and V must not be the same memory")
+    _here(K, V, keep)
+    layers, capacity, Hkv, d = K.shape
+    st = _lib.lib().pulsar_kv_compact(_ptr(K), _ptr(V), layers, capacity, Hkv, d, G, _ptr(keep),
+                                      keep.shape[0], _stream())
+    _lib.check(st, "pulsar_kv_compact")
+    return K, V
+
+
+def key_bounds(K, block: int):
+    """Channel minima and maxima of every block of `block` keys (16, 32, 64, 128
+    or 256).  K bf16 [n_shards, S, Hkv, d] -> bounds bf16 [n_shards, Hkv,
+    ceil(S / block), 2, d]."""
+    _need(K, torch.bfloat16, "K")
+    _here(K)
+    n_shards, S, Hkv, d = K.shape
+    blocks = -(-S // block) if block > 0 else 0
+    bounds = K.new_empty((n_shards, Hkv, blocks, 2, d))
+    st = _lib.lib().pulsar_key_bounds(_ptr(K), n_shards, S, Hkv, d, block, _ptr(bounds), _stream())
+    _lib.check(st, "pulsar_key_bounds")
+    return bounds
+
+
+def block_select_workspace_bytes(n_shards: int, Tq: int, blocks: int, Hkv: int) -> int:
+    return int(_lib.lib().pulsar_block_select_workspace_bytes(n_shards, Tq, blocks, Hkv))
+
+
+def block_select(q, bounds, topk: int, return_scores: bool = False, workspace=None):
+    """The topk blocks of each shard for every token and KV head, by the largest
+    q . k that their bounds allow.  q bf16 [Tq, Hq, d], bounds as ``key_bounds``
+    returns them -> sel int32 [n_shards, Tq, Hkv, topk], ascending (+ the scores
+    f32 [n_shards, Tq, Hkv, blocks])."""
+    _need(q, torch.bfloat16, "q")
+    _need(bounds, torch.bfloat16, "bounds")
+    Tq, Hq, d = q.shape
+    n_shards, Hkv, blocks, two, db = bounds.shape
+    if two != 2 or db != d:
+        raise ValueError("bounds must be [n_shards, Hkv, blocks, 2, d]")
+    sel = q.new_empty((n_shards, Tq, Hkv, max(topk, 0)), dtype=torch.int32)
+    lib = _lib.lib()
+    scores, need = None, 0
+    if return_scores:
+        scores = q.new_empty((n_shards, Tq, Hkv, blocks), dtype=torch.float32)
+    else:
+        need = lib.pulsar_block_select_workspace_bytes(n_shards, Tq, blocks, Hkv)
+        workspace = _scratch(workspace, need, q)
+    _here(q, bounds, workspace)
+    st = lib.pulsar_block_select(_ptr(q), _ptr(bounds), n_shards, Tq, blocks, Hq, Hkv, d, topk,
+                                 _ptr(sel), _ptr(scores), _ptr(workspace), need, _stream())
+    _lib.check(st, "pulsar_block_select")
+    return (sel, scores) if return_scores else sel
+
+
+def phase2_sparse_workspace_bytes(Tq: int, Hq: int, Hkv: int, d: int) -> int:
+    return int(_lib.lib().pulsar_phase2_sparse_workspace_bytes(Tq, Hq, Hkv, d))
+
+
+def phase2_sparse(q, K, V, sel, block: int, Kg=None, Vg=None, G: int = 0, mask=None,
+                  softmax_scale: float | None = None, o_dtype: int = OUT_F32, workspace=None):
+    """Attention of Tq new tokens over their selected blocks of the retained
+    shards and over the generation shard: q bf16 [Tq, Hq, d], K/V bf16 [n_shards,
+    S, Hkv, d], sel int32 [n_shards, Tq, Hkv, topk] (``block_select``; an entry
+    that is no block of the shard lists none), Kg/Vg bf16 [G + Tq, Hkv, d] (None:
+    the shards alone) up to each token itself, or by a tree's mask
+    -> (o [Tq, Hq, d] per o_dtype, lse f32 [Hq, Tq])."""
+    _need(q, torch.bfloat16, "q")
+    _need(K, torch.bfloat16, "K")
+    _need(V, torch.bfloat16, "V")
+    _need(sel, torch.int32, "sel")
+    Tq, Hq, d = q.shape
+    n_shards, S, Hkv, dk = K.shape
+    if dk != d or V.shape != K.shape:
+        raise ValueError("K/V must be [n_shards, S, Hkv, d]")
+    if sel.dim() != 4 or sel.shape[:3] != (n_shards, Tq, Hkv):
+        raise ValueError("sel must be [n_shards, Tq, Hkv, topk]")
+    if (Kg is None) != (Vg is None):
+        raise ValueError("Kg and Vg go together")
+    if Kg is not None:
+        _generation(Kg, Vg, G, Tq, Hkv, d)
+    if mask is not None:
+        _need_mask(mask, Tq)
+    scale = 1.0 / math.sqrt(d) if softmax_scale is None else softmax_scale
+    o = _out(q, o_dtype)
+    lse = q.new_empty((Hq, Tq), dtype=torch.float32)
+    lib = _lib.lib()
+    need = lib.pulsar_phase2_sparse_workspace_bytes(Tq, Hq, Hkv, d)
+    workspace = _scratch(workspace, need, q)
+    _here(q, K, V, sel, Kg, Vg, mask, workspace)
+    st = lib.pulsar_phase2_sparse(_ptr(q), _ptr(K), _ptr(V), _ptr(sel), n_shards, Tq, S, block,
+                                  sel.shape[3], _ptr(Kg), _ptr(Vg), G, _ptr(mask), Hq, Hkv, d,
+                                  scale, _ptr(o), o_dtype, _ptr(lse), _ptr(workspace), need,
+                                  _stream())
+    _lib.check(st, "pulsar_phase2_sparse")
+    return o, lse

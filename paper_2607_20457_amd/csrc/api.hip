@@ -8,9 +8,8 @@
 
 namespace {
 
-constexpr int kVersion = 5;
+constexpr int kVersion = 6;
 
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline bool is_pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
 
 // Shape checks shared by the Phase-1 calls (Eq. 3 row counts).
@@ -499,6 +498,43 @@ QueryPlan query_plan(int n_shards, int Tq, int64_t S, int64_t G, int Hq, int Hkv
   return p;
 }
 
+// The plan of a draft: the shards and the G appended rows, all visible to every
+// token, in partials; the drafts' own rows are folded into the merge.  In each
+// kernel the ranges are those of a query step over G rows, so the query step's
+// workspace of the same sizes holds them.
+QueryPlan tree_plan(int n_shards, int Tq, int64_t S, int64_t G, int Hq, int Hkv, int d) {
+  QueryPlan p{};
+  if (S <= 0) n_shards = 0;
+  p.gen_own = true;
+  p.decode = decode_applies(Tq, Hq, Hkv, d);
+  p.packed = !p.decode && packed_applies(Tq, Hq, Hkv, d);
+  if (p.packed) {
+    p.np_shard = packed_parts(n_shards, S, Hkv);
+    const int64_t ranges = (int64_t)n_shards * p.np_shard;
+    const int64_t len = n_shards > 0 ? (S + p.np_shard - 1) / p.np_shard : 0;
+    p.np_gen = G > 0 ? packed_parts(1, G, Hkv, (int)std::max<int64_t>(len, kPackedMinKeys)) : 0;
+    p.gen_own = ranges == 0 || (ranges + p.np_gen) * Hkv <= 256;
+    if (!p.gen_own)
+      p.np_gen = (int)std::min<int64_t>(ranges, (G + kPackedMinKeys - 1) / kPackedMinKeys);
+    p.parts = (int)ranges + (p.gen_own ? p.np_gen : 0);
+    return p;
+  }
+  const int rows = Tq * (Hq / Hkv);
+  p.gen_decode = p.decode || (Hq / Hkv <= 32 && G <= kGenDecodeRows && rows <= kGenDecodeQueryRows);
+  int min_keys = kDecodeMinKeys;
+  if (p.decode) {
+    p.np_shard = decode_shard_parts(n_shards, Tq, S, Hq, Hkv, d, true);
+    min_keys = std::max(min_keys, decode_min_keys(rows));
+  } else {
+    p.np_shard = n_shards > 0 ? attn_splits(n_shards, Tq, S, Hq, Hkv) : 0;
+  }
+  if (G > 0)
+    p.np_gen = p.gen_decode ? decode_parts(1, G, Hkv, gen_min_keys(rows, G, min_keys))
+                            : attn_splits(1, Tq, G, Hq, Hkv);
+  p.parts = n_shards * p.np_shard + p.np_gen;
+  return p;
+}
+
 // The most ranges of a generation shard of up to `rows` rows in a decode launch.
 int64_t gen_ranges_most(int query_rows, int64_t rows, int Hkv, int min_keys) {
   const int64_t cap = query_rows <= kDecodeRows ? (1023 + query_rows) / query_rows : 16;
@@ -764,6 +800,64 @@ int pulsar_phase2_query_noalloc(const void* q, const void* Kg, const void* Vg, i
   if (st != PULSAR_OK) return st;
   return phase2_query_run(plan, q, Kg, Vg, G, K, V, n_shards, Tq, S, Hq, Hkv, d, softmax_scale, o,
                           lse, ws, stream);
+}
+
+size_t pulsar_phase2_tree_workspace_bytes(int n_shards, int Tq, int64_t S, int64_t G, int Hq,
+                                          int Hkv, int d) {
+  return pulsar_phase2_query_workspace_bytes(n_shards, Tq, S, G, Hq, Hkv, d);
+}
+
+int pulsar_phase2_tree(const void* q, const void* Kg, const void* Vg, int64_t G,
+                       const uint32_t* mask, const void* K, const void* V, int n_shards, int Tq,
+                       int64_t S, int Hq, int Hkv, int d, float softmax_scale, void* o, int o_dtype,
+                       float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  const int chk = phase2_query_check(q, Kg, Vg, G, K, V, n_shards, Tq, S, Hq, Hkv, d,
+                                     softmax_scale, static_cast<const float*>(o));
+  if (chk != PULSAR_OK) return chk;
+  if (o_dtype != PULSAR_OUT_F32 && o_dtype != PULSAR_OUT_BF16) return PULSAR_EINVAL;
+  if (Tq == 0) return PULSAR_OK;
+  if (mask == nullptr) return PULSAR_EINVAL;
+  if (n_shards > 0 && S > 0 && (!aligned16(K) || !aligned16(V))) return PULSAR_EINVAL;
+  if ((int64_t)Tq * Hq > 0x7fffffff) return PULSAR_EUNSUPPORTED;
+  if (S == 0) n_shards = 0;
+  const QueryPlan plan = tree_plan(n_shards, Tq, S, G, Hq, Hkv, d);
+  if (plan.parts > 0 && (workspace == nullptr || !aligned16(workspace) ||
+                         workspace_bytes < parts_bytes(plan, Tq, Hq, d)))
+    return PULSAR_EWORKSPACE;
+
+  const uint16_t* const q16 = static_cast<const uint16_t*>(q);
+  const uint16_t* const kg = static_cast<const uint16_t*>(Kg);
+  const uint16_t* const vg = static_cast<const uint16_t*>(Vg);
+  const int64_t ostride = (int64_t)Tq * Hq * d, lstride = (int64_t)Hq * Tq;
+  float* po = static_cast<float*>(workspace);
+  float* pl = reinterpret_cast<float*>(static_cast<char*>(workspace) +
+                                       align16((size_t)plan.parts * ostride * 4));
+  hipStream_t const st = (hipStream_t)stream;
+  DecodeGen gen{kg, vg, G, plan.np_gen, plan.gen_own};
+  gen.cached = true;
+  int rc = PULSAR_OK;
+  if (plan.decode || plan.packed) {
+    if (plan.parts > 0)
+      rc = (plan.decode ? launch_decode : launch_packed)(
+          q16, static_cast<const uint16_t*>(K), static_cast<const uint16_t*>(V), n_shards, Tq, S,
+          Hq, Hkv, d, softmax_scale, po, pl, plan.np_shard, st, &gen);
+  } else {
+    const int part = n_shards * plan.np_shard;
+    if (n_shards > 0)
+      rc = launch_split_parts(q, K, V, n_shards, Tq, S, Hq, Hkv, d, softmax_scale, plan.np_shard,
+                              po, pl, st);
+    if (rc == PULSAR_OK && G > 0)
+      rc = plan.gen_decode
+               ? launch_decode(q16, nullptr, nullptr, 0, Tq, 0, Hq, Hkv, d, softmax_scale,
+                               po + part * ostride, pl + part * lstride, 1, st, &gen)
+               : launch_split_parts(q, Kg, Vg, 1, Tq, G, Hq, Hkv, d, softmax_scale, plan.np_gen,
+                                    po + part * ostride, pl + part * lstride, st);
+  }
+  if (rc != PULSAR_OK) return rc;
+  const int64_t row = (int64_t)Hkv * d;
+  const TreeRows tree{q16, kg + G * row, vg + G * row, mask, Hkv, softmax_scale};
+  return launch_tree_merge(po, pl, plan.parts, Tq, Hq, d, tree, o, o_dtype == PULSAR_OUT_BF16, lse,
+                           st);
 }
 
 }  // extern "C"

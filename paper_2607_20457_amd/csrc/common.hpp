@@ -17,6 +17,8 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 #define PULSAR_WAVE 64
 #define PULSAR_LDS_BYTES 163840  // 160 KB local data share per compute unit on gfx950
 
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
 // Row -> global position map of an assembled Phase-1 input (Eq. 3, sparse
 // position ids).  The summary region is a sequence of runs of m consecutive
 // positions, one run per selected chunk; run q = j*k + c starts at
@@ -184,7 +186,14 @@ struct DecodeGen {
   // each range its own partial, after the shards' parts; otherwise (packed
   // kernel only) range i joins the shards' part i
   bool own;
+  // only the rows [0, G), each visible to every token (a draft, whose own rows
+  // launch_tree_merge takes)
+  bool cached = false;
+  int64_t rows(int Tq) const { return cached ? G : G + Tq; }
 };
+// What a token sees past its own row where all rows are visible to it (rows are
+// below 2^24).
+constexpr int kSeesAll = 1 << 28;
 int launch_decode(const uint16_t* q, const uint16_t* K, const uint16_t* V, int n_shards, int Tq,
                   int64_t S, int Hq, int Hkv, int d, float scale, float* o, float* lse,
                   int nparts, hipStream_t stream, const DecodeGen* gen = nullptr);
@@ -246,6 +255,51 @@ int attn_rows_per_wg(int group, bool causal);  // query rows of one attention wo
 int launch_lse_merge(const float* o_parts, const float* lse_parts, int H, int nz, int Tq, int Hq,
                      int d, int64_t part_ostride, int64_t part_lstride, float* o, float* lse,
                      hipStream_t stream);
+// The same of one z into bf16.
+int launch_lse_merge_bf16(const float* o_parts, const float* lse_parts, int H, int Tq, int Hq,
+                          int d, void* o, float* lse, hipStream_t stream);
+
+// The drafted tokens' own rows, for the merge of their partials: rows of Kd / Vd
+// (bf16 [Tq, Hkv, d]), token t seeing those whose bit of mask[t] is set.
+struct TreeRows {
+  const uint16_t* q;  // bf16 [Tq, Hq, d]
+  const uint16_t* Kd;
+  const uint16_t* Vd;
+  const uint32_t* mask;  // [Tq, ceil(Tq / 32)]
+  int Hkv;
+  float scale;
+};
+int launch_tree_mask(const int32_t* parent, int T, uint32_t* mask, int32_t* depth,
+                     hipStream_t stream);
+int launch_tree_merge(const float* o_parts, const float* lse_parts, int H, int Tq, int Hq, int d,
+                      const TreeRows& tree, void* o, int o_bf16, float* lse, hipStream_t stream);
+int launch_kv_compact(void* K, void* V, int layers, int64_t capacity, int64_t row_bytes, int64_t G,
+                      const int32_t* keep, int n, hipStream_t stream);
+
+// Block-sparse reads of the retained shards (blocks.hip, sparse.hip).
+int launch_key_bounds(const uint16_t* K, int n_shards, int64_t S, int Hkv, int d, int block,
+                      uint16_t* bounds, hipStream_t stream);
+constexpr int kMaxSelectBlocks = 32768;  // blocks per shard whose keys fit in LDS
+int launch_block_scores(const uint16_t* q, const uint16_t* bounds, int n_shards, int Tq, int Hq,
+                        int Hkv, int d, int blocks, float* scores, hipStream_t stream);
+int launch_block_topk(const float* scores, int64_t rows, int blocks, int topk, int32_t* sel,
+                      hipStream_t stream);
+struct SparseLaunch {
+  const uint16_t* q;    // bf16 [Tq, Hq, d]
+  const uint16_t* K;    // bf16 [n_shards, S, Hkv, d]
+  const uint16_t* V;
+  const int32_t* sel;   // [n_shards, Tq, Hkv, topk]
+  const uint16_t* Kg;   // bf16 [G + Tq, Hkv, d], or NULL
+  const uint16_t* Vg;
+  const uint32_t* mask; // [Tq, ceil(Tq / 32)], or NULL for index-causal
+  int n_shards, Tq, Hq, Hkv, d, topk, block;
+  int64_t S, G;
+  float scale;
+};
+int sparse_parts(int Tq, int Hq, int Hkv, int64_t keys, int64_t gen_rows);
+int64_t sparse_part_rows_most(int Tq, int Hkv);
+int launch_sparse(const SparseLaunch& a, int parts, void* o, int o_bf16, float* lse,
+                  hipStream_t stream);
 
 // Rows of an assembled Phase-1 input gathered from a per-position tensor and
 // rotated per pos_mode (a pulsar_pos_mode).

@@ -54,6 +54,8 @@ struct DecodeArgs {
   int G;
   int gen_parts;      // its key ranges (0: no generation shard)
   int gen_part_len;
+  int gen_rows;       // G + Tq, or G of a draft
+  int gen_past;       // rows past its own that a token sees: 0, or kSeesAll
   int tile_tokens;    // tokens per 32-row tile, 32 / group
   int row_tiles;      // tiles over the Tq tokens
   float scale_log2;
@@ -97,7 +99,7 @@ void decode_attn_kernel(DecodeArgs a) {
     wi = (int)(rest - (int64_t)a.n_shards * shard_waves);
     nparts = a.gen_parts;
     part_len = a.gen_part_len;
-    S = (int64_t)a.G + a.Tq;
+    S = a.gen_rows;
     Kz = a.Kg;
     Vz = a.Vg;
   }
@@ -110,15 +112,15 @@ void decode_attn_kernel(DecodeArgs a) {
   const int kv_begin = part * part_len;
   int kv_end = (int)min((int64_t)kv_begin + part_len, S);
   // in the generation shard no row of the tile sees past its last token's own
-  if (gen) kv_end = min(kv_end, a.G + tok0 + R / a.group);
+  if (gen) kv_end = min(kv_end, a.G + a.gen_past + tok0 + R / a.group);
   const int nsteps = max(0, (kv_end - kv_begin + DEC_KEYS - 1) / DEC_KEYS);
   const float c2 = a.scale_log2;
   // Keys from vis_end on weigh zero for this lane's query row: the range's
   // end, and in the generation shard the rows after the token's own.
   int vis_end = kv_end;
-  if (gen) vis_end = min(vis_end, a.G + tok0 + l32 / a.group + 1);
+  if (gen) vis_end = min(vis_end, a.G + a.gen_past + tok0 + l32 / a.group + 1);
   // a step whose keys all lie below mask_from needs no mask in any lane
-  const int mask_from = gen ? min(kv_end, a.G + tok0 + 1) : kv_end;
+  const int mask_from = gen ? min(kv_end, a.G + a.gen_past + tok0 + 1) : kv_end;
 
   // K/V of this shard through buffer resources, 32-bit byte offsets.
   const int64_t zstride = S * a.Hkv * D;
@@ -382,12 +384,13 @@ int launch_decode(const uint16_t* q, const uint16_t* K, const uint16_t* V, int n
   if (a.tile_tokens < 1) return PULSAR_EUNSUPPORTED;
   a.row_tiles = (Tq + a.tile_tokens - 1) / a.tile_tokens;
   if (gen != nullptr && gen->nparts > 0) {
-    const int64_t rows = gen->G + Tq;
     a.Kg = gen->K;
     a.Vg = gen->V;
     a.G = (int)gen->G;
     a.gen_parts = gen->nparts;
-    a.gen_part_len = decode_part_len(rows, gen->nparts);
+    a.gen_rows = (int)gen->rows(Tq);
+    a.gen_past = gen->cached ? kSeesAll : 0;
+    a.gen_part_len = decode_part_len(a.gen_rows, gen->nparts);
   }
   a.scale_log2 = scale * 1.4426950408889634f;
   a.O = o;

@@ -54,6 +54,8 @@ struct PackedArgs {
   int G;
   int gen_parts;      // its key ranges (0: no generation shard)
   int gen_part_len;
+  int gen_rows;       // G + Tq, or G of a draft
+  int gen_past;       // rows past its own that a token sees: 0, or kSeesAll
   int gen_own;        // its ranges have workgroups of their own, after the shards'
   int tile_tokens;    // tokens per 32-row tile, 32 / group
   float scale_log2;
@@ -138,8 +140,8 @@ void packed_attn_kernel(PackedArgs a) {
     const int gi = a.gen_own ? z - n_ranges : z;  // range of the generation shard
     const bool has_gen = gi >= 0 && gi < a.gen_parts;
     const int gb = has_gen ? gi * a.gen_part_len : 0;
-    span[1] = make_span(a.Kg, a.Vg, (int64_t)a.G + a.Tq, gb,
-                        has_gen ? min(gb + a.gen_part_len, a.G + a.Tq) : 0);
+    span[1] = make_span(a.Kg, a.Vg, a.gen_rows, gb,
+                        has_gen ? min(gb + a.gen_part_len, a.gen_rows) : 0);
   }
   // steps 0 .. n0 - 1 are the shard's, then the generation shard's
   const int n0 = span[0].nsteps, nsteps = n0 + span[1].nsteps;
@@ -262,7 +264,7 @@ void packed_attn_kernel(PackedArgs a) {
       // after the row's own token too.
       auto mask = [&](int j, int t, f32x16& S) {
         const int vis_end =
-            j < n0 ? span[0].end : min(span[1].end, a.G + token(t) + 1);
+            j < n0 ? span[0].end : min(span[1].end, a.G + a.gen_past + token(t) + 1);
         const int k0 = key0(j);
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
@@ -636,7 +638,9 @@ int launch_packed(const uint16_t* q, const uint16_t* K, const uint16_t* V, int n
     a.Vg = gen->V;
     a.G = (int)gen->G;
     a.gen_parts = gen->nparts;
-    a.gen_part_len = packed_part_len(gen->G + Tq, gen->nparts);
+    a.gen_rows = (int)gen->rows(Tq);
+    a.gen_past = gen->cached ? kSeesAll : 0;
+    a.gen_part_len = packed_part_len(a.gen_rows, gen->nparts);
     a.gen_own = gen->own;
   }
   a.scale_log2 = scale * 1.4426950408889634f;

@@ -104,10 +104,10 @@ __device__ __forceinline__ bool is_nan(f32x4 x) {
 // their o holds must not count either: where a zero weight has met a NaN or an
 // infinity there (so that a is NaN), the pass is repeated with such parts left
 // out.  (To leave them out at once costs every merge 3 to 6 %.)
-template <int CH>
+template <int CH, typename OUT>
 __global__ __launch_bounds__(256) void lse_merge_kernel(
     const float* __restrict__ o_parts, const float* __restrict__ lse_parts, int H, int Tq, int Hq,
-    int d4, int64_t part_ostride, int64_t part_lstride, float* __restrict__ o,
+    int d4, int64_t part_ostride, int64_t part_lstride, OUT* __restrict__ o,
     float* __restrict__ lse, int64_t total) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= total) return;
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(256) void lse_merge_kernel(
     ell = m + __logf(sum);
     acc *= 1.f / sum;
   }
-  reinterpret_cast<f32x4*>(o)[z * (int64_t)Tq * Hq * d4 + orow] = acc;
+  o[z * (int64_t)Tq * Hq * d4 + orow] = __builtin_convertvector(acc, OUT);
   if (lse && dv == 0) lse[z * (int64_t)Hq * Tq + (int64_t)h * Tq + q] = ell;
 }
 
@@ -175,10 +175,10 @@ __global__ __launch_bounds__(256) void lse_merge_kernel(
 // all their loads issued together, so a merge waits for one round trip to
 // memory where CH * PG covers the parts; then the groups are folded across
 // lanes and, through LDS, across wavefronts.
-template <int DL, int THREADS>
+template <int DL, int THREADS, typename OUT>
 __global__ __launch_bounds__(THREADS) void lse_merge_wide_kernel(
     const float* __restrict__ o_parts, const float* __restrict__ lse_parts, int H, int Tq, int Hq,
-    int d4, int64_t part_ostride, int64_t part_lstride, float* __restrict__ o,
+    int d4, int64_t part_ostride, int64_t part_lstride, OUT* __restrict__ o,
     float* __restrict__ lse) {
   constexpr int PG = THREADS / DL;
   constexpr int W = THREADS / 64;
@@ -269,13 +269,14 @@ __global__ __launch_bounds__(THREADS) void lse_merge_wide_kernel(
     ell = m + __logf(sum);
     acc *= 1.f / sum;
   }
-  reinterpret_cast<f32x4*>(o)[z * (int64_t)Tq * Hq * d4 + orow + dv] = acc;
+  o[z * (int64_t)Tq * Hq * d4 + orow + dv] = __builtin_convertvector(acc, OUT);
   if (lse && dv == 0) lse[z * (int64_t)Hq * Tq + (int64_t)h * Tq + q] = ell;
 }
 
-int launch_lse_merge(const float* o_parts, const float* lse_parts, int H, int nz, int Tq, int Hq,
-                     int d, int64_t part_ostride, int64_t part_lstride, float* o, float* lse,
-                     hipStream_t stream) {
+template <typename OUT>
+static int launch_merge(const float* o_parts, const float* lse_parts, int H, int nz, int Tq, int Hq,
+                        int d, int64_t part_ostride, int64_t part_lstride, OUT* o, float* lse,
+                        hipStream_t stream) {
   const int64_t total = (int64_t)nz * Tq * Hq * (d / 4);
   if (total == 0) return PULSAR_OK;
   const int64_t rows = (int64_t)nz * Tq * Hq;
@@ -297,15 +298,30 @@ int launch_lse_merge(const float* o_parts, const float* lse_parts, int H, int nz
     const dim3 grid((unsigned)rows, (unsigned)slices);
     const int threads = total <= 8192 && H > 1024 / dl ? 512 : 256;
     const auto wide = threads == 512
-                          ? (dl == 16 ? lse_merge_wide_kernel<16, 512> : lse_merge_wide_kernel<32, 512>)
-                          : (dl == 16 ? lse_merge_wide_kernel<16, 256> : lse_merge_wide_kernel<32, 256>);
+                          ? (dl == 16 ? lse_merge_wide_kernel<16, 512, OUT> : lse_merge_wide_kernel<32, 512, OUT>)
+                          : (dl == 16 ? lse_merge_wide_kernel<16, 256, OUT> : lse_merge_wide_kernel<32, 256, OUT>);
     hipLaunchKernelGGL(wide, grid, dim3(threads), 0, stream, o_parts, lse_parts, H, Tq, Hq, d / 4,
                        part_ostride, part_lstride, o, lse);
     return hipGetLastError() == hipSuccess ? PULSAR_OK : PULSAR_EHIP;
   }
   const int64_t blocks = (total + 255) / 256;
-  const auto kern = H <= 2 ? lse_merge_kernel<2> : H <= 4 ? lse_merge_kernel<4> : lse_merge_kernel<8>;
+  const auto kern = H <= 2   ? lse_merge_kernel<2, OUT>
+                    : H <= 4 ? lse_merge_kernel<4, OUT>
+                             : lse_merge_kernel<8, OUT>;
   hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(256), 0, stream, o_parts, lse_parts, H,
                      Tq, Hq, d / 4, part_ostride, part_lstride, o, lse, total);
   return hipGetLastError() == hipSuccess ? PULSAR_OK : PULSAR_EHIP;
+}
+
+int launch_lse_merge(const float* o_parts, const float* lse_parts, int H, int nz, int Tq, int Hq,
+                     int d, int64_t part_ostride, int64_t part_lstride, float* o, float* lse,
+                     hipStream_t stream) {
+  return launch_merge(o_parts, lse_parts, H, nz, Tq, Hq, d, part_ostride, part_lstride,
+                      reinterpret_cast<f32x4*>(o), lse, stream);
+}
+
+int launch_lse_merge_bf16(const float* o_parts, const float* lse_parts, int H, int Tq, int Hq,
+                          int d, void* o, float* lse, hipStream_t stream) {
+  return launch_merge(o_parts, lse_parts, H, 1, Tq, Hq, d, (int64_t)Tq * Hq * d, (int64_t)Hq * Tq,
+                      static_cast<bf16x4*>(o), lse, stream);
 }

@@ -1,0 +1,347 @@
+"""Block-sparse Phase 2 on the GPU: key_bounds, block_select and phase2_sparse
+against oracle.blocks (tolerances: tests._blocks.check; selections bit-exact)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_20457_amd as P
+from oracle import blocks as ob
+from tests._blocks import (check, dev_i32, dev_mask, f64, host, normal, random_tree,
+                           sparse_reference, to_dev_bf16)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("ns,S,Hkv,d,block", [
+    (1, 1, 1, 64, 16), (1, 16, 1, 128, 16), (2, 17, 8, 128, 16), (4, 1021, 8, 128, 32),
+    (3, 640, 2, 64, 64), (5, 333, 16, 64, 128), (2, 1000, 3, 128, 256), (1, 300, 1, 64, 256)])
+def test_key_bounds(ns, S, Hkv, d, block):
+    k = normal(S, (ns, S, Hkv, d))
+    got = P.key_bounds(to_dev_bf16(k), block)
+    assert got.shape == (ns, Hkv, -(-S // block), 2, d)
+    assert np.array_equal(host(got), ob.key_bounds(f64(k), block))
+
+
+def test_key_bounds_of_special_values():
+    k = normal(7, (1, 40, 2, 64))
+    k[0, 3, 0, 5] = 0x7F80   # inf
+    k[0, 20, 1, 6] = 0xFF80  # -inf
+    k[0, 33, 0, 7] = 0x7FC0  # NaN
+    got = host(P.key_bounds(to_dev_bf16(k), 16))
+    assert got[0, 0, 0, 1, 5] == np.inf and got[0, 1, 1, 0, 6] == -np.inf
+    assert np.isnan(got[0, 0, 2, :, 7]).all()
+    rest = f64(k)
+    rest[0, 33, 0, 7] = 0.0
+    want = ob.key_bounds(rest, 16)
+    got[0, 0, 2, :, 7] = want[0, 0, 2, :, 7]
+    assert np.array_equal(got, want)
+
+
+def _select(ns, blocks, Hq, Hkv, d, Tq, topk, seed, bounds=None, q=None):
+    print(f"block_select: {ns}x{blocks} Hq={Hq} Hkv={Hkv} d={d} Tq={Tq} topk={topk}", flush=True)
+    if q is None:
+        q = normal(seed, (Tq, Hq, d))
+    if bounds is None:
+        x = np.sort(f64(normal(seed + 1, (ns, Hkv, blocks, 2, d))), axis=3)
+        bounds = torch.from_numpy(x).to(torch.bfloat16)
+    bounds = bounds.cuda()
+    sel, scores = P.block_select(to_dev_bf16(q), bounds, topk, return_scores=True)
+    want = ob.block_scores(f64(q), host(bounds))
+    assert np.array_equal(scores.cpu().numpy(), want)
+    assert np.array_equal(sel.cpu().numpy(), ob.block_select(want, topk))
+    again = P.block_select(to_dev_bf16(q), bounds, topk)
+    assert torch.equal(sel, again)
+
+
+@pytest.mark.parametrize("ns,blocks,Hq,Hkv,d,Tq,topk", [
+    (1, 1, 4, 1, 64, 1, 1), (16, 128, 32, 8, 128, 1, 4), (4, 32, 32, 8, 128, 3, 32),
+    (2, 63, 8, 8, 64, 17, 5), (1, 65, 16, 8, 128, 9, 64), (3, 17, 12, 1, 64, 3, 2),
+    (2, 40, 24, 1, 128, 2, 7), (1, 33, 64, 1, 64, 2, 3), (1, 256, 5, 1, 128, 4, 255),
+    (1, 257, 32, 8, 128, 2, 20), (1, 1025, 4, 1, 64, 5, 100), (1, 4096, 8, 2, 128, 2, 128),
+    (1, 4097, 4, 1, 64, 2, 1), (1, 16385, 4, 1, 64, 1, 500), (1, 32768, 1, 1, 64, 1, 4096),
+    (5, 94, 16, 16, 64, 64, 12)])
+def test_block_select(ns, blocks, Hq, Hkv, d, Tq, topk):
+    _select(ns, blocks, Hq, Hkv, d, Tq, topk, 3000 + blocks + Tq)
+
+
+def test_block_select_ties_go_to_the_lower_index():
+    for blocks, topk in ((100, 7), (700, 300), (5000, 4999)):
+        x = np.sort(f64(normal(9, (1, 1, 3, 2, 64))), axis=3)
+        pick = np.random.default_rng(blocks).integers(0, 3, blocks)
+        _select(1, blocks, 4, 1, 64, 2, topk, 10, torch.from_numpy(x[:, :, pick]).to(torch.bfloat16))
+    _select(1, 90, 4, 1, 64, 1, 11, 10, torch.zeros((1, 1, 90, 2, 64), dtype=torch.bfloat16))
+
+
+def test_block_select_near_ties():
+    # scores that differ in their last bits only: all blocks equal but for one channel
+    x = np.repeat(np.sort(f64(normal(14, (1, 1, 1, 2, 128))), axis=3), 300, axis=2)
+    x[0, 0, :, 1, 77] = x[0, 0, 0, 1, 77] * (1 + np.arange(300) % 5 / 128)
+    _select(1, 300, 4, 1, 128, 6, 50, 15, torch.from_numpy(x).to(torch.bfloat16))
+
+
+def test_block_select_of_special_values():
+    # a block with a bound that is not finite ranks first; large and tiny values
+    x = np.sort(f64(normal(16, (1, 2, 80, 2, 64))), axis=3)
+    x[0, 0, 70, 1, 3], x[0, 0, 60, 0, 4], x[0, 1, 50, :, 5] = np.inf, -np.inf, np.nan
+    x[0, 1, 20] *= 2.0 ** 100
+    x[0, 1, 21] *= 2.0 ** -100
+    b = torch.from_numpy(x).to(torch.bfloat16)
+    sel = P.block_select(to_dev_bf16(normal(17, (3, 8, 64))), b.cuda(), 2).cpu().numpy()
+    assert (sel[0, :, 0] == [60, 70]).all() and (sel[0, :, 1, 1] == 50).all()
+    _select(1, 80, 8, 2, 64, 3, 9, 17, b)
+
+
+def _sparse(Hq, Hkv, d, Tq, G, ns, S, block, topk, seed, gen=True, sees=None, sel=None,
+            bf16_out=False, q_scale=1.0, what="", k=None):
+    print(f"phase2_sparse parity: {what} Hq={Hq} Hkv={Hkv} d={d} Tq={Tq} G={G} {ns}x{S} "
+          f"block={block} topk={topk}", flush=True)
+    q = normal(seed, (Tq, Hq, d), q_scale)
+    if k is None:
+        k = normal(seed + 1, (ns, S, Hkv, d))
+    v = normal(seed + 2, (ns, S, Hkv, d))
+    kg, vg = ((normal(seed + i, (G + Tq, Hkv, d)) for i in (3, 4)) if gen else (None, None))
+    if sel is None:
+        u = np.random.default_rng(seed).random((ns, Tq, Hkv, -(-S // block)))
+        sel = np.sort(np.argsort(u, axis=3)[..., :topk], axis=3)
+    o, lse = P.phase2_sparse(
+        to_dev_bf16(q), to_dev_bf16(k), to_dev_bf16(v), dev_i32(sel), block,
+        to_dev_bf16(kg) if gen else None, to_dev_bf16(vg) if gen else None, G,
+        None if sees is None else dev_mask(sees), o_dtype=P.OUT_BF16 if bf16_out else P.OUT_F32)
+    ref, keys = sparse_reference(q, k, v, sel, block, kg, vg, G, sees, 1.0 / math.sqrt(d))
+    check(o, lse, ref, keys, what, bf16_out)
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,Tq,G,ns,S,block,topk", [
+    (32, 8, 128, 1, 45, 4, 1021, 16, 8),     # a generation step, ragged shards
+    (32, 8, 128, 1, 0, 1, 1, 16, 1),         # one key, one new token
+    (32, 8, 128, 1, 0, 1, 40, 16, 3),        # a block that ends inside a half
+    (32, 8, 128, 2, 3, 2, 200, 64, 2),
+    (16, 16, 64, 24, 30, 3, 301, 32, 5),     # one head per KV head
+    (4, 1, 64, 5, 31, 1, 33, 16, 3),         # every block: dense
+    (8, 2, 128, 70, 0, 2, 128, 32, 1),       # several tokens, one part each
+    (16, 8, 64, 3, 500, 1, 600, 128, 2),     # a long generation shard
+    (12, 1, 128, 2, 5, 1, 300, 256, 2),      # 12 heads per KV head
+    (24, 1, 64, 2, 5, 1, 90, 16, 3),         # 24 heads: two column tiles
+    (64, 1, 128, 1, 5, 1, 90, 16, 3),        # 64 heads: four
+    (32, 8, 128, 1, 7, 16, 64, 16, 4),       # many shards, all of their blocks
+    (4, 1, 64, 1, 0, 1, 9000, 16, 300),      # lists longer than a wave's table
+    (32, 8, 128, 130, 0, 1, 64, 16, 1),      # more workgroups than fill the chip
+])
+def test_sparse_shapes(Hq, Hkv, d, Tq, G, ns, S, block, topk):
+    _sparse(Hq, Hkv, d, Tq, G, ns, S, block, topk, 4000 + Hq + Tq + G + S, bf16_out=Tq % 2 == 0,
+            what="shapes")
+
+
+def test_sparse_without_a_generation_shard():
+    _sparse(32, 8, 128, 3, 0, 2, 300, 32, 4, 4100, gen=False, what="shards alone")
+
+
+def test_sparse_lists_nothing():
+    # empty lists, lists of no block, no shards, shards without keys
+    Tq, Hkv = 4, 2
+    none = np.full((2, Tq, Hkv, 3), -1)
+    _sparse(8, Hkv, 128, Tq, 0, 2, 100, 16, 3, 4110, sel=none, gen=False, what="all -1, no rows")
+    _sparse(8, Hkv, 128, Tq, 9, 2, 100, 16, 3, 4111, sel=none, what="all -1")
+    _sparse(8, Hkv, 64, Tq, 9, 2, 100, 16, 0, 4112, what="topk 0")
+    _sparse(8, Hkv, 64, Tq, 9, 0, 100, 16, 0, 4113, what="no shards")
+    _sparse(8, Hkv, 64, Tq, 9, 2, 0, 16, 0, 4114, what="no keys")
+    _sparse(8, Hkv, 64, Tq, 9, 2, 0, 16, 2, 4115, sel=np.zeros((2, Tq, Hkv, 2)), what="no keys listed")
+
+
+@pytest.mark.parametrize("block", [16, 64])
+def test_sparse_lists_with_gaps_and_repeats(block):
+    rng = np.random.default_rng(block)
+    sel = rng.integers(-3, 9, (3, 5, 2, 7))  # blocks outside [0, 7), repeated, in any order
+    sel[0, 0] = 2**31 - 1
+    sel[1, 1] = -2**31
+    _sparse(8, 2, 128, 5, 4, 3, 6 * block + 5, block, 7, 4120, sel=sel, what="gaps and repeats")
+    _sparse(8, 2, 128, 5, 0, 3, 6 * block + 5, block, 7, 4121, sel=sel, gen=False, what="no rows")
+
+
+def test_sparse_with_a_tree():
+    for Tq, G in ((1, 0), (13, 5), (40, 50), (70, 16), (33, 0)):
+        sees, _ = ob.tree_visible(random_tree(Tq, Tq, dead=(Tq // 2,) if Tq > 1 else ()))
+        _sparse(16, 4, 128, Tq, G, 2, 200, 32, 3, 4130 + Tq, sees=sees, what="tree")
+    sees = np.random.default_rng(5).random((50, 50)) < 0.3
+    _sparse(8, 8, 64, 50, 11, 1, 100, 16, 0, 4140, sees=sees, what="any visibility, no blocks")
+    sees[:] = False
+    _sparse(8, 8, 64, 50, 0, 1, 100, 16, 0, 4141, sees=sees, what="nothing seen")
+
+
+def test_sparse_peaked_and_rising_scores():
+    _sparse(32, 8, 128, 4, 9, 2, 600, 32, 8, 4150, q_scale=8.0, what="peaked")
+    # scores that rise far along the list: the reference is raised at every block
+    from paper_2607_20457_amd import workload
+    k = workload.bf16_bits_to_f32(normal(4161, (1, 800, 2, 128)))
+    k = workload.f32_to_bf16_bits(k * (1 + np.arange(800)[None, :, None, None] / 20))
+    _sparse(8, 2, 128, 2, 0, 1, 800, 16, 50, 4160, k=k, what="rising")
+
+
+@pytest.mark.parametrize("Tq", [1, 9])
+def test_unseen_rows_may_hold_anything(Tq):
+    # NaN and infinities in blocks that are not listed, behind a shard's end and in
+    # rows of the generation shard that a token does not see
+    Hq, Hkv, d, S, block, G = 8, 2, 128, 200, 16, 20
+    q = normal(61, (Tq, Hq, d))
+    k, v = (normal(s, (2, S, Hkv, d)) for s in (62, 63))
+    kg, vg = (normal(s, (G + Tq, Hkv, d)) for s in (64, 65))
+    sel = np.broadcast_to([1, 3, -1, 12], (2, Tq, Hkv, 4))  # block 12 has 8 keys
+    sees = np.tril(np.ones((Tq, Tq), bool))
+    bad = np.arange(Tq) % 3 == 1
+    sees[:, bad] = False
+    mask = dev_mask(sees)
+
+    def go(k, v, kg, vg):
+        return P.phase2_sparse(*map(to_dev_bf16, (q, k, v)), dev_i32(sel), block,
+                               *map(to_dev_bf16, (kg, vg)), G, mask)
+
+    ref = go(k, v, kg, vg)
+    listed = np.isin(np.arange(S) // block, (1, 3, 12))
+    for word in (0x7FC0, 0x7F80, 0xFF80):
+        kb, vb, kgb, vgb = k.copy(), v.copy(), kg.copy(), vg.copy()
+        kb[:, ~listed], vb[:, ~listed] = word, word
+        kgb[G:][bad], vgb[G:][bad] = word, word
+        for a, b in zip(go(kb, vb, kgb, vgb), ref):
+            assert torch.equal(a, b)
+    # the causal form: later tokens' rows
+    if Tq > 1:
+        args = (to_dev_bf16(q), to_dev_bf16(k), to_dev_bf16(v), dev_i32(sel), block)
+        ref = P.phase2_sparse(*args, to_dev_bf16(kg), to_dev_bf16(vg), G)
+        kg[G + 5:], vg[G + 5:] = 0x7FC0, 0x7F80
+        got = P.phase2_sparse(*args, to_dev_bf16(kg), to_dev_bf16(vg), G)
+        assert torch.equal(got[0][:5], ref[0][:5]) and torch.equal(got[1][:, :5], ref[1][:, :5])
+        assert torch.isnan(got[0][5:]).any()
+
+
+def test_sparse_of_every_block_is_the_query_step():
+    Tq, G, Hq, Hkv, d, S = 3, 33, 32, 8, 128, 300
+    q = to_dev_bf16(normal(71, (Tq, Hq, d)))
+    k, v = (to_dev_bf16(normal(s, (2, S, Hkv, d))) for s in (72, 73))
+    kg, vg = (to_dev_bf16(normal(s, (G + Tq, Hkv, d))) for s in (74, 75))
+    sel = dev_i32(np.broadcast_to(np.arange(19), (2, Tq, Hkv, 19)))
+    o, lse = P.phase2_sparse(q, k, v, sel, 16, kg, vg, G)
+    o2, lse2 = P.phase2_query(q, kg, vg, G, k, v)
+    assert np.allclose(host(lse), host(lse2), atol=1e-4)
+    assert np.abs(host(o) - host(o2)).max() <= 2.0 ** -6
+
+
+def test_sparse_partials_of_two_hosts_merge():
+    # the generation shard on one host, half of the shards on each
+    Tq, G, Hq, Hkv, d, S, block = 5, 12, 16, 4, 64, 150, 32
+    q = to_dev_bf16(normal(76, (Tq, Hq, d)))
+    k, v = (to_dev_bf16(normal(s, (4, S, Hkv, d))) for s in (77, 78))
+    kg, vg = (to_dev_bf16(normal(s, (G + Tq, Hkv, d))) for s in (79, 80))
+    sel = P.block_select(q, P.key_bounds(k, block), 2)
+    whole = P.phase2_sparse(q, k, v, sel, block, kg, vg, G)
+    one = P.phase2_sparse(q, k[:2], v[:2], sel[:2], block, kg, vg, G)
+    two = P.phase2_sparse(q, k[2:], v[2:], sel[2:], block)
+    o, lse = P.lse_merge(torch.stack([one[0], two[0]]), torch.stack([one[1], two[1]]))
+    assert np.allclose(host(lse), host(whole[1]), atol=1e-4)
+    assert np.abs(host(o) - host(whole[0])).max() <= 2.0 ** -6
+
+
+def test_sparse_beyond_four_gib_of_a_shard():
+    # rows whose byte offsets pass 32 bits
+    Hkv, d, S, block = 8, 128, 2200000, 64
+    K = torch.zeros((1, S, Hkv, d), dtype=torch.bfloat16, device="cuda")
+    V = torch.zeros_like(K)
+    blocks = -(-S // block)
+    pick = [0, blocks // 2, blocks - 1]
+    q = normal(91, (1, 32, d))
+    ks, vs = normal(92, (3, block, Hkv, d)), normal(93, (3, block, Hkv, d))
+    rows = []
+    for i, b in enumerate(pick):
+        n = min(block, S - b * block)
+        K[0, b * block:b * block + n] = to_dev_bf16(ks[i, :n])
+        V[0, b * block:b * block + n] = to_dev_bf16(vs[i, :n])
+        rows += [(i, r) for r in range(n)]
+    sel = dev_i32(np.broadcast_to(pick, (1, 1, Hkv, 3)))
+    o, lse = P.phase2_sparse(to_dev_bf16(q), K, V, sel, block)
+    kk = np.stack([f64(ks)[i, r] for i, r in rows])
+    vv = np.stack([f64(vs)[i, r] for i, r in rows])
+    ref = ob.counted_attention(f64(q), kk, vv, np.ones((1, 1, len(rows))), 1 / math.sqrt(d))
+    check(o, lse, ref, len(rows), "4 GiB")
+    got = P.key_bounds(K, block)
+    for i, b in enumerate(pick):
+        want = ob.key_bounds(f64(ks)[i:i + 1, :min(block, S - b * block)], block)
+        assert np.array_equal(host(got[:, :, b:b + 1]), want)
+
+
+def test_a_whole_step_with_drafts():
+    # bounds after the prefill; then a draft's mask, its selection, its attention
+    # over the selected blocks, and the accepted rows moved to the front
+    ns, S, block, topk, Hq, Hkv, d, G, Tq = 3, 500, 32, 4, 16, 4, 128, 40, 12
+    k, v = (normal(s, (ns, S, Hkv, d)) for s in (101, 102))
+    kg, vg = (normal(s, (G + Tq, Hkv, d)) for s in (103, 104))
+    q = normal(105, (Tq, Hq, d))
+    parent = random_tree(106, Tq)
+    K, V, Kg, Vg, Q = map(to_dev_bf16, (k, v, kg, vg, q))
+    bounds = P.key_bounds(K, block)
+    mask, depth = P.tree_mask(dev_i32(parent))
+    sel = P.block_select(Q, bounds, topk)
+    o, lse = P.phase2_sparse(Q, K, V, sel, block, Kg, Vg, G, mask)
+    sees, deep = ob.tree_visible(parent)
+    want = ob.block_select(ob.block_scores(f64(q), ob.key_bounds(f64(k), block)), topk)
+    assert np.array_equal(sel.cpu().numpy(), want)
+    ref, keys = sparse_reference(q, k, v, want, block, kg, vg, G, sees, 1 / math.sqrt(d))
+    check(o, lse, ref, keys, "step")
+    path = [int(np.argmax(deep))]
+    while parent[path[0]] >= 0:
+        path.insert(0, parent[path[0]])
+    P.kv_compact_(Kg[None], Vg[None], G, dev_i32(path + [-1] * (Tq - len(path))))
+    for got, x in ((Kg, kg), (Vg, vg)):
+        assert np.array_equal(got.view(torch.int16).cpu().numpy().view(np.uint16),
+                              ob.kv_compact(x[None], G, path)[0])
+
+
+def test_selection_and_attention_captured():
+    Tq, G, Hq, Hkv, d, ns, S, block, topk = 2, 30, 32, 8, 128, 4, 512, 32, 3
+    q = to_dev_bf16(normal(111, (Tq, Hq, d)))
+    k, v = (to_dev_bf16(normal(s, (ns, S, Hkv, d))) for s in (112, 113))
+    kg, vg = (to_dev_bf16(normal(s, (G + Tq, Hkv, d))) for s in (114, 115))
+
+    def step():
+        bounds = P.key_bounds(k, block)
+        sel = P.block_select(q, bounds, topk)
+        return (bounds, sel) + P.phase2_sparse(q, k, v, sel, block, kg, vg, G)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for i in range(3):
+        q.copy_(to_dev_bf16(normal(120 + i, (Tq, Hq, d))))
+        k[:, ::3].mul_(-1)
+        want = step()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(a, b), i
+
+
+def test_calls_on_two_streams_at_once():
+    Hq, Hkv, d, ns, S, block, topk = 32, 8, 128, 4, 2048, 32, 16
+    k, v = (to_dev_bf16(normal(s, (ns, S, Hkv, d))) for s in (131, 132))
+    qs = [to_dev_bf16(normal(133 + i, (2, Hq, d))) for i in range(2)]
+    bounds = P.key_bounds(k, block)
+
+    def step(q):
+        sel = P.block_select(q, bounds, topk)
+        return (sel,) + P.phase2_sparse(q, k, v, sel, block)
+
+    want = [step(q) for q in qs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in qs]
+    for _ in range(10):
+        got = []
+        for q, s in zip(qs, streams):
+            with torch.cuda.stream(s):
+                got.append(step(q))
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
