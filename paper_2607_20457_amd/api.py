@@ -7,6 +7,7 @@ computation happens in the HIP kernels behind ``libpulsar.so``.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 
 import torch
@@ -330,40 +331,50 @@ def phase2_query_noalloc(q, Kg, Vg, G: int, K=None, V=None, softmax_scale: float
     return o, lse
 
 
-def _here(*tensors):
-    """The tensors lie on the current device, whose current stream the call uses."""
-    dev = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != dev:
-            raise ValueError("tensors must be on the current device")
+_BF16 = torch.bfloat16
 
 
-def _generation(Kg, Vg, G, Tq, Hkv, d):
-    _need(Kg, torch.bfloat16, "Kg")
-    _need(Vg, torch.bfloat16, "Vg")
+def _check(dev, dtype, named):
+    """Every (tensor, name) is a contiguous tensor of dtype on device dev, the
+    current one, whose current stream the call uses."""
+    for t, name in named:
+        if t.get_device() != dev or t.dtype is not dtype or not t.is_contiguous():
+            _need(t, dtype, name)
+            raise ValueError(f"{name} must be on the current device")
+
+
+def _raw_stream(dev):
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
+def _generation_shape(Kg, Vg, G, Tq, Hkv, d):
     if G < 0 or Kg.shape != (G + Tq, Hkv, d) or Vg.shape != Kg.shape:
         raise ValueError("Kg/Vg must be [G + Tq, Hkv, d]")
 
 
-def _need_mask(mask, Tq):
-    _need(mask, torch.int32, "mask")
+def _mask_shape(mask, Tq):
     if mask.shape != (Tq, (Tq + 31) // 32):
         raise ValueError("mask must be [Tq, ceil(Tq / 32)]")
 
 
 def _out(q, o_dtype):
-    if o_dtype not in (OUT_F32, OUT_BF16):
+    if o_dtype == OUT_BF16:
+        return q.new_empty(q.shape)
+    if o_dtype != OUT_F32:
         raise ValueError("o_dtype must be OUT_F32 or OUT_BF16")
-    return q.new_empty(q.shape, dtype=torch.bfloat16 if o_dtype == OUT_BF16 else torch.float32)
+    return q.new_empty(q.shape, dtype=torch.float32)
 
 
-def _scratch(workspace, need, like):
-    """The caller's workspace where it is large enough, else a new one."""
-    if workspace is not None:
-        _need(workspace, workspace.dtype, "workspace")
-        if workspace.numel() * workspace.element_size() >= need:
-            return workspace
-    return like.new_empty(need, dtype=torch.uint8) if need else None
+def _scratch(workspace, need, dev, like):
+    """The caller's workspace where it is large enough, else a new one, and its
+    address (None where none is needed)."""
+    if workspace is not None and workspace.numel() * workspace.element_size() >= need:
+        _check(dev, workspace.dtype, ((workspace, "workspace"),))
+        return workspace, workspace.data_ptr()
+    if not need:
+        return None, None
+    workspace = like.new_empty(need, dtype=torch.uint8)
+    return workspace, workspace.data_ptr()
 
 
 def tree_mask(parent):
@@ -371,18 +382,20 @@ def tree_mask(parent):
     draft that each follows, -1 for the last token before them (any other value:
     no token) -> (mask int32 [T, ceil(T / 32)], each token's bits set for itself
     and its ancestors; depth int32 [T], its number of ancestors, -1 for none)."""
-    _need(parent, torch.int32, "parent")
+    dev = torch.cuda.current_device() if parent.is_cuda else None
+    _check(dev, torch.int32, ((parent, "parent"),))
     if parent.dim() != 1:
         raise ValueError("parent must be [T]")
-    _here(parent)
     T = parent.shape[0]
     mask = parent.new_empty((T, (T + 31) // 32))
     depth = parent.new_empty((T,))
-    st = _lib.lib().pulsar_tree_mask(_ptr(parent), T, _ptr(mask), _ptr(depth), _stream())
+    st = _lib.lib().pulsar_tree_mask(parent.data_ptr(), T, mask.data_ptr(), depth.data_ptr(),
+                                     _raw_stream(dev))
     _lib.check(st, "pulsar_tree_mask")
     return mask, depth
 
 
+@functools.lru_cache(maxsize=4096)
 def phase2_tree_workspace_bytes(n_shards: int, Tq: int, S: int, G: int, Hq: int, Hkv: int,
                                 d: int) -> int:
     return int(_lib.lib().pulsar_phase2_tree_workspace_bytes(n_shards, Tq, S, G, Hq, Hkv, d))
@@ -395,28 +408,28 @@ def phase2_tree(q, Kg, Vg, G: int, mask, K=None, V=None, softmax_scale: float | 
     of the generation shard Kg/Vg bf16 [G + Tq, Hkv, d], and those of the drafts'
     own rows that mask int32 [Tq, ceil(Tq / 32)] (``tree_mask``) sets for each
     -> (o [Tq, Hq, d] per o_dtype, lse f32 [Hq, Tq])."""
-    _need(q, torch.bfloat16, "q")
+    dev = torch.cuda.current_device() if q.is_cuda else None
+    _check(dev, _BF16, ((q, "q"), (Kg, "Kg"), (Vg, "Vg")))
+    _check(dev, torch.int32, ((mask, "mask"),))
     Tq, Hq, d = q.shape
     Hkv = Kg.shape[1]
-    _generation(Kg, Vg, G, Tq, Hkv, d)
-    _need_mask(mask, Tq)
-    n_shards, S = 0, 0
+    _generation_shape(Kg, Vg, G, Tq, Hkv, d)
+    _mask_shape(mask, Tq)
+    n_shards, S, k_ptr, v_ptr = 0, 0, None, None
     if K is not None:
-        _need(K, torch.bfloat16, "K")
-        _need(V, torch.bfloat16, "V")
-        n_shards, S = K.shape[0], K.shape[1]
+        _check(dev, _BF16, ((K, "K"), (V, "V")))
+        n_shards, S = K.shape[:2]
         if K.shape != (n_shards, S, Hkv, d) or V.shape != K.shape:
             raise ValueError("K/V must be [n_shards, S, Hkv, d]")
-    scale = 1.0 / math.sqrt(d) if softmax_scale is None else softmax_scale
+        k_ptr, v_ptr = K.data_ptr(), V.data_ptr()
     o = _out(q, o_dtype)
     lse = q.new_empty((Hq, Tq), dtype=torch.float32)
-    lib = _lib.lib()
-    need = lib.pulsar_phase2_tree_workspace_bytes(n_shards, Tq, S, G, Hq, Hkv, d)
-    workspace = _scratch(workspace, need, q)
-    _here(q, Kg, Vg, mask, K, V, workspace)
-    st = lib.pulsar_phase2_tree(_ptr(q), _ptr(Kg), _ptr(Vg), G, _ptr(mask), _ptr(K), _ptr(V),
-                                n_shards, Tq, S, Hq, Hkv, d, scale, _ptr(o), o_dtype, _ptr(lse),
-                                _ptr(workspace), need, _stream())
+    need = phase2_tree_workspace_bytes(n_shards, Tq, S, G, Hq, Hkv, d)
+    workspace, ws_ptr = _scratch(workspace, need, dev, q)
+    st = _lib.lib().pulsar_phase2_tree(
+        q.data_ptr(), Kg.data_ptr(), Vg.data_ptr(), G, mask.data_ptr(), k_ptr, v_ptr, n_shards, Tq,
+        S, Hq, Hkv, d, 1.0 / math.sqrt(d) if softmax_scale is None else softmax_scale,
+        o.data_ptr(), o_dtype, lse.data_ptr(), ws_ptr, need, _raw_stream(dev))
     _lib.check(st, "pulsar_phase2_tree")
     return o, lse
 
@@ -425,17 +438,16 @@ def kv_compact_(K, V, G: int, keep):
     """Rows G + keep[j] of every layer of K/V bf16 [layers, capacity, Hkv, d]
     moved to row G + j, in place.  keep int32 [n], rising; it ends at the first
     entry that is negative, does not rise or lies past the cache.  Returns K, V."""
-    _need(K, torch.bfloat16, "K")
-    _need(V, torch.bfloat16, "V")
-    _need(keep, torch.int32, "keep")
+    dev = torch.cuda.current_device() if K.is_cuda else None
+    _check(dev, _BF16, ((K, "K"), (V, "V")))
+    _check(dev, torch.int32, ((keep, "keep"),))
     if K.dim() != 4 or V.shape != K.shape or keep.dim() != 1:
         raise ValueError("K/V must be [layers, capacity, Hkv, d], keep [n]")
     if K.data_ptr() == V.data_ptr() and K.numel() > 0:
         raise ValueError("K and V must not be the same memory")
-    _here(K, V, keep)
     layers, capacity, Hkv, d = K.shape
-    st = _lib.lib().pulsar_kv_compact(_ptr(K), _ptr(V), layers, capacity, Hkv, d, G, _ptr(keep),
-                                      keep.shape[0], _stream())
+    st = _lib.lib().pulsar_kv_compact(K.data_ptr(), V.data_ptr(), layers, capacity, Hkv, d, G,
+                                      keep.data_ptr(), keep.shape[0], _raw_stream(dev))
     _lib.check(st, "pulsar_kv_compact")
     return K, V
 
@@ -444,12 +456,12 @@ def key_bounds(K, block: int):
     """Channel minima and maxima of every block of `block` keys (16, 32, 64, 128
     or 256).  K bf16 [n_shards, S, Hkv, d] -> bounds bf16 [n_shards, Hkv,
     ceil(S / block), 2, d]."""
-    _need(K, torch.bfloat16, "K")
-    _here(K)
+    dev = torch.cuda.current_device() if K.is_cuda else None
+    _check(dev, _BF16, ((K, "K"),))
     n_shards, S, Hkv, d = K.shape
-    blocks = -(-S // block) if block > 0 else 0
-    bounds = K.new_empty((n_shards, Hkv, blocks, 2, d))
-    st = _lib.lib().pulsar_key_bounds(_ptr(K), n_shards, S, Hkv, d, block, _ptr(bounds), _stream())
+    bounds = K.new_empty((n_shards, Hkv, -(-S // block) if block > 0 else 0, 2, d))
+    st = _lib.lib().pulsar_key_bounds(K.data_ptr(), n_shards, S, Hkv, d, block, bounds.data_ptr(),
+                                      _raw_stream(dev))
     _lib.check(st, "pulsar_key_bounds")
     return bounds
 
@@ -463,27 +475,27 @@ def block_select(q, bounds, topk: int, return_scores: bool = False, workspace=No
     q . k that their bounds allow.  q bf16 [Tq, Hq, d], bounds as ``key_bounds``
     returns them -> sel int32 [n_shards, Tq, Hkv, topk], ascending (+ the scores
     f32 [n_shards, Tq, Hkv, blocks])."""
-    _need(q, torch.bfloat16, "q")
-    _need(bounds, torch.bfloat16, "bounds")
+    dev = torch.cuda.current_device() if q.is_cuda else None
+    _check(dev, _BF16, ((q, "q"), (bounds, "bounds")))
     Tq, Hq, d = q.shape
     n_shards, Hkv, blocks, two, db = bounds.shape
     if two != 2 or db != d:
         raise ValueError("bounds must be [n_shards, Hkv, blocks, 2, d]")
     sel = q.new_empty((n_shards, Tq, Hkv, max(topk, 0)), dtype=torch.int32)
-    lib = _lib.lib()
-    scores, need = None, 0
+    scores, ws_ptr, need = None, None, 0
     if return_scores:
         scores = q.new_empty((n_shards, Tq, Hkv, blocks), dtype=torch.float32)
     else:
-        need = lib.pulsar_block_select_workspace_bytes(n_shards, Tq, blocks, Hkv)
-        workspace = _scratch(workspace, need, q)
-    _here(q, bounds, workspace)
-    st = lib.pulsar_block_select(_ptr(q), _ptr(bounds), n_shards, Tq, blocks, Hq, Hkv, d, topk,
-                                 _ptr(sel), _ptr(scores), _ptr(workspace), need, _stream())
+        need = block_select_workspace_bytes(n_shards, Tq, blocks, Hkv)
+        workspace, ws_ptr = _scratch(workspace, need, dev, q)
+    st = _lib.lib().pulsar_block_select(q.data_ptr(), bounds.data_ptr(), n_shards, Tq, blocks, Hq,
+                                        Hkv, d, topk, sel.data_ptr(), _ptr(scores), ws_ptr, need,
+                                        _raw_stream(dev))
     _lib.check(st, "pulsar_block_select")
     return (sel, scores) if return_scores else sel
 
 
+@functools.lru_cache(maxsize=4096)
 def phase2_sparse_workspace_bytes(Tq: int, Hq: int, Hkv: int, d: int) -> int:
     return int(_lib.lib().pulsar_phase2_sparse_workspace_bytes(Tq, Hq, Hkv, d))
 
@@ -496,32 +508,34 @@ def phase2_sparse(q, K, V, sel, block: int, Kg=None, Vg=None, G: int = 0, mask=N
     that is no block of the shard lists none), Kg/Vg bf16 [G + Tq, Hkv, d] (None:
     the shards alone) up to each token itself, or by a tree's mask
     -> (o [Tq, Hq, d] per o_dtype, lse f32 [Hq, Tq])."""
-    _need(q, torch.bfloat16, "q")
-    _need(K, torch.bfloat16, "K")
-    _need(V, torch.bfloat16, "V")
-    _need(sel, torch.int32, "sel")
+    dev = torch.cuda.current_device() if q.is_cuda else None
+    _check(dev, _BF16, ((q, "q"), (K, "K"), (V, "V")))
+    _check(dev, torch.int32, ((sel, "sel"),))
     Tq, Hq, d = q.shape
     n_shards, S, Hkv, dk = K.shape
     if dk != d or V.shape != K.shape:
         raise ValueError("K/V must be [n_shards, S, Hkv, d]")
     if sel.dim() != 4 or sel.shape[:3] != (n_shards, Tq, Hkv):
         raise ValueError("sel must be [n_shards, Tq, Hkv, topk]")
-    if (Kg is None) != (Vg is None):
-        raise ValueError("Kg and Vg go together")
-    if Kg is not None:
-        _generation(Kg, Vg, G, Tq, Hkv, d)
+    kg_ptr = vg_ptr = mask_ptr = None
+    if Kg is not None or Vg is not None:
+        if Kg is None or Vg is None:
+            raise ValueError("Kg and Vg go together")
+        _check(dev, _BF16, ((Kg, "Kg"), (Vg, "Vg")))
+        _generation_shape(Kg, Vg, G, Tq, Hkv, d)
+        kg_ptr, vg_ptr = Kg.data_ptr(), Vg.data_ptr()
     if mask is not None:
-        _need_mask(mask, Tq)
-    scale = 1.0 / math.sqrt(d) if softmax_scale is None else softmax_scale
+        _check(dev, torch.int32, ((mask, "mask"),))
+        _mask_shape(mask, Tq)
+        mask_ptr = mask.data_ptr()
     o = _out(q, o_dtype)
     lse = q.new_empty((Hq, Tq), dtype=torch.float32)
-    lib = _lib.lib()
-    need = lib.pulsar_phase2_sparse_workspace_bytes(Tq, Hq, Hkv, d)
-    workspace = _scratch(workspace, need, q)
-    _here(q, K, V, sel, Kg, Vg, mask, workspace)
-    st = lib.pulsar_phase2_sparse(_ptr(q), _ptr(K), _ptr(V), _ptr(sel), n_shards, Tq, S, block,
-                                  sel.shape[3], _ptr(Kg), _ptr(Vg), G, _ptr(mask), Hq, Hkv, d,
-                                  scale, _ptr(o), o_dtype, _ptr(lse), _ptr(workspace), need,
-                                  _stream())
+    need = phase2_sparse_workspace_bytes(Tq, Hq, Hkv, d)
+    workspace, ws_ptr = _scratch(workspace, need, dev, q)
+    st = _lib.lib().pulsar_phase2_sparse(
+        q.data_ptr(), K.data_ptr(), V.data_ptr(), sel.data_ptr(), n_shards, Tq, S, block,
+        sel.shape[3], kg_ptr, vg_ptr, G, mask_ptr, Hq, Hkv, d,
+        1.0 / math.sqrt(d) if softmax_scale is None else softmax_scale, o.data_ptr(), o_dtype,
+        lse.data_ptr(), ws_ptr, need, _raw_stream(dev))
     _lib.check(st, "pulsar_phase2_sparse")
     return o, lse

@@ -90,7 +90,7 @@ int pulsar_block_select(const void* q, const void* bounds, int n_shards, int Tq,
 
 size_t pulsar_phase2_sparse_workspace_bytes(int Tq, int Hq, int Hkv, int d) {
   if (Tq < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || d < 1) return 0;
-  return (size_t)sparse_part_rows_most(Tq, Hkv) * Hq * (d + 1) * 4;
+  return (size_t)sparse_part_rows_most(Tq, Hkv, d) * Hq * (d + 1) * 4;
 }
 
 int pulsar_phase2_sparse(const void* q, const void* K, const void* V, const int32_t* sel,
@@ -119,7 +119,7 @@ int pulsar_phase2_sparse(const void* q, const void* K, const void* V, const int3
   if (Kg != nullptr && (!aligned16(Kg) || !aligned16(Vg))) return PULSAR_EINVAL;
 
   const int64_t gen_rows = Kg != nullptr ? G + Tq : 0;
-  const int parts = sparse_parts(Tq, Hq, Hkv, keys, gen_rows);
+  const int parts = sparse_parts(Tq, Hkv, d, keys, gen_rows);
   SparseLaunch a{};
   a.q = static_cast<const uint16_t*>(q);
   a.K = static_cast<const uint16_t*>(K);

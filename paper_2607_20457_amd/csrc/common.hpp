@@ -296,8 +296,8 @@ struct SparseLaunch {
   int64_t S, G;
   float scale;
 };
-int sparse_parts(int Tq, int Hq, int Hkv, int64_t keys, int64_t gen_rows);
-int64_t sparse_part_rows_most(int Tq, int Hkv);
+int sparse_parts(int Tq, int Hkv, int d, int64_t keys, int64_t gen_rows);
+int64_t sparse_part_rows_most(int Tq, int Hkv, int d);
 int launch_sparse(const SparseLaunch& a, int parts, void* o, int o_bf16, float* lse,
                   hipStream_t stream);
 

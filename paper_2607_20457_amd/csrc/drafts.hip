@@ -40,12 +40,8 @@ __global__ __launch_bounds__(256) void tree_mask_kernel(const int32_t* __restric
 int launch_tree_mask(const int32_t* parent, int T, uint32_t* mask, int32_t* depth,
                      hipStream_t stream) {
   if (T == 0) return PULSAR_OK;
-  const int lds = T * 4;
-  if (hipFuncSetAttribute((const void*)tree_mask_kernel,
-                          hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
-    return PULSAR_EHIP;
-  hipLaunchKernelGGL(tree_mask_kernel, dim3((T + 255) / 256), dim3(256), lds, stream, parent, T,
-                     mask, depth);
+  hipLaunchKernelGGL(tree_mask_kernel, dim3((T + 255) / 256), dim3(256), (size_t)T * 4, stream,
+                     parent, T, mask, depth);
   return hipGetLastError() == hipSuccess ? PULSAR_OK : PULSAR_EHIP;
 }
 

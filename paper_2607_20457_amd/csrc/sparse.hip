@@ -6,16 +6,20 @@
 // halves are a 32-key step.  A workgroup of four waves takes one part of the steps
 // of one (token, KV head, 16 heads of the group): wave w steps w, w + 4, ... of
 // it, on its own; then the four states are merged through LDS.  A step of a wave:
-//   K   straight into registers as the A operand of S^T = K Q^T (16x16x32): tile
-//       h holds half h, row r its key r, so that the scores of a lane are keys
-//       4g .. 4g+3 of both halves, which is how PV takes them in;
-//   V   into the wave's LDS double buffer by loads that write LDS directly, read
-//       transposed as the A operand of O^T += V^T P^T;
+//   K, V  into the wave's LDS stage by loads that write LDS directly, whole rows
+//       by neighbouring lanes (K straight into registers, where neighbouring lanes
+//       hold different rows, kept the L1 cache busy with 64 accesses a load
+//       instead of 16: 128 tokens over 4096 keys each 149 us);
+//   S^T = K Q^T (16x16x32): tile h holds half h, row r its key r, so that the
+//       scores of a lane are keys 4g .. 4g+3 of both halves, which is how PV takes
+//       them in; then O^T += V^T P^T with V read transposed;
 //   softmax  online, log2 domain; the reference is raised, O and the sums
 //       rescaled, when a step's maximum exceeds it by more than 2^8.  P enters PV
-//       rounded to bf16 (2^-9 of each weight), O is divided by the sum of those
-//       rounded weights, the log-sum-exp uses the fp32 sum.
-// The next step's K and V are in flight while a step is multiplied.
+//       rounded to bf16 (2^-8 of each weight at most), O is divided by the sum of
+//       those rounded weights, the log-sum-exp uses the fp32 sum.
+// The next step's K is sent for once the scores have consumed this one's, its V
+// once PV has: each has the time of a step to arrive, with one stage per wave, and
+// two waves per SIMD (four at d 64) hide each other's waits.
 //
 // Where the halves lie is worked out for 32 steps at a time, one half per lane:
 // the row, the rows that may be loaded and the rows that the token sees.  A row
@@ -25,7 +29,6 @@
 // Heads fill the 16 columns of a tile only where 16 heads share a KV head, but the
 // rows read from memory or L2 bound the kernel, not the matrix work.
 #include <algorithm>
-#include <type_traits>
 
 #include "tiles.hpp"
 
@@ -54,20 +57,27 @@ struct SparseArgs {
 
 template <int D>
 struct SpLds {
-  static constexpr int STAGE = SP_KEYS * D * 2;              // a V step
+  static constexpr int STAGE = SP_KEYS * D * 2;              // a K or V step
   static constexpr int LOOP = SP_WAVES * 2 * STAGE;
   static constexpr int PITCH = D + 4;                        // floats of a state's column
   static constexpr int MERGE = SP_WAVES * 16 * (PITCH + 3) * 4;
   static constexpr int BYTES = LOOP > MERGE ? LOOP : MERGE;
+  static_assert(BYTES <= 65536, "two workgroups per compute unit");
 };
 
-__device__ __forceinline__ int64_t lane_value64(uint32_t lo, uint32_t hi, int lane) {
-  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, lane) << 32 |
-                   (uint32_t)__builtin_amdgcn_readlane(lo, lane));
+// The largest of the four lanes r, r + 16, r + 32, r + 48.
+__device__ __forceinline__ float max_of_rows(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  const float y = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const uint32_t v = __float_as_uint(y);
+  const auto b = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
 template <int D, typename OUT>
-__global__ __launch_bounds__(64 * SP_WAVES) __attribute__((amdgpu_waves_per_eu(2, 2)))
+__global__ __launch_bounds__(64 * SP_WAVES)
+__attribute__((amdgpu_waves_per_eu(D == 128 ? 2 : 4, D == 128 ? 2 : 4)))
 void sparse_attn_kernel(SparseArgs a) {
   using L = SpLds<D>;
   constexpr int CPR = D / 8;               // 16-byte chunks per row
@@ -110,16 +120,15 @@ void sparse_attn_kernel(SparseArgs a) {
   }
 
   // ---- where the halves lie: lane 2i + h, half h of the wave's step base + i -----
-  // row: of K (or Kg); info: the rows it sees (16 bits), the last row that may be
-  // loaded (4 bits), whether it is the generation shard's; seen: rows to copy from
-  uint32_t tab_lo = 0, tab_hi = 0, tab_info = 0;
+  // Byte offset of the half's first row in K (or Kg), and its rows: those that the
+  // token sees (bits 0-15) and those to load (bits 16-31).  A half of which nothing
+  // is seen is loaded as its neighbour.
+  uint32_t tab_lo = 0, tab_hi = 0, tab_rows = 0;
   auto fill = [&](int base) {
     const int st = step0 + wave + SP_WAVES * (base + (lane >> 1));
     int64_t row = 0;
-    int rows = 0;  // loadable rows from `row` on
     uint32_t sees = 0;
-    const bool gen = st >= a.sparse_steps;
-    if (st < step1 && !gen) {
+    if (st < step1 && st < a.sparse_steps) {
       const int e = st * 2 + (lane & 1);
       const int entry = e >> a.half_log2;
       if (entry < a.entries) {
@@ -130,13 +139,12 @@ void sparse_attn_kernel(SparseArgs a) {
             ((int64_t)b << (a.half_log2 + 4)) + ((e & ((1 << a.half_log2) - 1)) << 4);
         if (b >= 0 && b < a.blocks && at < a.S) {
           row = shard * a.S + at;
-          rows = (int)min((int64_t)16, a.S - at);
-          sees = (1u << rows) - 1;
+          sees = (1u << (int)min((int64_t)16, a.S - at)) - 1;
         }
       }
     } else if (st < step1) {
       const int at = (st - a.sparse_steps) * SP_KEYS + (lane & 1) * 16;
-      rows = max(0, min(16, gen_end - at));
+      const int rows = min(16, gen_end - at);
       if (rows > 0) {
         row = at;
         sees = (1u << rows) - 1;
@@ -156,65 +164,81 @@ void sparse_attn_kernel(SparseArgs a) {
         }
       }
     }
-    // a half of which nothing is seen is loaded as its neighbour
-    const uint32_t lo = (uint32_t)row, hi = (uint32_t)((uint64_t)row >> 32);
+    const uint64_t off = (uint64_t)row * row_bytes;
+    const uint32_t lo = (uint32_t)off, hi = (uint32_t)(off >> 32);
     const uint32_t n_lo = __shfl_xor((int)lo, 1, 64), n_hi = __shfl_xor((int)hi, 1, 64);
     const uint32_t n_sees = __shfl_xor((int)sees, 1, 64);
     tab_lo = sees ? lo : n_lo;
     tab_hi = sees ? hi : n_hi;
-    tab_info = sees | (sees ? sees : n_sees) << 16;
+    tab_rows = sees | (sees ? sees : n_sees) << 16;
   };
   struct Half {
-    uint32_t sees, load;  // rows that count; rows to load from
-    int64_t row;
+    uint32_t sees, load;
+    int64_t off;
   };
   auto half = [&](int j, int h) {
     const int at = 2 * (j & 31) + h;
-    const uint32_t info = __builtin_amdgcn_readlane(tab_info, at);
-    return Half{info & 0xffffu, info >> 16, lane_value64(tab_lo, tab_hi, at)};
+    const uint32_t rows = __builtin_amdgcn_readlane(tab_rows, at);
+    return Half{rows & 0xffffu, rows >> 16,
+                (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane(tab_hi, at) << 32 |
+                          (uint32_t)__builtin_amdgcn_readlane(tab_lo, at))};
   };
 
   // ---- loads of one step --------------------------------------------------------
-  auto rsrc_of = [&](const uint16_t* base, int64_t row) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(base + row * a.Hkv * D),
-                                             (short)0, (int)(16 * row_bytes), kBufferFlags);
+  // Lane l of segment i fills the 16-byte chunk position (64 i + l) % CPR of row
+  // (64 i + l) / CPR of a half with the chunk that its swizzle puts there: for K,
+  // so that 16 rows' chunks of one column lie in different banks; for V, so that
+  // the 32 bytes that a transposing read takes of each of 8 rows do.
+  auto k_swizzle = [](int row) { return CPR == 16 ? row & 15 : (row >> 1) & 7; };
+  auto v_swizzle8 = [](int row) { return CPR == 16 ? 2 * (row & 7) : 2 * ((row >> 1) & 3); };
+  constexpr int H_SEGS = L::STAGE / 2048;  // 1 KiB segments of a half
+  constexpr int SEG_ROWS = 64 / CPR;
+  const int seg_row = lane / CPR;
+  uint32_t k_off[H_SEGS], v_off[H_SEGS];  // byte offsets of a lane from segment row 0
+#pragma unroll
+  for (int i = 0; i < H_SEGS; ++i) {
+    const int row = i * SEG_ROWS + seg_row, at = lane % CPR;
+    k_off[i] = head_off + seg_row * row_bytes + (uint32_t)(at ^ k_swizzle(row)) * 16u;
+    v_off[i] = head_off + seg_row * row_bytes + (uint32_t)(at ^ v_swizzle8(row)) * 16u;
+  }
+  lds_u8* const k_lds = (lds_u8*)smem + wave * 2 * L::STAGE;
+  lds_u8* const v_lds = k_lds + L::STAGE;
+  struct Step {
+    Half half[2];
+    bool gen;
   };
-  lds_u8* const wave_lds = (lds_u8*)smem + wave * 2 * L::STAGE;
-  // row i of a half, or the first one that is seen
-  auto seen_row = [](uint32_t load, int i) {
-    return (load >> i) & 1 ? i : __builtin_ctz(load | 0x10000u) & 15;
+  auto step_at = [&](int j) {
+    return Step{{half(j, 0), half(j, 1)}, step0 + wave + SP_WAVES * j >= a.sparse_steps};
   };
-  auto issue = [&](int j, bf16x8 (&kf)[2][DS], int stage) {
-    const uint32_t st = __builtin_amdgcn_readfirstlane(
-        (uint32_t)(uintptr_t)(wave_lds + stage * L::STAGE));
-    const bool gen = step0 + wave + SP_WAVES * j >= a.sparse_steps;
-    const uint16_t* const kb = gen ? a.Kg : a.K;
-    const uint16_t* const vb = gen ? a.Vg : a.V;
+  // A row that is not to be loaded is loaded as the first one that is.
+  auto issue = [&](const Step& x, const uint16_t* base, lds_u8* lds,
+                   const uint32_t (&off)[H_SEGS]) {
+    const uint32_t st = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)lds);
+    const bool whole = (x.half[0].load & x.half[1].load) == 0xffffu;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const Half x = half(j, h);
-      const __amdgpu_buffer_rsrc_t kr = rsrc_of(kb, x.row);
-      const uint32_t off = seen_row(x.load, r) * row_bytes + head_off + 16u * g;
+      const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
+          reinterpret_cast<uint8_t*>(const_cast<uint16_t*>(base)) + x.half[h].off, (short)0,
+          (int)(16 * row_bytes), kBufferFlags);
+      if (whole) {
 #pragma unroll
-      for (int s = 0; s < DS; ++s) {
-        const auto v = __builtin_amdgcn_raw_buffer_load_b128(kr, off + 64u * s, 0, 0);
-        kf[h][s] = __builtin_bit_cast(bf16x8, v);
-      }
-    }
+        for (int i = 0; i < H_SEGS; ++i)
+          lds_dma16(rsrc, off[i], i * SEG_ROWS * row_bytes, st + (h * H_SEGS + i) * 1024);
+      } else {
+        const uint32_t load = x.half[h].load;
+        const int first = __builtin_ctz(load | 0x10000u) & 15;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const Half x = half(j, h);
-      const __amdgpu_buffer_rsrc_t vr = rsrc_of(vb, x.row);
-#pragma unroll
-      for (int i = 0; i < V_SEGS / 2; ++i) {
-        const int slot = i * 64 + lane;  // chunk slot within the half
-        const int row = slot / CPR;
-        const int chunk = (slot % CPR) ^ v_swizzle<D>(row);
-        lds_dma16(vr, seen_row(x.load, row) * row_bytes + head_off + chunk * 16u,
-                  st + (h * (V_SEGS / 2) + i) * 1024);
+        for (int i = 0; i < H_SEGS; ++i) {
+          const int row = i * SEG_ROWS + seg_row;
+          const int from = (load >> row) & 1 ? row : first;
+          lds_dma16(rsrc, off[i] + (from - seg_row) * row_bytes, st + (h * H_SEGS + i) * 1024);
+        }
       }
     }
   };
+  uint32_t k_at[DS];  // chunk 4s + g of row r of a half
+#pragma unroll
+  for (int s = 0; s < DS; ++s) k_at[s] = (r * CPR + ((4 * s + g) ^ k_swizzle(r))) * 16;
   // V^T rows e*16 .. of the step: lane (r, g) of a transposing read addresses row
   // 4g + r/4 of a half at head_dim 16e + 4 (r%4) and receives head_dim 16e + r of
   // keys 4g .. 4g+3 of it
@@ -223,7 +247,7 @@ void sparse_attn_kernel(SparseArgs a) {
     const int row = 4 * g + (r >> 2), q4 = r & 3;
 #pragma unroll
     for (int e = 0; e < DT; ++e)
-      v_at[e] = row * (2 * D) + 16 * ((2 * e + (q4 >> 1)) ^ v_swizzle<D>(row)) + 8 * (q4 & 1);
+      v_at[e] = row * (2 * D) + 16 * ((2 * e + (q4 >> 1)) ^ v_swizzle8(row)) + 8 * (q4 & 1);
   }
   auto v_frag = [&](const lds_u8* sV, int e) -> bf16x8 {
     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(sV + v_at[e]));
@@ -238,27 +262,34 @@ void sparse_attn_kernel(SparseArgs a) {
   for (int e = 0; e < DT; ++e) acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m_run = -INFINITY, l_run = 0.f, lr_run = 0.f;
 
-  bf16x8 kbuf[2][2][DS];
+  Step next{};
   if (nsteps > 0) {
     fill(0);
-    issue(0, kbuf[0], 0);
+    next = step_at(0);
+    issue(next, next.gen ? a.Kg : a.K, k_lds, k_off);
+    issue(next, next.gen ? a.Vg : a.V, v_lds, v_off);
   }
-  // one step; KB = j % 2, a compile-time index into the register buffers
-  auto step = [&](int j, auto kb_tag) {
-    constexpr int KB = decltype(kb_tag)::value;
-    const uint32_t sees[2] = {half(j, 0).sees, half(j, 1).sees};
+  for (int j = 0; j < nsteps; ++j) {
+    const uint32_t sees[2] = {next.half[0].sees, next.half[1].sees};
+    const bool more = j + 1 < nsteps;
+    // K(j) is in LDS once only V(j)'s loads are outstanding
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(V_SEGS) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
     f32x4 S[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       S[h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < DS; ++s)
-        S[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kbuf[KB][h][s], qf[s], S[h], 0, 0, 0);
+        S[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            *reinterpret_cast<const lds_bf16x8*>(k_lds + h * (L::STAGE / 2) + k_at[s]), qf[s],
+            S[h], 0, 0, 0);
     }
-    const bool more = j + 1 < nsteps;
+    __builtin_amdgcn_sched_barrier(0);
     if (more) {
       if (((j + 1) & 31) == 0) fill(j + 1);
-      issue(j + 1, kbuf[KB ^ 1], KB ^ 1);
+      next = step_at(j + 1);
+      issue(next, next.gen ? a.Kg : a.K, k_lds, k_off);
     }
     __builtin_amdgcn_sched_barrier(0);
     if ((sees[0] & sees[1]) != 0xffffu) {
@@ -271,8 +302,7 @@ void sparse_attn_kernel(SparseArgs a) {
     float mx = S[0][0];
 #pragma unroll
     for (int v = 1; v < 8; ++v) mx = fmaxf(mx, S[v >> 2][v & 3]);
-    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c2;
+    mx = max_of_rows(mx) * c2;
     if (__any(mx > m_run + SP_SLACK)) {
       const float m_new = mx > m_run + SP_SLACK ? mx : m_run;
       const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
@@ -297,21 +327,18 @@ void sparse_attn_kernel(SparseArgs a) {
       for (int v = 0; v < 8; v += 2)
         lr_run = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{P[v], P[v + 1]}, kOnes2, lr_run, false);
     }
-    // V(j) is in LDS once only the loads issued after it are outstanding
+    // V(j) is in LDS once only K(j + 1)'s loads are outstanding
     __builtin_amdgcn_sched_barrier(0);
-    if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * DS + V_SEGS) : "memory");
+    if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(V_SEGS) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
     if ((sees[0] | sees[1]) != 0) {
-      const lds_u8* sV = wave_lds + KB * L::STAGE;
 #pragma unroll
       for (int e = 0; e < DT; ++e)
-        acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_frag(sV, e), P, acc[e], 0, 0, 0);
+        acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_frag(v_lds, e), P, acc[e], 0, 0, 0);
     }
-  };
-  for (int j = 0; j < nsteps; j += 2) {
-    step(j, std::integral_constant<int, 0>{});
-    if (j + 1 < nsteps) step(j + 1, std::integral_constant<int, 1>{});
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) issue(next, next.gen ? a.Vg : a.V, v_lds, v_off);
   }
 
   // ---- the four waves' states, merged through LDS ---------------------------------
@@ -362,20 +389,20 @@ void sparse_attn_kernel(SparseArgs a) {
 
 }  // namespace
 
-// Parts per (token, KV head): enough workgroups for two on each compute unit, at
-// least one step for each wave of a workgroup.
-constexpr int kSparseTarget = 512;
+// Parts per (token, KV head): enough workgroups for all that the chip holds at
+// once (two on each compute unit, four at d 64), at least one step for each wave of
+// a workgroup.
+static int sparse_target(int d) { return d == 64 ? 1024 : 512; }
 
-int sparse_parts(int Tq, int Hq, int Hkv, int64_t keys, int64_t gen_rows) {
+int sparse_parts(int Tq, int Hkv, int d, int64_t keys, int64_t gen_rows) {
   const int64_t steps = (keys + SP_KEYS - 1) / SP_KEYS + (gen_rows + SP_KEYS - 1) / SP_KEYS;
-  const int64_t wgs = (int64_t)Tq * Hkv;
   const int64_t most = (steps + SP_WAVES - 1) / SP_WAVES;
-  return (int)std::max<int64_t>(1, std::min(kSparseTarget / wgs, most));
+  return (int)std::max<int64_t>(1, std::min(sparse_target(d) / ((int64_t)Tq * Hkv), most));
 }
 
 // Rows of partials (tokens times parts) of any call of up to Tq tokens.
-int64_t sparse_part_rows_most(int Tq, int Hkv) {
-  return std::max<int64_t>(0, std::min<int64_t>((int64_t)Tq * kSparseTarget, kSparseTarget / Hkv));
+int64_t sparse_part_rows_most(int Tq, int Hkv, int d) {
+  return Tq > 0 ? sparse_target(d) / Hkv : 0;
 }
 
 int launch_sparse(const SparseLaunch& x, int parts, void* o, int o_bf16, float* lse,
@@ -409,10 +436,7 @@ int launch_sparse(const SparseLaunch& x, int parts, void* o, int o_bf16, float* 
   a.lse = lse;
   const int64_t nwg = (int64_t)a.Hkv * a.Tq * a.col_tiles * parts;
   if (nwg > 0x7fffffff) return PULSAR_EUNSUPPORTED;
-  const auto go = [&](auto kern, int lds) {
-    if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds) !=
-        hipSuccess)
-      return (int)PULSAR_EHIP;
+  const auto go = [&](auto kern, size_t lds) {
     hipLaunchKernelGGL(kern, dim3((unsigned)nwg), dim3(64 * SP_WAVES), lds, stream, a);
     return (int)(hipGetLastError() == hipSuccess ? PULSAR_OK : PULSAR_EHIP);
   };

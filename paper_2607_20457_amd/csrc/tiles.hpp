@@ -29,6 +29,15 @@ __device__ __forceinline__ void lds_dma16(__amdgpu_buffer_rsrc_t rsrc, uint32_t 
                : "memory");
 }
 
+// The same with a scalar byte offset added.
+__device__ __forceinline__ void lds_dma16(__amdgpu_buffer_rsrc_t rsrc, uint32_t voffset,
+                                          uint32_t soffset, uint32_t lds_base) {
+  asm volatile("buffer_load_dwordx4 %0, %1, %2 offen lds"
+               :
+               : "v"(voffset), "s"(rsrc), "s"(soffset), "{m0}"(lds_base)
+               : "memory");
+}
+
 // Bits 2 and 3 exchanged: with K row r of a 32-key step holding key
 // swap_bits23(r), the scores come out of the matrix unit in the layout that PV
 // takes them in.
