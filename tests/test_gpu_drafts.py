@@ -248,9 +248,18 @@ def test_compact(layers, capacity, Hkv, d, G, keep):
 
 def test_compact_random_lists():
     rng = np.random.default_rng(83)
-    for n in (5, 16, 17, 100, 333):
+    for n in (5, 16, 17, 32, 33, 100, 333):
         keep = np.sort(rng.choice(500, size=n, replace=False))
         _compact(3, 600, 4, 64, 100, keep, f"{n} of 500")
+        for bad in (0, n // 2, n - 1):  # where the list ends
+            cut = keep.copy()
+            cut[bad] = -1
+            _compact(1, 600, 3, 8, 100, cut, f"{n} of 500, -1 at {bad}")
+    # many batches of rows, few columns; rows that stay; columns beyond a power of two
+    _compact(1, 4100, 1, 64, 50, np.sort(rng.choice(4000, size=3000, replace=False)), "3000")
+    _compact(2, 2000, 5, 72, 9, np.r_[0:700, 701:1900], "the first 700 stay")
+    _compact(1, 1500, 1, 8, 0, np.arange(1, 1500), "all by one")
+    _compact(130, 60, 9, 64, 2, np.arange(3, 58), "many layers")
 
 
 def test_compact_past_two_gib():
