@@ -515,14 +515,17 @@ int pulsar_key_bounds(const void* K, int n_shards, int64_t S, int Hkv, int d, in
  * sel       out int32 [n_shards, Tq, Hkv, topk]: block indices, ascending.
  * scores    out float [n_shards, Tq, Hkv, blocks], nullable.
  * workspace device buffer of at least pulsar_block_select_workspace_bytes
- *           bytes, 16-byte aligned (may be NULL when scores is given); contents
- *           on entry do not matter.
+ *           bytes, 16-byte aligned (may be NULL when that is 0, as for few blocks
+ *           and tokens, or scores is given); contents on entry do not matter.
+ *           Other shapes, also smaller ones, ask again.
+ * Without scores the blocks are ranked by matrix products in fp32, and those whose
+ * order these leave open by their exact scores: the selection is the same.
  * EINVAL: negative sizes, Hq % Hkv != 0, topk > blocks, NULL or misaligned
  *         pointers when there is work.  EWORKSPACE: workspace too small.
  * EUNSUPPORTED: d not in {64, 128}; blocks > 32768; n_shards * Hkv > 65535;
  *         Tq > 524280 or n_shards * Tq * Hkv >= 2^31.
  */
-size_t pulsar_block_select_workspace_bytes(int n_shards, int Tq, int blocks, int Hkv);
+size_t pulsar_block_select_workspace_bytes(int n_shards, int Tq, int blocks, int Hq, int Hkv);
 int pulsar_block_select(const void* q, const void* bounds, int n_shards, int Tq, int blocks, int Hq,
                         int Hkv, int d, int topk, int32_t* sel, float* scores, void* workspace,
                         size_t workspace_bytes, void* stream);

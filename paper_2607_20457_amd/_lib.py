@@ -53,7 +53,7 @@ SIGNATURES = {
     "pulsar_kv_compact": (_c_int, [_vp, _vp, _c_int, _c_i64, _c_int, _c_int, _c_i64, _vp, _c_int,
                                    _vp]),
     "pulsar_key_bounds": (_c_int, [_vp, _c_int, _c_i64, _c_int, _c_int, _c_int, _vp, _vp]),
-    "pulsar_block_select_workspace_bytes": (_c_size, [_c_int, _c_int, _c_int, _c_int]),
+    "pulsar_block_select_workspace_bytes": (_c_size, [_c_int, _c_int, _c_int, _c_int, _c_int]),
     "pulsar_block_select": (_c_int, [_vp, _vp, _c_int, _c_int, _c_int, _c_int, _c_int, _c_int,
                                      _c_int, _vp, _vp, _vp, _c_size, _vp]),
     "pulsar_phase2_sparse_workspace_bytes": (_c_size, [_c_int, _c_int, _c_int, _c_int]),

@@ -466,8 +466,9 @@ def key_bounds(K, block: int):
     return bounds
 
 
-def block_select_workspace_bytes(n_shards: int, Tq: int, blocks: int, Hkv: int) -> int:
-    return int(_lib.lib().pulsar_block_select_workspace_bytes(n_shards, Tq, blocks, Hkv))
+@functools.lru_cache(maxsize=4096)
+def block_select_workspace_bytes(n_shards: int, Tq: int, blocks: int, Hq: int, Hkv: int) -> int:
+    return int(_lib.lib().pulsar_block_select_workspace_bytes(n_shards, Tq, blocks, Hq, Hkv))
 
 
 def block_select(q, bounds, topk: int, return_scores: bool = False, workspace=None):
@@ -486,7 +487,7 @@ def block_select(q, bounds, topk: int, return_scores: bool = False, workspace=No
     if return_scores:
         scores = q.new_empty((n_shards, Tq, Hkv, blocks), dtype=torch.float32)
     else:
-        need = block_select_workspace_bytes(n_shards, Tq, blocks, Hkv)
+        need = block_select_workspace_bytes(n_shards, Tq, blocks, Hq, Hkv)
         workspace, ws_ptr = _scratch(workspace, need, dev, q)
     st = _lib.lib().pulsar_block_select(q.data_ptr(), bounds.data_ptr(), n_shards, Tq, blocks, Hq,
                                         Hkv, d, topk, sel.data_ptr(), _ptr(scores), ws_ptr, need,

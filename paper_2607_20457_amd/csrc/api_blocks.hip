@@ -55,9 +55,10 @@ int pulsar_key_bounds(const void* K, int n_shards, int64_t S, int Hkv, int d, in
                            static_cast<uint16_t*>(bounds), (hipStream_t)stream);
 }
 
-size_t pulsar_block_select_workspace_bytes(int n_shards, int Tq, int blocks, int Hkv) {
-  if (n_shards < 0 || Tq < 0 || blocks < 0 || Hkv < 1) return 0;
-  return (size_t)n_shards * Tq * Hkv * blocks * 4;
+size_t pulsar_block_select_workspace_bytes(int n_shards, int Tq, int blocks, int Hq, int Hkv) {
+  if (n_shards < 0 || Tq < 0 || blocks < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0) return 0;
+  if (select_fused(Tq, blocks, Hq / Hkv)) return 0;
+  return (size_t)n_shards * Hkv * ((size_t)Tq * blocks + (blocks + 15) / 16) * 4;
 }
 
 int pulsar_block_select(const void* q, const void* bounds, int n_shards, int Tq, int blocks, int Hq,
@@ -74,18 +75,35 @@ int pulsar_block_select(const void* q, const void* bounds, int n_shards, int Tq,
   if (rows == 0 || blocks == 0 || (topk == 0 && scores == nullptr)) return PULSAR_OK;
   if (q == nullptr || bounds == nullptr || (topk > 0 && sel == nullptr)) return PULSAR_EINVAL;
   if (!aligned16(q) || !aligned16(bounds)) return PULSAR_EINVAL;
-  float* s = scores;
-  if (s == nullptr) {
+  PickLaunch a{};
+  a.q = static_cast<const uint16_t*>(q);
+  a.bounds = static_cast<const uint16_t*>(bounds);
+  a.n_shards = n_shards;
+  a.Tq = Tq;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.d = d;
+  a.blocks = blocks;
+  a.topk = topk;
+  a.sel = sel;
+  if (scores != nullptr) {
+    const int st = launch_block_scores(a.q, a.bounds, n_shards, Tq, Hq, Hkv, d, blocks, scores,
+                                       (hipStream_t)stream);
+    if (st != PULSAR_OK || topk == 0) return st;
+    a.scores = scores;
+  } else if (!select_fused(Tq, blocks, Hq / Hkv)) {
     if (workspace == nullptr || !aligned16(workspace) ||
-        workspace_bytes < pulsar_block_select_workspace_bytes(n_shards, Tq, blocks, Hkv))
+        workspace_bytes < pulsar_block_select_workspace_bytes(n_shards, Tq, blocks, Hq, Hkv))
       return PULSAR_EWORKSPACE;
-    s = static_cast<float*>(workspace);
+    float* const near = static_cast<float*>(workspace);
+    float* const norms = near + rows * blocks;
+    const int st = launch_block_near(a.q, a.bounds, n_shards, Tq, Hq, Hkv, d, blocks, near, norms,
+                                     (hipStream_t)stream);
+    if (st != PULSAR_OK) return st;
+    a.scores = near;
+    a.norms = norms;
   }
-  const int st =
-      launch_block_scores(static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(bounds),
-                          n_shards, Tq, Hq, Hkv, d, blocks, s, (hipStream_t)stream);
-  if (st != PULSAR_OK || topk == 0) return st;
-  return launch_block_topk(s, rows, blocks, topk, sel, (hipStream_t)stream);
+  return launch_block_pick(a, (hipStream_t)stream);
 }
 
 size_t pulsar_phase2_sparse_workspace_bytes(int Tq, int Hq, int Hkv, int d) {

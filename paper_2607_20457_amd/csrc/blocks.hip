@@ -3,7 +3,7 @@
 // topk blocks of each shard.
 #include <algorithm>
 
-#include "common.hpp"
+#include "tiles.hpp"
 
 namespace {
 
@@ -51,13 +51,13 @@ __global__ __launch_bounds__(256) void key_bounds_kernel(const uint16_t* __restr
 // Scores: score[shard][t][kvh][b] = max over the heads of the group of
 // sum_i max(q_i lo_i, q_i hi_i) = sum_i max(q_i, 0) hi_i + min(q_i, 0) lo_i, in
 // fp64 (the products are exact, so that equal sums come out equal whatever the
-// kernel's order) and rounded once to fp32.  A score that is not a number, as
-// from a bound that is not finite, ranks above all: +inf.
+// order) and rounded once to fp32.  A score that is not a number, as from a bound
+// that is not finite, ranks above all: +inf.
 //
-// A wave takes 16 blocks as the rows of 16x16x4 fp64 matrix products and walks
-// over tiles of 16 (token, head) columns.  Lane (r, g) holds channels
-// g D/4 .. of its block, so that it loads whole 16-byte pieces; the channels of a
-// product are then D/4 apart, the same for both operands.
+// Where the caller wants the scores: a wave takes 16 blocks as the rows of 16x16x4
+// fp64 matrix products and walks over tiles of 16 (token, head) columns.  Lane (r,
+// g) holds channels g D/4 .. of its block, so that it loads whole 16-byte pieces;
+// the channels of a product are then D/4 apart, the same for both operands.
 template <int D>
 __global__ __launch_bounds__(256) void block_scores_kernel(
     const uint16_t* __restrict__ q, const uint16_t* __restrict__ bounds, int Tq, int Hq, int Hkv,
@@ -129,80 +129,694 @@ __global__ __launch_bounds__(256) void block_scores_kernel(
 }
 
 // ---------------------------------------------------------------------------
+// Near scores, for the selection alone: the same sums by bf16 matrix products
+// (16x16x32, exact products, fp32 sums).  The fp64 products bound the exact form (64
+// tokens, 4096 blocks of 8 KV heads: 112 us at 69 TFLOP/s); the selection needs them
+// only for the few blocks whose near scores lie within their errors of the last one
+// that it keeps.
+//
+// Error.  A sum of n = 2 D products in any order, each addition off by at most
+// 2^-23 of the running size, is off by n 2^-23 times the size sum_i |q_i| m_i <=
+// |q| |m| of the block, with m_i the larger magnitude of lo_i and hi_i and |.| the
+// Euclidean norm (at random values a quarter above the sum itself).  The fiftieth on
+// top covers the norms' rounding and that of the exact score to fp32.  Where |q| |m|
+// leaves the fp32 range all blocks are scored exactly; kNearLeast covers products
+// that vanish in it.
+template <int D>
+constexpr float kNearError = 2 * D * 0x1p-23f * 1.02f;
+constexpr float kNearLeast = 0x1p-90f;
+
+// Rows of 16-byte chunks in LDS, the chunks of a row permuted by it, so that the
+// same chunk of eight rows lies in different banks: CPR chunks a row.
+template <int CPR>
+__device__ __forceinline__ int chunk_at(int row, int chunk) {
+  return row * CPR + (chunk ^ (CPR == 8 ? (row >> 1) & 7 : row & 7));
+}
+
+// Reductions over lanes without LDS: exchanges within a row of 16, then of rows.
+template <int CTRL>
+__device__ __forceinline__ int dpp(int x) {
+  return __builtin_amdgcn_mov_dpp(x, CTRL, 0xf, 0xf, true);
+}
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) { return (uint32_t)dpp<CTRL>((int)x); }
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __int_as_float(dpp<CTRL>(__float_as_int(x)));
+}
+template <int CTRL>
+__device__ __forceinline__ double dpp(double x) {
+  const u32x2 u = __builtin_bit_cast(u32x2, x);
+  return __builtin_bit_cast(double, u32x2{dpp<CTRL>(u[0]), dpp<CTRL>(u[1])});
+}
+constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140;
+// op over the 16 lanes of a row; every lane has the result.
+template <typename T, typename OP>
+__device__ __forceinline__ T over_row(T x, OP op) {
+  x = op(x, dpp<kSwap1>(x));
+  x = op(x, dpp<kSwap2>(x));
+  x = op(x, dpp<kMirror8>(x));
+  return op(x, dpp<kMirror16>(x));
+}
+template <typename OP>
+__device__ __forceinline__ uint32_t over_wave(uint32_t x, OP op) {
+  x = over_row(x, op);
+  const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = op(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return op(b[0], b[1]);
+}
+struct Least {
+  __device__ uint32_t operator()(uint32_t x, uint32_t y) const { return min(x, y); }
+};
+struct Most {
+  template <typename T>
+  __device__ T operator()(T x, T y) const { return max(x, y); }
+};
+// The largest of a row's values, none of them negative or NaN.
+__device__ __forceinline__ float max_of_row_floats(float x) {
+  return __int_as_float(over_row(__float_as_int(x), Most{}));
+}
+// The sum of the four lanes r, r + 16, r + 32, r + 48.
+__device__ __forceinline__ float sum_of_rows(float x) {
+  x += __shfl_xor(x, 16, 64);
+  return x + __shfl_xor(x, 32, 64);
+}
+// A sum of squares that fp32 holds well enough for a norm; others are formed in fp64,
+// in which no square of a bf16 leaves the range.
+__device__ __forceinline__ bool in_range(float x) { return x > 0x1p-80f && x < 0x1p126f; }
+__device__ __forceinline__ float norm_of(double x) {
+  const float y = (float)__builtin_sqrt(x);
+  return y == y ? y : INFINITY;
+}
+struct Sum {
+  template <typename T>
+  __device__ T operator()(T x, T y) const { return x + y; }
+};
+// The sum of the lanes below.
+__device__ __forceinline__ int scan_below(int x) {
+  int y = x;
+  y += __builtin_amdgcn_update_dpp(0, y, 0x111, 0xf, 0xf, false);  // 1, 2, 4, 8 to the right
+  y += __builtin_amdgcn_update_dpp(0, y, 0x112, 0xf, 0xf, false);
+  y += __builtin_amdgcn_update_dpp(0, y, 0x114, 0xf, 0xf, false);
+  y += __builtin_amdgcn_update_dpp(0, y, 0x118, 0xf, 0xf, false);
+  y += __builtin_amdgcn_update_dpp(0, y, 0x142, 0xa, 0xf, false);  // row ends to the next row
+  y += __builtin_amdgcn_update_dpp(0, y, 0x143, 0xc, 0xf, false);  // lane 31's to the upper half
+  return y - x;
+}
+// The largest of `width` neighbouring lanes of a row of 16 (base: the first one) for
+// each of N values, where they are a power of two by exchanges within the row.
+template <int N>
+__device__ __forceinline__ void max_of_columns(int (&x)[N], int width, int base) {
+  if ((width & (width - 1)) == 0) {
+    if (width >= 2)
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = max(x[i], dpp<kSwap1>(x[i]));
+    if (width >= 4)
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = max(x[i], dpp<kSwap2>(x[i]));
+    if (width >= 8)
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = max(x[i], dpp<kMirror8>(x[i]));
+    if (width >= 16)
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = max(x[i], dpp<kMirror16>(x[i]));
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    int y = x[i];
+    for (int j = 0; j < width; ++j) y = max(y, __shfl(x[i], min(base + j, 63), 64));
+    x[i] = y;
+  }
+}
+
+// Lane (r, g): channels 32 s + 8 g .. of row r of 16 staged block rows (lo, then hi).
+template <int D>
+struct BoundsTile {
+  bf16x8 lo[D / 32], hi[D / 32];
+  __device__ __forceinline__ void read(const u32x4* rows, int r, int g) {
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s) {
+      lo[s] = __builtin_bit_cast(bf16x8, rows[chunk_at<D / 4>(r, 4 * s + g)]);
+      hi[s] = __builtin_bit_cast(bf16x8, rows[chunk_at<D / 4>(r, D / 8 + 4 * s + g)]);
+    }
+  }
+  // The largest |m| of the 16 blocks.
+  __device__ __forceinline__ float norm() const {
+    float sum = 0.f;
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float l = (float)lo[s][i], h = (float)hi[s][i];
+        sum += fmaxf(l * l, h * h) + 0.f * (l + h);  // (what is not finite stays so)
+      }
+    sum = sum_of_rows(sum);
+    if (__any(!in_range(sum))) {
+      double wide = 0.;
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const double l = (double)(float)lo[s][i], h = (double)(float)hi[s][i];
+          wide += (l * l > h * h ? l * l : h * h) + 0. * (l + h);
+        }
+      wide += __shfl_xor(wide, 16, 64);
+      wide += __shfl_xor(wide, 32, 64);
+      return max_of_row_floats(norm_of(wide));
+    }
+    return max_of_row_floats(__builtin_sqrtf(sum));
+  }
+};
+// 16 block rows b0 .. of 4 D bytes each, whole rows by neighbouring lanes; a row past
+// the last is loaded as the last.
+template <int D>
+__device__ __forceinline__ void stage_bounds(const uint16_t* bounds, int b0, int blocks, int lane,
+                                             u32x4* rows) {
+  constexpr int CPR = D / 4, U = 16 * CPR / 64;
+  u32x4 x[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int i = u * 64 + lane;
+    x[u] = reinterpret_cast<const u32x4*>(
+        bounds)[(int64_t)min(b0 + i / CPR, blocks - 1) * CPR + i % CPR];
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int i = u * 64 + lane;
+    rows[chunk_at<CPR>(i / CPR, i % CPR)] = x[u];
+  }
+}
+// Column r of 16 staged rows of q, channels 32 s + 8 g ..
+template <int D>
+__device__ __forceinline__ void read_columns(const u32x4* rows, int r, int g,
+                                             bf16x8 (&x)[D / 32]) {
+#pragma unroll
+  for (int s = 0; s < D / 32; ++s)
+    x[s] = __builtin_bit_cast(bf16x8, rows[chunk_at<D / 8>(r, 4 * s + g)]);
+}
+
+// Near scores of 16 blocks (rows 4g + v) and 16 columns of q (lane (r, g): channels
+// 32 s + 8 g .. of column r).  As 16-bit integers the larger of a bf16 and 0 is its
+// positive part, the smaller its negative part.
+template <int D>
+__device__ __forceinline__ f32x4 near_scores(const BoundsTile<D>& b, const bf16x8 (&q)[D / 32]) {
+  f32x4 up = {0.f, 0.f, 0.f, 0.f}, down = up;
+#pragma unroll
+  for (int s = 0; s < D / 32; ++s) {
+    const s16x8 x = __builtin_bit_cast(s16x8, q[s]);
+    const bf16x8 pos = __builtin_bit_cast(bf16x8, __builtin_elementwise_max(x, (s16x8){}));
+    const bf16x8 neg = __builtin_bit_cast(bf16x8, __builtin_elementwise_min(x, (s16x8){}));
+    up = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.hi[s], pos, up, 0, 0, 0);
+    down = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.lo[s], neg, down, 0, 0, 0);
+  }
+  return up + down;
+}
+
+// Scores as integers of the same order (their own inverse), which take one
+// instruction to compare across lanes; -0 ranks below 0.
+__device__ __forceinline__ int ordered(int x) { return x ^ ((x >> 31) & 0x7fffffff); }
+constexpr int kLeast = (int)0x80000000;
+__device__ __forceinline__ float ordered_float(int x) { return __int_as_float(ordered(x)); }
+// near[row][b] for every row (shard, t, kvh), and norms[shard][kvh][b / 16], the
+// largest |m| of 16 blocks.  A workgroup holds 64 blocks and walks over units of 16
+// columns, eight of them staged at a time: 16 / group tokens, or 16 heads of one
+// token of a larger group, whose units follow one another.
+// (The blocks pass through the same LDS first, so that four workgroups fit a compute
+// unit: 64 tokens over 4096 blocks of 8 KV heads are then one round of them.)
+constexpr int kUnits = 8;
+template <int D>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4)))
+void block_near_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ bounds, int Tq,
+                       int Hq, int Hkv, int blocks, int units, int units_per_wg,
+                       float* __restrict__ near, float* __restrict__ norms) {
+  constexpr int CQ = D / 8;
+  constexpr int PER = 256 / (16 * CQ), U = kUnits / PER;  // a thread's units: every PER-th, U
+  __shared__ u32x4 s_rows[kUnits][16 * CQ];
+  static_assert(kUnits * CQ == 4 * (D / 4), "the blocks take as much");
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, g = lane >> 4;
+  const int group = Hq / Hkv;
+  const int64_t shard = blockIdx.y / Hkv;
+  const int kvh = (int)(blockIdx.y - shard * Hkv);
+  const int row_tile = blockIdx.x * 4 + wave, row_tiles = (blocks + 15) / 16;
+  const int b0 = row_tile * 16;
+  const int tokens = max(16 / group, 1);
+  const int passes = (group + 15) / 16;
+  const int width = min(group, 16);
+  const int tl = group >= 16 ? 0 : r / group;
+  const int base = lane - r + tl * width;
+  const int first = blockIdx.z * units_per_wg, last = min(first + units_per_wg, units);
+  // one chunk of U units from u0 on, all loads in flight
+  const int c = threadIdx.x / CQ % 16, chunk = threadIdx.x % CQ;
+  const int cl = group >= 16 ? 0 : c / group;
+  const int unit0 = wave / (4 / PER);
+  u32x4 staged[U];
+  auto fetch = [&](int u0) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int u = u0 + i * PER + unit0;
+      const int t = (passes == 1 ? u : u / passes) * tokens + cl;
+      const int h = group >= 16 ? (passes == 1 ? 0 : u % passes) * 16 + c : c - cl * group;
+      staged[i] = u32x4{0u, 0u, 0u, 0u};
+      if (u < last && cl < tokens && t < Tq && h < group)
+        staged[i] =
+            reinterpret_cast<const u32x4*>(q)[((int64_t)t * Hq + kvh * group + h) * CQ + chunk];
+    }
+  };
+  fetch(first);
+  BoundsTile<D> b;
+  {
+    u32x4* const mine = &s_rows[0][0] + wave * 16 * (D / 4);
+    stage_bounds<D>(bounds + (int64_t)blockIdx.y * blocks * 2 * D, b0, blocks, lane, mine);
+    b.read(mine, r, g);  // (the wave's own rows)
+  }
+  if (blockIdx.z == 0) {
+    const float norm = b.norm();
+    if (lane == 0 && b0 < blocks) norms[(int64_t)blockIdx.y * row_tiles + row_tile] = norm;
+  }
+  int top[4];  // of the 4 blocks of a lane
+  for (int u0 = first; u0 < last; u0 += kUnits) {
+    __syncthreads();  // the rows before have been read
+    const int n = min(kUnits, last - u0);
+#pragma unroll
+    for (int i = 0; i < U; ++i) s_rows[i * PER + unit0][chunk_at<CQ>(c, chunk)] = staged[i];
+    __syncthreads();
+    if (u0 + kUnits < last) fetch(u0 + kUnits);
+    for (int u = 0; u < n; ++u) {
+      const int t = (passes == 1 ? u0 + u : (u0 + u) / passes) * tokens + tl;
+      const int pass = passes == 1 ? 0 : (u0 + u) % passes;
+      bf16x8 x[D / 32];
+      read_columns<D>(s_rows[u], r, g, x);
+      const f32x4 score = near_scores<D>(b, x);
+      int now[4];
+#pragma unroll
+      for (int v = 0; v < 4; ++v) now[v] = ordered(__float_as_int(score[v]));
+      if (passes == 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top[i] = now[i];
+      } else {  // columns past the group's heads, staged as zeros, score nothing
+        const bool live = pass * 16 + r < group;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          top[i] = max(pass == 0 ? kLeast : top[i], live ? now[i] : kLeast);
+        if (pass + 1 < passes) continue;
+      }
+      int all[4] = {top[0], top[1], top[2], top[3]};
+      max_of_columns(all, width, base);
+      if (r != tl * width || tl >= tokens || t >= Tq || b0 >= blocks) continue;
+      const int64_t row = (shard * Tq + t) * Hkv + kvh;
+      float* const dst = near + row * blocks + b0 + 4 * g;
+      if ((blocks & 3) == 0 && b0 + 16 <= blocks) {
+        *reinterpret_cast<f32x4*>(dst) = f32x4{ordered_float(all[0]), ordered_float(all[1]),
+                                               ordered_float(all[2]), ordered_float(all[3])};
+      } else {
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+          if (b0 + 4 * g + v < blocks) dst[v] = ordered_float(all[v]);
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
 // The topk largest of a row of scores, in index order; of equal scores the lower
 // index.  W waves hold the row as rising integers in registers, R values per lane,
-// and bisect the value of the smallest one kept, counting with ballots.
+// and look for a value that topk of them reach: one wave bisects, counting with
+// ballots; several narrow the range by histograms of 256 bins in LDS (4096 values:
+// two to three rounds, where a bisection takes a barrier for each of about twelve).
+//
+// NEAR: the row holds near scores off by at most E.  With a the topk-th largest of
+// them and b the next, a - b > 2 E settles the selection.  Otherwise a block above
+// a + 2 E is kept, one below a - 2 E is not (at most topk - 1 exact scores lie above
+// a + E, and at least topk reach a - E), and those between are scored exactly, 16
+// lanes to a block, and take part in a second selection with their exact scores.
+//
+// FUSED: eight waves form the row's near scores first, 16 blocks at a time, and
+// hand them over through LDS.
 __device__ __forceinline__ uint32_t rising(float s) {
   const uint32_t u = __float_as_uint(s == 0.f ? 0.f : s);  // -0 ranks as 0
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+__device__ __forceinline__ float unrising(uint32_t k) {
+  return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
+}
+constexpr uint32_t kKept = 0xffffffffu;  // above every score's key; 0 is below
 
-template <int W, int R>
-__global__ __launch_bounds__(64 * W) void block_topk_kernel(const float* __restrict__ scores,
-                                                            int blocks, int topk,
-                                                            int32_t* __restrict__ sel) {
+enum PickMode : int { PICK_EXACT, PICK_NEAR, PICK_FUSED };
+constexpr int kFusedWaves = 8;
+constexpr int kFusedHeads = 64;    // heads per KV head that a fused row stages
+constexpr int kFusedBlocks = 512;  // and its blocks at most
+
+template <int D>
+struct FusedLds {
+  u32x4 bounds[kFusedWaves][16 * (D / 4)];
+  u32x4 q[kFusedHeads * (D / 8)];
+  uint32_t row[kFusedBlocks];
+  float norm[kFusedWaves];
+};
+
+// Near scores of a row into s_row; the largest |m| of the wave's blocks is returned.
+template <int D>
+__device__ __forceinline__ float fused_scores(const uint16_t* qt, const uint16_t* bt, int group,
+                                              int blocks, float* s_row, FusedLds<D>& l) {
+  constexpr int CQ = D / 8;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int r = lane & 15, g = lane >> 4;
+  float most = 0.f;
+  stage_bounds<D>(bt, wave * 16, blocks, lane, l.bounds[wave]);
+  for (int i = threadIdx.x; i < (group + 15) / 16 * 16 * CQ; i += 64 * kFusedWaves) {
+    const int c = i / CQ;
+    u32x4 x = {0u, 0u, 0u, 0u};
+    if (c < group) x = reinterpret_cast<const u32x4*>(qt)[i];
+    l.q[(c & ~15) * CQ + chunk_at<CQ>(c & 15, i % CQ)] = x;
+  }
+  __syncthreads();
+  for (int b0 = wave * 16; b0 < blocks; b0 += kFusedWaves * 16) {
+    BoundsTile<D> b;
+    b.read(l.bounds[wave], r, g);
+    most = fmaxf(most, b.norm());
+    int top[4] = {kLeast, kLeast, kLeast, kLeast};
+    for (int h0 = 0; h0 < group; h0 += 16) {
+      const bool live = h0 + r < group;
+      bf16x8 x[D / 32];
+      read_columns<D>(l.q + h0 * CQ, r, g, x);
+      const f32x4 score = near_scores<D>(b, x);
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+        top[v] = max(top[v], live ? ordered(__float_as_int(score[v])) : kLeast);
+    }
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const float x = ordered_float(over_row(top[v], Most{}));
+      if (r == 0 && b0 + 4 * g + v < blocks) s_row[b0 + 4 * g + v] = x;
+    }
+    if (b0 + kFusedWaves * 16 < blocks)
+      stage_bounds<D>(bt, b0 + kFusedWaves * 16, blocks, lane, l.bounds[wave]);
+  }
+  return most;
+}
+
+template <int D, int W, int R, int MODE>
+__global__ __launch_bounds__(MODE == PICK_FUSED ? 64 * kFusedWaves : 64 * W)
+void block_pick_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ bounds,
+                       const float* __restrict__ scores, const float* __restrict__ norms, int Tq,
+                       int Hq, int Hkv, int blocks, int topk, int32_t* __restrict__ sel) {
+  extern __shared__ uint32_t s_dynamic[];  // NEAR: [blocks]
+  uint32_t* s_row = s_dynamic;
   __shared__ int s_n[2][W];
   __shared__ int s_gt[W], s_eq[W];
   __shared__ uint32_t s_lo[W], s_hi[W];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ int s_bin[W > 1 ? 256 : 1], s_found[3];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t row = blockIdx.x;
-  const float* src = scores + row * blocks;
+  const int kvh = (int)(row % Hkv);
+  const int64_t st = row / Hkv;
+  const int t = (int)(st % Tq);
+  const int group = Hq / Hkv;
+  const uint16_t* const qt = q + ((int64_t)t * Hq + kvh * group) * D;
+  const uint16_t* const bt = bounds + ((st / Tq) * Hkv + kvh) * blocks * 2 * D;
+  const uint64_t below = (1ull << lane) - 1;
+
+  float most = 0.f;
+  if constexpr (MODE == PICK_FUSED) {
+    static_assert(W == 1, "one wave selects");
+    __shared__ FusedLds<D> s_fused;
+    s_row = s_fused.row;
+    const float mine =
+        fused_scores<D>(qt, bt, group, blocks, reinterpret_cast<float*>(s_row), s_fused);
+    if (lane == 0) s_fused.norm[wave] = mine;
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 0; w < kFusedWaves; ++w) most = fmaxf(most, s_fused.norm[w]);
+  } else if constexpr (MODE == PICK_NEAR) {
+    const int n = (blocks + 15) / 16;
+    const float* const p = norms + ((st / Tq) * Hkv + kvh) * n;
+    for (int i = tid; i < n; i += 64 * W) most = fmaxf(most, p[i]);
+  }
+  // the selecting waves meet; one alone only keeps its LDS accesses in order
+  auto sync = [&]() {
+    if constexpr (W > 1) {
+      __syncthreads();
+    } else {
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+  };
+
   const int i0 = wave * (64 * R) + lane;
-  uint32_t key[R];  // 0 past the row's end, below every score
-  uint32_t lo = 0xffffffffu, hi = 0;
+  uint32_t key[R];  // 0 past the row's end
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const int at = i0 + 64 * i;
-    key[i] = at < blocks ? rising(src[at]) : 0u;
-    lo = min(lo, at < blocks ? key[i] : 0xffffffffu);
-    hi = max(hi, key[i]);
+    if constexpr (MODE == PICK_FUSED)
+      key[i] = at < blocks ? rising(__uint_as_float(s_row[at])) : 0u;
+    else
+      key[i] = at < blocks ? rising(scores[row * blocks + at]) : 0u;
   }
-#pragma unroll
-  for (int x = 32; x >= 1; x >>= 1) {
-    lo = min(lo, (uint32_t)__shfl_xor((int)lo, x, 64));
-    hi = max(hi, (uint32_t)__shfl_xor((int)hi, x, 64));
-  }
-  if (W > 1) {
-    if (lane == 0) {
-      s_lo[wave] = lo;
-      s_hi[wave] = hi;
-    }
+  int turn = 0;
+  auto total = [&](int n) {  // over the waves
+    if (W == 1) return n;
+    if (lane == 0) s_n[turn & 1][wave] = n;
     __syncthreads();
+    n = 0;
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-      lo = min(lo, s_lo[w]);
-      hi = max(hi, s_hi[w]);
-    }
-  }
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  hi = __builtin_amdgcn_readfirstlane(hi);
-  // the largest value that at least topk scores reach
-  for (int it = 0; lo < hi; ++it) {
-    const uint32_t mid = lo + (hi - lo) / 2 + 1;
-    int n = 0;
-#pragma unroll
-    for (int i = 0; i < R; ++i) n += __popcll(__ballot(key[i] >= mid));
+    for (int w = 0; w < W; ++w) n += s_n[turn & 1][w];
+    ++turn;
+    return __builtin_amdgcn_readfirstlane(n);
+  };
+  auto spread = [&](uint32_t lo, uint32_t hi) {  // the smallest lo, the largest hi
+    lo = over_wave(lo, Least{});
+    hi = over_wave(hi, Most{});
     if (W > 1) {
-      if (lane == 0) s_n[it & 1][wave] = n;
       __syncthreads();
-      n = 0;
+      if (lane == 0) {
+        s_lo[wave] = lo;
+        s_hi[wave] = hi;
+      }
+      __syncthreads();
 #pragma unroll
-      for (int w = 0; w < W; ++w) n += s_n[it & 1][w];
-      n = __builtin_amdgcn_readfirstlane(n);
+      for (int w = 0; w < W; ++w) {
+        lo = min(lo, s_lo[w]);
+        hi = max(hi, s_hi[w]);
+      }
     }
-    if (n >= topk) lo = mid;
-    else hi = mid - 1;
-    if (n == topk) break;
+    return u32x2{(uint32_t)__builtin_amdgcn_readfirstlane(lo),
+                 (uint32_t)__builtin_amdgcn_readfirstlane(hi)};
+  };
+  // A value that `reach` >= topk keys reach, and fewer than topk a larger one where
+  // reach > topk.  `kept` keys are kKept, those that are 0 take no part.
+  uint32_t cut = 0;
+  int reach = 0;
+  auto find_cut = [&](int kept) {
+    uint32_t lo = kKept, hi = 0;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      // (as the last of all numbers a 0 is passed over, kKept as the first)
+      lo = min(lo, key[i] - 1);
+      hi = max(hi, key[i] + 1);
+    }
+    const u32x2 ends = spread(lo, hi);
+    lo = ends[0] + 1;
+    hi = ends[1] - 1;
+    if constexpr (W == 1) {
+      reach = 0;
+      while (lo < hi) {
+        const uint32_t mid = lo + (hi - lo) / 2 + 1;
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < R; ++i) n += __popcll(__ballot(key[i] >= mid));
+        if (n >= topk) {
+          lo = mid;
+          reach = n;
+        } else {
+          hi = mid - 1;
+        }
+        if (n == topk) break;
+      }
+      if (reach == 0) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) reach += __popcll(__ballot(key[i] >= lo));
+      }
+      cut = lo;
+    } else {
+      int above = kept;  // keys above hi
+      while (true) {
+        const uint32_t span = hi - lo;
+        const int shift = span > 255u ? 24 - __builtin_clz(span) : 0;  // span >> shift <= 255
+        for (int i = tid; i < 256; i += 64 * W) s_bin[i] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+          if (key[i] - lo <= span) atomicAdd(&s_bin[(key[i] - lo) >> shift], 1);
+        __syncthreads();
+        if (wave == 0) {  // four bins per lane, from the highest; counted from the top
+          int c[4], sum = 0;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            c[k] = s_bin[255 - 4 * lane - k];
+            sum += c[k];
+          }
+          int before = above + scan_below(sum);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if (before < topk && before + c[k] >= topk) {
+              s_found[0] = 255 - 4 * lane - k;
+              s_found[1] = before + c[k];
+              s_found[2] = before;
+            }
+            before += c[k];
+          }
+        }
+        __syncthreads();
+        const uint32_t bin = __builtin_amdgcn_readfirstlane(s_found[0]);
+        reach = __builtin_amdgcn_readfirstlane(s_found[1]);
+        above = __builtin_amdgcn_readfirstlane(s_found[2]);
+        lo += bin << shift;
+        hi = min(hi, lo + ((1u << shift) - 1));
+        cut = lo;
+        if (reach == topk || shift == 0) break;
+      }
+    }
+  };
+  find_cut(0);
+
+  if constexpr (MODE != PICK_EXACT) {
+    // the smallest key that reaches the cut, the largest that does not
+    uint32_t a = kKept, b = 0;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      if (key[i] >= cut) a = min(a, key[i]);
+      else b = max(b, key[i]);
+    }
+    const u32x2 ends = spread(a, b);
+    // the largest |q| of the group's heads: a wave takes every W-th
+    float norm = 0.f;
+    for (int h = wave; h < group; h += W) {
+      float y[D / 64], x = 0.f;
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) {
+        y[i] = __uint_as_float((uint32_t)qt[h * D + lane * (D / 64) + i] << 16);
+        x += y[i] * y[i];
+      }
+      x = sum_of_rows(over_row(x, Sum{}));
+      if (in_range(x)) {
+        norm = fmaxf(norm, __builtin_sqrtf(x));
+        continue;
+      }
+      double wide = 0.;
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) wide += (double)y[i] * (double)y[i];
+      wide = over_row(wide, Sum{});
+      wide += __shfl_xor(wide, 16, 64);
+      wide += __shfl_xor(wide, 32, 64);
+      norm = fmaxf(norm, norm_of(wide));
+    }
+    if (MODE == PICK_NEAR || W > 1) {  // (not negative: they rank as their bits)
+      norm = __uint_as_float(spread(0u, __float_as_uint(norm))[1]);
+      most = __uint_as_float(spread(0u, __float_as_uint(most))[1]);
+    }
+    const bool zeros = (norm == 0.f && most < INFINITY) || (most == 0.f && norm < INFINITY);
+    // (all scores of zeros are 0)
+    const float E = zeros ? 0.f : fmaxf(norm * most * kNearError<D>, kNearLeast);
+    const float fa = unrising(ends[0]);
+    const bool settled = topk == blocks ||
+                         (reach == topk && fa - unrising(ends[1]) > 2 * E) || zeros;
+    if (!settled) {
+      // an infinite E leaves all open
+      const bool none = !(E < INFINITY);
+      const uint32_t above = none ? kKept - 1 : rising(fa + 2 * E);
+      const uint32_t under = none ? 1u : rising(fa - 2 * E);
+      uint32_t open = 0;  // bit i: key i is to be scored
+      int n = 0, kept = 0;
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const bool in = key[i] > above, may = !in && key[i] >= under;
+        key[i] = in ? kKept : 0u;
+        if (may) open |= 1u << i;
+        n += __popcll(__ballot(may));
+        kept += __popcll(__ballot(in));
+      }
+      kept = total(kept);
+      // their indices, listed after those of the waves before
+      int at = 0, all = n;
+      if (W > 1) {
+        if (lane == 0) s_gt[wave] = n;
+        __syncthreads();
+        all = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+          at += w < wave ? s_gt[w] : 0;
+          all += s_gt[w];
+        }
+      }
+      const int mine = at;
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const uint64_t vote = __ballot((open >> i) & 1);
+        if ((open >> i) & 1) s_row[at + __popcll(vote & below)] = i0 + 64 * i;
+        at += __popcll(vote);
+      }
+      sync();
+      constexpr int N = D / 16;  // channels per lane
+      typedef __bf16 bf16xN __attribute__((ext_vector_type(N)));
+      typedef double f64xN __attribute__((ext_vector_type(N)));
+      const int sub = tid & 15;
+      for (int c = tid >> 4; c < all; c += 4 * W) {
+        const uint16_t* p = bt + (int64_t)s_row[c] * 2 * D + sub * N;
+        const auto lo = __builtin_convertvector(*reinterpret_cast<const bf16xN*>(p), f64xN);
+        const auto hi = __builtin_convertvector(*reinterpret_cast<const bf16xN*>(p + D), f64xN);
+        float best = -INFINITY;
+        constexpr int HU = 4;  // heads at a time
+        for (int h0 = 0; h0 < group; h0 += HU) {
+          bf16xN y[HU];
+#pragma unroll
+          for (int u = 0; u < HU; ++u)
+            y[u] = *reinterpret_cast<const bf16xN*>(qt + min(h0 + u, group - 1) * D + sub * N);
+#pragma unroll
+          for (int u = 0; u < HU; ++u) {
+            const auto z = __builtin_convertvector(y[u], f64xN);
+            double x = 0.;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+              x = __builtin_fma(z[i] < 0. ? 0. : z[i], hi[i], x);
+              x = __builtin_fma(z[i] < 0. ? z[i] : 0., lo[i], x);
+            }
+            const float s = (float)over_row(x, Sum{});
+            best = fmaxf(best, s != s ? INFINITY : s);
+          }
+        }
+        if (sub == 0) s_row[c] = rising(best);
+      }
+      sync();
+      at = mine;
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const uint64_t vote = __ballot((open >> i) & 1);
+        if ((open >> i) & 1) key[i] = s_row[at + __popcll(vote & below)];
+        at += __popcll(vote);
+      }
+      find_cut(kept);
+    }
   }
-  // all above it, and of those equal to it the first ones that still fit
+
+  // All that reach the cut, or all above it and of those equal to it the first ones
+  // that still fit.
+  const bool every = reach == topk;
   int gt = 0, eq = 0;
 #pragma unroll
   for (int i = 0; i < R; ++i) {
-    gt += __popcll(__ballot(key[i] > lo));
-    eq += __popcll(__ballot(key[i] == lo));
+    gt += __popcll(__ballot(every ? key[i] >= cut : key[i] > cut));
+    eq += __popcll(__ballot(!every && key[i] == cut));
   }
   int gt0 = 0, eq0 = 0, gts = gt;  // before this wave; in all
   if (W > 1) {
+    __syncthreads();
     if (lane == 0) {
       s_gt[wave] = gt;
       s_eq[wave] = eq;
@@ -217,13 +831,14 @@ __global__ __launch_bounds__(64 * W) void block_topk_kernel(const float* __restr
     }
   }
   const int room = topk - gts;
-  const uint64_t below = (1ull << lane) - 1;
 #pragma unroll
   for (int i = 0; i < R; ++i) {
-    const uint64_t vg = __ballot(key[i] > lo), ve = __ballot(key[i] == lo);
+    const bool over = every ? key[i] >= cut : key[i] > cut;
+    const bool level = !every && key[i] == cut;
+    const uint64_t vg = __ballot(over), ve = __ballot(level);
     const int e = eq0 + __popcll(ve & below);
     const int at = gt0 + __popcll(vg & below) + min(e, room);
-    if (key[i] > lo || (key[i] == lo && e < room)) sel[row * topk + at] = i0 + 64 * i;
+    if (over || (level && e < room)) sel[row * topk + at] = i0 + 64 * i;
     gt0 += __popcll(vg);
     eq0 += __popcll(ve);
   }
@@ -255,16 +870,59 @@ int launch_block_scores(const uint16_t* q, const uint16_t* bounds, int n_shards,
   return hipGetLastError() == hipSuccess ? PULSAR_OK : PULSAR_EHIP;
 }
 
-int launch_block_topk(const float* scores, int64_t rows, int blocks, int topk, int32_t* sel,
-                      hipStream_t stream) {
+int launch_block_near(const uint16_t* q, const uint16_t* bounds, int n_shards, int Tq, int Hq,
+                      int Hkv, int d, int blocks, float* near, float* norms, hipStream_t stream) {
+  const int group = Hq / Hkv, tokens = std::max(16 / group, 1), passes = (group + 15) / 16;
+  const int64_t units = (int64_t)((Tq + tokens - 1) / tokens) * passes;
+  // a token's passes stay in one workgroup
+  const int per = std::max(kUnits / passes, 1) * passes;
+  const int64_t z = (units + per - 1) / per;
+  if (units > 0x7fffffff || z > 65535) return PULSAR_EUNSUPPORTED;
+  const dim3 grid((blocks + 63) / 64, n_shards * Hkv, (unsigned)z);
+  const auto kern = d == 128 ? block_near_kernel<128> : block_near_kernel<64>;
+  hipLaunchKernelGGL(kern, grid, dim3(256), 0, stream, q, bounds, Tq, Hq, Hkv, blocks, (int)units,
+                     per, near, norms);
+  return hipGetLastError() == hipSuccess ? PULSAR_OK : PULSAR_EHIP;
+}
+
+namespace {
+template <int D, int MODE>
+int pick(const PickLaunch& a, hipStream_t stream) {
   const auto go = [&](auto kern, int waves) {
-    hipLaunchKernelGGL(kern, dim3((unsigned)rows), dim3(64 * waves), 0, stream, scores, blocks,
-                       topk, sel);
-    return hipGetLastError() == hipSuccess ? PULSAR_OK : PULSAR_EHIP;
+    const size_t lds = MODE == PICK_NEAR ? (size_t)a.blocks * 4 : 0;
+    if (lds > 32768) {
+      if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)lds) != hipSuccess)
+        return (int)PULSAR_EHIP;
+    }
+    hipLaunchKernelGGL(kern, dim3((unsigned)((int64_t)a.n_shards * a.Tq * a.Hkv)),
+                       dim3(64 * waves), lds, stream, a.q, a.bounds, a.scores, a.norms, a.Tq, a.Hq,
+                       a.Hkv, a.blocks, a.topk, a.sel);
+    return (int)(hipGetLastError() == hipSuccess ? PULSAR_OK : PULSAR_EHIP);
   };
-  if (blocks <= 256) return go(block_topk_kernel<1, 4>, 1);
-  if (blocks <= 1024) return go(block_topk_kernel<4, 4>, 4);
-  if (blocks <= 4096) return go(block_topk_kernel<16, 4>, 16);
-  if (blocks <= 16384) return go(block_topk_kernel<16, 16>, 16);
-  return go(block_topk_kernel<16, 32>, 16);
+  if constexpr (MODE == PICK_FUSED) {
+    return a.blocks <= 128 ? go(block_pick_kernel<D, 1, 2, MODE>, kFusedWaves)
+                           : go(block_pick_kernel<D, 1, 8, MODE>, kFusedWaves);
+  } else {
+    if (a.blocks <= 256) return go(block_pick_kernel<D, 1, 4, MODE>, 1);
+    if (a.blocks <= 1024) return go(block_pick_kernel<D, 4, 4, MODE>, 4);
+    if (a.blocks <= 4096) return go(block_pick_kernel<D, 8, 8, MODE>, 8);
+    if (a.blocks <= 16384) return go(block_pick_kernel<D, 16, 16, MODE>, 16);
+    return go(block_pick_kernel<D, 16, 32, MODE>, 16);
+  }
+}
+}  // namespace
+
+int launch_block_pick(const PickLaunch& a, hipStream_t stream) {
+  if (a.scores == nullptr)
+    return a.d == 128 ? pick<128, PICK_FUSED>(a, stream) : pick<64, PICK_FUSED>(a, stream);
+  if (a.norms == nullptr)
+    return a.d == 128 ? pick<128, PICK_EXACT>(a, stream) : pick<64, PICK_EXACT>(a, stream);
+  return a.d == 128 ? pick<128, PICK_NEAR>(a, stream) : pick<64, PICK_NEAR>(a, stream);
+}
+
+// A workgroup per row forms the scores itself where that is one launch of little
+// work: few blocks, and few tokens that would each read them again.
+bool select_fused(int Tq, int blocks, int group) {
+  return blocks <= kFusedBlocks && Tq <= 8 && group <= kFusedHeads;
 }

@@ -282,8 +282,20 @@ int launch_key_bounds(const uint16_t* K, int n_shards, int64_t S, int Hkv, int d
 constexpr int kMaxSelectBlocks = 32768;  // blocks per shard whose keys fit in LDS
 int launch_block_scores(const uint16_t* q, const uint16_t* bounds, int n_shards, int Tq, int Hq,
                         int Hkv, int d, int blocks, float* scores, hipStream_t stream);
-int launch_block_topk(const float* scores, int64_t rows, int blocks, int topk, int32_t* sel,
-                      hipStream_t stream);
+// Near scores [rows][blocks] of the rows (shard, token, KV head), and the norms
+// [n_shards][Hkv][ceil(blocks / 16)] that bound their errors.
+int launch_block_near(const uint16_t* q, const uint16_t* bounds, int n_shards, int Tq, int Hq,
+                      int Hkv, int d, int blocks, float* near, float* norms, hipStream_t stream);
+struct PickLaunch {
+  const uint16_t* q;
+  const uint16_t* bounds;
+  const float* scores;  // NULL: formed by the same launch
+  const float* norms;   // of near scores; NULL: the scores are exact
+  int n_shards, Tq, Hq, Hkv, d, blocks, topk;
+  int32_t* sel;
+};
+int launch_block_pick(const PickLaunch& a, hipStream_t stream);
+bool select_fused(int Tq, int blocks, int group);
 struct SparseLaunch {
   const uint16_t* q;    // bf16 [Tq, Hq, d]
   const uint16_t* K;    // bf16 [n_shards, S, Hkv, d]

@@ -65,16 +65,6 @@ struct SpLds {
   static_assert(BYTES <= 65536, "two workgroups per compute unit");
 };
 
-// The largest of the four lanes r, r + 16, r + 32, r + 48.
-__device__ __forceinline__ float max_of_rows(float x) {
-  const uint32_t u = __float_as_uint(x);
-  const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  const float y = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  const uint32_t v = __float_as_uint(y);
-  const auto b = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-
 template <int D, typename OUT>
 __global__ __launch_bounds__(64 * SP_WAVES)
 __attribute__((amdgpu_waves_per_eu(D == 128 ? 2 : 4, D == 128 ? 2 : 4)))

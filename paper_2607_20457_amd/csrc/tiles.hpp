@@ -38,6 +38,16 @@ __device__ __forceinline__ void lds_dma16(__amdgpu_buffer_rsrc_t rsrc, uint32_t 
                : "memory");
 }
 
+// The largest of the four lanes r, r + 16, r + 32, r + 48.
+__device__ __forceinline__ float max_of_rows(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  const float y = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const uint32_t v = __float_as_uint(y);
+  const auto b = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
 // Bits 2 and 3 exchanged: with K row r of a 32-key step holding key
 // swap_bits23(r), the scores come out of the matrix unit in the layout that PV
 // takes them in.

@@ -106,9 +106,10 @@ def test_block_select():
         assert call(**kw) == EINVAL, kw
     for kw in (dict(d=96), dict(blocks=32769), dict(n_shards=8192), dict(Tq=600000)):
         assert call(**kw) == EUNSUP, kw
-    need = P.block_select_workspace_bytes(2, 3, 50, 8)
-    assert need == 2 * 3 * 8 * 50 * 4
-    assert call(ws=None) == EWS and call(wsb=need - 1) == EWS and call(ws=FAKE + 8) == EWS
+    need = P.block_select_workspace_bytes(2, 3, 600, 32, 8)
+    assert need > 0
+    for kw in (dict(ws=None), dict(wsb=need - 1), dict(ws=FAKE + 8)):
+        assert call(blocks=600, **kw) == EWS, kw
     for kw in (dict(n_shards=0), dict(Tq=0), dict(blocks=0, topk=0), dict(topk=0, sel=None)):
         assert call(**kw, ws=None) == 0, kw
 

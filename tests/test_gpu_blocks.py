@@ -81,6 +81,19 @@ def test_block_select_near_ties():
     _select(1, 300, 4, 1, 128, 6, 50, 15, torch.from_numpy(x).to(torch.bfloat16))
 
 
+@pytest.mark.parametrize("blocks,Tq", [(90, 2), (700, 9), (5000, 2)])
+def test_block_select_of_zeros_and_tiny_values(blocks, Tq):
+    # all scores equal, by a query of zeros or keys of zeros; products that vanish in fp32
+    x = np.sort(f64(normal(18, (1, 1, blocks, 2, 64))), axis=3)
+    b = torch.from_numpy(x).to(torch.bfloat16)
+    q = normal(19, (Tq, 4, 64))
+    q[0] = 0
+    _select(1, blocks, 4, 1, 64, Tq, 11, 20, b, q)
+    _select(1, blocks, 4, 1, 64, Tq, 11, 20, torch.zeros_like(b))
+    q = normal(21, (Tq, 4, 64), 2.0 ** -70)
+    _select(1, blocks, 4, 1, 64, Tq, 11, 20, (b.double() * 2.0 ** -60).to(torch.bfloat16), q)
+
+
 def test_block_select_of_special_values():
     # a block with a bound that is not finite ranks first; large and tiny values
     x = np.sort(f64(normal(16, (1, 2, 80, 2, 64))), axis=3)
