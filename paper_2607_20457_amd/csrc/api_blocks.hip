@@ -108,7 +108,7 @@ int pulsar_block_select(const void* q, const void* bounds, int n_shards, int Tq,
 
 size_t pulsar_phase2_sparse_workspace_bytes(int Tq, int Hq, int Hkv, int d) {
   if (Tq < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || d < 1) return 0;
-  return (size_t)sparse_part_rows_most(Tq, Hkv, d) * Hq * (d + 1) * 4;
+  return (size_t)sparse_part_rows_most(Tq, Hq, Hkv, d) * Hq * (d + 1) * 4;
 }
 
 int pulsar_phase2_sparse(const void* q, const void* K, const void* V, const int32_t* sel,
@@ -137,7 +137,8 @@ int pulsar_phase2_sparse(const void* q, const void* K, const void* V, const int3
   if (Kg != nullptr && (!aligned16(Kg) || !aligned16(Vg))) return PULSAR_EINVAL;
 
   const int64_t gen_rows = Kg != nullptr ? G + Tq : 0;
-  const int parts = sparse_parts(Tq, Hkv, d, keys, gen_rows);
+  const SparsePlan plan = sparse_plan(n_shards, Tq, S, Hq, Hkv, d, block, topk, gen_rows);
+  const int parts = plan.parts;
   SparseLaunch a{};
   a.q = static_cast<const uint16_t*>(q);
   a.K = static_cast<const uint16_t*>(K);
@@ -157,7 +158,7 @@ int pulsar_phase2_sparse(const void* q, const void* K, const void* V, const int3
   a.G = G;
   a.scale = softmax_scale;
   const bool bf16 = o_dtype == PULSAR_OUT_BF16;
-  if (parts == 1) return launch_sparse(a, 1, o, bf16, lse, (hipStream_t)stream);
+  if (parts == 1) return launch_sparse(a, plan, o, bf16, lse, (hipStream_t)stream);
 
   const int64_t orows = (int64_t)parts * Tq * Hq;
   if (workspace == nullptr || !aligned16(workspace) ||
@@ -165,7 +166,7 @@ int pulsar_phase2_sparse(const void* q, const void* K, const void* V, const int3
     return PULSAR_EWORKSPACE;
   float* po = static_cast<float*>(workspace);
   float* pl = po + orows * d;
-  const int st = launch_sparse(a, parts, po, false, pl, (hipStream_t)stream);
+  const int st = launch_sparse(a, plan, po, false, pl, (hipStream_t)stream);
   if (st != PULSAR_OK) return st;
   return bf16 ? launch_lse_merge_bf16(po, pl, parts, Tq, Hq, d, o, lse, (hipStream_t)stream)
               : launch_lse_merge(po, pl, parts, 1, Tq, Hq, d, (int64_t)Tq * Hq * d,

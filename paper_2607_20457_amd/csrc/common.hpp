@@ -308,10 +308,21 @@ struct SparseLaunch {
   int64_t S, G;
   float scale;
 };
-int sparse_parts(int Tq, int Hkv, int d, int64_t keys, int64_t gen_rows);
-int64_t sparse_part_rows_most(int Tq, int Hkv, int d);
-int launch_sparse(const SparseLaunch& a, int parts, void* o, int o_bf16, float* lse,
+struct SparsePlan {
+  int tokens;  // per tile
+  int parts;   // of a tile's keys
+  int waves;   // of a workgroup
+};
+SparsePlan sparse_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int d, int block, int topk,
+                       int64_t gen_rows);
+int64_t sparse_part_rows_most(int Tq, int Hq, int Hkv, int d);
+int launch_sparse(const SparseLaunch& a, const SparsePlan& plan, void* o, int o_bf16, float* lse,
                   hipStream_t stream);
+// Partials over all rows of the shards and the first G appended rows, by the same
+// tiles.
+bool dense_tiles_apply(int Hq, int Hkv);
+int dense_parts(int n_shards, int Tq, int64_t S, int64_t G, int Hq, int Hkv, int d);
+int launch_dense(const SparseLaunch& a, int parts, float* o, float* lse, hipStream_t stream);
 
 // Rows of an assembled Phase-1 input gathered from a per-position tensor and
 // rotated per pos_mode (a pulsar_pos_mode).

@@ -1,11 +1,20 @@
-// Phase-2 attention of new tokens over the blocks of the retained shards that were
-// selected for each of them (and KV head), and over the generation shard.
+// Phase-2 attention of few new tokens by 16-row tiles of (token, head) rows: over
+// the blocks of the retained shards that were selected for each token (and KV head)
+// and over the generation shard; or over all keys, for the partials of drafts.
 //
-// Work.  A token's keys are a list of 16-key halves: the halves of its selected
-// blocks in the list's order, then those of the generation shard's rows.  Two
-// halves are a 32-key step.  A workgroup of four waves takes one part of the steps
-// of one (token, KV head, 16 heads of the group): wave w steps w, w + 4, ... of
-// it, on its own; then the four states are merged through LDS.  A step of a wave:
+// Work.  A tile is the columns of one pass over keys: one token's heads (16 of them
+// at a time), or as many tokens as fit.  Its keys are a list of 16-key halves, two of
+// them a 32-key step:
+//   LISTED  one token: its listed blocks in the list's order, then the generation
+//           shard's rows;
+//   UNION   several tokens: the blocks that any of them lists, each with the tokens
+//           that list it, found in LDS; then the generation shard's rows.  Where
+//           neighbouring tokens list the same blocks these are read and multiplied
+//           once, and else no column does more than it would alone;
+//   DENSE   all rows of the shards, then the appended rows.
+// A workgroup takes one part of the steps of one tile: wave w of NW the steps w,
+// w + NW, ... of it, on its own; then the waves' states are merged through LDS.  A
+// step of a wave:
 //   K, V  into the wave's LDS stage by loads that write LDS directly, whole rows
 //       by neighbouring lanes (K straight into registers, where neighbouring lanes
 //       hold different rows, kept the L1 cache busy with 64 accesses a load
@@ -21,110 +30,243 @@
 // once PV has: each has the time of a step to arrive, with one stage per wave, and
 // two waves per SIMD (four at d 64) hide each other's waits.
 //
-// Where the halves lie is worked out for 32 steps at a time, one half per lane:
-// the row, the rows that may be loaded and the rows that the token sees.  A row
-// that it does not see is loaded as a copy of one that it does, so that nothing
-// a masked row holds can reach the output; a step without any such row is left out.
-//
-// Heads fill the 16 columns of a tile only where 16 heads share a KV head, but the
-// rows read from memory or L2 bound the kernel, not the matrix work.
+// What must not be seen.  A row that no column sees is loaded as a copy of one that
+// some column does, and a step without any such row is left out.  Of the rows that
+// only some columns see, weights of zero keep the others clear of them unless they
+// hold a NaN or an infinity: a pass that ends with a NaN is repeated key by key, each
+// key's product taken over only into the columns that see it.
 #include <algorithm>
+#include <type_traits>
 
 #include "tiles.hpp"
 
 namespace {
 
-constexpr int SP_WAVES = 4;
 constexpr int SP_KEYS = 32;       // keys per step
 constexpr float SP_SLACK = 8.0f;  // log2 slack before the reference is raised
+// A union's list in LDS, in entries, and its map, a byte per block: as much as leaves
+// room for all the workgroups that the registers do.
+constexpr int sp_list(int d) { return d == 64 ? 1792 : 3072; }
+constexpr int sp_map(int d) { return d == 64 ? 32768 : 65536; }
+
+enum SparseMode : int { SP_LISTED, SP_UNION, SP_DENSE };
 
 struct SparseArgs {
   const uint16_t *q, *K, *V, *Kg, *Vg;
   const int32_t* sel;
   const uint32_t* mask;
-  int Tq, Hq, Hkv, group, col_tiles;
-  int topk, entries;     // listed blocks per shard; of all shards
+  int Tq, Hq, Hkv, group;
+  int tile_tokens;       // tokens per tile
+  int token_tiles;       // tiles over the tokens
+  int col_tiles;         // tiles over a token's heads (1 where a tile holds them all)
+  int n_shards, topk, entries;  // listed blocks per shard; of all shards
   int half_log2;         // log2 of a block's halves
   int blocks;            // blocks per shard
-  int gen_rows;          // G + Tq, or 0 without a generation shard
-  int64_t S, G;
-  int sparse_steps;      // steps of the listed blocks; the generation shard's follow
-  int parts, part_steps;
+  int gen_rows;          // G + Tq (DENSE: G), or 0 without a generation shard
+  int64_t S, G;          // (DENSE: S is of all shards)
+  int list_steps;        // LISTED, DENSE: steps of the shards; the generation shard's follow
+  int parts, part_steps; // (UNION: counted per tile)
   float scale_log2;
-  void* O;               // parts > 1: float [parts, Tq, Hq, D]; else the output
+  int o_bf16;
+  void* O;               // parts > 1, DENSE: float [parts, Tq, Hq, D]; else the output
   float* lse;            // [parts, Hq, Tq]; nullable for the output
 };
 
-template <int D>
+typedef __attribute__((address_space(4))) SparseArgs ConstArgs;
+
+template <int D, int NW, int MODE>
 struct SpLds {
   static constexpr int STAGE = SP_KEYS * D * 2;              // a K or V step
-  static constexpr int LOOP = SP_WAVES * 2 * STAGE;
+  static constexpr int LOOP = NW * 2 * STAGE;
   static constexpr int PITCH = D + 4;                        // floats of a state's column
-  static constexpr int MERGE = SP_WAVES * 16 * (PITCH + 3) * 4;
-  static constexpr int BYTES = LOOP > MERGE ? LOOP : MERGE;
-  static_assert(BYTES <= 65536, "two workgroups per compute unit");
+  static constexpr int MERGE = NW * 16 * (PITCH + 3) * 4;
+  static constexpr int REUSED = LOOP > MERGE ? LOOP : MERGE;
+  // UNION: the list, and the sums of its waves
+  static constexpr int LIST = sp_list(D);
+  static constexpr int BYTES = REUSED + (MODE == SP_UNION ? LIST * 4 + 64 : 0);
+  static_assert(MODE != SP_UNION || REUSED >= sp_map(D), "the map passes through the stages");
 };
 
-template <int D, typename OUT>
-__global__ __launch_bounds__(64 * SP_WAVES)
+template <int D, int NW, int MODE>
+__global__ __launch_bounds__(64 * NW)
 __attribute__((amdgpu_waves_per_eu(D == 128 ? 2 : 4, D == 128 ? 2 : 4)))
 void sparse_attn_kernel(SparseArgs a) {
-  using L = SpLds<D>;
+  using L = SpLds<D, NW, MODE>;
   constexpr int CPR = D / 8;               // 16-byte chunks per row
   constexpr int DS = D / 32;               // k-steps of S
   constexpr int DT = D / 16;               // 16-row tiles of O^T
   constexpr int V_SEGS = L::STAGE / 1024;  // 1 KiB segments: one 16-byte load per lane each
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
 
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // the arguments as they lie in memory, for what few steps need
+  // (kept in registers with the rest they do not fit)
+  auto reread = [&]() {
+    auto p = (const ConstArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return p;
+  };
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, g = lane >> 4;
-  // workgroup -> (KV head, token, heads, part), the KV head fastest: with eight of
-  // them each XCD reads one head's keys
+  // workgroup -> (KV head, token tile, heads, part), the KV head fastest: with eight
+  // of them each XCD reads one head's keys
   int64_t wg = blockIdx.x;
   const int kvh = (int)(wg % a.Hkv);
   wg /= a.Hkv;
-  const int t = (int)(wg % a.Tq);
-  wg /= a.Tq;
-  const int tile = (int)(wg % a.col_tiles);
+  const int t0 = (int)(wg % a.token_tiles) * a.tile_tokens;
+  wg /= a.token_tiles;
+  const int heads0 = (int)(wg % a.col_tiles) * 16;
   const int part = (int)(wg / a.col_tiles);
-  const int gen_end =
-      a.gen_rows == 0 ? 0 : a.mask ? a.gen_rows : (int)(a.G + t + 1);  // rows it may see
-  const int total = a.sparse_steps + (gen_end + SP_KEYS - 1) / SP_KEYS;
-  const int step0 = part * a.part_steps, step1 = min(step0 + a.part_steps, total);
-  const int nsteps = max(0, (step1 - step0 - wave + SP_WAVES - 1) / SP_WAVES);
+  const int tokens = min(a.tile_tokens, a.Tq - t0);  // of this tile
   const float c2 = a.scale_log2;
   const uint32_t row_bytes = (uint32_t)(a.Hkv * D * 2);
   const uint32_t head_off = (uint32_t)(kvh * D * 2);
 
-  // ---- Q fragments (B operand): column r = head tile * 16 + r of the group ------
-  const int col = tile * 16 + r;
-  const int head = kvh * a.group + col;
-  const bool live = col < a.group;
+  // ---- Q fragments (B operand): column r = token tl of the tile, head ------------
+  const int tl = a.tile_tokens == 1 ? 0 : r / a.group;
+  const int col = heads0 + r - tl * a.group;  // head of the group
+  const bool live = tl < tokens && col < a.group;
+  const int t = t0 + (live ? tl : 0);
+  const int head = kvh * a.group + (live ? col : 0);
   bf16x8 qf[DS];
   {
-    const bf16x8* src = reinterpret_cast<const bf16x8*>(
-                            a.q + ((int64_t)t * a.Hq + (live ? head : 0)) * D) + g;
+    const bf16x8* src =
+        reinterpret_cast<const bf16x8*>(a.q + ((int64_t)t * a.Hq + head) * D) + g;
 #pragma unroll
     for (int s = 0; s < DS; ++s) qf[s] = live ? src[4 * s] : bf16x8{};
   }
 
+  // ---- the union of the tile's lists --------------------------------------------
+  // A byte per block of all shards, bit i set where token i lists it, through the
+  // stages' LDS; then its non-zero bytes in order, block << 8 | byte.  A token that
+  // lists a block twice has its tile processed token by token (`doubled`).
+  uint32_t* const list = reinterpret_cast<uint32_t*>(smem + L::REUSED);
+  int listed = 0;
+  bool doubled = false;
+  if constexpr (MODE == SP_UNION) {
+    int* const s_sum = reinterpret_cast<int*>(list + L::LIST);
+    uint32_t* const map = reinterpret_cast<uint32_t*>(smem);
+    const int quads = (a.n_shards * a.blocks + 15) / 16;  // 16 blocks each
+    for (int i = tid; i < quads; i += 64 * NW)
+      reinterpret_cast<u32x4*>(map)[i] = u32x4{0u, 0u, 0u, 0u};
+    if (tid == 0) s_sum[NW] = 0;
+    __syncthreads();
+    const int per_token = a.entries;
+    for (int i = tid; i < tokens * per_token; i += 64 * NW) {
+      const int token = i / per_token, e = i - token * per_token;
+      const int shard = e / a.topk;
+      const int b = a.sel[(((int64_t)shard * a.Tq + t0 + token) * a.Hkv + kvh) * a.topk +
+                          (e - shard * a.topk)];
+      if (b < 0 || b >= a.blocks) continue;
+      const int at = shard * a.blocks + b;
+      const uint32_t bit = 1u << (8 * (at & 3) + token);
+      if (atomicOr(&map[at >> 2], bit) & bit) s_sum[NW] = 1;
+    }
+    __syncthreads();
+    doubled = __builtin_amdgcn_readfirstlane(s_sum[NW]) != 0;
+    for (int i0 = 0; i0 < quads; i0 += 64 * NW) {
+      u32x4 w = {0u, 0u, 0u, 0u};
+      if (i0 + tid < quads) w = reinterpret_cast<const u32x4*>(map)[i0 + tid];
+      int n = 0;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) n += ((w[k / 4] >> (8 * (k % 4))) & 0xffu) != 0;
+      int at = wave_excl_scan(n);
+      if (lane == 63) s_sum[wave] = at + n;
+      __syncthreads();
+      int sum = 0;
+#pragma unroll
+      for (int k = 0; k < NW; ++k) {
+        at += k < wave ? s_sum[k] : 0;
+        sum += s_sum[k];
+      }
+      at += listed;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const uint32_t who = (w[k / 4] >> (8 * (k % 4))) & 0xffu;
+        if (who) list[at++] = (16 * (i0 + tid) + k) << 8 | who;
+      }
+      listed += sum;
+      __syncthreads();
+    }
+    listed = __builtin_amdgcn_readfirstlane(listed);
+  }
+
+  // ---- the tile's steps -----------------------------------------------------------
+  // (`one`: the token whose list is read where a tile is processed token by token)
+  const uint32_t tile_bits = (1u << tokens) - 1;
+  const int gen_end = a.gen_rows == 0                ? 0
+                      : MODE == SP_DENSE || a.mask ? a.gen_rows
+                                                     : (int)(a.G + t0 + tokens);
+  int list_steps, step0, step1, nsteps, one = 0;
+  auto plan = [&]() {
+    const int halves = MODE == SP_UNION ? (doubled ? a.entries : listed) << a.half_log2 : 0;
+    list_steps = MODE == SP_UNION ? (halves + 1) / 2 : a.list_steps;
+    // the generation shard's rows once, with the first token's list
+    const int gen_steps = MODE == SP_UNION && one > 0 ? 0 : (gen_end + SP_KEYS - 1) / SP_KEYS;
+    const int total = list_steps + gen_steps;
+    const int per = MODE == SP_UNION ? (total + a.parts - 1) / a.parts : a.part_steps;
+    step0 = part * per;
+    step1 = min(step0 + per, total);
+    nsteps = max(0, (step1 - step0 - wave + NW - 1) / NW);
+  };
+  // The rows at .. at + 15 of the generation shard that token `token` sees.
+  auto gen_sees = [&](int at, int token) -> uint32_t {
+    const ConstArgs& a = *reread();
+    const int end = MODE == SP_DENSE || a.mask ? a.gen_rows : (int)(a.G + token + 1);
+    const int rows = min(16, end - at);
+    if (rows <= 0) return 0u;
+    uint32_t sees = (1u << rows) - 1;
+    if (MODE != SP_DENSE && a.mask != nullptr && at + rows > a.G) {
+      // drafts at - G .. are visible by the token's bits
+      const int words = (a.Tq + 31) / 32;
+      const uint32_t* bits = a.mask + (int64_t)token * words;
+      const int from = (int)(at - a.G);
+      uint64_t w;
+      if (from < 0) {
+        w = ((uint64_t)bits[0] << -from) | ((1u << -from) - 1);
+      } else {
+        const int i = from >> 5;
+        w = (bits[i] | (i + 1 < words ? (uint64_t)bits[i + 1] << 32 : 0)) >> (from & 31);
+      }
+      sees &= (uint32_t)w;
+    }
+    return sees;
+  };
+
   // ---- where the halves lie: lane 2i + h, half h of the wave's step base + i -----
-  // Byte offset of the half's first row in K (or Kg), and its rows: those that the
-  // token sees (bits 0-15) and those to load (bits 16-31).  A half of which nothing
-  // is seen is loaded as its neighbour.
-  uint32_t tab_lo = 0, tab_hi = 0, tab_rows = 0;
+  // Byte offset of the half's first row in K (or Kg), and its rows: those that some
+  // column sees (bits 0-15) and those to load (bits 16-31); UNION: the tokens that
+  // see a listed half.  A half of which nothing is seen is loaded as its neighbour.
+  uint32_t tab_lo = 0, tab_hi = 0, tab_rows = 0, tab_tokens = 0;
   auto fill = [&](int base) {
-    const int st = step0 + wave + SP_WAVES * (base + (lane >> 1));
+    const ConstArgs& a = *reread();
+    const int st = step0 + wave + NW * (base + (lane >> 1));
     int64_t row = 0;
-    uint32_t sees = 0;
-    if (st < step1 && st < a.sparse_steps) {
+    uint32_t sees = 0, who = tile_bits;
+    if (st < step1 && st < list_steps) {
       const int e = st * 2 + (lane & 1);
-      const int entry = e >> a.half_log2;
-      if (entry < a.entries) {
-        const int shard = entry / a.topk;
-        const int b = a.sel[(((int64_t)shard * a.Tq + t) * a.Hkv + kvh) * a.topk +
-                            (entry - shard * a.topk)];
+      if constexpr (MODE == SP_DENSE) {
+        const int64_t at = (int64_t)e * 16;
+        if (at < a.S) {
+          row = at;
+          sees = (1u << (int)min((int64_t)16, a.S - at)) - 1;
+        }
+      } else {
+        const int entry = e >> a.half_log2;
+        int shard = 0, b = -1;
+        if (MODE == SP_UNION && !doubled) {
+          if (entry < listed) {
+            const uint32_t x = list[entry];
+            who = x & 0xffu;
+            shard = (int)(x >> 8) / a.blocks;
+            b = (int)(x >> 8) - shard * a.blocks;
+          }
+        } else if (entry < a.entries) {
+          shard = entry / a.topk;
+          b = a.sel[(((int64_t)shard * a.Tq + t0 + one) * a.Hkv + kvh) * a.topk +
+                    (entry - shard * a.topk)];
+          who = 1u << one;
+        }
         const int64_t at =
             ((int64_t)b << (a.half_log2 + 4)) + ((e & ((1 << a.half_log2) - 1)) << 4);
         if (b >= 0 && b < a.blocks && at < a.S) {
@@ -133,25 +275,12 @@ void sparse_attn_kernel(SparseArgs a) {
         }
       }
     } else if (st < step1) {
-      const int at = (st - a.sparse_steps) * SP_KEYS + (lane & 1) * 16;
-      const int rows = min(16, gen_end - at);
-      if (rows > 0) {
-        row = at;
-        sees = (1u << rows) - 1;
-        if (a.mask != nullptr && at + rows > a.G) {
-          // drafts at - G .. are visible by the token's bits
-          const int words = (a.Tq + 31) / 32;
-          const uint32_t* bits = a.mask + (int64_t)t * words;
-          const int from = (int)(at - a.G);
-          uint64_t w;
-          if (from < 0) {
-            w = ((uint64_t)bits[0] << -from) | ((1u << -from) - 1);
-          } else {
-            const int i = from >> 5;
-            w = (bits[i] | (i + 1 < words ? (uint64_t)bits[i + 1] << 32 : 0)) >> (from & 31);
-          }
-          sees &= (uint32_t)w;
-        }
+      const int at = (st - list_steps) * SP_KEYS + (lane & 1) * 16;
+      row = at < gen_end ? at : 0;
+      if constexpr (MODE == SP_UNION) {
+        for (int i = 0; i < tokens; ++i) sees |= gen_sees(at, t0 + i);
+      } else {
+        sees = gen_sees(at, t0);
       }
     }
     const uint64_t off = (uint64_t)row * row_bytes;
@@ -161,15 +290,18 @@ void sparse_attn_kernel(SparseArgs a) {
     tab_lo = sees ? lo : n_lo;
     tab_hi = sees ? hi : n_hi;
     tab_rows = sees | (sees ? sees : n_sees) << 16;
+    // (a half that is not seen at all is seen by nobody: as its neighbour)
+    const uint32_t n_who = MODE == SP_UNION ? __shfl_xor((int)who, 1, 64) : 0u;
+    const uint32_t own = sees ? who : n_who, other = n_sees ? n_who : who;
+    tab_tokens = lane & 1 ? other | own << 8 : own | other << 8;
   };
   struct Half {
-    uint32_t sees, load;
+    uint32_t rows;  // seen, and << 16 to load
     int64_t off;
   };
   auto half = [&](int j, int h) {
     const int at = 2 * (j & 31) + h;
-    const uint32_t rows = __builtin_amdgcn_readlane(tab_rows, at);
-    return Half{rows & 0xffffu, rows >> 16,
+    return Half{(uint32_t)__builtin_amdgcn_readlane(tab_rows, at),
                 (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane(tab_hi, at) << 32 |
                           (uint32_t)__builtin_amdgcn_readlane(tab_lo, at))};
   };
@@ -195,16 +327,15 @@ void sparse_attn_kernel(SparseArgs a) {
   lds_u8* const v_lds = k_lds + L::STAGE;
   struct Step {
     Half half[2];
-    bool gen;
+    int st;
   };
-  auto step_at = [&](int j) {
-    return Step{{half(j, 0), half(j, 1)}, step0 + wave + SP_WAVES * j >= a.sparse_steps};
-  };
+  auto step_at = [&](int j) { return Step{{half(j, 0), half(j, 1)}, step0 + wave + NW * j}; };
+  auto is_gen = [&](const Step& x) { return x.st >= list_steps; };
   // A row that is not to be loaded is loaded as the first one that is.
   auto issue = [&](const Step& x, const uint16_t* base, lds_u8* lds,
                    const uint32_t (&off)[H_SEGS]) {
     const uint32_t st = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)lds);
-    const bool whole = (x.half[0].load & x.half[1].load) == 0xffffu;
+    const bool whole = (x.half[0].rows & x.half[1].rows) >> 16 == 0xffffu;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
@@ -215,7 +346,7 @@ void sparse_attn_kernel(SparseArgs a) {
         for (int i = 0; i < H_SEGS; ++i)
           lds_dma16(rsrc, off[i], i * SEG_ROWS * row_bytes, st + (h * H_SEGS + i) * 1024);
       } else {
-        const uint32_t load = x.half[h].load;
+        const uint32_t load = x.half[h].rows >> 16;
         const int first = __builtin_ctz(load | 0x10000u) & 15;
 #pragma unroll
         for (int i = 0; i < H_SEGS; ++i) {
@@ -248,97 +379,172 @@ void sparse_attn_kernel(SparseArgs a) {
   };
 
   f32x4 acc[DT];
+  float m_run, l_run, lr_run;
+  auto clear = [&]() {
 #pragma unroll
-  for (int e = 0; e < DT; ++e) acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m_run = -INFINITY, l_run = 0.f, lr_run = 0.f;
-
-  Step next{};
-  if (nsteps > 0) {
-    fill(0);
-    next = step_at(0);
-    issue(next, next.gen ? a.Kg : a.K, k_lds, k_off);
-    issue(next, next.gen ? a.Vg : a.V, v_lds, v_off);
-  }
-  for (int j = 0; j < nsteps; ++j) {
-    const uint32_t sees[2] = {next.half[0].sees, next.half[1].sees};
-    const bool more = j + 1 < nsteps;
-    // K(j) is in LDS once only V(j)'s loads are outstanding
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(V_SEGS) : "memory");
-    __builtin_amdgcn_sched_barrier(0);
-    f32x4 S[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      S[h] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int s = 0; s < DS; ++s)
-        S[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-            *reinterpret_cast<const lds_bf16x8*>(k_lds + h * (L::STAGE / 2) + k_at[s]), qf[s],
-            S[h], 0, 0, 0);
+    for (int e = 0; e < DT; ++e) acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m_run = -INFINITY;
+    l_run = lr_run = 0.f;
+  };
+  // The wave's steps of the present plan; `guard`: key by key (see above).
+  auto run = [&](auto guard_tag) {
+    constexpr bool guard = decltype(guard_tag)::value;
+    Step next{};
+    if (nsteps > 0) {
+      fill(0);
+      next = step_at(0);
+      issue(next, is_gen(next) ? a.Kg : a.K, k_lds, k_off);
+      issue(next, is_gen(next) ? a.Vg : a.V, v_lds, v_off);
     }
-    __builtin_amdgcn_sched_barrier(0);
-    if (more) {
-      if (((j + 1) & 31) == 0) fill(j + 1);
-      next = step_at(j + 1);
-      issue(next, next.gen ? a.Kg : a.K, k_lds, k_off);
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    if ((sees[0] & sees[1]) != 0xffffu) {
+    for (int j = 0; j < nsteps; ++j) {
+      // the keys of the step that some column sees, and the tokens that list it
+      const uint32_t seen = (next.half[0].rows & 0xffffu) | next.half[1].rows << 16;
+      const int st = next.st;
+      const uint32_t who =
+          MODE == SP_UNION ? (uint32_t)__builtin_amdgcn_readlane(tab_tokens, 2 * (j & 31)) : 0u;
+      const bool more = j + 1 < nsteps;
+      // K(j) is in LDS once only V(j)'s loads are outstanding
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(V_SEGS) : "memory");
+      __builtin_amdgcn_sched_barrier(0);
+      f32x4 S[2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < 2; ++h) {
+        S[h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int v = 0; v < 4; ++v)
-          if (!((sees[h] >> (4 * g + v)) & 1)) S[h][v] = -INFINITY;
-    }
-    float mx = S[0][0];
-#pragma unroll
-    for (int v = 1; v < 8; ++v) mx = fmaxf(mx, S[v >> 2][v & 3]);
-    mx = max_of_rows(mx) * c2;
-    if (__any(mx > m_run + SP_SLACK)) {
-      const float m_new = mx > m_run + SP_SLACK ? mx : m_run;
-      const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
-#pragma unroll
-      for (int e = 0; e < DT; ++e) acc[e] *= alpha;
-      l_run *= alpha;
-      lr_run *= alpha;
-      m_run = m_new;
-    }
-    // a column that has seen no key takes its weights against 0: they come out 0
-    const float m_use = m_run == -INFINITY ? 0.f : m_run;
-    bf16x8 P;
-    {
-      f32x8 p;
-#pragma unroll
-      for (int v = 0; v < 8; ++v) {
-        p[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[v >> 2][v & 3], c2, -m_use));
-        l_run += p[v];
+        for (int s = 0; s < DS; ++s)
+          S[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              *reinterpret_cast<const lds_bf16x8*>(k_lds + h * (L::STAGE / 2) + k_at[s]), qf[s],
+              S[h], 0, 0, 0);
       }
-      P = __builtin_convertvector(p, bf16x8);
+      __builtin_amdgcn_sched_barrier(0);
+      if (more) {
+        if (((j + 1) & 31) == 0) fill(j + 1);
+        next = step_at(j + 1);
+        issue(next, is_gen(next) ? a.Kg : a.K, k_lds, k_off);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      // UNION: a column sees all of the step's keys or none where all rows are seen and
+      // both halves are listed by the same tokens (`every`), else some of them
+      uint32_t vis = seen;
+      bool every = true, mine = true;
+      if constexpr (MODE == SP_UNION) {
+        if (st < list_steps) {
+          every = !guard && seen == 0xffffffffu && (who & 0xffu) == who >> 8;
+          mine = (who >> tl) & 1;
+          if (!every)
+            vis &= (mine ? 0xffffu : 0u) | ((who >> (8 + tl)) & 1 ? 0xffff0000u : 0u);
+        } else {
+          const int at = (st - list_steps) * SP_KEYS;
+          if (a.mask != nullptr || at + SP_KEYS > a.G) {
+            vis = gen_sees(at, t) | gen_sees(at + 16, t) << 16;
+            every = false;
+          }
+        }
+      }
+      if (MODE == SP_UNION ? !every || seen != 0xffffffffu : seen != 0xffffffffu) {
 #pragma unroll
-      for (int v = 0; v < 8; v += 2)
-        lr_run = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{P[v], P[v + 1]}, kOnes2, lr_run, false);
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+            if (!((vis >> (16 * h + 4 * g + v)) & 1)) S[h][v] = -INFINITY;
+      }
+      float mx = S[0][0];
+#pragma unroll
+      for (int v = 1; v < 8; ++v) mx = fmaxf(mx, S[v >> 2][v & 3]);
+      mx = max_of_rows(mx) * c2;
+      if (MODE == SP_UNION && every) mx = mine ? mx : -INFINITY;
+      if (__any(mx > m_run + SP_SLACK)) {
+        const float m_new = mx > m_run + SP_SLACK ? mx : m_run;
+        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+#pragma unroll
+        for (int e = 0; e < DT; ++e) acc[e] *= alpha;
+        l_run *= alpha;
+        lr_run *= alpha;
+        m_run = m_new;
+      }
+      // a column that has seen no key takes its weights against 0: they come out 0
+      float m_use = m_run == -INFINITY ? 0.f : m_run;
+      // (against infinity the weights of a step that it does not see come out 0, or not
+      // a number, which the pass's end finds)
+      if (MODE == SP_UNION && every) m_use = mine ? m_use : INFINITY;
+      bf16x8 P;
+      {
+        f32x8 p;
+#pragma unroll
+        for (int v = 0; v < 8; ++v) {
+          p[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[v >> 2][v & 3], c2, -m_use));
+          l_run += p[v];
+        }
+        P = __builtin_convertvector(p, bf16x8);
+#pragma unroll
+        for (int v = 0; v < 8; v += 2)
+          lr_run = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{P[v], P[v + 1]}, kOnes2, lr_run, false);
+      }
+      // V(j) is in LDS once only K(j + 1)'s loads are outstanding
+      __builtin_amdgcn_sched_barrier(0);
+      if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(V_SEGS) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+      if (seen != 0) {
+        if constexpr (MODE == SP_UNION && guard) {
+          for (int k = 0; k < SP_KEYS; ++k) {
+            // key k sits in slots of lane group (k % 16) / 4
+            const int slot = (k & 3) + (k >> 4) * 4;
+            u32x4 keep = {0u, 0u, 0u, 0u};
+            if (g == ((k >> 2) & 3)) {
+#pragma unroll
+              for (int x = 0; x < 4; ++x)
+                keep[x] = slot >> 1 == x ? (slot & 1 ? 0xffff0000u : 0xffffu) : 0u;
+            }
+#pragma unroll
+            for (int e = 0; e < DT; ++e) {
+              const bf16x8 v = __builtin_bit_cast(
+                  bf16x8, __builtin_bit_cast(u32x4, v_frag(v_lds, e)) & keep);
+              const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P, acc[e], 0, 0, 0);
+              if ((vis >> k) & 1) acc[e] = x;
+            }
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < DT; ++e)
+            acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_frag(v_lds, e), P, acc[e], 0, 0, 0);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (more) issue(next, is_gen(next) ? a.Vg : a.V, v_lds, v_off);
     }
-    // V(j) is in LDS once only K(j + 1)'s loads are outstanding
-    __builtin_amdgcn_sched_barrier(0);
-    if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(V_SEGS) : "memory");
-    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-    if ((sees[0] | sees[1]) != 0) {
+  };
+  if constexpr (MODE == SP_UNION) {
+    __syncthreads();  // the map has been read: the stages are free
+    const int turns = doubled ? tokens : 1;
+    auto pass = [&](auto guard) {
+      clear();
+      for (one = 0; one < turns; ++one) {
+        plan();
+        run(guard);
+      }
+      bool bad = false;
 #pragma unroll
       for (int e = 0; e < DT; ++e)
-        acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_frag(v_lds, e), P, acc[e], 0, 0, 0);
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    if (more) issue(next, next.gen ? a.Vg : a.V, v_lds, v_off);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) bad |= acc[e][v] != acc[e][v];
+      return __builtin_amdgcn_readfirstlane(__any(bad)) != 0;
+    };
+    if (pass(std::false_type{})) pass(std::true_type{});
+  } else {
+    clear();
+    plan();
+    run(std::false_type{});
   }
 
-  // ---- the four waves' states, merged through LDS ---------------------------------
+  // ---- the waves' states, merged through LDS --------------------------------------
   l_run += __shfl_xor(l_run, 16, 64);
   l_run += __shfl_xor(l_run, 32, 64);
   lr_run += __shfl_xor(lr_run, 16, 64);
   lr_run += __shfl_xor(lr_run, 32, 64);
   __syncthreads();  // every wave is done with its stages
   float* const states = reinterpret_cast<float*>(smem);
-  float* const sums = states + SP_WAVES * 16 * L::PITCH;
+  float* const sums = states + NW * 16 * L::PITCH;
   {
     float* const mine = states + (wave * 16 + r) * L::PITCH;
 #pragma unroll
@@ -352,15 +558,16 @@ void sparse_attn_kernel(SparseArgs a) {
   __syncthreads();
   // thread -> (column, four consecutive values), a row of D / 4 threads at a time
   constexpr int DL = D / 4;
-  const int dv = threadIdx.x % DL;
-  for (int c = threadIdx.x / DL; c < min(16, a.group - tile * 16); c += 64 * SP_WAVES / DL) {
+  const int dv = tid % DL;
+  const int cols = a.tile_tokens == 1 ? min(16, a.group - heads0) : tokens * a.group;
+  for (int c = tid / DL; c < cols; c += 64 * NW / DL) {
     float m = -INFINITY, l = 0.f, lr = 0.f;
 #pragma unroll
-    for (int w = 0; w < SP_WAVES; ++w) m = fmaxf(m, sums[(w * 16 + c) * 3]);
+    for (int w = 0; w < NW; ++w) m = fmaxf(m, sums[(w * 16 + c) * 3]);
     const float use = m == -INFINITY ? 0.f : m;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < SP_WAVES; ++w) {
+    for (int w = 0; w < NW; ++w) {
       const float* x = sums + (w * 16 + c) * 3;
       const float e = __builtin_amdgcn_exp2f(x[0] - use);
       l += e * x[1];
@@ -368,35 +575,85 @@ void sparse_attn_kernel(SparseArgs a) {
       o += e * *reinterpret_cast<const f32x4*>(states + (w * 16 + c) * L::PITCH + 4 * dv);
     }
     o *= lr != 0.f ? 1.f / lr : 0.f;  // (a NaN score leaves a NaN sum)
-    const int hd = kvh * a.group + tile * 16 + c;
-    const int64_t at = ((int64_t)part * a.Tq + t) * a.Hq + hd;
-    static_cast<OUT*>(a.O)[at * DL + dv] = __builtin_convertvector(o, OUT);
+    const int ct = a.tile_tokens == 1 ? 0 : c / a.group;
+    const int hd = kvh * a.group + heads0 + c - ct * a.group;
+    const int64_t at = ((int64_t)part * a.Tq + t0 + ct) * a.Hq + hd;
+    if (a.o_bf16)
+      static_cast<bf16x4*>(a.O)[at * DL + dv] = __builtin_convertvector(o, bf16x4);
+    else
+      static_cast<f32x4*>(a.O)[at * DL + dv] = o;
     if (dv == 0 && a.lse != nullptr)
-      a.lse[((int64_t)part * a.Hq + hd) * a.Tq + t] =
+      a.lse[((int64_t)part * a.Hq + hd) * a.Tq + t0 + ct] =
           l != 0.f ? (m + __log2f(l)) * 0.69314718055994531f : -INFINITY;
   }
 }
 
+template <int D, int NW, int MODE>
+int launch_tiles(const SparseArgs& a, hipStream_t stream) {
+  constexpr size_t lds = SpLds<D, NW, MODE>::BYTES;
+  const int64_t nwg = (int64_t)a.Hkv * a.token_tiles * a.col_tiles * a.parts;
+  if (nwg > 0x7fffffff) return PULSAR_EUNSUPPORTED;
+  const auto kern = sparse_attn_kernel<D, NW, MODE>;
+  if (lds > 65536 &&
+      hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize,
+                          (int)lds) != hipSuccess)
+    return PULSAR_EHIP;
+  hipLaunchKernelGGL(kern, dim3((unsigned)nwg), dim3(64 * NW), lds, stream, a);
+  return hipGetLastError() == hipSuccess ? PULSAR_OK : PULSAR_EHIP;
+}
+
+// Workgroups of four waves that the chip holds at once: two on each compute unit,
+// four at d 64.
+int tiles_at_once(int d) { return d == 64 ? 1024 : 512; }
+
+int64_t steps_of(int64_t keys) { return (keys + SP_KEYS - 1) / SP_KEYS; }
+
 }  // namespace
 
-// Parts per (token, KV head): enough workgroups for all that the chip holds at
-// once (two on each compute unit, four at d 64), at least one step for each wave of
-// a workgroup.
-static int sparse_target(int d) { return d == 64 ? 1024 : 512; }
+// Tokens whose lists one tile reads together: as many as fit its 16 columns, where the
+// union's map and list hold them and the rows that the tokens read one by one are
+// enough to pay for finding it.  Tokens that draw a quarter of the same blocks each,
+// one by one / together, us: 128 tokens, 2.2 GB 84 / 71; 64 of 2 heads of 64 (8 KV
+// heads), 560 MB 31 / 27; 32 tokens, 290 MB 19 / 22; 16 tokens, 275 MB 24 / 27.  (The
+// more they share the more it gives.)
+constexpr int64_t kUnionBytes = 400 << 20;
 
-int sparse_parts(int Tq, int Hkv, int d, int64_t keys, int64_t gen_rows) {
-  const int64_t steps = (keys + SP_KEYS - 1) / SP_KEYS + (gen_rows + SP_KEYS - 1) / SP_KEYS;
-  const int64_t most = (steps + SP_WAVES - 1) / SP_WAVES;
-  return (int)std::max<int64_t>(1, std::min(sparse_target(d) / ((int64_t)Tq * Hkv), most));
+static int union_tokens(int Tq, int Hkv, int group, int d, int64_t blocks, int64_t entries,
+                        int64_t steps) {
+  const int fit = std::min(std::min(16 / group, 8), Tq);
+  if (fit < 2 || blocks > sp_map(d) || entries * fit > sp_list(d)) return 1;
+  return Tq * Hkv * steps * (SP_KEYS * d * 4) >= kUnionBytes ? fit : 1;
+}
+
+SparsePlan sparse_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int d, int block, int topk,
+                       int64_t gen_rows) {
+  SparsePlan p{};
+  const int group = Hq / Hkv;
+  const int64_t entries = S > 0 ? (int64_t)n_shards * topk : 0;
+  const int64_t steps = steps_of(entries * block) + steps_of(gen_rows);
+  p.tokens = union_tokens(Tq, Hkv, group, d, S > 0 ? n_shards * ((S + block - 1) / block) : 0,
+                          entries, steps);
+  const int64_t tiles = (int64_t)((Tq + p.tokens - 1) / p.tokens) * Hkv * ((group + 15) / 16);
+  p.waves = 4;
+  p.parts = (int)std::max<int64_t>(1, std::min(tiles_at_once(d) / tiles, (steps + 3) / 4));
+  // One token of few steps: eight waves, and no merge (4 x 8 blocks of 16 keys and 46
+  // rows, 18 steps: 7.2 us against 7.7 in five parts, and a launch less).
+  if (p.tokens == 1 && p.parts > 1 && steps <= 32) {
+    p.waves = 8;
+    p.parts = 1;
+  }
+  return p;
 }
 
 // Rows of partials (tokens times parts) of any call of up to Tq tokens.
-int64_t sparse_part_rows_most(int Tq, int Hkv, int d) {
-  return Tq > 0 ? sparse_target(d) / Hkv : 0;
+int64_t sparse_part_rows_most(int Tq, int Hq, int Hkv, int d) {
+  if (Tq <= 0) return 0;
+  // of tiles of several tokens: all of a tile's tokens have its parts
+  return (int64_t)tiles_at_once(d) / Hkv * std::min(std::max(std::min(16 / (Hq / Hkv), 8), 1), Tq);
 }
 
-int launch_sparse(const SparseLaunch& x, int parts, void* o, int o_bf16, float* lse,
-                  hipStream_t stream) {
+namespace {
+SparseArgs tile_args(const SparseLaunch& x, int tokens, int parts) {
   SparseArgs a{};
   a.q = x.q;
   a.K = x.K;
@@ -409,30 +666,60 @@ int launch_sparse(const SparseLaunch& x, int parts, void* o, int o_bf16, float* 
   a.Hq = x.Hq;
   a.Hkv = x.Hkv;
   a.group = x.Hq / x.Hkv;
+  a.tile_tokens = tokens;
+  a.token_tiles = (x.Tq + tokens - 1) / tokens;
   a.col_tiles = (a.group + 15) / 16;
+  a.n_shards = x.n_shards;
+  a.G = x.G;
+  a.parts = parts;
+  a.scale_log2 = x.scale * 1.4426950408889634f;
+  return a;
+}
+}  // namespace
+
+int launch_sparse(const SparseLaunch& x, const SparsePlan& p, void* o, int o_bf16, float* lse,
+                  hipStream_t stream) {
+  SparseArgs a = tile_args(x, p.tokens, p.parts);
   a.topk = x.topk;
   a.entries = x.S > 0 ? x.n_shards * x.topk : 0;
   a.half_log2 = __builtin_ctz(x.block) - 4;
   a.blocks = (int)((x.S + x.block - 1) / x.block);
+  if (a.entries == 0) a.n_shards = 0;
   a.gen_rows = x.Kg != nullptr ? (int)(x.G + x.Tq) : 0;
   a.S = x.S;
-  a.G = x.G;
-  a.sparse_steps = (int)(((int64_t)a.entries * x.block + SP_KEYS - 1) / SP_KEYS);
-  const int steps = a.sparse_steps + (a.gen_rows + SP_KEYS - 1) / SP_KEYS;
-  a.parts = parts;
-  a.part_steps = std::max(1, (steps + parts - 1) / parts);
-  a.scale_log2 = x.scale * 1.4426950408889634f;
+  a.list_steps = (int)steps_of((int64_t)a.entries * x.block);
+  const int64_t steps = a.list_steps + steps_of(a.gen_rows);
+  a.part_steps = (int)std::max<int64_t>(1, (steps + p.parts - 1) / p.parts);
+  a.O = o;
+  a.o_bf16 = o_bf16;
+  a.lse = lse;
+  if (p.tokens > 1)
+    return x.d == 128 ? launch_tiles<128, 4, SP_UNION>(a, stream)
+                      : launch_tiles<64, 4, SP_UNION>(a, stream);
+  if (p.waves == 8)
+    return x.d == 128 ? launch_tiles<128, 8, SP_LISTED>(a, stream)
+                      : launch_tiles<64, 8, SP_LISTED>(a, stream);
+  return x.d == 128 ? launch_tiles<128, 4, SP_LISTED>(a, stream)
+                    : launch_tiles<64, 4, SP_LISTED>(a, stream);
+}
+
+// Partials of all tokens over all rows of the shards and the first G appended rows.
+bool dense_tiles_apply(int Hq, int Hkv) { return Hq / Hkv <= 16; }
+int dense_parts(int n_shards, int Tq, int64_t S, int64_t G, int Hq, int Hkv, int d) {
+  const int tokens = 16 / (Hq / Hkv);
+  const int64_t tiles = (int64_t)((Tq + tokens - 1) / tokens) * Hkv;
+  const int64_t steps = steps_of(n_shards * S) + steps_of(G);
+  return (int)std::max<int64_t>(1, std::min(tiles_at_once(d) / tiles, (steps + 3) / 4));
+}
+int launch_dense(const SparseLaunch& x, int parts, float* o, float* lse, hipStream_t stream) {
+  SparseArgs a = tile_args(x, 16 / (x.Hq / x.Hkv), parts);
+  a.S = x.n_shards * x.S;
+  a.gen_rows = (int)x.G;
+  a.list_steps = (int)steps_of(a.S);
+  const int64_t steps = a.list_steps + steps_of(x.G);
+  a.part_steps = (int)std::max<int64_t>(1, (steps + parts - 1) / parts);
   a.O = o;
   a.lse = lse;
-  const int64_t nwg = (int64_t)a.Hkv * a.Tq * a.col_tiles * parts;
-  if (nwg > 0x7fffffff) return PULSAR_EUNSUPPORTED;
-  const auto go = [&](auto kern, size_t lds) {
-    hipLaunchKernelGGL(kern, dim3((unsigned)nwg), dim3(64 * SP_WAVES), lds, stream, a);
-    return (int)(hipGetLastError() == hipSuccess ? PULSAR_OK : PULSAR_EHIP);
-  };
-  if (o_bf16)
-    return x.d == 128 ? go(sparse_attn_kernel<128, bf16x4>, SpLds<128>::BYTES)
-                      : go(sparse_attn_kernel<64, bf16x4>, SpLds<64>::BYTES);
-  return x.d == 128 ? go(sparse_attn_kernel<128, f32x4>, SpLds<128>::BYTES)
-                    : go(sparse_attn_kernel<64, f32x4>, SpLds<64>::BYTES);
+  return x.d == 128 ? launch_tiles<128, 4, SP_DENSE>(a, stream)
+                    : launch_tiles<64, 4, SP_DENSE>(a, stream);
 }

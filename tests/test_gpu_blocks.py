@@ -220,12 +220,63 @@ def test_unseen_rows_may_hold_anything(Tq):
             assert torch.equal(a, b)
     # the causal form: later tokens' rows
     if Tq > 1:
-        args = (to_dev_bf16(q), to_dev_bf16(k), to_dev_bf16(v), dev_i32(sel), block)
-        ref = P.phase2_sparse(*args, to_dev_bf16(kg), to_dev_bf16(vg), G)
-        kg[G + 5:], vg[G + 5:] = 0x7FC0, 0x7F80
-        got = P.phase2_sparse(*args, to_dev_bf16(kg), to_dev_bf16(vg), G)
-        assert torch.equal(got[0][:5], ref[0][:5]) and torch.equal(got[1][:, :5], ref[1][:, :5])
-        assert torch.isnan(got[0][5:]).any()
+        got = P.phase2_sparse(*map(to_dev_bf16, (q, k, v)), dev_i32(sel), block,
+                              to_dev_bf16(np.where(np.arange(G + Tq)[:, None, None] < G + 5, kg,
+                                                   np.uint16(0x7FC0))),
+                              to_dev_bf16(np.where(np.arange(G + Tq)[:, None, None] < G + 5, vg,
+                                                   np.uint16(0x7F80))), G)
+        ref, keys = sparse_reference(q[:5], k, v, sel[:, :5], block, kg[:G + 5], vg[:G + 5], G, None,
+                                     1 / math.sqrt(d))
+        check(got[0][:5], got[1][:, :5], ref, keys, "causal")
+        assert torch.isnan(got[0][5:]).all()
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,block", [(16, 4, 128, 32), (8, 8, 64, 16), (4, 2, 128, 16)])
+def test_blocks_of_other_tokens_may_hold_anything(Hq, Hkv, d, block):
+    # neighbouring tokens list blocks of their own and shared ones; what a token's own
+    # block holds reaches no other token, and shows in that token
+    Tq, S, G = 11, 20 * block + 3, 7
+    q = normal(66, (Tq, Hq, d))
+    k, v = (normal(s, (1, S, Hkv, d)) for s in (67, 68))
+    kg, vg = (normal(s, (G + Tq, Hkv, d)) for s in (69, 70))
+    sel = np.empty((1, Tq, Hkv, 4), dtype=np.int64)
+    sel[0, :, :] = [0, 2, 4, 20]
+    sel[0, :, :, 3] = np.arange(Tq)[:, None] + 7
+    sel[0, 5, :, 0] = 20
+    ref, keys = sparse_reference(q, k, v, sel, block, kg, vg, G, None, 1 / math.sqrt(d))
+    for word in (0x7FC0, 0x7F80, 0xFF80):
+        bad = v.copy()
+        bad[0, 10 * block:11 * block] = word  # token 3's block
+        o, lse = P.phase2_sparse(*map(to_dev_bf16, (q, k, bad)), dev_i32(sel), block,
+                                 *map(to_dev_bf16, (kg, vg)), G)
+        assert not torch.isfinite(o[3]).any()
+        others = np.arange(Tq) != 3
+        part = (ref[0][others], ref[1][:, others], ref[2][others], ref[3])
+        check(o[torch.from_numpy(others).cuda()], lse[:, torch.from_numpy(others).cuda()], part,
+              keys, f"{word:x}")
+
+
+def test_sparse_tokens_that_share_lists():
+    # tiles of tokens whose lists are the same, overlap, or have nothing in common, in
+    # any order, and one token that lists a block twice
+    rng = np.random.default_rng(8)
+    for Hq, Hkv, d, Tq, ns, S, block, topk in (
+            (32, 8, 128, 13, 2, 1000, 32, 6), (16, 16, 64, 33, 3, 700, 16, 9),
+            (16, 2, 128, 6, 1, 4000, 64, 20), (4, 2, 64, 40, 2, 500, 16, 5)):
+        blocks = -(-S // block)
+        same = rng.permutation(blocks)[:topk]
+        sel = np.broadcast_to(same, (ns, Tq, Hkv, topk)).copy()
+        _sparse(Hq, Hkv, d, Tq, 5, ns, S, block, topk, 4170, sel=sel, what="the same lists")
+        for t in range(0, Tq, 2):
+            sel[:, t] = np.sort(rng.permutation(blocks)[:topk])
+        _sparse(Hq, Hkv, d, Tq, 5, ns, S, block, topk, 4171, sel=sel, what="some the same")
+        sel[ns - 1, Tq // 2, 0, 1] = sel[ns - 1, Tq // 2, 0, 0]
+        _sparse(Hq, Hkv, d, Tq, 5, ns, S, block, topk, 4172, sel=sel, what="one twice")
+
+
+def test_sparse_lists_too_long_for_a_union():
+    _sparse(4, 2, 64, 9, 3, 1, 14000, 16, 500, 4180, what="long lists")
+    _sparse(4, 1, 128, 3, 3, 70, 16 * 1000, 16, 1, 4181, what="many blocks")
 
 
 def test_sparse_of_every_block_is_the_query_step():
