@@ -450,9 +450,11 @@ int gen_min_keys(int query_rows, int64_t rows, int min_keys) {
 }
 
 struct QueryPlan {
+  bool dense;       // (drafts) everything in one launch of 16-row tiles
   bool decode;      // everything in one decode launch
   bool packed;      // everything in one packed launch
   bool gen_decode;  // the generation shard in a decode launch
+  bool gen_dense;   // (drafts) the appended rows in 16-row tiles
   bool gen_own;     // the generation shard's ranges have partials of their own
   int np_shard, np_gen;  // key ranges per shard / of the generation shard's rows
   int parts;
@@ -498,6 +500,21 @@ QueryPlan query_plan(int n_shards, int Tq, int64_t S, int64_t G, int Hq, int Hkv
   return p;
 }
 
+// Whether a draft's partials come from 16-row tiles, each of which reads all K/V: its
+// launch is short, and what the tiles read again comes from L2, so up to 280 MB over
+// all tiles (140 at d 64), and for one tile of heads of 128 whatever the length.
+// Drafts of 1 / 8 / 12 / 64 tokens, 32 / 8 heads of 128, query step's kernels / tiles,
+// us with the merge: 4 x 1021 keys 12.9 / 9.9, 15.9 / 13.6, 18.3 / 13.7, 39 / 24; 8 x
+// 4096 30 / 28, 41 / 33, 34 / 38, 67 / 114; 16 x 8192 102 / 98, 112 / 123, 104 / 147.
+// 16 / 16 heads of 64, 8 x 4096: 16 tokens (one tile) 30.2 / 29.9, 24 (two) 32 / 35; 8 /
+// 2 heads of 128: 16 tokens (four tiles of 34 MB) 21 / 17, 24 (six) 25.5 / 26.6.
+static bool dense_pays(int n_shards, int Tq, int64_t S, int64_t G, int Hq, int Hkv, int d) {
+  if (!dense_tiles_apply(Hq, Hkv)) return false;
+  const int64_t tokens = 16 / (Hq / Hkv), tiles = (Tq + tokens - 1) / tokens;
+  const int64_t bytes = (n_shards * S + G) * Hkv * d * 4;
+  return (tiles == 1 && d == 128) || tiles * bytes <= (d == 64 ? 140 : 280) * (int64_t)1000000;
+}
+
 // The plan of a draft: the shards and the G appended rows, all visible to every
 // token, in partials; the drafts' own rows are folded into the merge.  In each
 // kernel the ranges are those of a query step over G rows, so the query step's
@@ -506,6 +523,11 @@ QueryPlan tree_plan(int n_shards, int Tq, int64_t S, int64_t G, int Hq, int Hkv,
   QueryPlan p{};
   if (S <= 0) n_shards = 0;
   p.gen_own = true;
+  if (dense_pays(n_shards, Tq, S, G, Hq, Hkv, d)) {
+    p.dense = true;
+    p.parts = n_shards * S + G > 0 ? dense_parts(n_shards, Tq, S, G, Hq, Hkv, d) : 0;
+    return p;
+  }
   p.decode = decode_applies(Tq, Hq, Hkv, d);
   p.packed = !p.decode && packed_applies(Tq, Hq, Hkv, d);
   if (p.packed) {
@@ -520,6 +542,8 @@ QueryPlan tree_plan(int n_shards, int Tq, int64_t S, int64_t G, int Hq, int Hkv,
     return p;
   }
   const int rows = Tq * (Hq / Hkv);
+  // beside the attention kernel's shards, appended rows that a few tiles read
+  p.gen_dense = !p.decode && G > 0 && dense_pays(0, Tq, 0, G, Hq, Hkv, d);
   p.gen_decode = p.decode || (Hq / Hkv <= 32 && G <= kGenDecodeRows && rows <= kGenDecodeQueryRows);
   int min_keys = kDecodeMinKeys;
   if (p.decode) {
@@ -529,8 +553,9 @@ QueryPlan tree_plan(int n_shards, int Tq, int64_t S, int64_t G, int Hq, int Hkv,
     p.np_shard = n_shards > 0 ? attn_splits(n_shards, Tq, S, Hq, Hkv) : 0;
   }
   if (G > 0)
-    p.np_gen = p.gen_decode ? decode_parts(1, G, Hkv, gen_min_keys(rows, G, min_keys))
-                            : attn_splits(1, Tq, G, Hq, Hkv);
+    p.np_gen = p.gen_dense    ? dense_parts(0, Tq, 0, G, Hq, Hkv, d)
+               : p.gen_decode ? decode_parts(1, G, Hkv, gen_min_keys(rows, G, min_keys))
+                              : attn_splits(1, Tq, G, Hq, Hkv);
   p.parts = n_shards * p.np_shard + p.np_gen;
   return p;
 }
@@ -804,7 +829,13 @@ int pulsar_phase2_query_noalloc(const void* q, const void* Kg, const void* Vg, i
 
 size_t pulsar_phase2_tree_workspace_bytes(int n_shards, int Tq, int64_t S, int64_t G, int Hq,
                                           int Hkv, int d) {
-  return pulsar_phase2_query_workspace_bytes(n_shards, Tq, S, G, Hq, Hkv, d);
+  const size_t need = pulsar_phase2_query_workspace_bytes(n_shards, Tq, S, G, Hq, Hkv, d);
+  if (need == 0 || !dense_tiles_apply(Hq, Hkv)) return need;
+  // and the most partials of the 16-row tiles, in whichever number of parts: alone, or
+  // of the appended rows beside the attention kernel's
+  const int64_t rows = dense_part_rows_most(Tq, Hq, Hkv, d);
+  const size_t tiles = align16((size_t)rows * Hq * d * 4) + align16((size_t)rows * Hq * 4);
+  return decode_applies(Tq, Hq, Hkv, d) ? std::max(need, tiles) : need + tiles;
 }
 
 int pulsar_phase2_tree(const void* q, const void* Kg, const void* Vg, int64_t G,
@@ -836,22 +867,40 @@ int pulsar_phase2_tree(const void* q, const void* Kg, const void* Vg, int64_t G,
   DecodeGen gen{kg, vg, G, plan.np_gen, plan.gen_own};
   gen.cached = true;
   int rc = PULSAR_OK;
-  if (plan.decode || plan.packed) {
+  SparseLaunch tiles{};
+  tiles.q = q16;
+  tiles.K = static_cast<const uint16_t*>(K);
+  tiles.V = static_cast<const uint16_t*>(V);
+  tiles.Kg = kg;
+  tiles.Vg = vg;
+  tiles.n_shards = plan.dense ? n_shards : 0;
+  tiles.Tq = Tq;
+  tiles.Hq = Hq;
+  tiles.Hkv = Hkv;
+  tiles.d = d;
+  tiles.S = S;
+  tiles.G = G;
+  tiles.scale = softmax_scale;
+  if (plan.dense) {
+    if (plan.parts > 0) rc = launch_dense(tiles, plan.parts, po, pl, st);
+  } else if (plan.decode || plan.packed) {
     if (plan.parts > 0)
       rc = (plan.decode ? launch_decode : launch_packed)(
           q16, static_cast<const uint16_t*>(K), static_cast<const uint16_t*>(V), n_shards, Tq, S,
           Hq, Hkv, d, softmax_scale, po, pl, plan.np_shard, st, &gen);
   } else {
     const int part = n_shards * plan.np_shard;
+    float* const go = po + part * ostride;
+    float* const gl = pl + part * lstride;
     if (n_shards > 0)
       rc = launch_split_parts(q, K, V, n_shards, Tq, S, Hq, Hkv, d, softmax_scale, plan.np_shard,
                               po, pl, st);
     if (rc == PULSAR_OK && G > 0)
-      rc = plan.gen_decode
-               ? launch_decode(q16, nullptr, nullptr, 0, Tq, 0, Hq, Hkv, d, softmax_scale,
-                               po + part * ostride, pl + part * lstride, 1, st, &gen)
-               : launch_split_parts(q, Kg, Vg, 1, Tq, G, Hq, Hkv, d, softmax_scale, plan.np_gen,
-                                    po + part * ostride, pl + part * lstride, st);
+      rc = plan.gen_dense    ? launch_dense(tiles, plan.np_gen, go, gl, st)
+           : plan.gen_decode ? launch_decode(q16, nullptr, nullptr, 0, Tq, 0, Hq, Hkv, d,
+                                             softmax_scale, go, gl, 1, st, &gen)
+                             : launch_split_parts(q, Kg, Vg, 1, Tq, G, Hq, Hkv, d, softmax_scale,
+                                                  plan.np_gen, go, gl, st);
   }
   if (rc != PULSAR_OK) return rc;
   const int64_t row = (int64_t)Hkv * d;

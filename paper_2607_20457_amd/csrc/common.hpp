@@ -322,6 +322,7 @@ int launch_sparse(const SparseLaunch& a, const SparsePlan& plan, void* o, int o_
 // tiles.
 bool dense_tiles_apply(int Hq, int Hkv);
 int dense_parts(int n_shards, int Tq, int64_t S, int64_t G, int Hq, int Hkv, int d);
+int64_t dense_part_rows_most(int Tq, int Hq, int Hkv, int d);
 int launch_dense(const SparseLaunch& a, int parts, float* o, float* lse, hipStream_t stream);
 
 // Rows of an assembled Phase-1 input gathered from a per-position tensor and

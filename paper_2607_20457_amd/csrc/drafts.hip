@@ -78,24 +78,59 @@ __global__ __launch_bounds__(THREADS) void tree_merge_kernel(
   const int words = (Tq + 31) / 32;
   const uint32_t* const bits = tree.mask + (int64_t)t * words;
 
+  // The first loads go out together: the mask, the first parts; then, once the mask is
+  // there, the group's first row.
   uint32_t word = tid < Tq ? bits[tid >> 5] : 0u;
-  f32x4 q = __builtin_convertvector(
+  const f32x4 q = __builtin_convertvector(
       reinterpret_cast<const bf16x4*>(tree.q + row * D)[dv], f32x4);
-
   const float* lp = lse_parts + (int64_t)h * Tq + t;
   const f32x4* op = reinterpret_cast<const f32x4*>(o_parts) + row * DL + dv;
   const int64_t ostride = (int64_t)Tq * Hq * DL, lstride = (int64_t)Tq * Hq;
-  float m = -INFINITY, sum = 0.f;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int p0 = pg; p0 < H; p0 += CH * PG) {
-    float l[CH];
-    f32x4 v[CH];
+  float l[CH];
+  f32x4 v[CH];
+  auto load_parts = [&](int p0) {
 #pragma unroll
     for (int u = 0; u < CH; ++u) {
       const int p = min(p0 + u * PG, H - 1);  // a part past the last weighs zero
       l[u] = lp[p * lstride];
       v[u] = op[p * ostride];
     }
+  };
+  if (H > 0) load_parts(pg);
+
+  const int64_t stride = (int64_t)tree.Hkv * D;
+  const uint16_t* const Kh = tree.Kd + (int64_t)kvh * D;
+  const uint16_t* const Vh = tree.Vd + (int64_t)kvh * D;
+  bf16x4 k4 = {}, v4 = {};
+  auto load_row = [&](int i) {
+    const int64_t off = s_list[i] * stride;
+    k4 = reinterpret_cast<const bf16x4*>(Kh + off)[dv];
+    v4 = reinterpret_cast<const bf16x4*>(Vh + off)[dv];
+  };
+  // The drafts from j0 on that the token sees, listed; their number.
+  auto list_rows = [&](int j0) {
+    const int j = j0 + tid;
+    const bool sees = (word >> (j & 31)) & 1u;
+    const uint64_t vote = __ballot(sees && j < Tq);
+    if (lane == 0) s_cnt[wave] = __popcll(vote);
+    __syncthreads();
+    int at = 0, n = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      at += w < wave ? s_cnt[w] : 0;
+      n += s_cnt[w];
+    }
+    if ((vote >> lane) & 1) s_list[at + __popcll(vote & ((1ull << lane) - 1))] = j;
+    __syncthreads();
+    return n;
+  };
+  int n = list_rows(0);
+  if (pg < n) load_row(pg);
+
+  float m = -INFINITY, sum = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int p0 = pg; p0 < H; p0 += CH * PG) {
+    if (p0 != pg) load_parts(p0);
     float nm = m;
 #pragma unroll
     for (int u = 0; u < CH; ++u)
@@ -113,40 +148,25 @@ __global__ __launch_bounds__(THREADS) void tree_merge_kernel(
     m = nm;
   }
 
-  const int64_t stride = (int64_t)tree.Hkv * D;
-  const uint16_t* const Kh = tree.Kd + (int64_t)kvh * D;
-  const uint16_t* const Vh = tree.Vd + (int64_t)kvh * D;
   for (int j0 = 0; j0 < Tq; j0 += THREADS) {
-    const int j = j0 + tid;
     if (j0 > 0) {
       __syncthreads();  // the list of the drafts before has been read
-      word = j < Tq ? bits[j >> 5] : 0u;
+      word = j0 + tid < Tq ? bits[(j0 + tid) >> 5] : 0u;
+      n = list_rows(j0);
+      if (pg < n) load_row(pg);
     }
-    const bool sees = (word >> (j & 31)) & 1u;
-    const uint64_t vote = __ballot(sees && j < Tq);
-    if (lane == 0) s_cnt[wave] = __popcll(vote);
-    __syncthreads();
-    int at = 0, n = 0;
-#pragma unroll
-    for (int w = 0; w < W; ++w) {
-      at += w < wave ? s_cnt[w] : 0;
-      n += s_cnt[w];
-    }
-    if ((vote >> lane) & 1) s_list[at + __popcll(vote & ((1ull << lane) - 1))] = j;
-    __syncthreads();
     for (int i = pg; i < n; i += PG) {
-      const int64_t off = s_list[i] * stride;
-      const f32x4 k = __builtin_convertvector(reinterpret_cast<const bf16x4*>(Kh + off)[dv], f32x4);
-      const f32x4 v = __builtin_convertvector(reinterpret_cast<const bf16x4*>(Vh + off)[dv], f32x4);
+      const f32x4 k = __builtin_convertvector(k4, f32x4), x = __builtin_convertvector(v4, f32x4);
+      if (i + PG < n) load_row(i + PG);
       float s = (q[0] * k[0] + q[1] * k[1]) + (q[2] * k[2] + q[3] * k[3]);
 #pragma unroll
-      for (int x = 1; x < DL; x <<= 1) s += __shfl_xor(s, x, 64);
+      for (int lanes = 1; lanes < DL; lanes <<= 1) s += __shfl_xor(s, lanes, 64);
       s *= tree.scale;
       const float nm = fmaxf(m, s);
       const float use = nm == -INFINITY ? 0.f : nm;
       const float alpha = __expf(m - use), w = __expf(s - use);
       sum = sum * alpha + w;
-      acc = acc * alpha + w * v;
+      acc = acc * alpha + w * x;
       m = nm;
     }
   }

@@ -108,15 +108,16 @@ void sparse_attn_kernel(SparseArgs a) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, g = lane >> 4;
-  // workgroup -> (KV head, token tile, heads, part), the KV head fastest: with eight
-  // of them each XCD reads one head's keys
-  int64_t wg = blockIdx.x;
-  const int kvh = (int)(wg % a.Hkv);
-  wg /= a.Hkv;
-  const int t0 = (int)(wg % a.token_tiles) * a.tile_tokens;
-  wg /= a.token_tiles;
-  const int heads0 = (int)(wg % a.col_tiles) * 16;
-  const int part = (int)(wg / a.col_tiles);
+  // Workgroup -> (token tile, heads) of a (KV head, part).  Workgroups go to the eight
+  // XCDs in turn, each with an L2 of its own: all tiles of one head's part, which read
+  // the same keys (or blocks that they share), go to one of them, one after another.
+  int64_t wg = blockIdx.x >> 3;
+  const int tile = (int)(wg % (a.token_tiles * a.col_tiles));
+  wg = wg / (a.token_tiles * a.col_tiles) * 8 + (blockIdx.x & 7);
+  if (wg >= (int64_t)a.Hkv * a.parts) return;
+  const int kvh = (int)(wg % a.Hkv), part = (int)(wg / a.Hkv);
+  const int t0 = tile % a.token_tiles * a.tile_tokens;
+  const int heads0 = tile / a.token_tiles * 16;
   const int tokens = min(a.tile_tokens, a.Tq - t0);  // of this tile
   const float c2 = a.scale_log2;
   const uint32_t row_bytes = (uint32_t)(a.Hkv * D * 2);
@@ -591,7 +592,8 @@ void sparse_attn_kernel(SparseArgs a) {
 template <int D, int NW, int MODE>
 int launch_tiles(const SparseArgs& a, hipStream_t stream) {
   constexpr size_t lds = SpLds<D, NW, MODE>::BYTES;
-  const int64_t nwg = (int64_t)a.Hkv * a.token_tiles * a.col_tiles * a.parts;
+  const int64_t nwg =
+      ((int64_t)a.Hkv * a.parts + 7) / 8 * 8 * ((int64_t)a.token_tiles * a.col_tiles);
   if (nwg > 0x7fffffff) return PULSAR_EUNSUPPORTED;
   const auto kern = sparse_attn_kernel<D, NW, MODE>;
   if (lds > 65536 &&
@@ -710,6 +712,12 @@ int dense_parts(int n_shards, int Tq, int64_t S, int64_t G, int Hq, int Hkv, int
   const int64_t tiles = (int64_t)((Tq + tokens - 1) / tokens) * Hkv;
   const int64_t steps = steps_of(n_shards * S) + steps_of(G);
   return (int)std::max<int64_t>(1, std::min(tiles_at_once(d) / tiles, (steps + 3) / 4));
+}
+// Rows of partials of any call of up to Tq tokens: a part of every token, or the
+// chip's workgroups' tiles.
+int64_t dense_part_rows_most(int Tq, int Hq, int Hkv, int d) {
+  const int tokens = 16 / (Hq / Hkv);
+  return std::max<int64_t>(Tq, (int64_t)tiles_at_once(d) / Hkv * std::min(tokens, Tq));
 }
 int launch_dense(const SparseLaunch& x, int parts, float* o, float* lse, hipStream_t stream) {
   SparseArgs a = tile_args(x, 16 / (x.Hq / x.Hkv), parts);
