@@ -359,10 +359,10 @@ def _mask_shape(mask, Tq):
 
 def _out(q, o_dtype):
     if o_dtype == OUT_BF16:
-        return q.new_empty(q.shape)
+        return torch.empty_like(q)
     if o_dtype != OUT_F32:
         raise ValueError("o_dtype must be OUT_F32 or OUT_BF16")
-    return q.new_empty(q.shape, dtype=torch.float32)
+    return torch.empty_like(q, dtype=torch.float32)
 
 
 def _scratch(workspace, need, dev, like):

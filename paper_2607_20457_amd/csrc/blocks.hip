@@ -2,6 +2,7 @@
 // bounds of every block of keys, the score that a block's bounds allow, and the
 // topk blocks of each shard.
 #include <algorithm>
+#include <type_traits>
 
 #include "tiles.hpp"
 
@@ -262,16 +263,20 @@ struct BoundsTile {
       hi[s] = __builtin_bit_cast(bf16x8, rows[chunk_at<D / 4>(r, D / 8 + 4 * s + g)]);
     }
   }
-  // The largest |m| of the 16 blocks.
+  // The largest |m| of the 16 blocks.  (Without the sign bits magnitudes rank as
+  // integers, what is not a number last.)
   __device__ __forceinline__ float norm() const {
+    bf16x8 big[D / 32];
     float sum = 0.f;
 #pragma unroll
-    for (int s = 0; s < D / 32; ++s)
+    for (int s = 0; s < D / 32; ++s) {
+      const auto bits = [](bf16x8 x) {
+        return __builtin_bit_cast(s16x8, __builtin_bit_cast(u32x4, x) & 0x7fff7fffu);
+      };
+      big[s] = __builtin_bit_cast(bf16x8, __builtin_elementwise_max(bits(lo[s]), bits(hi[s])));
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float l = (float)lo[s][i], h = (float)hi[s][i];
-        sum += fmaxf(l * l, h * h) + 0.f * (l + h);  // (what is not finite stays so)
-      }
+      for (int i = 0; i < 8; ++i) sum = __builtin_fmaf((float)big[s][i], (float)big[s][i], sum);
+    }
     sum = sum_of_rows(sum);
     if (__any(!in_range(sum))) {
       double wide = 0.;
@@ -279,8 +284,8 @@ struct BoundsTile {
       for (int s = 0; s < D / 32; ++s)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const double l = (double)(float)lo[s][i], h = (double)(float)hi[s][i];
-          wide += (l * l > h * h ? l * l : h * h) + 0. * (l + h);
+          const double x = (double)(float)big[s][i];
+          wide += x * x;
         }
       wide += __shfl_xor(wide, 16, 64);
       wide += __shfl_xor(wide, 32, 64);
@@ -315,6 +320,26 @@ __device__ __forceinline__ void read_columns(const u32x4* rows, int r, int g,
 #pragma unroll
   for (int s = 0; s < D / 32; ++s)
     x[s] = __builtin_bit_cast(bf16x8, rows[chunk_at<D / 8>(r, 4 * s + g)]);
+}
+
+// |q| of one head, by a wave: two channels (one at D = 64) to a lane.
+template <int D>
+__device__ __forceinline__ float head_norm(const uint16_t* q, int lane) {
+  float y[D / 64], x = 0.f;
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) {
+    y[i] = __uint_as_float((uint32_t)q[lane * (D / 64) + i] << 16);
+    x += y[i] * y[i];
+  }
+  x = sum_of_rows(over_row(x, Sum{}));
+  if (in_range(x)) return __builtin_sqrtf(x);
+  double wide = 0.;
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) wide += (double)y[i] * (double)y[i];
+  wide = over_row(wide, Sum{});
+  wide += __shfl_xor(wide, 16, 64);
+  wide += __shfl_xor(wide, 32, 64);
+  return norm_of(wide);
 }
 
 // Near scores of 16 blocks (rows 4g + v) and 16 columns of q (lane (r, g): channels
@@ -475,7 +500,7 @@ struct FusedLds {
   u32x4 bounds[kFusedWaves][16 * (D / 4)];
   u32x4 q[kFusedHeads * (D / 8)];
   uint32_t row[kFusedBlocks];
-  float norm[kFusedWaves];
+  float norm[kFusedWaves], head_norm[kFusedWaves];
 };
 
 // Near scores of a row into s_row; the largest |m| of the wave's blocks is returned.
@@ -541,18 +566,24 @@ void block_pick_kernel(const uint16_t* __restrict__ q, const uint16_t* __restric
   const uint16_t* const bt = bounds + ((st / Tq) * Hkv + kvh) * blocks * 2 * D;
   const uint64_t below = (1ull << lane) - 1;
 
-  float most = 0.f;
+  float most = 0.f, heads = 0.f;
+  __shared__ std::conditional_t<MODE == PICK_FUSED, FusedLds<D>, int> s_fused;
   if constexpr (MODE == PICK_FUSED) {
     static_assert(W == 1, "one wave selects");
-    __shared__ FusedLds<D> s_fused;
     s_row = s_fused.row;
-    const float mine =
-        fused_scores<D>(qt, bt, group, blocks, reinterpret_cast<float*>(s_row), s_fused);
+    float mine = 0.f;  // each wave's heads
+    for (int h = wave; h < group; h += kFusedWaves)
+      mine = fmaxf(mine, head_norm<D>(qt + h * D, lane));
+    if (lane == 0) s_fused.head_norm[wave] = mine;
+    mine = fused_scores<D>(qt, bt, group, blocks, reinterpret_cast<float*>(s_row), s_fused);
     if (lane == 0) s_fused.norm[wave] = mine;
     __syncthreads();
     if (wave > 0) return;
 #pragma unroll
-    for (int w = 0; w < kFusedWaves; ++w) most = fmaxf(most, s_fused.norm[w]);
+    for (int w = 0; w < kFusedWaves; ++w) {
+      most = fmaxf(most, s_fused.norm[w]);
+      heads = fmaxf(heads, s_fused.head_norm[w]);
+    }
   } else if constexpr (MODE == PICK_NEAR) {
     const int n = (blocks + 15) / 16;
     const float* const p = norms + ((st / Tq) * Hkv + kvh) * n;
@@ -697,25 +728,10 @@ void block_pick_kernel(const uint16_t* __restrict__ q, const uint16_t* __restric
     const u32x2 ends = spread(a, b);
     // the largest |q| of the group's heads: a wave takes every W-th
     float norm = 0.f;
-    for (int h = wave; h < group; h += W) {
-      float y[D / 64], x = 0.f;
-#pragma unroll
-      for (int i = 0; i < D / 64; ++i) {
-        y[i] = __uint_as_float((uint32_t)qt[h * D + lane * (D / 64) + i] << 16);
-        x += y[i] * y[i];
-      }
-      x = sum_of_rows(over_row(x, Sum{}));
-      if (in_range(x)) {
-        norm = fmaxf(norm, __builtin_sqrtf(x));
-        continue;
-      }
-      double wide = 0.;
-#pragma unroll
-      for (int i = 0; i < D / 64; ++i) wide += (double)y[i] * (double)y[i];
-      wide = over_row(wide, Sum{});
-      wide += __shfl_xor(wide, 16, 64);
-      wide += __shfl_xor(wide, 32, 64);
-      norm = fmaxf(norm, norm_of(wide));
+    if constexpr (MODE == PICK_FUSED) {
+      norm = heads;
+    } else {
+      for (int h = wave; h < group; h += W) norm = fmaxf(norm, head_norm<D>(qt + h * D, lane));
     }
     if (MODE == PICK_NEAR || W > 1) {  // (not negative: they rank as their bits)
       norm = __uint_as_float(spread(0u, __float_as_uint(norm))[1]);
@@ -768,16 +784,41 @@ void block_pick_kernel(const uint16_t* __restrict__ q, const uint16_t* __restric
       typedef double f64xN __attribute__((ext_vector_type(N)));
       const int sub = tid & 15;
       for (int c = tid >> 4; c < all; c += 4 * W) {
-        const uint16_t* p = bt + (int64_t)s_row[c] * 2 * D + sub * N;
-        const auto lo = __builtin_convertvector(*reinterpret_cast<const bf16xN*>(p), f64xN);
-        const auto hi = __builtin_convertvector(*reinterpret_cast<const bf16xN*>(p + D), f64xN);
+        // channels sub N .. of the block and of each head: a fused row that took one
+        // round has its blocks, and always its heads, in LDS
+        const int b = (int)s_row[c];
+        bf16xN lo16, hi16;
+        constexpr int PER = 8 / N;  // lanes to a 16-byte chunk
+        const bool staged = MODE == PICK_FUSED && blocks <= kFusedWaves * 16;
+        if constexpr (MODE == PICK_FUSED) {
+          if (staged) {
+            const u32x4* const rows = s_fused.bounds[b >> 4];
+            lo16 = reinterpret_cast<const bf16xN*>(
+                rows + chunk_at<D / 4>(b & 15, sub / PER))[sub % PER];
+            hi16 = reinterpret_cast<const bf16xN*>(
+                rows + chunk_at<D / 4>(b & 15, D / 8 + sub / PER))[sub % PER];
+          }
+        }
+        if (!staged) {
+          const bf16xN* const p = reinterpret_cast<const bf16xN*>(bt + (int64_t)b * 2 * D) + sub;
+          lo16 = p[0];
+          hi16 = p[16];
+        }
+        const auto lo = __builtin_convertvector(lo16, f64xN);
+        const auto hi = __builtin_convertvector(hi16, f64xN);
         float best = -INFINITY;
         constexpr int HU = 4;  // heads at a time
         for (int h0 = 0; h0 < group; h0 += HU) {
           bf16xN y[HU];
 #pragma unroll
-          for (int u = 0; u < HU; ++u)
-            y[u] = *reinterpret_cast<const bf16xN*>(qt + min(h0 + u, group - 1) * D + sub * N);
+          for (int u = 0; u < HU; ++u) {
+            const int h = min(h0 + u, group - 1);
+            if constexpr (MODE == PICK_FUSED)
+              y[u] = reinterpret_cast<const bf16xN*>(
+                  s_fused.q + (h & ~15) * (D / 8) + chunk_at<D / 8>(h & 15, sub / PER))[sub % PER];
+            else
+              y[u] = *reinterpret_cast<const bf16xN*>(qt + h * D + sub * N);
+          }
 #pragma unroll
           for (int u = 0; u < HU; ++u) {
             const auto z = __builtin_convertvector(y[u], f64xN);
@@ -795,13 +836,33 @@ void block_pick_kernel(const uint16_t* __restrict__ q, const uint16_t* __restric
       }
       sync();
       at = mine;
+      if (all <= 64) {
+        // few: every wave ranks them, one to a lane (they are listed by index, so of
+        // equal ones the earlier is the better)
+        const uint32_t own = lane < all ? s_row[lane] : 0u;
+        int better = 0;
+        for (int k = 0; k < all; ++k) {
+          const uint32_t x = __builtin_amdgcn_readlane(own, k);
+          better += x > own || (x == own && k < lane);
+        }
+        const uint64_t taken = __ballot(lane < all && better < topk - kept);
 #pragma unroll
-      for (int i = 0; i < R; ++i) {
-        const uint64_t vote = __ballot((open >> i) & 1);
-        if ((open >> i) & 1) key[i] = s_row[at + __popcll(vote & below)];
-        at += __popcll(vote);
+        for (int i = 0; i < R; ++i) {
+          const uint64_t vote = __ballot((open >> i) & 1);
+          if ((open >> i) & 1) key[i] = (taken >> (at + __popcll(vote & below))) & 1 ? kKept : 0u;
+          at += __popcll(vote);
+        }
+        cut = kKept;
+        reach = topk;
+      } else {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          const uint64_t vote = __ballot((open >> i) & 1);
+          if ((open >> i) & 1) key[i] = s_row[at + __popcll(vote & below)];
+          at += __popcll(vote);
+        }
+        find_cut(kept);
       }
-      find_cut(kept);
     }
   }
 
