@@ -442,8 +442,9 @@ int pulsar_tree_mask(const int32_t* parent, int T, uint32_t* mask, int32_t* dept
  * lse = -inf.  Rows of the new tokens that t does not see are not read for it:
  * what they hold, NaN and infinities included, cannot reach its output.
  *
- * The partials of the shards and the G rows are those of pulsar_phase2_query;
- * the merge folds each token's own branch in, in fp32.
+ * The shards and the G rows give partials by the kernels of pulsar_phase2_query, or
+ * by 16-row tiles of (token, head) rows where these are faster; the merge folds each
+ * token's own branch in, in fp32.
  *
  * q, Kg, Vg, G, K, V, lse  as for pulsar_phase2_query (row G + t of Kg and Vg
  *           is token t's own); K and V 16-byte aligned.
@@ -457,7 +458,7 @@ int pulsar_tree_mask(const int32_t* parent, int T, uint32_t* mask, int32_t* dept
  *           pulsar_phase2_query the size never drops when n_shards, Tq, S or G
  *           grows.
  * Errors: as pulsar_phase2_query, plus EINVAL for an unknown o_dtype or a NULL
- *         mask when Tq > 0.
+ *         mask when Tq > 0, and EUNSUPPORTED for Tq * Hq >= 2^24.
  */
 size_t pulsar_phase2_tree_workspace_bytes(int n_shards, int Tq, int64_t S, int64_t G, int Hq,
                                           int Hkv, int d);
@@ -471,7 +472,7 @@ int pulsar_phase2_tree(const void* q, const void* Kg, const void* Vg, int64_t G,
  * rows that a policy keeps), moved to its front, in place, in K and V of every
  * layer: row G + keep[j] becomes row G + j.  All other rows stay as they are.
  *
- * K, V    bf16 [layers, capacity, Hkv, d], 16-byte aligned; not the same memory.
+ * K, V    bf16 [layers, capacity, Hkv, d], 16-byte aligned; no memory in common.
  * keep    int32 [n], rising, each in [0, capacity - G).  The list ends at the
  *         first entry that is negative, not above the one before it, or past
  *         the cache: the number of rows that a step accepts may stay on the
@@ -523,7 +524,8 @@ int pulsar_key_bounds(const void* K, int n_shards, int64_t S, int Hkv, int d, in
  * EINVAL: negative sizes, Hq % Hkv != 0, topk > blocks, NULL or misaligned
  *         pointers when there is work.  EWORKSPACE: workspace too small.
  * EUNSUPPORTED: d not in {64, 128}; blocks > 32768; n_shards * Hkv > 65535;
- *         Tq > 524280 or n_shards * Tq * Hkv >= 2^31.
+ *         Tq > 524280 (65535 where more than 16 heads read a KV head);
+ *         n_shards * Tq * Hkv >= 2^23 (2^22 for more than 4096 blocks).
  */
 size_t pulsar_block_select_workspace_bytes(int n_shards, int Tq, int blocks, int Hq, int Hkv);
 int pulsar_block_select(const void* q, const void* bounds, int n_shards, int Tq, int blocks, int Hq,
@@ -559,7 +561,9 @@ int pulsar_block_select(const void* q, const void* bounds, int n_shards, int Tq,
  *         is work, only one of Kg and Vg, a mask or G > 0 without them, scale
  *         not finite and > 0, unknown o_dtype.  EWORKSPACE: workspace too small.
  * EUNSUPPORTED: d not in {64, 128}; another block; S >= 2^31; G + Tq >= 2^24;
- *         2^30 listed keys or more; a row of K of 16 MiB or more.
+ *         2^30 listed keys or more; a row of K of 16 MiB or more; more workgroups
+ *         than a launch holds (none below Tq * H * ceil(Hq / Hkv / 16) = 2^24, H being
+ *         Hkv rounded up to a multiple of 8).
  */
 size_t pulsar_phase2_sparse_workspace_bytes(int Tq, int Hq, int Hkv, int d);
 int pulsar_phase2_sparse(const void* q, const void* K, const void* V, const int32_t* sel,

@@ -343,6 +343,12 @@ def _check(dev, dtype, named):
             raise ValueError(f"{name} must be on the current device")
 
 
+def _int32(x, name):
+    """The C entry points take x as an int: a larger one would wrap around."""
+    if not -(1 << 31) <= x < 1 << 31:
+        raise ValueError(f"{name} out of range")
+
+
 def _raw_stream(dev):
     return torch._C._cuda_getCurrentRawStream(dev)
 
@@ -443,8 +449,8 @@ def kv_compact_(K, V, G: int, keep):
     _check(dev, torch.int32, ((keep, "keep"),))
     if K.dim() != 4 or V.shape != K.shape or keep.dim() != 1:
         raise ValueError("K/V must be [layers, capacity, Hkv, d], keep [n]")
-    if K.data_ptr() == V.data_ptr() and K.numel() > 0:
-        raise ValueError("K and V must not be the same memory")
+    if abs(K.data_ptr() - V.data_ptr()) < 2 * K.numel():
+        raise ValueError("K and V must not share memory")
     layers, capacity, Hkv, d = K.shape
     st = _lib.lib().pulsar_kv_compact(K.data_ptr(), V.data_ptr(), layers, capacity, Hkv, d, G,
                                       keep.data_ptr(), keep.shape[0], _raw_stream(dev))
@@ -459,6 +465,7 @@ def key_bounds(K, block: int):
     dev = torch.cuda.current_device() if K.is_cuda else None
     _check(dev, _BF16, ((K, "K"),))
     n_shards, S, Hkv, d = K.shape
+    _int32(block, "block")
     bounds = K.new_empty((n_shards, Hkv, -(-S // block) if block > 0 else 0, 2, d))
     st = _lib.lib().pulsar_key_bounds(K.data_ptr(), n_shards, S, Hkv, d, block, bounds.data_ptr(),
                                       _raw_stream(dev))
@@ -482,6 +489,7 @@ def block_select(q, bounds, topk: int, return_scores: bool = False, workspace=No
     n_shards, Hkv, blocks, two, db = bounds.shape
     if two != 2 or db != d:
         raise ValueError("bounds must be [n_shards, Hkv, blocks, 2, d]")
+    _int32(topk, "topk")
     sel = q.new_empty((n_shards, Tq, Hkv, max(topk, 0)), dtype=torch.int32)
     scores, ws_ptr, need = None, None, 0
     if return_scores:
@@ -514,6 +522,7 @@ def phase2_sparse(q, K, V, sel, block: int, Kg=None, Vg=None, G: int = 0, mask=N
     _check(dev, torch.int32, ((sel, "sel"),))
     Tq, Hq, d = q.shape
     n_shards, S, Hkv, dk = K.shape
+    _int32(block, "block")
     if dk != d or V.shape != K.shape:
         raise ValueError("K/V must be [n_shards, S, Hkv, d]")
     if sel.dim() != 4 or sel.shape[:3] != (n_shards, Tq, Hkv):

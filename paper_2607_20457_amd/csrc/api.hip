@@ -849,7 +849,7 @@ int pulsar_phase2_tree(const void* q, const void* Kg, const void* Vg, int64_t G,
   if (Tq == 0) return PULSAR_OK;
   if (mask == nullptr) return PULSAR_EINVAL;
   if (n_shards > 0 && S > 0 && (!aligned16(K) || !aligned16(V))) return PULSAR_EINVAL;
-  if ((int64_t)Tq * Hq > 0x7fffffff) return PULSAR_EUNSUPPORTED;
+  if (!grid_fits((int64_t)Tq * Hq, 256)) return PULSAR_EUNSUPPORTED;
   if (S == 0) n_shards = 0;
   const QueryPlan plan = tree_plan(n_shards, Tq, S, G, Hq, Hkv, d);
   if (plan.parts > 0 && (workspace == nullptr || !aligned16(workspace) ||

@@ -70,7 +70,8 @@ int pulsar_block_select(const void* q, const void* bounds, int n_shards, int Tq,
   if (d != 64 && d != 128) return PULSAR_EUNSUPPORTED;
   if (blocks > kMaxSelectBlocks || Tq >= PULSAR_MAX_ROWS) return PULSAR_EUNSUPPORTED;
   const int64_t rows = (int64_t)n_shards * Tq * Hkv;
-  if (rows > kMaxInt || (int64_t)n_shards * Hkv > 65535 || (Tq + 7) / 8 > 65535)
+  if (!grid_fits(rows, blocks > 4096 ? 1024 : 512) || (int64_t)n_shards * Hkv > 65535 ||
+      Tq > (Hq / Hkv > 16 ? 65535 : 65535 * 8))
     return PULSAR_EUNSUPPORTED;
   if (rows == 0 || blocks == 0 || (topk == 0 && scores == nullptr)) return PULSAR_OK;
   if (q == nullptr || bounds == nullptr || (topk > 0 && sel == nullptr)) return PULSAR_EINVAL;

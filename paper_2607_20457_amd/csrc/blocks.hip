@@ -912,7 +912,7 @@ int launch_key_bounds(const uint16_t* K, int n_shards, int64_t S, int Hkv, int d
   const int64_t blocks = (S + block - 1) / block;
   const int64_t total = n_shards * blocks * (Hkv * d / 8);
   const int64_t nwg = (total + 255) / 256;
-  if (nwg > 0x7fffffff) return PULSAR_EUNSUPPORTED;
+  if (!grid_fits(nwg, 256)) return PULSAR_EUNSUPPORTED;
   hipLaunchKernelGGL(key_bounds_kernel, dim3((unsigned)nwg), dim3(256), 0, stream, K, S, Hkv, d,
                      block, (int)blocks, bounds, total);
   return hipGetLastError() == hipSuccess ? PULSAR_OK : PULSAR_EHIP;
@@ -938,7 +938,6 @@ int launch_block_near(const uint16_t* q, const uint16_t* bounds, int n_shards, i
   // a token's passes stay in one workgroup
   const int per = std::max(kUnits / passes, 1) * passes;
   const int64_t z = (units + per - 1) / per;
-  if (units > 0x7fffffff || z > 65535) return PULSAR_EUNSUPPORTED;
   const dim3 grid((blocks + 63) / 64, n_shards * Hkv, (unsigned)z);
   const auto kern = d == 128 ? block_near_kernel<128> : block_near_kernel<64>;
   hipLaunchKernelGGL(kern, grid, dim3(256), 0, stream, q, bounds, Tq, Hq, Hkv, blocks, (int)units,

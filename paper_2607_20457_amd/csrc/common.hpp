@@ -17,6 +17,12 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 #define PULSAR_WAVE 64
 #define PULSAR_LDS_BYTES 163840  // 160 KB local data share per compute unit on gfx950
 
+// Whether a launch of that many workgroups is one: a dimension's threads are counted
+// in 32 bits.
+inline bool grid_fits(int64_t workgroups, int threads) {
+  return workgroups <= 0xffffffffll / threads;
+}
+
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Row -> global position map of an assembled Phase-1 input (Eq. 3, sparse

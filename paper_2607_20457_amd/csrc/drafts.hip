@@ -141,9 +141,10 @@ __global__ __launch_bounds__(THREADS) void tree_merge_kernel(
     acc *= alpha;
 #pragma unroll
     for (int u = 0; u < CH; ++u) {
-      const float w = p0 + u * PG < H ? __expf(l[u] - use) : 0.f;
+      const bool part = p0 + u * PG < H;
+      const float w = part ? __expf(l[u] - use) : 0.f;
       sum += w;
-      acc += w * v[u];
+      acc += w * (part ? v[u] : f32x4{0.f, 0.f, 0.f, 0.f});  // (zero would not heed an infinity)
     }
     m = nm;
   }
@@ -336,7 +337,7 @@ int launch_kv_compact(void* K, void* V, int layers, int64_t capacity, int64_t ro
                          (int64_t)2 * layers * ((row16 + cols - 1) / cols) < 256))
       cols /= 2;
     const int groups = (row16 + cols - 1) / cols;
-    if ((int64_t)layers * groups > 0x7fffffff) return PULSAR_EUNSUPPORTED;
+    if (!grid_fits((int64_t)layers * groups, kCompactThreads)) return PULSAR_EUNSUPPORTED;
     hipLaunchKernelGGL(kv_compact_many_kernel<4>, dim3((unsigned)(layers * groups), 2),
                        dim3(kCompactThreads), 0, stream, (u32x4*)K, (u32x4*)V, capacity * row16,
                        row16, G, past, keep, n, cols, groups);

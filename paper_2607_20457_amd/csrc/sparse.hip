@@ -46,7 +46,7 @@ constexpr int SP_KEYS = 32;       // keys per step
 constexpr float SP_SLACK = 8.0f;  // log2 slack before the reference is raised
 // A union's list in LDS, in entries, and its map, a byte per block: as much as leaves
 // room for all the workgroups that the registers do.
-constexpr int sp_list(int d) { return d == 64 ? 1792 : 3072; }
+constexpr int sp_list(int d) { return d == 64 ? 1792 : 3584; }
 constexpr int sp_map(int d) { return d == 64 ? 32768 : 65536; }
 
 enum SparseMode : int { SP_LISTED, SP_UNION, SP_DENSE };
@@ -505,10 +505,24 @@ void sparse_attn_kernel(SparseArgs a) {
               if ((vis >> k) & 1) acc[e] = x;
             }
           }
-        } else {
+        } else if (MODE == SP_UNION || seen == 0xffffffffu) {
 #pragma unroll
           for (int e = 0; e < DT; ++e)
             acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_frag(v_lds, e), P, acc[e], 0, 0, 0);
+        } else {
+          // zeros in place of the copies, whose weights of zero an infinity would not heed
+          u32x4 keep;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const uint32_t two = seen >> (16 * (x >> 1) + 4 * g + 2 * (x & 1));
+            keep[x] = (two & 1 ? 0xffffu : 0u) | (two & 2 ? 0xffff0000u : 0u);
+          }
+#pragma unroll
+          for (int e = 0; e < DT; ++e) {
+            const bf16x8 v = __builtin_bit_cast(
+                bf16x8, __builtin_bit_cast(u32x4, v_frag(v_lds, e)) & keep);
+            acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P, acc[e], 0, 0, 0);
+          }
         }
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -594,7 +608,7 @@ int launch_tiles(const SparseArgs& a, hipStream_t stream) {
   constexpr size_t lds = SpLds<D, NW, MODE>::BYTES;
   const int64_t nwg =
       ((int64_t)a.Hkv * a.parts + 7) / 8 * 8 * ((int64_t)a.token_tiles * a.col_tiles);
-  if (nwg > 0x7fffffff) return PULSAR_EUNSUPPORTED;
+  if (!grid_fits(nwg, 64 * NW)) return PULSAR_EUNSUPPORTED;
   const auto kern = sparse_attn_kernel<D, NW, MODE>;
   if (lds > 65536 &&
       hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize,
@@ -624,7 +638,7 @@ static int union_tokens(int Tq, int Hkv, int group, int d, int64_t blocks, int64
                         int64_t steps) {
   const int fit = std::min(std::min(16 / group, 8), Tq);
   if (fit < 2 || blocks > sp_map(d) || entries * fit > sp_list(d)) return 1;
-  return Tq * Hkv * steps * (SP_KEYS * d * 4) >= kUnionBytes ? fit : 1;
+  return (int64_t)Tq * Hkv * steps * (SP_KEYS * d * 4) >= kUnionBytes ? fit : 1;
 }
 
 SparsePlan sparse_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int d, int block, int topk,

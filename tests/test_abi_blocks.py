@@ -45,7 +45,8 @@ def test_phase2_tree():
                dict(q=FAKE + 2), dict(Kg=FAKE + 8), dict(K=FAKE + 8), dict(V=FAKE + 4),
                dict(o=FAKE + 4)):
         assert call(**kw) == EINVAL, kw
-    for kw in (dict(d=96), dict(Hq=24), dict(G=1 << 24), dict(S=1 << 20, Hkv=8)):
+    for kw in (dict(d=96), dict(Hq=24), dict(G=1 << 24), dict(S=1 << 20, Hkv=8),
+               dict(Tq=1 << 19, Kg=FAKE, G=0)):
         assert call(**kw) == EUNSUP, kw
     need = P.phase2_tree_workspace_bytes(2, 5, 100, 10, 32, 8, 128)
     assert need > 0
@@ -104,7 +105,9 @@ def test_block_select():
                dict(d=0), dict(topk=-1), dict(topk=51), dict(q=None), dict(bounds=None),
                dict(sel=None), dict(q=FAKE + 8), dict(bounds=FAKE + 8)):
         assert call(**kw) == EINVAL, kw
-    for kw in (dict(d=96), dict(blocks=32769), dict(n_shards=8192), dict(Tq=600000)):
+    for kw in (dict(d=96), dict(blocks=32769), dict(n_shards=8192), dict(Tq=600000),
+               dict(Tq=65536, Hkv=1), dict(n_shards=8, Tq=1 << 17),
+               dict(n_shards=8, Tq=1 << 16, blocks=4097)):
         assert call(**kw) == EUNSUP, kw
     need = P.block_select_workspace_bytes(2, 3, 600, 32, 8)
     assert need > 0
@@ -128,7 +131,8 @@ def test_phase2_sparse():
                dict(V=FAKE + 8), dict(Kg=FAKE + 8), dict(o=FAKE + 8)):
         assert call(**kw) == EINVAL, kw
     for kw in (dict(d=96), dict(block=24), dict(block=8), dict(S=1 << 31), dict(G=1 << 24),
-               dict(topk=1 << 25), dict(Hkv=1 << 17, Hq=1 << 17)):
+               dict(topk=1 << 25), dict(Hkv=1 << 17, Hq=1 << 17), dict(Tq=1 << 23),
+               dict(Tq=1 << 20, Hkv=1, Hq=32)):
         assert call(**kw) == EUNSUP, kw
     assert P.phase2_sparse_workspace_bytes(3, 32, 8, 128) > 0
     for kw in (dict(ws=None), dict(wsb=16), dict(ws=FAKE + 8)):

@@ -274,6 +274,116 @@ def test_sparse_tokens_that_share_lists():
         _sparse(Hq, Hkv, d, Tq, 5, ns, S, block, topk, 4172, sel=sel, what="one twice")
 
 
+def _fill_up(sel, Hq, Hkv, d, block, rng):
+    """The lists filled up with -1, at any place, to where neighbouring tokens' lists are
+    read together: 400 MB of listed keys, and as many entries per tile as its list holds."""
+    ns, Tq, _, topk = sel.shape
+    steps = -(-(400 << 20) // (Tq * Hkv * 32 * d * 4))
+    wide = -(-steps * 32 // block // ns) + 1
+    tokens = min(16 // (Hq // Hkv), 8, Tq)
+    assert wide >= topk and tokens > 1 and ns * wide * tokens <= (3584 if d == 128 else 1792)
+    sel = np.concatenate([sel, np.full((ns, Tq, Hkv, wide - topk), -1)], axis=3)
+    return rng.permuted(sel, axis=3)
+
+
+TOGETHER = [  # Hq, Hkv, d, Tq, ns, S, block, topk
+    (32, 8, 128, 13, 2, 1000, 32, 6),     # four tokens per tile, one in the last
+    (16, 16, 64, 33, 3, 700, 16, 9),      # eight
+    (16, 2, 128, 6, 1, 4000, 64, 20),     # two
+    (4, 2, 64, 40, 2, 1500, 128, 5),      # eight of two heads
+    (12, 4, 128, 10, 2, 900, 64, 5),      # five of three heads: 15 columns
+    (20, 4, 64, 8, 1, 1030, 128, 6),      # three of five heads
+    (28, 4, 128, 7, 1, 1300, 128, 7),     # two of seven
+]
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,Tq,ns,S,block,topk", TOGETHER)
+def test_tokens_read_together(Hq, Hkv, d, Tq, ns, S, block, topk):
+    rng = np.random.default_rng(Hq + Tq)
+    blocks = -(-S // block)
+
+    def go(sel, seed, what, **kw):
+        _sparse(Hq, Hkv, d, Tq, kw.pop("G", 5), ns, S, block, topk, seed,
+                sel=_fill_up(sel, Hq, Hkv, d, block, rng), what=what, **kw)
+
+    same = np.sort(rng.permutation(blocks)[:topk])
+    sel = np.broadcast_to(same, (ns, Tq, Hkv, topk)).copy()
+    go(sel, 4190, "the same lists", bf16_out=True)
+    for t in range(0, Tq, 2):
+        sel[:, t] = np.sort(rng.permutation(blocks)[:topk])
+    go(sel, 4191, "some the same")
+    go(sel, 4192, "peaked", q_scale=8.0)
+    sees, _ = ob.tree_visible(random_tree(Tq, Tq, dead=(Tq // 2,)))
+    go(sel, 4193, "a tree", sees=sees, G=40)
+    go(sel, 4194, "no appended rows", gen=False, G=0)
+    sel[:] = rng.integers(-2, blocks + 2, sel.shape)
+    sel[:, Tq - 1] = -1
+    go(sel, 4195, "gaps and repeats", gen=False, G=0)
+    sel[ns - 1, Tq // 2, 0, :] = blocks - 1
+    go(sel, 4196, "one many times")
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,Tq,ns,S,block,topk", TOGETHER[:4])
+def test_tokens_read_together_keep_their_rows(Hq, Hkv, d, Tq, ns, S, block, topk):
+    # what a block that one token alone lists holds, and the rows of drafts that few see,
+    # reaches no other token, and shows in that one
+    rng = np.random.default_rng(Hq)
+    blocks, G = -(-S // block), 20
+    q = normal(66, (Tq, Hq, d))
+    k, v = (normal(s, (ns, S, Hkv, d)) for s in (67, 68))
+    kg, vg = (normal(s, (G + Tq, Hkv, d)) for s in (69, 70))
+    sel = np.broadcast_to(np.r_[:topk - 1, blocks - 1], (ns, Tq, Hkv, topk)).copy()
+    sel[0, 3, :, 1] = blocks - 2  # token 3's own
+    sel = _fill_up(sel, Hq, Hkv, d, block, rng)
+    sees = np.tril(np.ones((Tq, Tq), bool))
+    sees[:, 4] = False
+    sees[4, 4] = True  # draft 4: its own alone
+    ref, keys = sparse_reference(q, k, v, sel, block, kg, vg, G, sees, 1 / math.sqrt(d))
+    for t, where in ((3, "block"), (4, "draft")):
+        others = np.arange(Tq) != t
+        part = (ref[0][others], ref[1][:, others], ref[2][others], ref[3])
+        pick = torch.from_numpy(others).cuda()
+        for word in (0x7FC0, 0x7F80, 0xFF80):
+            for what in ("K", "V"):
+                x = {"K": k.copy(), "V": v.copy(), "Kg": kg.copy(), "Vg": vg.copy()}
+                if where == "block":
+                    x[what][0, (blocks - 2) * block:(blocks - 1) * block] = word
+                else:
+                    x[what + "g"][G + 4] = word
+                dev = {n: to_dev_bf16(y) for n, y in x.items()}
+                o, lse = P.phase2_sparse(to_dev_bf16(q), dev["K"], dev["V"], dev_i32(sel), block,
+                                         dev["Kg"], dev["Vg"], G, dev_mask(sees))
+                check(o[pick], lse[:, pick], part, keys, f"{where} {what} {word:x}")
+                # (an infinite score of either sign per channel: NaN; a head whose q has
+                # one sign alone would be another)
+                assert not torch.isfinite(o[t]).any(), f"{where} {what} {word:x}"
+
+
+def test_infinities_that_are_seen():
+    # an infinite value in a row that a token sees is its output, however the work is split
+    Tq, G, Hq, Hkv, d, ns, S, block = 3, 700, 32, 8, 128, 5, 611, 16
+    q = normal(141, (Tq, Hq, d))
+    k, v = (normal(s, (ns, S, Hkv, d)) for s in (142, 143))
+    kg, vg = (normal(s, (G + Tq, Hkv, d)) for s in (144, 145))
+    sel = np.broadcast_to(np.arange(39), (ns, Tq, Hkv, 39))
+    sees = np.tril(np.ones((Tq, Tq), bool))
+    for n, place in enumerate(((0, 0), (ns - 1, S - 1), (ns - 1, S - 3), (2, 300), "gen", "own")):
+        vb, vgb = v.copy(), vg.copy()
+        if place == "gen":
+            vgb[G - 1] = 0x7F80
+        elif place == "own":
+            vgb[G] = 0x7F80
+        else:
+            vb[place] = 0x7F80
+        a = [to_dev_bf16(x) for x in (q, kg, vgb, k, vb)]
+        for o, lse in (P.phase2_tree(a[0], a[1], a[2], G, dev_mask(sees), a[3], a[4]),
+                       P.phase2_tree(a[0], a[1], a[2], G, dev_mask(sees)) if n > 3 else (None,) * 2,
+                       P.phase2_sparse(a[0], a[3], a[4], dev_i32(sel), block, a[1], a[2], G)):
+            if o is not None:
+                assert torch.isposinf(o).all(), place
+                assert torch.isfinite(lse).all(), place
+
+
 def test_sparse_lists_too_long_for_a_union():
     _sparse(4, 2, 64, 9, 3, 1, 14000, 16, 500, 4180, what="long lists")
     _sparse(4, 1, 128, 3, 3, 70, 16 * 1000, 16, 1, 4181, what="many blocks")

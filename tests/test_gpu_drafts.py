@@ -216,6 +216,79 @@ def test_tree_workspace_sized_once():
                 assert torch.equal(o, ref[0]) and torch.equal(lse, ref[1]), (Tq, g0, h, s)
 
 
+def test_tree_over_more_than_four_gib():
+    # shards of 2 GB each in one launch: rows whose byte offsets pass 32 bits
+    ns, Hq, Hkv, d, S, G = 3, 32, 8, 128, 1000000, 2
+    q = normal(76, (1, Hq, d))
+    q[:, :, 0] = 0x4100  # 8
+    ks, vs = normal(77, (6, Hkv, d)), normal(78, (6, Hkv, d))
+    ks[:, :, 0] = 0
+    kg, vg = (normal(s, (G + 1, Hkv, d)) for s in (79, 80))
+    kg[:, :, 0] = 0
+    K = torch.zeros((ns, S, Hkv, d), dtype=torch.bfloat16, device="cuda")
+    V = torch.ones_like(K)
+    K[..., 0] = -256.0  # scores below -180: weights of 0 beside those of the six
+    at = [(0, 0), (0, S - 1), (1, 0), (1, 77777), (2, 400001), (2, S - 1)]
+    for i, (h, r) in enumerate(at):
+        K[h, r], V[h, r] = to_dev_bf16(ks[i]), to_dev_bf16(vs[i])
+    o, lse = P.phase2_tree(to_dev_bf16(q), to_dev_bf16(kg), to_dev_bf16(vg), G,
+                           dev_mask(np.ones((1, 1), bool)), K, V)
+    ref, keys = tree_reference(q, kg, vg, G, np.ones((1, 1), bool), ks[None], vs[None],
+                               1 / math.sqrt(d))
+    check(o, lse, ref, keys, "4 GiB")
+
+
+def test_refusals_of_device_tensors():
+    bf = {"dtype": torch.bfloat16, "device": "cuda"}
+    q, kg, k = torch.zeros(2, 8, 64, **bf), torch.zeros(6, 4, 64, **bf), torch.zeros(1, 40, 4, 64, **bf)
+    mask, sel = dev_i32([[1], [3]]), dev_i32(np.zeros((1, 2, 4, 1)))
+    bounds = P.key_bounds(k, 16)
+    keep = dev_i32([0, 1])
+    wrong = [
+        lambda: P.tree_mask(mask), lambda: P.tree_mask(keep.long()), lambda: P.tree_mask(keep.cpu()),
+        lambda: P.tree_mask(dev_i32(range(8))[::2]),
+        lambda: P.phase2_tree(q.float(), kg, kg, 4, mask), lambda: P.phase2_tree(q, kg, kg, 3, mask),
+        lambda: P.phase2_tree(q, kg, kg[:5], 4, mask), lambda: P.phase2_tree(q, kg, kg, 4, mask[:1]),
+        lambda: P.phase2_tree(q, kg, kg, 4, mask.cpu()),
+        lambda: P.phase2_tree(q, kg, kg, 4, mask, k, k[:, :9]),
+        lambda: P.phase2_tree(q, kg, kg, 4, mask, k[:, ::2], k[:, ::2]),
+        lambda: P.phase2_tree(q, kg, kg, 4, mask, o_dtype=7),
+        lambda: P.phase2_tree(q, kg.cpu(), kg, 4, mask),
+        lambda: P.phase2_tree(q.transpose(0, 1).contiguous().transpose(0, 1), kg, kg, 4, mask),
+        lambda: P.kv_compact_(k, k, 0, keep), lambda: P.kv_compact_(k, k.clone()[:, :9], 0, keep),
+        lambda: P.kv_compact_(torch.zeros(3, 9, 1, 8, **bf)[:2], torch.zeros(2, 9, 1, 8), 0, keep),
+        lambda: P.kv_compact_(k, k.clone(), 0, keep[None]),
+        lambda: P.key_bounds(k.float(), 16), lambda: P.key_bounds(k, (1 << 32) + 16),
+        lambda: P.key_bounds(k, 16 - (1 << 32)),
+        lambda: P.block_select(q, bounds[..., :32].contiguous(), 1),
+        lambda: P.block_select(q, bounds, (1 << 32) + 1),
+        lambda: P.block_select(q, bounds, 2 - (1 << 32)), lambda: P.block_select(q, bounds.cpu(), 1),
+        lambda: P.phase2_sparse(q, k, k[:, :9].contiguous(), sel, 16),
+        lambda: P.phase2_sparse(q, k, k, sel[:, :1].contiguous(), 16),
+        lambda: P.phase2_sparse(q, k, k, sel.long(), 16), lambda: P.phase2_sparse(q, k, k, sel, 16, kg),
+        lambda: P.phase2_sparse(q, k, k, sel, 16, kg, kg, 3),
+        lambda: P.phase2_sparse(q, k, k, sel, 16, kg, kg, 4, mask[:, :0]),
+        lambda: P.phase2_sparse(q, k, k, sel, (1 << 32) + 16),
+    ]
+    for i, fn in enumerate(wrong):
+        with pytest.raises(ValueError):
+            fn()
+            pytest.fail(f"call {i} was not refused")
+    both = torch.zeros(2, 1, 40, 4, 64, **bf)
+    shared = both.view(-1)[:both.numel() // 2 + 8 * 4 * 64]
+    with pytest.raises(ValueError):  # the second half begins inside the first
+        P.kv_compact_(shared[:40 * 256].view(1, 40, 4, 64),
+                      shared[8 * 256:].view(1, 40, 4, 64), 0, keep)
+    for fn in (lambda: P.key_bounds(k, 24), lambda: P.key_bounds(k, 0),
+               lambda: P.block_select(q, bounds, 4), lambda: P.block_select(q, bounds, -1),
+               lambda: P.phase2_sparse(q, k, k, sel, 24), lambda: P.kv_compact_(k, k.clone(), 39, keep),
+               lambda: P.kv_compact_(k, k.clone(), -1, keep),
+               lambda: P.phase2_sparse(q, k, k, sel, 16, softmax_scale=0.0),
+               lambda: P.phase2_sparse(q, k, k, sel, 16, mask=mask)):
+        with pytest.raises(RuntimeError):
+            fn()
+
+
 def _compact(layers, capacity, Hkv, d, G, keep, what):
     shape = (layers, capacity, Hkv, d)
     k, v = normal(81, shape), normal(82, shape)
