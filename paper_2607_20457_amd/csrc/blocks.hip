@@ -364,6 +364,7 @@ __device__ __forceinline__ f32x4 near_scores(const BoundsTile<D>& b, const bf16x
 __device__ __forceinline__ int ordered(int x) { return x ^ ((x >> 31) & 0x7fffffff); }
 constexpr int kLeast = (int)0x80000000;
 __device__ __forceinline__ float ordered_float(int x) { return __int_as_float(ordered(x)); }
+
 // near[row][b] for every row (shard, t, kvh), and norms[shard][kvh][b / 16], the
 // largest |m| of 16 blocks.  A workgroup holds 64 blocks and walks over units of 16
 // columns, eight of them staged at a time: 16 / group tokens, or 16 heads of one
@@ -739,7 +740,9 @@ void block_pick_kernel(const uint16_t* __restrict__ q, const uint16_t* __restric
     }
     const bool zeros = (norm == 0.f && most < INFINITY) || (most == 0.f && norm < INFINITY);
     // (all scores of zeros are 0)
-    const float E = zeros ? 0.f : fmaxf(norm * most * kNearError<D>, kNearLeast);
+    // (no number where one of the norms is 0 and the other infinite)
+    const float off = norm * most * kNearError<D>;
+    const float E = zeros ? 0.f : off < INFINITY ? fmaxf(off, kNearLeast) : INFINITY;
     const float fa = unrising(ends[0]);
     const bool settled = topk == blocks ||
                          (reach == topk && fa - unrising(ends[1]) > 2 * E) || zeros;

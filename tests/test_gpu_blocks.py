@@ -106,6 +106,37 @@ def test_block_select_of_special_values():
     _select(1, 80, 8, 2, 64, 3, 9, 17, b)
 
 
+@pytest.mark.parametrize("blocks,Tq", [(90, 2), (700, 9), (5000, 2)])
+def test_block_select_of_subnormal_values(blocks, Tq):
+    # subnormal queries or bounds beside large factors
+    x = np.sort(f64(normal(24, (1, 1, blocks, 2, 64))), axis=3)
+    q = f64(normal(25, (Tq, 4, 64)))
+
+    def words(x):
+        return torch.from_numpy(x).to(torch.bfloat16).view(torch.int16).numpy().view(np.uint16)
+
+    for a, b in ((-128, 120), (120, -128), (-128, 0)):
+        _select(1, blocks, 4, 1, 64, Tq, 11, 26, torch.from_numpy(x * 2.0 ** b).to(torch.bfloat16),
+                words(q * 2.0 ** a))
+
+
+@pytest.mark.parametrize("blocks,Tq", [(90, 2), (700, 9), (5000, 2)])
+@pytest.mark.parametrize("word", [0x7FC0, 0xFFC0, 0x7F80, 0xFF80])
+def test_block_select_of_zeros_and_what_is_not_finite(blocks, Tq, word):
+    # 0 times a bound, or a query, that is not finite is no number: +inf
+    x = np.sort(f64(normal(22, (1, 1, blocks, 2, 64))), axis=3)
+    b = torch.from_numpy(x).to(torch.bfloat16)
+    bits = b.view(torch.int16)
+    for i in (blocks - 1, blocks // 2, 40):
+        bits[0, 0, i, i % 2, i % 64] = word - (1 << 16) if word >> 15 else word
+    q = np.zeros((Tq, 4, 64), dtype=np.uint16)
+    _select(1, blocks, 4, 1, 64, Tq, 2, 23, b, q)
+    _select(1, blocks, 4, 1, 64, Tq, 7, 23, b, q)
+    q[:, 2, 9] = word
+    _select(1, blocks, 4, 1, 64, Tq, 7, 23, torch.zeros_like(b), q)
+    _select(1, blocks, 4, 1, 64, Tq, 7, 23, b, q)
+
+
 def _sparse(Hq, Hkv, d, Tq, G, ns, S, block, topk, seed, gen=True, sees=None, sel=None,
             bf16_out=False, q_scale=1.0, what="", k=None):
     print(f"phase2_sparse parity: {what} Hq={Hq} Hkv={Hkv} d={d} Tq={Tq} G={G} {ns}x{S} "
