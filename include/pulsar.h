@@ -557,6 +557,8 @@ int pulsar_block_select(const void* q, const void* bounds, int n_shards, int Tq,
  *           bytes, 16-byte aligned (may be NULL when that is 0); contents on
  *           entry do not matter.  The size holds for any number of tokens up to
  *           Tq and for any shards, lists and appended rows.
+ *           pulsar_phase2_sparse_call_bytes is what a call of just these sizes
+ *           takes (gen_rows: G + Tq, or 0 without Kg), often nothing.
  * EINVAL: negative sizes, Hq % Hkv != 0, NULL or misaligned pointers when there
  *         is work, only one of Kg and Vg, a mask or G > 0 without them, scale
  *         not finite and > 0, unknown o_dtype.  EWORKSPACE: workspace too small.
@@ -566,6 +568,8 @@ int pulsar_block_select(const void* q, const void* bounds, int n_shards, int Tq,
  *         Hkv rounded up to a multiple of 8).
  */
 size_t pulsar_phase2_sparse_workspace_bytes(int Tq, int Hq, int Hkv, int d);
+size_t pulsar_phase2_sparse_call_bytes(int n_shards, int Tq, int64_t S, int block, int topk,
+                                       int64_t gen_rows, int Hq, int Hkv, int d);
 int pulsar_phase2_sparse(const void* q, const void* K, const void* V, const int32_t* sel,
                          int n_shards, int Tq, int64_t S, int block, int topk, const void* Kg,
                          const void* Vg, int64_t G, const uint32_t* mask, int Hq, int Hkv, int d,

@@ -57,6 +57,8 @@ SIGNATURES = {
     "pulsar_block_select": (_c_int, [_vp, _vp, _c_int, _c_int, _c_int, _c_int, _c_int, _c_int,
                                      _c_int, _vp, _vp, _vp, _c_size, _vp]),
     "pulsar_phase2_sparse_workspace_bytes": (_c_size, [_c_int, _c_int, _c_int, _c_int]),
+    "pulsar_phase2_sparse_call_bytes": (_c_size, [_c_int, _c_int, _c_i64, _c_int, _c_int, _c_i64,
+                                                  _c_int, _c_int, _c_int]),
     "pulsar_phase2_sparse": (_c_int, [_vp, _vp, _vp, _vp, _c_int, _c_int, _c_i64, _c_int, _c_int,
                                       _vp, _vp, _c_i64, _vp, _c_int, _c_int, _c_int, _c_float,
                                       _vp, _c_int, _vp, _vp, _c_size, _vp]),

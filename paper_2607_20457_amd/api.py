@@ -394,7 +394,7 @@ def tree_mask(parent):
         raise ValueError("parent must be [T]")
     T = parent.shape[0]
     mask = parent.new_empty((T, (T + 31) // 32))
-    depth = parent.new_empty((T,))
+    depth = torch.empty_like(parent)
     st = _lib.lib().pulsar_tree_mask(parent.data_ptr(), T, mask.data_ptr(), depth.data_ptr(),
                                      _raw_stream(dev))
     _lib.check(st, "pulsar_tree_mask")
@@ -509,6 +509,12 @@ def phase2_sparse_workspace_bytes(Tq: int, Hq: int, Hkv: int, d: int) -> int:
     return int(_lib.lib().pulsar_phase2_sparse_workspace_bytes(Tq, Hq, Hkv, d))
 
 
+@functools.lru_cache(maxsize=4096)
+def _sparse_call_bytes(n_shards, Tq, S, block, topk, gen_rows, Hq, Hkv, d):
+    return int(_lib.lib().pulsar_phase2_sparse_call_bytes(n_shards, Tq, S, block, topk, gen_rows,
+                                                          Hq, Hkv, d))
+
+
 def phase2_sparse(q, K, V, sel, block: int, Kg=None, Vg=None, G: int = 0, mask=None,
                   softmax_scale: float | None = None, o_dtype: int = OUT_F32, workspace=None):
     """Attention of Tq new tokens over their selected blocks of the retained
@@ -540,7 +546,9 @@ def phase2_sparse(q, K, V, sel, block: int, Kg=None, Vg=None, G: int = 0, mask=N
         mask_ptr = mask.data_ptr()
     o = _out(q, o_dtype)
     lse = q.new_empty((Hq, Tq), dtype=torch.float32)
-    need = phase2_sparse_workspace_bytes(Tq, Hq, Hkv, d)
+    # (the plan takes the appended rows 32 at a time: few sizes to remember)
+    gen_rows = (G + Tq + 31 & ~31) if kg_ptr else 0
+    need = _sparse_call_bytes(n_shards, Tq, S, block, sel.shape[3], gen_rows, Hq, Hkv, d)
     workspace, ws_ptr = _scratch(workspace, need, dev, q)
     st = _lib.lib().pulsar_phase2_sparse(
         q.data_ptr(), K.data_ptr(), V.data_ptr(), sel.data_ptr(), n_shards, Tq, S, block,

@@ -112,6 +112,15 @@ size_t pulsar_phase2_sparse_workspace_bytes(int Tq, int Hq, int Hkv, int d) {
   return (size_t)sparse_part_rows_most(Tq, Hq, Hkv, d) * Hq * (d + 1) * 4;
 }
 
+size_t pulsar_phase2_sparse_call_bytes(int n_shards, int Tq, int64_t S, int block, int topk,
+                                       int64_t gen_rows, int Hq, int Hkv, int d) {
+  if (n_shards < 0 || Tq < 1 || S < 0 || topk < 0 || gen_rows < 0 || Hq < 1 || Hkv < 1 ||
+      Hq % Hkv != 0 || (d != 64 && d != 128) || !block_supported(block))
+    return 0;
+  const int parts = sparse_plan(n_shards, Tq, S, Hq, Hkv, d, block, topk, gen_rows).parts;
+  return parts == 1 ? 0 : (size_t)parts * Tq * Hq * (d + 1) * 4;
+}
+
 int pulsar_phase2_sparse(const void* q, const void* K, const void* V, const int32_t* sel,
                          int n_shards, int Tq, int64_t S, int block, int topk, const void* Kg,
                          const void* Vg, int64_t G, const uint32_t* mask, int Hq, int Hkv, int d,

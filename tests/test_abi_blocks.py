@@ -157,6 +157,36 @@ def test_phase2_sparse_workspace_serves_fewer_tokens():
                         assert call(Tq=Tq, n_shards=n, S=99999, topk=topk, G=G, wsb=size) != EWS
 
 
+def test_phase2_sparse_call_bytes():
+    # what a call takes: never more than the size for all calls, and neither less
+    lib = _lib.lib()
+    names = ("q K V sel n_shards Tq S block topk Kg Vg G mask Hq Hkv d scale o o_dtype lse ws wsb "
+             "stream")
+    for Hq, Hkv, d in ((32, 8, 128), (4, 1, 64), (16, 16, 64), (64, 1, 128), (28, 4, 128)):
+        call = caller("pulsar_phase2_sparse", names, q=FAKE, K=FAKE, V=FAKE, sel=FAKE, block=32,
+                      S=99999, Hq=Hq, Hkv=Hkv, d=d, scale=0.1, o=FAKE, o_dtype=0, ws=FAKE)
+        for Tq in (1, 2, 5, 64, 1000):
+            for n, topk, G in ((0, 0, 0), (1, 1, 0), (1, 300, 31), (16, 64, 5000), (2, 9, 100000)):
+                for gen in (0, G + Tq):
+                    size = lib.pulsar_phase2_sparse_call_bytes(n, Tq, 99999, 32, topk, gen, Hq, Hkv,
+                                                               d)
+                    assert size <= P.phase2_sparse_workspace_bytes(Tq, Hq, Hkv, d)
+                    if gen:
+                        assert size == lib.pulsar_phase2_sparse_call_bytes(
+                            n, Tq, 99999, 32, topk, gen + 31 & ~31, Hq, Hkv, d)
+                    kv = dict(Kg=FAKE, Vg=FAKE, G=G) if gen else dict(G=0)
+                    if size:
+                        assert call(n_shards=n, Tq=Tq, topk=topk, wsb=size - 1, **kv) == EWS
+                    if not torch.cuda.is_available():
+                        assert call(n_shards=n, Tq=Tq, topk=topk, wsb=size, **kv) != EWS
+    for bad in ((-1, 1, 1, 32, 1, 0, 8, 8, 64), (1, 0, 1, 32, 1, 0, 8, 8, 64),
+                (1, 1, -1, 32, 1, 0, 8, 8, 64), (1, 1, 1, 24, 1, 0, 8, 8, 64),
+                (1, 1, 1, 32, -1, 0, 8, 8, 64), (1, 1, 1, 32, 1, -1, 8, 8, 64),
+                (1, 1, 1, 32, 1, 0, 8, 3, 64), (1, 1, 1, 32, 1, 0, 8, 0, 64),
+                (1, 1, 1, 32, 1, 0, 8, 8, 96)):
+        assert lib.pulsar_phase2_sparse_call_bytes(*bad) == 0
+
+
 def test_binding_refuses_host_tensors():
     t = torch.zeros((1, 32, 1, 64), dtype=torch.bfloat16)
     i = torch.zeros(4, dtype=torch.int32)
