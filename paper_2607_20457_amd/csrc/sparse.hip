@@ -87,7 +87,7 @@ struct SpLds {
   static_assert(MODE != SP_UNION || REUSED >= sp_map(D), "the map passes through the stages");
 };
 
-template <int D, int NW, int MODE>
+template <int D, int NW, int MODE, int CG>
 __global__ __launch_bounds__(64 * NW)
 __attribute__((amdgpu_waves_per_eu(D == 128 ? 2 : 4, D == 128 ? 2 : 4)))
 void sparse_attn_kernel(SparseArgs a) {
@@ -119,22 +119,26 @@ void sparse_attn_kernel(SparseArgs a) {
   const int t0 = tile % a.token_tiles * a.tile_tokens;
   const int heads0 = tile / a.token_tiles * 16;
   const int tokens = min(a.tile_tokens, a.Tq - t0);  // of this tile
+  const int per = CG > 1 ? 16 / a.group : a.tile_tokens;  // of 16 columns
   const float c2 = a.scale_log2;
   const uint32_t row_bytes = (uint32_t)(a.Hkv * D * 2);
   const uint32_t head_off = (uint32_t)(kvh * D * 2);
 
-  // ---- Q fragments (B operand): column r = token tl of the tile, head ------------
-  const int tl = a.tile_tokens == 1 ? 0 : r / a.group;
-  const int col = heads0 + r - tl * a.group;  // head of the group
-  const bool live = tl < tokens && col < a.group;
-  const int t = t0 + (live ? tl : 0);
-  const int head = kvh * a.group + (live ? col : 0);
-  bf16x8 qf[DS];
-  {
-    const bf16x8* src =
-        reinterpret_cast<const bf16x8*>(a.q + ((int64_t)t * a.Hq + head) * D) + g;
+  // ---- Q fragments (B operand): column r of group c = token tl of the tile, head ----
+  int tl[CG], t[CG];
+  bf16x8 qf[CG][DS];
 #pragma unroll
-    for (int s = 0; s < DS; ++s) qf[s] = live ? src[4 * s] : bf16x8{};
+  for (int c = 0; c < CG; ++c) {
+    const int nth = a.tile_tokens == 1 ? 0 : r / a.group;
+    tl[c] = c * per + nth;
+    const int col = heads0 + r - nth * a.group;  // head of the group
+    const bool live = nth < per && tl[c] < tokens && col < a.group;
+    t[c] = t0 + (live ? tl[c] : 0);
+    const int head = kvh * a.group + (live ? col : 0);
+    const bf16x8* src =
+        reinterpret_cast<const bf16x8*>(a.q + ((int64_t)t[c] * a.Hq + head) * D) + g;
+#pragma unroll
+    for (int s = 0; s < DS; ++s) qf[c][s] = live ? src[4 * s] : bf16x8{};
   }
 
   // ---- the union of the tile's lists --------------------------------------------
@@ -379,13 +383,16 @@ void sparse_attn_kernel(SparseArgs a) {
                               (s16x8){lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
   };
 
-  f32x4 acc[DT];
-  float m_run, l_run, lr_run;
+  f32x4 acc[CG][DT];
+  float m_run[CG], l_run[CG], lr_run[CG];
   auto clear = [&]() {
 #pragma unroll
-    for (int e = 0; e < DT; ++e) acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-    m_run = -INFINITY;
-    l_run = lr_run = 0.f;
+    for (int c = 0; c < CG; ++c) {
+#pragma unroll
+      for (int e = 0; e < DT; ++e) acc[c][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+      m_run[c] = -INFINITY;
+      l_run[c] = lr_run[c] = 0.f;
+    }
   };
   // The wave's steps of the present plan; `guard`: key by key (see above).
   auto run = [&](auto guard_tag) {
@@ -407,15 +414,19 @@ void sparse_attn_kernel(SparseArgs a) {
       // K(j) is in LDS once only V(j)'s loads are outstanding
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(V_SEGS) : "memory");
       __builtin_amdgcn_sched_barrier(0);
-      f32x4 S[2];
+      f32x4 S[CG][2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        S[h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < DS; ++s)
-          S[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-              *reinterpret_cast<const lds_bf16x8*>(k_lds + h * (L::STAGE / 2) + k_at[s]), qf[s],
-              S[h], 0, 0, 0);
+        for (int c = 0; c < CG; ++c) S[c][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < DS; ++s) {
+          const bf16x8 k =
+              *reinterpret_cast<const lds_bf16x8*>(k_lds + h * (L::STAGE / 2) + k_at[s]);
+#pragma unroll
+          for (int c = 0; c < CG; ++c)
+            S[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[c][s], S[c][h], 0, 0, 0);
+        }
       }
       __builtin_amdgcn_sched_barrier(0);
       if (more) {
@@ -426,60 +437,70 @@ void sparse_attn_kernel(SparseArgs a) {
       __builtin_amdgcn_sched_barrier(0);
       // UNION: a column sees all of the step's keys or none where all rows are seen and
       // both halves are listed by the same tokens (`every`), else some of them
-      uint32_t vis = seen;
-      bool every = true, mine = true;
-      if constexpr (MODE == SP_UNION) {
-        if (st < list_steps) {
-          every = !guard && seen == 0xffffffffu && (who & 0xffu) == who >> 8;
-          mine = (who >> tl) & 1;
-          if (!every)
-            vis &= (mine ? 0xffffu : 0u) | ((who >> (8 + tl)) & 1 ? 0xffff0000u : 0u);
-        } else {
-          const int at = (st - list_steps) * SP_KEYS;
-          if (a.mask != nullptr || at + SP_KEYS > a.G) {
-            vis = gen_sees(at, t) | gen_sees(at + 16, t) << 16;
-            every = false;
+      uint32_t vis[CG];
+      bf16x8 P[CG];
+#pragma unroll
+      for (int c = 0; c < CG; ++c) {
+        vis[c] = seen;
+        bool every = true, mine = true;
+        if constexpr (MODE == SP_UNION) {
+          if (st < list_steps) {
+            // (16 columns whose tokens list neither half weigh nothing)
+            if (CG > 1 && ((who | who >> 8) >> (c * per) & ((1u << per) - 1)) == 0) {
+              P[c] = bf16x8{};
+              vis[c] = 0;
+              continue;
+            }
+            every = !guard && seen == 0xffffffffu && (who & 0xffu) == who >> 8;
+            mine = (who >> tl[c]) & 1;
+            if (!every)
+              vis[c] &= (mine ? 0xffffu : 0u) | ((who >> (8 + tl[c])) & 1 ? 0xffff0000u : 0u);
+          } else {
+            const int at = (st - list_steps) * SP_KEYS;
+            if (a.mask != nullptr || at + SP_KEYS > a.G) {
+              vis[c] = gen_sees(at, t[c]) | gen_sees(at + 16, t[c]) << 16;
+              every = false;
+            }
           }
         }
-      }
-      if (MODE == SP_UNION ? !every || seen != 0xffffffffu : seen != 0xffffffffu) {
+        f32x4(&Sc)[2] = S[c];
+        if (MODE == SP_UNION ? !every || seen != 0xffffffffu : seen != 0xffffffffu) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int v = 0; v < 4; ++v)
-            if (!((vis >> (16 * h + 4 * g + v)) & 1)) S[h][v] = -INFINITY;
-      }
-      float mx = S[0][0];
+            for (int v = 0; v < 4; ++v)
+              if (!((vis[c] >> (16 * h + 4 * g + v)) & 1)) Sc[h][v] = -INFINITY;
+        }
+        float mx = Sc[0][0];
 #pragma unroll
-      for (int v = 1; v < 8; ++v) mx = fmaxf(mx, S[v >> 2][v & 3]);
-      mx = max_of_rows(mx) * c2;
-      if (MODE == SP_UNION && every) mx = mine ? mx : -INFINITY;
-      if (__any(mx > m_run + SP_SLACK)) {
-        const float m_new = mx > m_run + SP_SLACK ? mx : m_run;
-        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+        for (int v = 1; v < 8; ++v) mx = fmaxf(mx, Sc[v >> 2][v & 3]);
+        mx = max_of_rows(mx) * c2;
+        if (MODE == SP_UNION && every) mx = mine ? mx : -INFINITY;
+        if (__any(mx > m_run[c] + SP_SLACK)) {
+          const float m_new = mx > m_run[c] + SP_SLACK ? mx : m_run[c];
+          const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[c] - m_new);
 #pragma unroll
-        for (int e = 0; e < DT; ++e) acc[e] *= alpha;
-        l_run *= alpha;
-        lr_run *= alpha;
-        m_run = m_new;
-      }
-      // a column that has seen no key takes its weights against 0: they come out 0
-      float m_use = m_run == -INFINITY ? 0.f : m_run;
-      // (against infinity the weights of a step that it does not see come out 0, or not
-      // a number, which the pass's end finds)
-      if (MODE == SP_UNION && every) m_use = mine ? m_use : INFINITY;
-      bf16x8 P;
-      {
+          for (int e = 0; e < DT; ++e) acc[c][e] *= alpha;
+          l_run[c] *= alpha;
+          lr_run[c] *= alpha;
+          m_run[c] = m_new;
+        }
+        // a column that has seen no key takes its weights against 0: they come out 0
+        float m_use = m_run[c] == -INFINITY ? 0.f : m_run[c];
+        // (against infinity the weights of a step that it does not see come out 0, or not
+        // a number, which the pass's end finds)
+        if (MODE == SP_UNION && every) m_use = mine ? m_use : INFINITY;
         f32x8 p;
 #pragma unroll
         for (int v = 0; v < 8; ++v) {
-          p[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[v >> 2][v & 3], c2, -m_use));
-          l_run += p[v];
+          p[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(Sc[v >> 2][v & 3], c2, -m_use));
+          l_run[c] += p[v];
         }
-        P = __builtin_convertvector(p, bf16x8);
+        P[c] = __builtin_convertvector(p, bf16x8);
 #pragma unroll
         for (int v = 0; v < 8; v += 2)
-          lr_run = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{P[v], P[v + 1]}, kOnes2, lr_run, false);
+          lr_run[c] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{P[c][v], P[c][v + 1]}, kOnes2,
+                                                      lr_run[c], false);
       }
       // V(j) is in LDS once only K(j + 1)'s loads are outstanding
       __builtin_amdgcn_sched_barrier(0);
@@ -501,14 +522,22 @@ void sparse_attn_kernel(SparseArgs a) {
             for (int e = 0; e < DT; ++e) {
               const bf16x8 v = __builtin_bit_cast(
                   bf16x8, __builtin_bit_cast(u32x4, v_frag(v_lds, e)) & keep);
-              const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P, acc[e], 0, 0, 0);
-              if ((vis >> k) & 1) acc[e] = x;
+#pragma unroll
+              for (int c = 0; c < CG; ++c) {
+                const f32x4 x =
+                    __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P[c], acc[c][e], 0, 0, 0);
+                if ((vis[c] >> k) & 1) acc[c][e] = x;
+              }
             }
           }
         } else if (MODE == SP_UNION || seen == 0xffffffffu) {
 #pragma unroll
-          for (int e = 0; e < DT; ++e)
-            acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_frag(v_lds, e), P, acc[e], 0, 0, 0);
+          for (int e = 0; e < DT; ++e) {
+            const bf16x8 v = v_frag(v_lds, e);
+#pragma unroll
+            for (int c = 0; c < CG; ++c)
+              acc[c][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P[c], acc[c][e], 0, 0, 0);
+          }
         } else {
           // zeros in place of the copies, whose weights of zero an infinity would not heed
           u32x4 keep;
@@ -521,7 +550,7 @@ void sparse_attn_kernel(SparseArgs a) {
           for (int e = 0; e < DT; ++e) {
             const bf16x8 v = __builtin_bit_cast(
                 bf16x8, __builtin_bit_cast(u32x4, v_frag(v_lds, e)) & keep);
-            acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P, acc[e], 0, 0, 0);
+            acc[0][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P[0], acc[0][e], 0, 0, 0);
           }
         }
       }
@@ -540,9 +569,11 @@ void sparse_attn_kernel(SparseArgs a) {
       }
       bool bad = false;
 #pragma unroll
-      for (int e = 0; e < DT; ++e)
+      for (int c = 0; c < CG; ++c)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) bad |= acc[e][v] != acc[e][v];
+        for (int e = 0; e < DT; ++e)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) bad |= acc[c][e][v] != acc[c][e][v];
       return __builtin_amdgcn_readfirstlane(__any(bad)) != 0;
     };
     if (pass(std::false_type{})) pass(std::true_type{});
@@ -553,63 +584,67 @@ void sparse_attn_kernel(SparseArgs a) {
   }
 
   // ---- the waves' states, merged through LDS --------------------------------------
-  l_run += __shfl_xor(l_run, 16, 64);
-  l_run += __shfl_xor(l_run, 32, 64);
-  lr_run += __shfl_xor(lr_run, 16, 64);
-  lr_run += __shfl_xor(lr_run, 32, 64);
-  __syncthreads();  // every wave is done with its stages
   float* const states = reinterpret_cast<float*>(smem);
   float* const sums = states + NW * 16 * L::PITCH;
-  {
-    float* const mine = states + (wave * 16 + r) * L::PITCH;
-#pragma unroll
-    for (int e = 0; e < DT; ++e) *reinterpret_cast<f32x4*>(mine + 16 * e + 4 * g) = acc[e];
-    if (g == 0) {
-      sums[(wave * 16 + r) * 3] = m_run;
-      sums[(wave * 16 + r) * 3 + 1] = l_run;
-      sums[(wave * 16 + r) * 3 + 2] = lr_run;
-    }
-  }
-  __syncthreads();
-  // thread -> (column, four consecutive values), a row of D / 4 threads at a time
   constexpr int DL = D / 4;
   const int dv = tid % DL;
-  const int cols = a.tile_tokens == 1 ? min(16, a.group - heads0) : tokens * a.group;
-  for (int c = tid / DL; c < cols; c += 64 * NW / DL) {
-    float m = -INFINITY, l = 0.f, lr = 0.f;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) m = fmaxf(m, sums[(w * 16 + c) * 3]);
-    const float use = m == -INFINITY ? 0.f : m;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int c = 0; c < CG; ++c) {
+    l_run[c] += __shfl_xor(l_run[c], 16, 64);
+    l_run[c] += __shfl_xor(l_run[c], 32, 64);
+    lr_run[c] += __shfl_xor(lr_run[c], 16, 64);
+    lr_run[c] += __shfl_xor(lr_run[c], 32, 64);
+    __syncthreads();  // every wave is done with its stages, or the states before
+    {
+      float* const mine = states + (wave * 16 + r) * L::PITCH;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const float* x = sums + (w * 16 + c) * 3;
-      const float e = __builtin_amdgcn_exp2f(x[0] - use);
-      l += e * x[1];
-      lr += e * x[2];
-      o += e * *reinterpret_cast<const f32x4*>(states + (w * 16 + c) * L::PITCH + 4 * dv);
+      for (int e = 0; e < DT; ++e) *reinterpret_cast<f32x4*>(mine + 16 * e + 4 * g) = acc[c][e];
+      if (g == 0) {
+        sums[(wave * 16 + r) * 3] = m_run[c];
+        sums[(wave * 16 + r) * 3 + 1] = l_run[c];
+        sums[(wave * 16 + r) * 3 + 2] = lr_run[c];
+      }
     }
-    o *= lr != 0.f ? 1.f / lr : 0.f;  // (a NaN score leaves a NaN sum)
-    const int ct = a.tile_tokens == 1 ? 0 : c / a.group;
-    const int hd = kvh * a.group + heads0 + c - ct * a.group;
-    const int64_t at = ((int64_t)part * a.Tq + t0 + ct) * a.Hq + hd;
-    if (a.o_bf16)
-      static_cast<bf16x4*>(a.O)[at * DL + dv] = __builtin_convertvector(o, bf16x4);
-    else
-      static_cast<f32x4*>(a.O)[at * DL + dv] = o;
-    if (dv == 0 && a.lse != nullptr)
-      a.lse[((int64_t)part * a.Hq + hd) * a.Tq + t0 + ct] =
-          l != 0.f ? (m + __log2f(l)) * 0.69314718055994531f : -INFINITY;
+    __syncthreads();
+    // thread -> (column, four consecutive values), a row of D / 4 threads at a time
+    const int cols = a.tile_tokens == 1 ? min(16, a.group - heads0)
+                                        : min(per, tokens - c * per) * a.group;
+    for (int x = tid / DL; x < cols; x += 64 * NW / DL) {
+      float m = -INFINITY, l = 0.f, lr = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) m = fmaxf(m, sums[(w * 16 + x) * 3]);
+      const float use = m == -INFINITY ? 0.f : m;
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const float* y = sums + (w * 16 + x) * 3;
+        const float e = __builtin_amdgcn_exp2f(y[0] - use);
+        l += e * y[1];
+        lr += e * y[2];
+        o += e * *reinterpret_cast<const f32x4*>(states + (w * 16 + x) * L::PITCH + 4 * dv);
+      }
+      o *= lr != 0.f ? 1.f / lr : 0.f;  // (a NaN score leaves a NaN sum)
+      const int nth = a.tile_tokens == 1 ? 0 : x / a.group;
+      const int hd = kvh * a.group + heads0 + x - nth * a.group;
+      const int64_t at = ((int64_t)part * a.Tq + t0 + c * per + nth) * a.Hq + hd;
+      if (a.o_bf16)
+        static_cast<bf16x4*>(a.O)[at * DL + dv] = __builtin_convertvector(o, bf16x4);
+      else
+        static_cast<f32x4*>(a.O)[at * DL + dv] = o;
+      if (dv == 0 && a.lse != nullptr)
+        a.lse[((int64_t)part * a.Hq + hd) * a.Tq + t0 + c * per + nth] =
+            l != 0.f ? (m + __log2f(l)) * 0.69314718055994531f : -INFINITY;
+    }
   }
 }
 
-template <int D, int NW, int MODE>
+template <int D, int NW, int MODE, int CG = 1>
 int launch_tiles(const SparseArgs& a, hipStream_t stream) {
   constexpr size_t lds = SpLds<D, NW, MODE>::BYTES;
   const int64_t nwg =
       ((int64_t)a.Hkv * a.parts + 7) / 8 * 8 * ((int64_t)a.token_tiles * a.col_tiles);
   if (!grid_fits(nwg, 64 * NW)) return PULSAR_EUNSUPPORTED;
-  const auto kern = sparse_attn_kernel<D, NW, MODE>;
+  const auto kern = sparse_attn_kernel<D, NW, MODE, CG>;
   if (lds > 65536 &&
       hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize,
                           (int)lds) != hipSuccess)
@@ -633,12 +668,19 @@ int64_t steps_of(int64_t keys) { return (keys + SP_KEYS - 1) / SP_KEYS; }
 // heads), 560 MB 31 / 27; 32 tokens, 290 MB 19 / 22; 16 tokens, 275 MB 24 / 27.  (The
 // more they share the more it gives.)
 constexpr int64_t kUnionBytes = 400 << 20;
-
+// Two groups of 16 columns at d 128 (at d 64 they do not fit the registers of four waves),
+// as many tokens as a block's byte holds.
+static int tile_tokens_most(int group, int d) {
+  return std::min(16 / group * (d == 128 ? 2 : 1), 8);
+}
 static int union_tokens(int Tq, int Hkv, int group, int d, int64_t blocks, int64_t entries,
                         int64_t steps) {
-  const int fit = std::min(std::min(16 / group, 8), Tq);
-  if (fit < 2 || blocks > sp_map(d) || entries * fit > sp_list(d)) return 1;
-  return (int64_t)Tq * Hkv * steps * (SP_KEYS * d * 4) >= kUnionBytes ? fit : 1;
+  if (blocks > sp_map(d) || (int64_t)Tq * Hkv * steps * (SP_KEYS * d * 4) < kUnionBytes) return 1;
+  for (const int most : {tile_tokens_most(group, d), std::min(16 / group, 8)}) {
+    const int fit = std::min(most, Tq);
+    if (fit > 1 && std::min(entries * fit, blocks) <= sp_list(d)) return fit;
+  }
+  return 1;
 }
 
 SparsePlan sparse_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int d, int block, int topk,
@@ -665,7 +707,7 @@ SparsePlan sparse_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int d, 
 int64_t sparse_part_rows_most(int Tq, int Hq, int Hkv, int d) {
   if (Tq <= 0) return 0;
   // of tiles of several tokens: all of a tile's tokens have its parts
-  return (int64_t)tiles_at_once(d) / Hkv * std::min(std::max(std::min(16 / (Hq / Hkv), 8), 1), Tq);
+  return (int64_t)tiles_at_once(d) / Hkv * std::min(std::max(tile_tokens_most(Hq / Hkv, d), 1), Tq);
 }
 
 namespace {
@@ -709,6 +751,7 @@ int launch_sparse(const SparseLaunch& x, const SparsePlan& p, void* o, int o_bf1
   a.O = o;
   a.o_bf16 = o_bf16;
   a.lse = lse;
+  if (p.tokens > std::max(16 / a.group, 1)) return launch_tiles<128, 4, SP_UNION, 2>(a, stream);
   if (p.tokens > 1)
     return x.d == 128 ? launch_tiles<128, 4, SP_UNION>(a, stream)
                       : launch_tiles<64, 4, SP_UNION>(a, stream);
