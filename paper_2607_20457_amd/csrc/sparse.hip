@@ -7,8 +7,9 @@
 // them a 32-key step:
 //   LISTED  one token: its listed blocks in the list's order, then the generation
 //           shard's rows;
-//   UNION   several tokens: the blocks that any of them lists, each with the tokens
-//           that list it, found in LDS; then the generation shard's rows.  Where
+//   UNION   several tokens, in one or two groups of 16 columns: the blocks that any of
+//           them lists, each with the tokens that list it, found in LDS; then the
+//           generation shard's rows.  Where
 //           neighbouring tokens list the same blocks these are read and multiplied
 //           once, and else no column does more than it would alone;
 //   DENSE   all rows of the shards, then the appended rows.
@@ -241,7 +242,9 @@ void sparse_attn_kernel(SparseArgs a) {
   // ---- where the halves lie: lane 2i + h, half h of the wave's step base + i -----
   // Byte offset of the half's first row in K (or Kg), and its rows: those that some
   // column sees (bits 0-15) and those to load (bits 16-31); UNION: the tokens that
-  // see a listed half.  A half of which nothing is seen is loaded as its neighbour.
+  // see a listed half, and kEvery where both are seen whole, by the same ones.  A half
+  // of which nothing is seen is loaded as its neighbour.
+  constexpr uint32_t kEvery = 1u << 16;
   uint32_t tab_lo = 0, tab_hi = 0, tab_rows = 0, tab_tokens = 0;
   auto fill = [&](int base) {
     const ConstArgs& a = *reread();
@@ -299,6 +302,8 @@ void sparse_attn_kernel(SparseArgs a) {
     const uint32_t n_who = MODE == SP_UNION ? __shfl_xor((int)who, 1, 64) : 0u;
     const uint32_t own = sees ? who : n_who, other = n_sees ? n_who : who;
     tab_tokens = lane & 1 ? other | own << 8 : own | other << 8;
+    if (MODE == SP_UNION && st < list_steps && sees == 0xffffu && n_sees == 0xffffu && own == other)
+      tab_tokens |= kEvery;
   };
   struct Half {
     uint32_t rows;  // seen, and << 16 to load
@@ -333,52 +338,61 @@ void sparse_attn_kernel(SparseArgs a) {
   struct Step {
     Half half[2];
     int st;
+    uint32_t tokens;
   };
-  auto step_at = [&](int j) { return Step{{half(j, 0), half(j, 1)}, step0 + wave + NW * j}; };
+  auto step_at = [&](int j) {
+    return Step{{half(j, 0), half(j, 1)}, step0 + wave + NW * j,
+                MODE == SP_UNION
+                    ? (uint32_t)__builtin_amdgcn_readlane(tab_tokens, 2 * (j & 31)) : 0u};
+  };
   auto is_gen = [&](const Step& x) { return x.st >= list_steps; };
   // A row that is not to be loaded is loaded as the first one that is.
   auto issue = [&](const Step& x, const uint16_t* base, lds_u8* lds,
                    const uint32_t (&off)[H_SEGS]) {
     const uint32_t st = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)lds);
-    const bool whole = (x.half[0].rows & x.half[1].rows) >> 16 == 0xffffu;
+    __amdgpu_buffer_rsrc_t rsrc[2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
+    for (int h = 0; h < 2; ++h)
+      rsrc[h] = __builtin_amdgcn_make_buffer_rsrc(
           reinterpret_cast<uint8_t*>(const_cast<uint16_t*>(base)) + x.half[h].off, (short)0,
           (int)(16 * row_bytes), kBufferFlags);
-      if (whole) {
+    if ((x.half[0].rows & x.half[1].rows) >> 16 == 0xffffu) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < H_SEGS; ++i)
-          lds_dma16(rsrc, off[i], i * SEG_ROWS * row_bytes, st + (h * H_SEGS + i) * 1024);
-      } else {
+          lds_dma16(rsrc[h], off[i], i * SEG_ROWS * row_bytes, st + (h * H_SEGS + i) * 1024);
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
         const uint32_t load = x.half[h].rows >> 16;
         const int first = __builtin_ctz(load | 0x10000u) & 15;
 #pragma unroll
         for (int i = 0; i < H_SEGS; ++i) {
           const int row = i * SEG_ROWS + seg_row;
           const int from = (load >> row) & 1 ? row : first;
-          lds_dma16(rsrc, off[i] + (from - seg_row) * row_bytes, st + (h * H_SEGS + i) * 1024);
+          lds_dma16(rsrc[h], off[i] + (from - seg_row) * row_bytes, st + (h * H_SEGS + i) * 1024);
         }
       }
     }
   };
-  uint32_t k_at[DS];  // chunk 4s + g of row r of a half
+  const lds_u8* k_at[DS];  // chunk 4s + g of row r of a half
 #pragma unroll
-  for (int s = 0; s < DS; ++s) k_at[s] = (r * CPR + ((4 * s + g) ^ k_swizzle(r))) * 16;
+  for (int s = 0; s < DS; ++s) k_at[s] = k_lds + (r * CPR + ((4 * s + g) ^ k_swizzle(r))) * 16;
   // V^T rows e*16 .. of the step: lane (r, g) of a transposing read addresses row
   // 4g + r/4 of a half at head_dim 16e + 4 (r%4) and receives head_dim 16e + r of
   // keys 4g .. 4g+3 of it
-  uint32_t v_at[DT];
+  const lds_u8* v_at[DT];
   {
     const int row = 4 * g + (r >> 2), q4 = r & 3;
 #pragma unroll
     for (int e = 0; e < DT; ++e)
-      v_at[e] = row * (2 * D) + 16 * ((2 * e + (q4 >> 1)) ^ v_swizzle8(row)) + 8 * (q4 & 1);
+      v_at[e] = v_lds + row * (2 * D) + 16 * ((2 * e + (q4 >> 1)) ^ v_swizzle8(row)) + 8 * (q4 & 1);
   }
-  auto v_frag = [&](const lds_u8* sV, int e) -> bf16x8 {
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(sV + v_at[e]));
+  auto v_frag = [&](int e) -> bf16x8 {
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)v_at[e]);
     const s16x4 hi =
-        __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(sV + v_at[e] + 16 * (2 * D)));
+        __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(v_at[e] + 16 * (2 * D)));
     return __builtin_bit_cast(bf16x8,
                               (s16x8){lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
   };
@@ -408,8 +422,7 @@ void sparse_attn_kernel(SparseArgs a) {
       // the keys of the step that some column sees, and the tokens that list it
       const uint32_t seen = (next.half[0].rows & 0xffffu) | next.half[1].rows << 16;
       const int st = next.st;
-      const uint32_t who =
-          MODE == SP_UNION ? (uint32_t)__builtin_amdgcn_readlane(tab_tokens, 2 * (j & 31)) : 0u;
+      const uint32_t who = next.tokens;
       const bool more = j + 1 < nsteps;
       // K(j) is in LDS once only V(j)'s loads are outstanding
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(V_SEGS) : "memory");
@@ -422,7 +435,7 @@ void sparse_attn_kernel(SparseArgs a) {
 #pragma unroll
         for (int s = 0; s < DS; ++s) {
           const bf16x8 k =
-              *reinterpret_cast<const lds_bf16x8*>(k_lds + h * (L::STAGE / 2) + k_at[s]);
+              *reinterpret_cast<const lds_bf16x8*>(k_at[s] + h * (L::STAGE / 2));
 #pragma unroll
           for (int c = 0; c < CG; ++c)
             S[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[c][s], S[c][h], 0, 0, 0);
@@ -435,47 +448,43 @@ void sparse_attn_kernel(SparseArgs a) {
         issue(next, is_gen(next) ? a.Kg : a.K, k_lds, k_off);
       }
       __builtin_amdgcn_sched_barrier(0);
-      // UNION: a column sees all of the step's keys or none where all rows are seen and
-      // both halves are listed by the same tokens (`every`), else some of them
+      // UNION: a column sees all of the step's keys or none (`every`), else some of them
       uint32_t vis[CG];
-      bf16x8 P[CG];
+      const bool every = MODE == SP_UNION && !guard && (who & kEvery) != 0;
 #pragma unroll
-      for (int c = 0; c < CG; ++c) {
-        vis[c] = seen;
-        bool every = true, mine = true;
-        if constexpr (MODE == SP_UNION) {
-          if (st < list_steps) {
-            // (16 columns whose tokens list neither half weigh nothing)
-            if (CG > 1 && ((who | who >> 8) >> (c * per) & ((1u << per) - 1)) == 0) {
-              P[c] = bf16x8{};
-              vis[c] = 0;
-              continue;
-            }
-            every = !guard && seen == 0xffffffffu && (who & 0xffu) == who >> 8;
-            mine = (who >> tl[c]) & 1;
-            if (!every)
-              vis[c] &= (mine ? 0xffffu : 0u) | ((who >> (8 + tl[c])) & 1 ? 0xffff0000u : 0u);
-          } else {
+      for (int c = 0; c < CG; ++c) vis[c] = seen;
+      if (!every && (MODE == SP_UNION || seen != 0xffffffffu)) {
+#pragma unroll
+        for (int c = 0; c < CG; ++c) {
+          if constexpr (MODE == SP_UNION) {
             const int at = (st - list_steps) * SP_KEYS;
-            if (a.mask != nullptr || at + SP_KEYS > a.G) {
+            if (st < list_steps)
+              vis[c] &= ((who >> tl[c]) & 1 ? 0xffffu : 0u) |
+                        ((who >> (8 + tl[c])) & 1 ? 0xffff0000u : 0u);
+            else if (a.mask != nullptr || at + SP_KEYS > a.G)
               vis[c] = gen_sees(at, t[c]) | gen_sees(at + 16, t[c]) << 16;
-              every = false;
-            }
           }
-        }
-        f32x4(&Sc)[2] = S[c];
-        if (MODE == SP_UNION ? !every || seen != 0xffffffffu : seen != 0xffffffffu) {
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int v = 0; v < 4; ++v)
-              if (!((vis[c] >> (16 * h + 4 * g + v)) & 1)) Sc[h][v] = -INFINITY;
+              if (!((vis[c] >> (16 * h + 4 * g + v)) & 1)) S[c][h][v] = -INFINITY;
         }
-        float mx = Sc[0][0];
+      }
+      bf16x8 P[CG];
 #pragma unroll
-        for (int v = 1; v < 8; ++v) mx = fmaxf(mx, Sc[v >> 2][v & 3]);
+      for (int c = 0; c < CG; ++c) {
+        // (16 columns whose tokens see nothing of the step weigh nothing)
+        if (CG > 1 && ((who | who >> 8) >> (c * per) & ((1u << per) - 1) & 0xffu) == 0) {
+          P[c] = bf16x8{};
+          continue;
+        }
+        const bool mine = !every || ((who >> tl[c]) & 1);
+        float mx = S[c][0][0];
+#pragma unroll
+        for (int v = 1; v < 8; ++v) mx = fmaxf(mx, S[c][v >> 2][v & 3]);
         mx = max_of_rows(mx) * c2;
-        if (MODE == SP_UNION && every) mx = mine ? mx : -INFINITY;
+        if (MODE == SP_UNION) mx = mine ? mx : -INFINITY;
         if (__any(mx > m_run[c] + SP_SLACK)) {
           const float m_new = mx > m_run[c] + SP_SLACK ? mx : m_run[c];
           const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[c] - m_new);
@@ -489,11 +498,11 @@ void sparse_attn_kernel(SparseArgs a) {
         float m_use = m_run[c] == -INFINITY ? 0.f : m_run[c];
         // (against infinity the weights of a step that it does not see come out 0, or not
         // a number, which the pass's end finds)
-        if (MODE == SP_UNION && every) m_use = mine ? m_use : INFINITY;
+        if (MODE == SP_UNION) m_use = mine ? m_use : INFINITY;
         f32x8 p;
 #pragma unroll
         for (int v = 0; v < 8; ++v) {
-          p[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(Sc[v >> 2][v & 3], c2, -m_use));
+          p[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[c][v >> 2][v & 3], c2, -m_use));
           l_run[c] += p[v];
         }
         P[c] = __builtin_convertvector(p, bf16x8);
@@ -521,7 +530,7 @@ void sparse_attn_kernel(SparseArgs a) {
 #pragma unroll
             for (int e = 0; e < DT; ++e) {
               const bf16x8 v = __builtin_bit_cast(
-                  bf16x8, __builtin_bit_cast(u32x4, v_frag(v_lds, e)) & keep);
+                  bf16x8, __builtin_bit_cast(u32x4, v_frag(e)) & keep);
 #pragma unroll
               for (int c = 0; c < CG; ++c) {
                 const f32x4 x =
@@ -533,7 +542,7 @@ void sparse_attn_kernel(SparseArgs a) {
         } else if (MODE == SP_UNION || seen == 0xffffffffu) {
 #pragma unroll
           for (int e = 0; e < DT; ++e) {
-            const bf16x8 v = v_frag(v_lds, e);
+            const bf16x8 v = v_frag(e);
 #pragma unroll
             for (int c = 0; c < CG; ++c)
               acc[c][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P[c], acc[c][e], 0, 0, 0);
@@ -549,7 +558,7 @@ void sparse_attn_kernel(SparseArgs a) {
 #pragma unroll
           for (int e = 0; e < DT; ++e) {
             const bf16x8 v = __builtin_bit_cast(
-                bf16x8, __builtin_bit_cast(u32x4, v_frag(v_lds, e)) & keep);
+                bf16x8, __builtin_bit_cast(u32x4, v_frag(e)) & keep);
             acc[0][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P[0], acc[0][e], 0, 0, 0);
           }
         }
@@ -661,12 +670,12 @@ int64_t steps_of(int64_t keys) { return (keys + SP_KEYS - 1) / SP_KEYS; }
 
 }  // namespace
 
-// Tokens whose lists one tile reads together: as many as fit its 16 columns, where the
+// Tokens whose lists one tile reads together: as many as fit its columns, where the
 // union's map and list hold them and the rows that the tokens read one by one are
 // enough to pay for finding it.  Tokens that draw a quarter of the same blocks each,
-// one by one / together, us: 128 tokens, 2.2 GB 84 / 71; 64 of 2 heads of 64 (8 KV
-// heads), 560 MB 31 / 27; 32 tokens, 290 MB 19 / 22; 16 tokens, 275 MB 24 / 27.  (The
-// more they share the more it gives.)
+// one by one / together, us: 128 tokens, 2.2 GB 84 / 58 (65 in one group of columns);
+// 64 of 2 heads of 64 (8 KV heads), 560 MB 32 / 25; 32 tokens, 290 MB 20 / 21; 16
+// tokens, 275 MB 24 / 24.  (The more they share the more it gives.)
 constexpr int64_t kUnionBytes = 400 << 20;
 // Two groups of 16 columns at d 128 (at d 64 they do not fit the registers of four waves),
 // as many tokens as a block's byte holds.

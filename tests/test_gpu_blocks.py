@@ -307,12 +307,12 @@ def test_sparse_tokens_that_share_lists():
 
 def _fill_up(sel, Hq, Hkv, d, block, rng):
     """The lists filled up with -1, at any place, to where neighbouring tokens' lists are
-    read together: 400 MB of listed keys, and as many entries per tile as its list holds."""
+    read together: 400 MB of listed keys."""
     ns, Tq, _, topk = sel.shape
     steps = -(-(400 << 20) // (Tq * Hkv * 32 * d * 4))
     wide = -(-steps * 32 // block // ns) + 1
-    tokens = min(16 // (Hq // Hkv), 8, Tq)
-    assert wide >= topk and tokens > 1 and ns * wide * tokens <= (3584 if d == 128 else 1792)
+    tokens = min(16 // (Hq // Hkv) * (2 if d == 128 else 1), 8, Tq)
+    assert wide >= topk and tokens > 1 and ns * wide <= 1792
     sel = np.concatenate([sel, np.full((ns, Tq, Hkv, wide - topk), -1)], axis=3)
     return rng.permuted(sel, axis=3)
 
@@ -325,6 +325,9 @@ TOGETHER = [  # Hq, Hkv, d, Tq, ns, S, block, topk
     (12, 4, 128, 10, 2, 900, 64, 5),      # five of three heads: 15 columns
     (20, 4, 64, 8, 1, 1030, 128, 6),      # three of five heads
     (28, 4, 128, 7, 1, 1300, 128, 7),     # two of seven
+    (16, 8, 128, 9, 2, 900, 64, 5),       # eight of two heads of 128: one group of columns
+    (32, 8, 128, 4, 2, 3000, 128, 9),     # four, all there are
+    (16, 1, 128, 5, 1, 2000, 256, 6),     # two of sixteen, a group of columns each
 ]
 
 
