@@ -342,19 +342,28 @@ __device__ __forceinline__ float head_norm(const uint16_t* q, int lane) {
   return norm_of(wide);
 }
 
-// Near scores of 16 blocks (rows 4g + v) and 16 columns of q (lane (r, g): channels
-// 32 s + 8 g .. of column r).  As 16-bit integers the larger of a bf16 and 0 is its
-// positive part, the smaller its negative part.
+// As 16-bit integers the larger of a bf16 and 0 is its positive part, the smaller its
+// negative part.
+template <typename T>
+__device__ __forceinline__ T positive(T x) {
+  return __builtin_bit_cast(
+      T, __builtin_elementwise_max(__builtin_bit_cast(s16x8, x), (s16x8){}));
+}
+template <typename T>
+__device__ __forceinline__ T negative(T x) {
+  return __builtin_bit_cast(
+      T, __builtin_elementwise_min(__builtin_bit_cast(s16x8, x), (s16x8){}));
+}
+// Near scores of 16 blocks (rows 4g + v) and the parts of 16 columns of q (lane (r, g):
+// channels 32 s + 8 g .. of column r).
 template <int D>
-__device__ __forceinline__ f32x4 near_scores(const BoundsTile<D>& b, const bf16x8 (&q)[D / 32]) {
+__device__ __forceinline__ f32x4 near_scores(const BoundsTile<D>& b, const bf16x8 (&pos)[D / 32],
+                                             const bf16x8 (&neg)[D / 32]) {
   f32x4 up = {0.f, 0.f, 0.f, 0.f}, down = up;
 #pragma unroll
   for (int s = 0; s < D / 32; ++s) {
-    const s16x8 x = __builtin_bit_cast(s16x8, q[s]);
-    const bf16x8 pos = __builtin_bit_cast(bf16x8, __builtin_elementwise_max(x, (s16x8){}));
-    const bf16x8 neg = __builtin_bit_cast(bf16x8, __builtin_elementwise_min(x, (s16x8){}));
-    up = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.hi[s], pos, up, 0, 0, 0);
-    down = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.lo[s], neg, down, 0, 0, 0);
+    up = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.hi[s], pos[s], up, 0, 0, 0);
+    down = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.lo[s], neg[s], down, 0, 0, 0);
   }
   return up + down;
 }
@@ -366,12 +375,15 @@ constexpr int kLeast = (int)0x80000000;
 __device__ __forceinline__ float ordered_float(int x) { return __int_as_float(ordered(x)); }
 
 // near[row][b] for every row (shard, t, kvh), and norms[shard][kvh][b / 16], the
-// largest |m| of 16 blocks.  A workgroup holds 64 blocks and walks over units of 16
-// columns, eight of them staged at a time: 16 / group tokens, or 16 heads of one
-// token of a larger group, whose units follow one another.
+// largest |m| of 16 blocks.  A workgroup holds 64 blocks and walks over eight units of 16
+// columns: 16 / group tokens, or 16 heads of one token of a larger group, whose units
+// follow one another.  Bound by instructions: q is split into its parts once, where it
+// is staged, not by each wave (64 tokens over 4096 blocks of 8 KV heads, 15.5 -> 15.0 us;
+// 4 or 16 units per workgroup 17 and 18 us).
 // (The blocks pass through the same LDS first, so that four workgroups fit a compute
-// unit: 64 tokens over 4096 blocks of 8 KV heads are then one round of them.)
-constexpr int kUnits = 8;
+// unit: that call is then one round of them.)
+constexpr int kUnits = 4;    // staged at a time
+constexpr int kUnitsWg = 8;  // of a workgroup
 template <int D>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4)))
 void block_near_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ bounds, int Tq,
@@ -379,8 +391,8 @@ void block_near_kernel(const uint16_t* __restrict__ q, const uint16_t* __restric
                        float* __restrict__ near, float* __restrict__ norms) {
   constexpr int CQ = D / 8;
   constexpr int PER = 256 / (16 * CQ), U = kUnits / PER;  // a thread's units: every PER-th, U
-  __shared__ u32x4 s_rows[kUnits][16 * CQ];
-  static_assert(kUnits * CQ == 4 * (D / 4), "the blocks take as much");
+  __shared__ u32x4 s_rows[kUnits][2][16 * CQ];  // q's positive and negative parts
+  static_assert(kUnits * 2 * CQ == 4 * (D / 4), "the blocks take as much");
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
@@ -415,7 +427,7 @@ void block_near_kernel(const uint16_t* __restrict__ q, const uint16_t* __restric
   fetch(first);
   BoundsTile<D> b;
   {
-    u32x4* const mine = &s_rows[0][0] + wave * 16 * (D / 4);
+    u32x4* const mine = &s_rows[0][0][0] + wave * 16 * (D / 4);
     stage_bounds<D>(bounds + (int64_t)blockIdx.y * blocks * 2 * D, b0, blocks, lane, mine);
     b.read(mine, r, g);  // (the wave's own rows)
   }
@@ -428,15 +440,19 @@ void block_near_kernel(const uint16_t* __restrict__ q, const uint16_t* __restric
     __syncthreads();  // the rows before have been read
     const int n = min(kUnits, last - u0);
 #pragma unroll
-    for (int i = 0; i < U; ++i) s_rows[i * PER + unit0][chunk_at<CQ>(c, chunk)] = staged[i];
+    for (int i = 0; i < U; ++i) {
+      s_rows[i * PER + unit0][0][chunk_at<CQ>(c, chunk)] = positive(staged[i]);
+      s_rows[i * PER + unit0][1][chunk_at<CQ>(c, chunk)] = negative(staged[i]);
+    }
     __syncthreads();
     if (u0 + kUnits < last) fetch(u0 + kUnits);
     for (int u = 0; u < n; ++u) {
       const int t = (passes == 1 ? u0 + u : (u0 + u) / passes) * tokens + tl;
       const int pass = passes == 1 ? 0 : (u0 + u) % passes;
-      bf16x8 x[D / 32];
-      read_columns<D>(s_rows[u], r, g, x);
-      const f32x4 score = near_scores<D>(b, x);
+      bf16x8 pos[D / 32], neg[D / 32];
+      read_columns<D>(s_rows[u][0], r, g, pos);
+      read_columns<D>(s_rows[u][1], r, g, neg);
+      const f32x4 score = near_scores<D>(b, pos, neg);
       int now[4];
 #pragma unroll
       for (int v = 0; v < 4; ++v) now[v] = ordered(__float_as_int(score[v]));
@@ -527,9 +543,14 @@ __device__ __forceinline__ float fused_scores(const uint16_t* qt, const uint16_t
     int top[4] = {kLeast, kLeast, kLeast, kLeast};
     for (int h0 = 0; h0 < group; h0 += 16) {
       const bool live = h0 + r < group;
-      bf16x8 x[D / 32];
+      bf16x8 x[D / 32], pos[D / 32], neg[D / 32];
       read_columns<D>(l.q + h0 * CQ, r, g, x);
-      const f32x4 score = near_scores<D>(b, x);
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s) {
+        pos[s] = positive(x[s]);
+        neg[s] = negative(x[s]);
+      }
+      const f32x4 score = near_scores<D>(b, pos, neg);
 #pragma unroll
       for (int v = 0; v < 4; ++v)
         top[v] = max(top[v], live ? ordered(__float_as_int(score[v])) : kLeast);
@@ -552,9 +573,8 @@ void block_pick_kernel(const uint16_t* __restrict__ q, const uint16_t* __restric
                        int Hq, int Hkv, int blocks, int topk, int32_t* __restrict__ sel) {
   extern __shared__ uint32_t s_dynamic[];  // NEAR: [blocks]
   uint32_t* s_row = s_dynamic;
-  __shared__ int s_n[2][W];
   __shared__ int s_gt[W], s_eq[W];
-  __shared__ uint32_t s_lo[W], s_hi[W];
+  __shared__ u32x4 s_ends[W];
   __shared__ int s_bin[W > 1 ? 256 : 1], s_found[3];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -605,41 +625,38 @@ void block_pick_kernel(const uint16_t* __restrict__ q, const uint16_t* __restric
   uint32_t key[R];  // 0 past the row's end
 #pragma unroll
   for (int i = 0; i < R; ++i) {
-    const int at = i0 + 64 * i;
-    if constexpr (MODE == PICK_FUSED)
-      key[i] = at < blocks ? rising(__uint_as_float(s_row[at])) : 0u;
-    else
-      key[i] = at < blocks ? rising(scores[row * blocks + at]) : 0u;
+    const int at = min(i0 + 64 * i, blocks - 1);
+    if constexpr (MODE == PICK_FUSED) key[i] = s_row[at];
+    else key[i] = __float_as_uint(scores[row * blocks + at]);
   }
-  int turn = 0;
-  auto total = [&](int n) {  // over the waves
-    if (W == 1) return n;
-    if (lane == 0) s_n[turn & 1][wave] = n;
-    __syncthreads();
-    n = 0;
+  // the largest |q| of the group's heads: a wave takes every W-th
+  if constexpr (MODE == PICK_NEAR)
+    for (int h = wave; h < group; h += W) heads = fmaxf(heads, head_norm<D>(qt + h * D, lane));
 #pragma unroll
-    for (int w = 0; w < W; ++w) n += s_n[turn & 1][w];
-    ++turn;
-    return __builtin_amdgcn_readfirstlane(n);
-  };
-  auto spread = [&](uint32_t lo, uint32_t hi) {  // the smallest lo, the largest hi
-    lo = over_wave(lo, Least{});
-    hi = over_wave(hi, Most{});
-    if (W > 1) {
+  for (int i = 0; i < R; ++i) key[i] = i0 + 64 * i < blocks ? rising(__uint_as_float(key[i])) : 0u;
+  // The smallest lo, the largest of each other value.
+  auto spread = [&](uint32_t lo, uint32_t hi, float x = 0.f, float y = 0.f) {
+    u32x4 all = {over_wave(lo, Least{}), over_wave(hi, Most{}), 0u, 0u};
+    if (W > 1) {  // (x and y are not negative: they rank as their bits)
+      all[2] = over_wave(__float_as_uint(x), Most{});
+      all[3] = over_wave(__float_as_uint(y), Most{});
       __syncthreads();
-      if (lane == 0) {
-        s_lo[wave] = lo;
-        s_hi[wave] = hi;
-      }
+      if (lane == 0) s_ends[wave] = all;
       __syncthreads();
 #pragma unroll
       for (int w = 0; w < W; ++w) {
-        lo = min(lo, s_lo[w]);
-        hi = max(hi, s_hi[w]);
+        const u32x4 other = s_ends[w];
+        all[0] = min(all[0], other[0]);
+#pragma unroll
+        for (int k = 1; k < 4; ++k) all[k] = max(all[k], other[k]);
       }
+    } else if (MODE == PICK_NEAR) {
+      all[2] = over_wave(__float_as_uint(x), Most{});
+      all[3] = over_wave(__float_as_uint(y), Most{});
     }
-    return u32x2{(uint32_t)__builtin_amdgcn_readfirstlane(lo),
-                 (uint32_t)__builtin_amdgcn_readfirstlane(hi)};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) all[k] = __builtin_amdgcn_readfirstlane(all[k]);
+    return all;
   };
   // A value that `reach` >= topk keys reach, and fewer than topk a larger one where
   // reach > topk.  `kept` keys are kKept, those that are 0 take no part.
@@ -653,9 +670,13 @@ void block_pick_kernel(const uint16_t* __restrict__ q, const uint16_t* __restric
       lo = min(lo, key[i] - 1);
       hi = max(hi, key[i] + 1);
     }
-    const u32x2 ends = spread(lo, hi);
+    const u32x4 ends = spread(lo, hi, heads, most);
     lo = ends[0] + 1;
     hi = ends[1] - 1;
+    if constexpr (MODE == PICK_NEAR) {
+      heads = __uint_as_float(ends[2]);
+      most = __uint_as_float(ends[3]);
+    }
     if constexpr (W == 1) {
       reach = 0;
       while (lo < hi) {
@@ -726,22 +747,11 @@ void block_pick_kernel(const uint16_t* __restrict__ q, const uint16_t* __restric
       if (key[i] >= cut) a = min(a, key[i]);
       else b = max(b, key[i]);
     }
-    const u32x2 ends = spread(a, b);
-    // the largest |q| of the group's heads: a wave takes every W-th
-    float norm = 0.f;
-    if constexpr (MODE == PICK_FUSED) {
-      norm = heads;
-    } else {
-      for (int h = wave; h < group; h += W) norm = fmaxf(norm, head_norm<D>(qt + h * D, lane));
-    }
-    if (MODE == PICK_NEAR || W > 1) {  // (not negative: they rank as their bits)
-      norm = __uint_as_float(spread(0u, __float_as_uint(norm))[1]);
-      most = __uint_as_float(spread(0u, __float_as_uint(most))[1]);
-    }
-    const bool zeros = (norm == 0.f && most < INFINITY) || (most == 0.f && norm < INFINITY);
+    const u32x4 ends = spread(a, b);
+    const bool zeros = (heads == 0.f && most < INFINITY) || (most == 0.f && heads < INFINITY);
     // (all scores of zeros are 0)
     // (no number where one of the norms is 0 and the other infinite)
-    const float off = norm * most * kNearError<D>;
+    const float off = heads * most * kNearError<D>;
     const float E = zeros ? 0.f : off < INFINITY ? fmaxf(off, kNearLeast) : INFINITY;
     const float fa = unrising(ends[0]);
     const bool settled = topk == blocks ||
@@ -761,18 +771,23 @@ void block_pick_kernel(const uint16_t* __restrict__ q, const uint16_t* __restric
         n += __popcll(__ballot(may));
         kept += __popcll(__ballot(in));
       }
-      kept = total(kept);
       // their indices, listed after those of the waves before
       int at = 0, all = n;
       if (W > 1) {
-        if (lane == 0) s_gt[wave] = n;
+        if (lane == 0) {
+          s_gt[wave] = n;
+          s_eq[wave] = kept;
+        }
         __syncthreads();
-        all = 0;
+        all = kept = 0;
 #pragma unroll
         for (int w = 0; w < W; ++w) {
           at += w < wave ? s_gt[w] : 0;
           all += s_gt[w];
+          kept += s_eq[w];
         }
+        all = __builtin_amdgcn_readfirstlane(all);
+        kept = __builtin_amdgcn_readfirstlane(kept);
       }
       const int mine = at;
 #pragma unroll
@@ -939,7 +954,7 @@ int launch_block_near(const uint16_t* q, const uint16_t* bounds, int n_shards, i
   const int group = Hq / Hkv, tokens = std::max(16 / group, 1), passes = (group + 15) / 16;
   const int64_t units = (int64_t)((Tq + tokens - 1) / tokens) * passes;
   // a token's passes stay in one workgroup
-  const int per = std::max(kUnits / passes, 1) * passes;
+  const int per = std::max(kUnitsWg / passes, 1) * passes;
   const int64_t z = (units + per - 1) / per;
   const dim3 grid((blocks + 63) / 64, n_shards * Hkv, (unsigned)z);
   const auto kern = d == 128 ? block_near_kernel<128> : block_near_kernel<64>;
