@@ -670,22 +670,22 @@ int64_t steps_of(int64_t keys) { return (keys + SP_KEYS - 1) / SP_KEYS; }
 
 }  // namespace
 
-// Tokens whose lists one tile reads together: as many as fit its columns, where the
-// union's map and list hold them and the rows that the tokens read one by one are
-// enough to pay for finding it.  Tokens that draw a quarter of the same blocks each,
-// one by one / together, us: 128 tokens, 2.2 GB 84 / 58 (65 in one group of columns);
-// 64 of 2 heads of 64 (8 KV heads), 560 MB 32 / 25; 32 tokens, 290 MB 20 / 21; 16
-// tokens, 275 MB 24 / 24.  (The more they share the more it gives.)
-constexpr int64_t kUnionBytes = 400 << 20;
-// Two groups of 16 columns at d 128 (at d 64 they do not fit the registers of four waves),
-// as many tokens as a block's byte holds.
+// Tokens whose lists one tile reads together, where the rows that they read one by one
+// are enough to pay for finding the union: as many as fit 16 columns, or two groups of
+// 16 at d 128 (at d 64 these do not fit the registers of four waves), a block's byte and
+// the union's map and list.  Tokens that draw a quarter of the same blocks each, us, one
+// by one / 16 columns / 32: 32 heads of 128 over 8, 277 MB 24.4 / 28.0 / 28.8, 415 MB
+// 30.3 / 30.2 / 31.4, 587 MB 27.9 / 26.4 / 28.5, 837 MB 44.5 / 36.4 / 35.0, 2.2 GB 84 / 65
+// / 58; 16 of 64 over 16 and 8, 147 MB 16.2 / 16.9, 219 MB 19.6 / 20.1, 223 MB 18.9 / 18.5,
+// 292 MB 22.0 / 20.2, 447 MB 24.6 / 22.0.  (The more they share the more it gives.)
 static int tile_tokens_most(int group, int d) {
   return std::min(16 / group * (d == 128 ? 2 : 1), 8);
 }
 static int union_tokens(int Tq, int Hkv, int group, int d, int64_t blocks, int64_t entries,
                         int64_t steps) {
-  if (blocks > sp_map(d) || (int64_t)Tq * Hkv * steps * (SP_KEYS * d * 4) < kUnionBytes) return 1;
-  for (const int most : {tile_tokens_most(group, d), std::min(16 / group, 8)}) {
+  const int64_t mb = (int64_t)Tq * Hkv * steps * (SP_KEYS * d * 4) / 1000000;
+  if (blocks > sp_map(d) || mb < (d == 64 ? 250 : 400)) return 1;
+  for (const int most : {mb < 800 ? 1 : tile_tokens_most(group, d), std::min(16 / group, 8)}) {
     const int fit = std::min(most, Tq);
     if (fit > 1 && std::min(entries * fit, blocks) <= sp_list(d)) return fit;
   }

@@ -305,40 +305,39 @@ def test_sparse_tokens_that_share_lists():
         _sparse(Hq, Hkv, d, Tq, 5, ns, S, block, topk, 4172, sel=sel, what="one twice")
 
 
-def _fill_up(sel, Hq, Hkv, d, block, rng):
-    """The lists filled up with -1, at any place, to where neighbouring tokens' lists are
-    read together: 400 MB of listed keys."""
+def _fill_up(sel, Hkv, d, block, mb, rng):
+    """The lists filled up with -1, at any place, to that many MB of listed keys."""
     ns, Tq, _, topk = sel.shape
-    steps = -(-(400 << 20) // (Tq * Hkv * 32 * d * 4))
+    steps = -(-mb * 1000000 // (Tq * Hkv * 32 * d * 4))
     wide = -(-steps * 32 // block // ns) + 1
-    tokens = min(16 // (Hq // Hkv) * (2 if d == 128 else 1), 8, Tq)
-    assert wide >= topk and tokens > 1 and ns * wide <= 1792
+    assert wide >= topk
     sel = np.concatenate([sel, np.full((ns, Tq, Hkv, wide - topk), -1)], axis=3)
     return rng.permuted(sel, axis=3)
 
 
-TOGETHER = [  # Hq, Hkv, d, Tq, ns, S, block, topk
-    (32, 8, 128, 13, 2, 1000, 32, 6),     # four tokens per tile, one in the last
-    (16, 16, 64, 33, 3, 700, 16, 9),      # eight
-    (16, 2, 128, 6, 1, 4000, 64, 20),     # two
-    (4, 2, 64, 40, 2, 1500, 128, 5),      # eight of two heads
-    (12, 4, 128, 10, 2, 900, 64, 5),      # five of three heads: 15 columns
-    (20, 4, 64, 8, 1, 1030, 128, 6),      # three of five heads
-    (28, 4, 128, 7, 1, 1300, 128, 7),     # two of seven
-    (16, 8, 128, 9, 2, 900, 64, 5),       # eight of two heads of 128: one group of columns
-    (32, 8, 128, 4, 2, 3000, 128, 9),     # four, all there are
-    (16, 1, 128, 5, 1, 2000, 256, 6),     # two of sixteen, a group of columns each
+TOGETHER = [  # Hq, Hkv, d, Tq, ns, S, block, topk, MB: tiles of several tokens
+    (32, 8, 128, 13, 2, 1000, 32, 6, 800),    # eight tokens in 32 columns
+    (16, 16, 64, 33, 3, 700, 16, 9, 400),     # eight in eight
+    (16, 2, 128, 6, 1, 4000, 64, 20, 800),    # four of eight heads, two in the last
+    (4, 2, 64, 40, 2, 1500, 128, 5, 400),     # eight of two heads
+    (32, 8, 128, 13, 2, 1000, 32, 6, 400),    # four in 16 columns, one in the last
+    (12, 4, 128, 10, 2, 900, 64, 5, 800),     # eight of three heads: 15 columns and nine
+    (20, 4, 64, 8, 1, 1030, 128, 6, 400),     # three of five heads
+    (28, 4, 128, 7, 1, 1300, 128, 7, 800),    # four of seven
+    (16, 8, 128, 9, 2, 900, 64, 5, 800),      # eight of two heads: 16 columns
+    (32, 8, 128, 4, 2, 3000, 128, 9, 800),    # four, all there are
+    (16, 1, 128, 5, 1, 2000, 256, 6, 800),    # two of sixteen heads
 ]
 
 
-@pytest.mark.parametrize("Hq,Hkv,d,Tq,ns,S,block,topk", TOGETHER)
-def test_tokens_read_together(Hq, Hkv, d, Tq, ns, S, block, topk):
+@pytest.mark.parametrize("Hq,Hkv,d,Tq,ns,S,block,topk,mb", TOGETHER)
+def test_tokens_read_together(Hq, Hkv, d, Tq, ns, S, block, topk, mb):
     rng = np.random.default_rng(Hq + Tq)
     blocks = -(-S // block)
 
     def go(sel, seed, what, **kw):
         _sparse(Hq, Hkv, d, Tq, kw.pop("G", 5), ns, S, block, topk, seed,
-                sel=_fill_up(sel, Hq, Hkv, d, block, rng), what=what, **kw)
+                sel=_fill_up(sel, Hkv, d, block, mb, rng), what=what, **kw)
 
     same = np.sort(rng.permutation(blocks)[:topk])
     sel = np.broadcast_to(same, (ns, Tq, Hkv, topk)).copy()
@@ -357,8 +356,8 @@ def test_tokens_read_together(Hq, Hkv, d, Tq, ns, S, block, topk):
     go(sel, 4196, "one many times")
 
 
-@pytest.mark.parametrize("Hq,Hkv,d,Tq,ns,S,block,topk", TOGETHER[:4])
-def test_tokens_read_together_keep_their_rows(Hq, Hkv, d, Tq, ns, S, block, topk):
+@pytest.mark.parametrize("Hq,Hkv,d,Tq,ns,S,block,topk,mb", TOGETHER[:5])
+def test_tokens_read_together_keep_their_rows(Hq, Hkv, d, Tq, ns, S, block, topk, mb):
     # what a block that one token alone lists holds, and the rows of drafts that few see,
     # reaches no other token, and shows in that one
     rng = np.random.default_rng(Hq)
@@ -368,7 +367,7 @@ def test_tokens_read_together_keep_their_rows(Hq, Hkv, d, Tq, ns, S, block, topk
     kg, vg = (normal(s, (G + Tq, Hkv, d)) for s in (69, 70))
     sel = np.broadcast_to(np.r_[:topk - 1, blocks - 1], (ns, Tq, Hkv, topk)).copy()
     sel[0, 3, :, 1] = blocks - 2  # token 3's own
-    sel = _fill_up(sel, Hq, Hkv, d, block, rng)
+    sel = _fill_up(sel, Hkv, d, block, mb, rng)
     sees = np.tril(np.ones((Tq, Tq), bool))
     sees[:, 4] = False
     sees[4, 4] = True  # draft 4: its own alone
