@@ -475,7 +475,7 @@ void sparse_attn_kernel(SparseArgs a) {
 #pragma unroll
       for (int c = 0; c < CG; ++c) {
         // (16 columns whose tokens see nothing of the step weigh nothing)
-        if (CG > 1 && ((who | who >> 8) >> (c * per) & ((1u << per) - 1) & 0xffu) == 0) {
+        if (CG > 1 && (((who | who >> 8) & 0xffu) >> (c * per) & ((1u << per) - 1)) == 0) {
           P[c] = bf16x8{};
           continue;
         }
