@@ -531,6 +531,78 @@ def test_selection_and_attention_captured():
             assert torch.equal(a, b), i
 
 
+def test_one_workspace_for_all_calls():
+    # a loop's own workspace, full of NaN before every call; a smaller one is not used
+    Tq, G, Hq, Hkv, d, ns, S, block, topk = 20, 300, 32, 8, 128, 2, 20000, 16, 60
+    q = to_dev_bf16(normal(151, (Tq, Hq, d)))
+    k, v = (to_dev_bf16(normal(s, (ns, S, Hkv, d))) for s in (152, 153))
+    kg, vg = (to_dev_bf16(normal(s, (G + Tq, Hkv, d))) for s in (154, 155))
+    bounds = P.key_bounds(k, block)
+    blocks = bounds.shape[2]
+    mask, _ = P.tree_mask(dev_i32(random_tree(156, Tq)))
+    size = max(P.phase2_sparse_workspace_bytes(Tq, Hq, Hkv, d),
+               P.block_select_workspace_bytes(ns, Tq, blocks, Hq, Hkv),
+               P.phase2_tree_workspace_bytes(ns, Tq, S, G, Hq, Hkv, d))
+    whole = torch.full((size // 4 + 4097,), 7.0, device="cuda")
+    ws, behind = whole[:size // 4 + 1], whole[size // 4 + 1:]
+    few = torch.empty(16, device="cuda")
+    for n in (Tq, 3, 1):
+        qn, m = q[:n], mask[:n, :(n + 31) // 32].contiguous()
+        want = None
+        for w in (None, ws, few):
+            out = []
+            for fn in (lambda: P.block_select(qn, bounds, topk, workspace=w),
+                       lambda: P.phase2_sparse(qn, k, v, out[0], block, kg[:G + n], vg[:G + n], G,
+                                               workspace=w),
+                       lambda: P.phase2_tree(qn, kg[:G + n], vg[:G + n], G, m, k, v, workspace=w)):
+                ws.fill_(math.nan)
+                few.fill_(math.nan)
+                r = fn()
+                out += [r] if torch.is_tensor(r) else r
+            want = want or out
+            assert all(torch.equal(a, b) for a, b in zip(out, want)), n
+            assert torch.isnan(few).all()
+    assert (behind == 7).all()
+
+
+def test_graphs_that_share_a_workspace():
+    # two captured steps of different sizes through one workspace, replayed in turn
+    G, Hq, Hkv, d, ns, S, block, topk = 40, 32, 8, 128, 2, 20000, 16, 60
+    k, v = (to_dev_bf16(normal(s, (ns, S, Hkv, d))) for s in (161, 162))
+    kg, vg = (to_dev_bf16(normal(s, (G + 12, Hkv, d))) for s in (163, 164))
+    qs = [to_dev_bf16(normal(165 + n, (n, Hq, d))) for n in (12, 1)]
+    bounds = P.key_bounds(k, block)
+    masks = [P.tree_mask(dev_i32(random_tree(n, n)))[0] for n in (12, 1)]
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
+
+    def step(q, mask):
+        n = q.shape[0]
+        sel = P.block_select(q, bounds, topk, workspace=ws)
+        return (sel,) + P.phase2_sparse(q, k, v, sel, block, kg[:G + n], vg[:G + n], G, mask,
+                                        workspace=ws) + P.phase2_tree(
+            q, kg[:G + n], vg[:G + n], G, mask, k, v, workspace=ws)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for q, m in zip(qs, masks):
+            step(q, m)
+    side.synchronize()
+    graphs, outs = [], []
+    for q, m in zip(qs, masks):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            outs.append(step(q, m))
+    for i in range(3):
+        for q in qs:
+            q.mul_(-1)
+        kg[:G].mul_(-1)
+        for g in (graphs if i % 2 else graphs[::-1]):
+            g.replay()
+        torch.cuda.synchronize()
+        for q, m, out in zip(qs, masks, outs):
+            assert all(torch.equal(a, b) for a, b in zip(out, step(q, m))), i
+
+
 def test_calls_on_two_streams_at_once():
     Hq, Hkv, d, ns, S, block, topk = 32, 8, 128, 4, 2048, 32, 16
     k, v = (to_dev_bf16(normal(s, (ns, S, Hkv, d))) for s in (131, 132))

@@ -335,6 +335,33 @@ def test_compact_random_lists():
     _compact(130, 60, 9, 64, 2, np.arange(3, 58), "many layers")
 
 
+@pytest.mark.parametrize("n", [7, 200])
+def test_compact_captured_and_replayed(n):
+    # the list changes on the device between the replays, its length with it
+    layers, capacity, Hkv, d, G = 3, 400, 2, 64, 50
+    k, v = (normal(s, (layers, capacity, Hkv, d)) for s in (84, 85))
+    K, V = to_dev_bf16(k), to_dev_bf16(v)
+    keep = dev_i32(np.full(n, -1))
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        P.kv_compact_(K, V, G, keep)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        P.kv_compact_(K, V, G, keep)
+    rng = np.random.default_rng(n)
+    for i in range(4):
+        rows = np.full(n, -1)
+        m = (n, n // 2, 0, n)[i]
+        rows[:m] = np.sort(rng.choice(capacity - G, size=m, replace=False))
+        keep.copy_(dev_i32(rows))
+        graph.replay()
+        torch.cuda.synchronize()
+        k, v = (ob.kv_compact(x, G, rows) for x in (k, v))
+        for got, x in ((K, k), (V, v)):
+            assert np.array_equal(got.view(torch.int16).cpu().numpy().view(np.uint16), x), i
+
+
 def test_compact_past_two_gib():
     # a layer behind the 32-bit offsets of the cache
     layers, capacity, Hkv, d, G = 3, 530000, 8, 128, 500000
