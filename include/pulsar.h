@@ -564,8 +564,7 @@ int pulsar_block_select(const void* q, const void* bounds, int n_shards, int Tq,
  *         not finite and > 0, unknown o_dtype.  EWORKSPACE: workspace too small.
  * EUNSUPPORTED: d not in {64, 128}; another block; S >= 2^31; G + Tq >= 2^24;
  *         2^30 listed keys or more; a row of K of 16 MiB or more; more workgroups
- *         than a launch holds (none below Tq * H * ceil(Hq / Hkv / 16) = 2^24, H being
- *         Hkv rounded up to a multiple of 8).
+ *         than a launch holds (none below Tq * Hkv * ceil(Hq / Hkv / 16) = 2^23).
  */
 size_t pulsar_phase2_sparse_workspace_bytes(int Tq, int Hq, int Hkv, int d);
 size_t pulsar_phase2_sparse_call_bytes(int n_shards, int Tq, int64_t S, int block, int topk,

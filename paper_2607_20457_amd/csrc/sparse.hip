@@ -60,6 +60,7 @@ struct SparseArgs {
   int tile_tokens;       // tokens per tile
   int token_tiles;       // tiles over the tokens
   int col_tiles;         // tiles over a token's heads (1 where a tile holds them all)
+  int slices;            // XCDs over which the tiles of a head's part are spread
   int n_shards, topk, entries;  // listed blocks per shard; of all shards
   int half_log2;         // log2 of a block's halves
   int blocks;            // blocks per shard
@@ -111,11 +112,15 @@ void sparse_attn_kernel(SparseArgs a) {
   const int r = lane & 15, g = lane >> 4;
   // Workgroup -> (token tile, heads) of a (KV head, part).  Workgroups go to the eight
   // XCDs in turn, each with an L2 of its own: all tiles of one head's part, which read
-  // the same keys (or blocks that they share), go to one of them, one after another.
+  // the same keys (or blocks that they share), go to one of them, one after another;
+  // where there are few such parts, to `slices` of them.
+  const int tiles = a.token_tiles * a.col_tiles, deep = (tiles + a.slices - 1) / a.slices;
   int64_t wg = blockIdx.x >> 3;
-  const int tile = (int)(wg % (a.token_tiles * a.col_tiles));
-  wg = wg / (a.token_tiles * a.col_tiles) * 8 + (blockIdx.x & 7);
-  if (wg >= (int64_t)a.Hkv * a.parts) return;
+  const int in = (int)(wg % deep);
+  wg = wg / deep * 8 + (blockIdx.x & 7);
+  const int tile = in * a.slices + (int)(wg % a.slices);
+  wg /= a.slices;
+  if (wg >= (int64_t)a.Hkv * a.parts || tile >= tiles) return;
   const int kvh = (int)(wg % a.Hkv), part = (int)(wg / a.Hkv);
   const int t0 = tile % a.token_tiles * a.tile_tokens;
   const int heads0 = tile / a.token_tiles * 16;
@@ -650,8 +655,9 @@ void sparse_attn_kernel(SparseArgs a) {
 template <int D, int NW, int MODE, int CG = 1>
 int launch_tiles(const SparseArgs& a, hipStream_t stream) {
   constexpr size_t lds = SpLds<D, NW, MODE>::BYTES;
-  const int64_t nwg =
-      ((int64_t)a.Hkv * a.parts + 7) / 8 * 8 * ((int64_t)a.token_tiles * a.col_tiles);
+  const int64_t tiles = (int64_t)a.token_tiles * a.col_tiles;
+  const int64_t nwg = ((int64_t)a.Hkv * a.parts * a.slices + 7) / 8 * 8 *
+                      ((tiles + a.slices - 1) / a.slices);
   if (!grid_fits(nwg, 64 * NW)) return PULSAR_EUNSUPPORTED;
   const auto kern = sparse_attn_kernel<D, NW, MODE, CG>;
   if (lds > 65536 &&
@@ -670,21 +676,23 @@ int64_t steps_of(int64_t keys) { return (keys + SP_KEYS - 1) / SP_KEYS; }
 
 }  // namespace
 
-// Tokens whose lists one tile reads together, where the rows that they read one by one
-// are enough to pay for finding the union: as many as fit 16 columns, or two groups of
-// 16 at d 128 (at d 64 these do not fit the registers of four waves), a block's byte and
-// the union's map and list.  Tokens that draw a quarter of the same blocks each, us, one
-// by one / 16 columns / 32: 32 heads of 128 over 8, 277 MB 24.4 / 28.0 / 28.8, 415 MB
-// 30.3 / 30.2 / 31.4, 587 MB 27.9 / 26.4 / 28.5, 837 MB 44.5 / 36.4 / 35.0, 2.2 GB 84 / 65
-// / 58; 16 of 64 over 16 and 8, 147 MB 16.2 / 16.9, 219 MB 19.6 / 20.1, 223 MB 18.9 / 18.5,
-// 292 MB 22.0 / 20.2, 447 MB 24.6 / 22.0.  (The more they share the more it gives.)
+// Tokens whose lists one tile reads together, where their own tiles are more than a
+// workgroup for each compute unit and the rows that they read one by one enough to pay
+// for finding the union: as many as fit 16 columns, or two groups of 16 at d 128 (at d
+// 64 these do not fit the registers of four waves), a block's byte and the union's map
+// and list.  Tokens that draw a quarter of the same blocks each, us, one by one / 16
+// columns / 32: 32 heads of 128 over 8, 256 tiles 558 MB 27.6 / 31.7 / 34.6, 288 of 326 MB
+// 25.7 / 22.4 / 25.3, 512 of 587 MB 27.5 / 27.0 / 29.0, 384 of 837 MB 45.0 / 36.9 / 35.8,
+// 1024 of 2.2 GB 84 / 65 / 58; 16 over 2, 512 tiles 638 MB 28.6 / 30.7 / 33.6; 16 of 64
+// over 16, 384 tiles 223 MB 17.9 / 18.9, 640 of 372 MB 24.0 / 20.7; 4 over 2, 512 of 319 MB
+// 17.4 / 19.8.  (The more they share the more it gives.)
 static int tile_tokens_most(int group, int d) {
   return std::min(16 / group * (d == 128 ? 2 : 1), 8);
 }
 static int union_tokens(int Tq, int Hkv, int group, int d, int64_t blocks, int64_t entries,
                         int64_t steps) {
   const int64_t mb = (int64_t)Tq * Hkv * steps * (SP_KEYS * d * 4) / 1000000;
-  if (blocks > sp_map(d) || mb < (d == 64 ? 250 : 400)) return 1;
+  if (blocks > sp_map(d) || (int64_t)Tq * Hkv <= 256 || mb < (group <= 4 ? 320 : 800)) return 1;
   for (const int most : {mb < 800 ? 1 : tile_tokens_most(group, d), std::min(16 / group, 8)}) {
     const int fit = std::min(most, Tq);
     if (fit > 1 && std::min(entries * fit, blocks) <= sp_list(d)) return fit;
@@ -701,13 +709,22 @@ SparsePlan sparse_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int d, 
   p.tokens = union_tokens(Tq, Hkv, group, d, S > 0 ? n_shards * ((S + block - 1) / block) : 0,
                           entries, steps);
   const int64_t tiles = (int64_t)((Tq + p.tokens - 1) / p.tokens) * Hkv * ((group + 15) / 16);
+  const int64_t fill = tiles_at_once(d) / tiles, most = (steps + 3) / 4;
   p.waves = 4;
-  p.parts = (int)std::max<int64_t>(1, std::min(tiles_at_once(d) / tiles, (steps + 3) / 4));
-  // One token of few steps: eight waves, and no merge (4 x 8 blocks of 16 keys and 46
-  // rows, 18 steps: 7.2 us against 7.7 in five parts, and a launch less).
-  if (p.tokens == 1 && p.parts > 1 && steps <= 32) {
+  p.parts = (int)std::max<int64_t>(1, std::min(fill, most));
+  if (p.tokens > 1 || p.parts == 1) return p;
+  // Eight waves: for few steps in one part, so without a merge (4 x 8 blocks of 16 keys
+  // and 46 rows, 18 steps: 7.2 us against 7.7 in five parts and a launch less); where the
+  // workgroups fill the chip in fewer parts, as many as are one on each compute unit
+  // (four waves / eight, us: 64 tiles of 67 steps 13.0 / 12.4, 128 of 68 15.4 / 14.5, 256
+  // of 69 20.0 / 16.6, 176 of 130 30 / 26; at d 64 128 of 131 18.6 / 16.0, 384 of 71 18.8 /
+  // 17.4; but 192 of 259 there 40 / 45).
+  if (steps <= (d == 64 ? 40 : 32)) {
     p.waves = 8;
     p.parts = 1;
+  } else if (fill < most && !(d == 64 && tiles > 128 && tiles <= 256 && steps > 160)) {
+    p.waves = 8;
+    p.parts = (int)std::max<int64_t>(1, std::min(256 / tiles, (steps + 7) / 8));
   }
   return p;
 }
@@ -739,6 +756,12 @@ SparseArgs tile_args(const SparseLaunch& x, int tokens, int parts) {
   a.n_shards = x.n_shards;
   a.G = x.G;
   a.parts = parts;
+  // all XCDs at work, evenly: few parts that are no multiple of eight are cut
+  const int64_t units = (int64_t)x.Hkv * parts;
+  a.slices = 1;
+  if (units < 32)
+    while (units * a.slices % 8 != 0 && a.slices * 2 <= (int64_t)a.token_tiles * a.col_tiles)
+      a.slices *= 2;
   a.scale_log2 = x.scale * 1.4426950408889634f;
   return a;
 }

@@ -132,7 +132,7 @@ def test_phase2_sparse():
         assert call(**kw) == EINVAL, kw
     for kw in (dict(d=96), dict(block=24), dict(block=8), dict(S=1 << 31), dict(G=1 << 24),
                dict(topk=1 << 25), dict(Hkv=1 << 17, Hq=1 << 17), dict(Tq=1 << 23, Hq=128),
-               dict(Tq=1 << 20, Hkv=1, Hq=32)):
+               dict(Tq=1 << 23, Hkv=1, Hq=32)):
         assert call(**kw) == EUNSUP, kw
     assert P.phase2_sparse_workspace_bytes(3, 32, 8, 128) > 0
     for kw in (dict(ws=None), dict(wsb=16), dict(ws=FAKE + 8)):

@@ -316,17 +316,16 @@ def _fill_up(sel, Hkv, d, block, mb, rng):
 
 
 TOGETHER = [  # Hq, Hkv, d, Tq, ns, S, block, topk, MB: tiles of several tokens
-    (32, 8, 128, 13, 2, 1000, 32, 6, 800),    # eight tokens in 32 columns
-    (16, 16, 64, 33, 3, 700, 16, 9, 400),     # eight in eight
-    (16, 2, 128, 6, 1, 4000, 64, 20, 800),    # four of eight heads, two in the last
-    (4, 2, 64, 40, 2, 1500, 128, 5, 400),     # eight of two heads
-    (32, 8, 128, 13, 2, 1000, 32, 6, 400),    # four in 16 columns, one in the last
-    (12, 4, 128, 10, 2, 900, 64, 5, 800),     # eight of three heads: 15 columns and nine
-    (20, 4, 64, 8, 1, 1030, 128, 6, 400),     # three of five heads
-    (28, 4, 128, 7, 1, 1300, 128, 7, 800),    # four of seven
-    (16, 8, 128, 9, 2, 900, 64, 5, 800),      # eight of two heads: 16 columns
-    (32, 8, 128, 4, 2, 3000, 128, 9, 800),    # four, all there are
-    (16, 1, 128, 5, 1, 2000, 256, 6, 800),    # two of sixteen heads
+    (32, 8, 128, 35, 2, 1000, 32, 6, 800),    # eight tokens in 32 columns, three in the last
+    (16, 16, 64, 33, 3, 700, 16, 9, 400),     # eight in eight, one in the last
+    (16, 2, 128, 130, 1, 1300, 64, 20, 800),  # four of eight heads, two in the last
+    (4, 2, 64, 131, 2, 500, 128, 3, 400),     # eight of two heads
+    (32, 8, 128, 33, 2, 1000, 32, 6, 400),    # four in 16 columns, one in the last
+    (12, 4, 128, 66, 2, 300, 64, 5, 800),     # eight of three heads: 15 columns and nine
+    (20, 4, 64, 65, 1, 530, 128, 5, 800),     # three of five heads
+    (28, 4, 128, 66, 1, 700, 128, 6, 800),    # four of seven
+    (16, 8, 128, 34, 2, 500, 64, 5, 800),     # eight of two heads: 16 columns
+    (16, 1, 128, 257, 1, 500, 64, 6, 800),    # two of sixteen heads
 ]
 
 
