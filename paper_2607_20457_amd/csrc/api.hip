@@ -501,18 +501,18 @@ QueryPlan query_plan(int n_shards, int Tq, int64_t S, int64_t G, int Hq, int Hkv
 }
 
 // Whether a draft's partials come from 16-row tiles, each of which reads all K/V: its
-// launch is short, and what the tiles read again comes from L2, so up to 280 MB over
+// launch is short, and what the tiles read again comes from L2, so up to 420 MB over
 // all tiles (140 at d 64), and for one tile of heads of 128 whatever the length.
-// Drafts of 1 / 8 / 12 / 64 tokens, 32 / 8 heads of 128, query step's kernels / tiles,
-// us with the merge: 4 x 1021 keys 12.9 / 9.9, 15.9 / 13.6, 18.3 / 13.7, 39 / 24; 8 x
-// 4096 30 / 28, 41 / 33, 34 / 38, 67 / 114; 16 x 8192 102 / 98, 112 / 123, 104 / 147.
-// 16 / 16 heads of 64, 8 x 4096: 16 tokens (one tile) 30.2 / 29.9, 24 (two) 32 / 35; 8 /
-// 2 heads of 128: 16 tokens (four tiles of 34 MB) 21 / 17, 24 (six) 25.5 / 26.6.
+// Query step's kernels / tiles, us with the merge: 32 / 8 heads of 128, 1 / 12 / 64 / 96
+// tokens (24 tiles of 17 MB) over 4 x 1021 keys 12.5 / 10.3, 16.2 / 12.0, 40 / 23, 43 / 35;
+// 1 / 12 / 16 (four of 134) over 8 x 4096 29.3 / 26.8, 32.0 / 31.9, 32.9 / 35.7; 8 / 2 heads,
+// 48 (twelve of 34) / 96 over 8 x 4096 34.5 / 26.8, 40 / 43; 16 / 16 heads of 64, 16 (one
+// of 67) / 24 tokens over 8 x 4096 28.4 / 28.1, 30.5 / 32.1.
 static bool dense_pays(int n_shards, int Tq, int64_t S, int64_t G, int Hq, int Hkv, int d) {
   if (!dense_tiles_apply(Hq, Hkv)) return false;
   const int64_t tokens = 16 / (Hq / Hkv), tiles = (Tq + tokens - 1) / tokens;
   const int64_t bytes = (n_shards * S + G) * Hkv * d * 4;
-  return (tiles == 1 && d == 128) || tiles * bytes <= (d == 64 ? 140 : 280) * (int64_t)1000000;
+  return (tiles == 1 && d == 128) || tiles * bytes <= (d == 64 ? 140 : 420) * (int64_t)1000000;
 }
 
 // The plan of a draft: the shards and the G appended rows, all visible to every

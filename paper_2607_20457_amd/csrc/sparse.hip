@@ -674,6 +674,24 @@ int tiles_at_once(int d) { return d == 64 ? 1024 : 512; }
 
 int64_t steps_of(int64_t keys) { return (keys + SP_KEYS - 1) / SP_KEYS; }
 
+// XCDs over which the `tiles` of each of `units` (KV head, part) pairs are spread: few
+// pairs that are no multiple of eight, so that all XCDs are at work.
+int tile_slices(int64_t units, int64_t tiles) {
+  int slices = 1;
+  if (units < 32)
+    while (units * slices % 8 != 0 && slices * 2 <= tiles) slices *= 2;
+  return slices;
+}
+// The most parts, up to `parts`, whose workgroups an XCD holds at once.
+int parts_at_once(int64_t parts, int Hkv, int64_t tiles, int64_t held) {
+  while (parts > 1) {
+    const int slices = tile_slices(Hkv * parts, tiles);
+    if ((Hkv * parts * slices + 7) / 8 * ((tiles + slices - 1) / slices) <= held) break;
+    --parts;
+  }
+  return (int)std::max<int64_t>(parts, 1);
+}
+
 }  // namespace
 
 // Tokens whose lists one tile reads together, where their own tiles are more than a
@@ -708,10 +726,11 @@ SparsePlan sparse_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int d, 
   const int64_t steps = steps_of(entries * block) + steps_of(gen_rows);
   p.tokens = union_tokens(Tq, Hkv, group, d, S > 0 ? n_shards * ((S + block - 1) / block) : 0,
                           entries, steps);
-  const int64_t tiles = (int64_t)((Tq + p.tokens - 1) / p.tokens) * Hkv * ((group + 15) / 16);
+  const int64_t own = (int64_t)((Tq + p.tokens - 1) / p.tokens) * ((group + 15) / 16);
+  const int64_t tiles = own * Hkv;
   const int64_t fill = tiles_at_once(d) / tiles, most = (steps + 3) / 4;
   p.waves = 4;
-  p.parts = (int)std::max<int64_t>(1, std::min(fill, most));
+  p.parts = parts_at_once(std::min(fill, most), Hkv, own, tiles_at_once(d) / 8);
   if (p.tokens > 1 || p.parts == 1) return p;
   // Eight waves: for few steps in one part, so without a merge (4 x 8 blocks of 16 keys
   // and 46 rows, 18 steps: 7.2 us against 7.7 in five parts and a launch less); where the
@@ -724,7 +743,7 @@ SparsePlan sparse_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int d, 
     p.parts = 1;
   } else if (fill < most && !(d == 64 && tiles > 128 && tiles <= 256 && steps > 160)) {
     p.waves = 8;
-    p.parts = (int)std::max<int64_t>(1, std::min(256 / tiles, (steps + 7) / 8));
+    p.parts = parts_at_once(std::min(256 / tiles, (steps + 7) / 8), Hkv, own, 32);
   }
   return p;
 }
@@ -756,12 +775,7 @@ SparseArgs tile_args(const SparseLaunch& x, int tokens, int parts) {
   a.n_shards = x.n_shards;
   a.G = x.G;
   a.parts = parts;
-  // all XCDs at work, evenly: few parts that are no multiple of eight are cut
-  const int64_t units = (int64_t)x.Hkv * parts;
-  a.slices = 1;
-  if (units < 32)
-    while (units * a.slices % 8 != 0 && a.slices * 2 <= (int64_t)a.token_tiles * a.col_tiles)
-      a.slices *= 2;
+  a.slices = tile_slices((int64_t)x.Hkv * parts, (int64_t)a.token_tiles * a.col_tiles);
   a.scale_log2 = x.scale * 1.4426950408889634f;
   return a;
 }
@@ -796,11 +810,29 @@ int launch_sparse(const SparseLaunch& x, const SparsePlan& p, void* o, int o_bf1
 
 // Partials of all tokens over all rows of the shards and the first G appended rows.
 bool dense_tiles_apply(int Hq, int Hkv) { return Hq / Hkv <= 16; }
+static SparsePlan dense_plan(int64_t keys, int Tq, int64_t G, int Hq, int Hkv, int d) {
+  SparsePlan p{};
+  p.tokens = 16 / (Hq / Hkv);
+  const int64_t own = (Tq + p.tokens - 1) / p.tokens, tiles = own * Hkv;
+  const int64_t steps = steps_of(keys) + steps_of(G);
+  const int64_t fill = tiles_at_once(d) / tiles, most = (steps + 3) / 4;
+  p.waves = 4;
+  p.parts = parts_at_once(std::min(fill, most), Hkv, own, tiles_at_once(d) / 8);
+  // Eight waves as for lists, except over long ranges and where they leave many compute
+  // units without work (with the merge, four waves / eight, us: 12 tokens of 32 / 8 heads
+  // of 128 over 4 x 1021 keys 14.0 / 11.9, 64 of 8 / 2 15.0 / 13.4; but 48 of 32 / 8 20.4 /
+  // 20.9, one over 16 x 8192 99 / 104).
+  if (fill < most && tiles <= 256) {
+    const int parts = parts_at_once(std::min(256 / tiles, (steps + 7) / 8), Hkv, own, 32);
+    if (steps <= 96 * parts && (d == 64 || 20 * parts >= 9 * p.parts)) {
+      p.waves = 8;
+      p.parts = parts;
+    }
+  }
+  return p;
+}
 int dense_parts(int n_shards, int Tq, int64_t S, int64_t G, int Hq, int Hkv, int d) {
-  const int tokens = 16 / (Hq / Hkv);
-  const int64_t tiles = (int64_t)((Tq + tokens - 1) / tokens) * Hkv;
-  const int64_t steps = steps_of(n_shards * S) + steps_of(G);
-  return (int)std::max<int64_t>(1, std::min(tiles_at_once(d) / tiles, (steps + 3) / 4));
+  return dense_plan(n_shards * S, Tq, G, Hq, Hkv, d).parts;
 }
 // Rows of partials of any call of up to Tq tokens: a part of every token, or the
 // chip's workgroups' tiles.
@@ -817,6 +849,9 @@ int launch_dense(const SparseLaunch& x, int parts, float* o, float* lse, hipStre
   a.part_steps = (int)std::max<int64_t>(1, (steps + parts - 1) / parts);
   a.O = o;
   a.lse = lse;
+  if (dense_plan(a.S, x.Tq, x.G, x.Hq, x.Hkv, x.d).waves == 8)
+    return x.d == 128 ? launch_tiles<128, 8, SP_DENSE>(a, stream)
+                      : launch_tiles<64, 8, SP_DENSE>(a, stream);
   return x.d == 128 ? launch_tiles<128, 4, SP_DENSE>(a, stream)
                     : launch_tiles<64, 4, SP_DENSE>(a, stream);
 }

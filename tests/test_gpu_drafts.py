@@ -96,6 +96,21 @@ def test_tree_shapes(Hq, Hkv, d, Tq, G, ns, S):
     _tree(Hq, Hkv, d, Tq, G, ns, S, 2000 + Hq + Tq + G, bf16_out=Tq % 2 == 0, what="shapes")
 
 
+@pytest.mark.parametrize("Hq,Hkv,d,Tq,G,ns,S", [
+    # more bytes than 16-row tiles read again: the query step's kernels
+    (16, 16, 64, 20, 45, 3, 6000),   # decode kernel
+    (16, 16, 64, 40, 10, 3, 4100),   # packed kernel, appended rows in ranges of their own
+    (16, 16, 64, 40, 300, 20, 620),  # packed kernel, a full chip: appended rows join
+    (16, 16, 64, 40, 12000, 0, 0),   # packed kernel, appended rows alone
+    (16, 4, 64, 100, 300, 2, 3000),  # attention kernel, appended rows in 16-row tiles
+    (16, 4, 64, 100, 6000, 1, 500),  # attention kernel for both
+    (16, 8, 64, 200, 3000, 1, 500),  # attention kernel, appended rows in the decode kernel
+    (32, 8, 128, 20, 64, 4, 6000),   # d 128
+])
+def test_tree_shapes_of_the_query_step(Hq, Hkv, d, Tq, G, ns, S):
+    _tree(Hq, Hkv, d, Tq, G, ns, S, 2100 + Hq + Tq + G, bf16_out=Tq % 40 == 0, what="query step")
+
+
 def test_tree_rows_without_any_key():
     # rows whose mask is empty: over nothing they give 0 and -inf, over shards the shards
     Tq = 40
