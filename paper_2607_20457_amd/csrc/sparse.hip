@@ -9,9 +9,9 @@
 //           shard's rows;
 //   UNION   several tokens, in one or two groups of 16 columns: the blocks that any of
 //           them lists, each with the tokens that list it, found in LDS; then the
-//           generation shard's rows.  Where
-//           neighbouring tokens list the same blocks these are read and multiplied
-//           once, and else no column does more than it would alone;
+//           generation shard's rows.  Where neighbouring tokens list the same blocks
+//           these are read and multiplied once, and else no column does more than it
+//           would alone;
 //   DENSE   all rows of the shards, then the appended rows.
 // A workgroup takes one part of the steps of one tile: wave w of NW the steps w,
 // w + NW, ... of it, on its own; then the waves' states are merged through LDS.  A
