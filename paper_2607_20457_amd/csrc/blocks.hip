@@ -52,9 +52,21 @@ __global__ __launch_bounds__(256) void key_bounds_kernel(const uint16_t* __restr
 // Scores: score[shard][t][kvh][b] = max over the heads of the group of
 // sum_i max(q_i lo_i, q_i hi_i) = sum_i max(q_i, 0) hi_i + min(q_i, 0) lo_i, in
 // fp64 (the products are exact, so that equal sums come out equal whatever the
-// order) and rounded once to fp32.  A score that is not a number, as from a bound
-// that is not finite, ranks above all: +inf.
-//
+// order) and rounded once to fp32.  A score that is not a number, and that of a block
+// with any bound that is not finite, ranks above all: +inf.
+
+// Whether any of the bf16 is an infinity or NaN (one step above their exponent carries
+// into the sign bit).
+template <typename T>
+__device__ __forceinline__ bool any_not_finite(T x) {
+  typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) / 4)));
+  const words w = (__builtin_bit_cast(words, x) & 0x7f807f80u) + 0x00800080u;
+  uint32_t all = 0;
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(T) / 4); ++i) all |= w[i];
+  return (all & 0x80008000u) != 0;
+}
+
 // Where the caller wants the scores: a wave takes 16 blocks as the rows of 16x16x4
 // fp64 matrix products and walks over tiles of 16 (token, head) columns.  Lane (r,
 // g) holds channels g D/4 .. of its block, so that it loads whole 16-byte pieces;
@@ -81,6 +93,11 @@ __global__ __launch_bounds__(256) void block_scores_kernel(
       hi[i] = reinterpret_cast<const bf16x8*>(p + D)[i];
     }
   }
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < N / 8; ++i) bad |= any_not_finite(lo[i]) || any_not_finite(hi[i]);
+  const uint64_t vote = __ballot(bad);  // bit r of each 16: row r
+  const uint32_t infinite = (uint32_t)(vote | vote >> 16 | vote >> 32 | vote >> 48);
   // columns: 16 / group tokens of `group` heads, or 16 heads of one token at a time
   const int tokens = max(16 / group, 1);
   const int passes = (group + 15) / 16;
@@ -111,7 +128,7 @@ __global__ __launch_bounds__(256) void block_scores_kernel(
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
         float s = (float)(up[v] + down[v]);
-        s = s != s ? INFINITY : s;
+        s = s != s || (infinite >> (4 * v + g)) & 1 ? INFINITY : s;
         best[v] = fmaxf(best[v], live ? s : -INFINITY);
       }
     }
@@ -824,7 +841,8 @@ void block_pick_kernel(const uint16_t* __restrict__ q, const uint16_t* __restric
         }
         const auto lo = __builtin_convertvector(lo16, f64xN);
         const auto hi = __builtin_convertvector(hi16, f64xN);
-        float best = -INFINITY;
+        const uint64_t bad = __ballot(any_not_finite(lo16) || any_not_finite(hi16));
+        float best = (bad >> (lane & 48)) & 0xffff ? INFINITY : -INFINITY;
         constexpr int HU = 4;  // heads at a time
         for (int h0 = 0; h0 < group; h0 += HU) {
           bf16xN y[HU];

@@ -1,0 +1,39 @@
+"""block_select and phase2_sparse where their dispatch, their lists and their
+values have edges, against oracle.blocks."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_20457_amd as P
+from oracle import blocks as ob
+from tests._blocks import f64, host, normal, to_dev_bf16
+
+pytestmark = pytest.mark.gpu
+
+
+def _both_selections(q, bounds, topk, what):
+    """The selection with scores and the one without, which has to be the same."""
+    print(f"block_select: {what} {tuple(bounds.shape)} Tq={q.shape[0]} topk={topk}", flush=True)
+    sel, scores = P.block_select(to_dev_bf16(q), bounds.cuda(), topk, return_scores=True)
+    assert torch.equal(sel, P.block_select(to_dev_bf16(q), bounds.cuda(), topk)), what
+    return sel.cpu().numpy(), scores.cpu().numpy()
+
+
+def _single_key_bounds(seed, blocks, d):
+    """Blocks of one key each, so that scores have either sign."""
+    x = f64(normal(seed, (1, 1, blocks, 1, d)))
+    return torch.from_numpy(np.repeat(x, 2, axis=3)).to(torch.bfloat16)
+
+
+@pytest.mark.parametrize("blocks,Hq,d,Tq", [(90, 4, 64, 2), (200, 4, 128, 9), (250, 24, 64, 12)])
+def test_one_bound_alone_that_is_not_finite(blocks, Hq, d, Tq):
+    # a lower bound of +inf or an upper one of -inf beside a finite one: +inf as well
+    b = _single_key_bounds(210, blocks, d)
+    b[0, 0, 7, 0, 3], b[0, 0, 50, 1, 60], b[0, 0, 80, 0, 21], b[0, 0, 81, 1, 20] = (
+        np.inf, -np.inf, -np.inf, np.nan)
+    q = normal(211, (Tq, Hq, d))
+    want = ob.block_scores(f64(q), host(b))
+    for topk in (2, 4, 9):
+        sel, scores = _both_selections(q, b, topk, "one bound")
+        assert np.array_equal(scores, want)
+        assert np.array_equal(sel, ob.block_select(want, topk)), topk
