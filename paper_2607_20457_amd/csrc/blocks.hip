@@ -748,7 +748,8 @@ void block_pick_kernel(const uint16_t* __restrict__ q, const uint16_t* __restric
         reach = __builtin_amdgcn_readfirstlane(s_found[1]);
         above = __builtin_amdgcn_readfirstlane(s_found[2]);
         lo += bin << shift;
-        hi = min(hi, lo + ((1u << shift) - 1));
+        // (a distance from lo: below the keys of infinities lo + 2^shift passes 32 bits)
+        hi = lo + min(hi - lo, (1u << shift) - 1);
         cut = lo;
         if (reach == topk || shift == 0) break;
       }

@@ -37,3 +37,19 @@ def test_one_bound_alone_that_is_not_finite(blocks, Hq, d, Tq):
         sel, scores = _both_selections(q, b, topk, "one bound")
         assert np.array_equal(scores, want)
         assert np.array_equal(sel, ob.block_select(want, topk)), topk
+
+
+@pytest.mark.parametrize("blocks", [300, 700, 1500, 5000, 17000])
+def test_more_infinite_scores_than_are_selected(blocks):
+    # of several blocks that rank as +inf, beside scores below 0, the first ones
+    b = _single_key_bounds(200, blocks, 64)
+    bad = np.sort(np.random.default_rng(blocks).permutation(blocks)[:6])
+    for i, at in enumerate(bad):
+        b[0, 0, at, i % 2, 5 * i] = (np.inf, -np.inf, np.nan)[i % 3]
+    q = normal(201, (9, 4, 64))
+    want = ob.block_scores(f64(q), host(b))
+    assert (want.min(axis=3) < 0).all()
+    for topk in (1, 2, 5, 6, 20):
+        sel, scores = _both_selections(q, b, topk, "infinite scores")
+        assert np.array_equal(scores, want)
+        assert np.array_equal(sel, ob.block_select(want, topk)), topk
