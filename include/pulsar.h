@@ -507,9 +507,10 @@ int pulsar_key_bounds(const void* K, int n_shards, int64_t S, int Hkv, int d, in
  * largest q . k that a key within the block's bounds can have for any of the
  * heads that read g:
  *   max over h of sum_i max(q_thi lo_bi, q_thi hi_bi),
- * formed in fp64 and rounded once to fp32.  Blocks rank by the fp32 score, then
- * by the lower index; a score that is not a number, as a bound that is not
- * finite gives, counts as +inf.
+ * formed in fp64, as sixteen sums of d / 16 consecutive channels added two by two, and
+ * rounded once to fp32.  Blocks rank by the fp32 score, then by the lower index; a score
+ * that is not a number, and that of a block with any bound that is not finite, counts
+ * as +inf.
  *
  * q         bf16 [Tq, Hq, d], 16-byte aligned.
  * bounds    bf16 [n_shards, Hkv, blocks, 2, d] as written by pulsar_key_bounds.

@@ -11,7 +11,8 @@ All arithmetic is fp64 on inputs that are already bf16-rounded.
   that is listed c times weighing c times.  No key at all gives o = 0, lse = -inf.
 * Block bounds: the smallest and largest value of every channel over a block's keys.
 * Block score: max over the heads of a KV head's group of
-  sum_i max(q_i lo_i, q_i hi_i), rounded once to fp32; what is not a number is +inf.
+  sum_i max(q_i lo_i, q_i hi_i), in sixteen parts of consecutive channels that are
+  added two by two, and rounded once to fp32; what is not a number is +inf.
 * Selection: the topk blocks by score, then by the lower index, in index order.
 * Compaction: row G + keep[j] to row G + j while the list rises within the cache.
 """
@@ -85,6 +86,16 @@ def key_bounds(K, block):
     return out
 
 
+def _sum_of_parts(x):
+    """x [..., d] summed in the order of a block score."""
+    x = np.concatenate([x, np.zeros(x.shape[:-1] + (-x.shape[-1] % 16,))], axis=-1)
+    x = x.reshape(x.shape[:-1] + (16, x.shape[-1] // 16))
+    x = np.add.accumulate(x, axis=-1)[..., -1]
+    while x.shape[-1] > 1:
+        x = x[..., ::2] + x[..., 1::2]
+    return x[..., 0]
+
+
 def block_scores(q, bounds):
     """q [Tq, Hq, d], bounds [n, Hkv, blocks, 2, d] -> float32 [n, Tq, Hkv, blocks]."""
     q, bounds = np.asarray(q, dtype=np.float64), np.asarray(bounds, dtype=np.float64)
@@ -96,8 +107,8 @@ def block_scores(q, bounds):
         for t in range(Tq):
             for g in range(Hkv):
                 x = q[t, g * group:(g + 1) * group, None, None, :]
-                s = np.maximum(x * bounds[:, g, :, 0], x * bounds[:, g, :, 1]).sum(-1)
-                s = s.astype(np.float32)
+                s = np.maximum(x * bounds[:, g, :, 0], x * bounds[:, g, :, 1])
+                s = _sum_of_parts(s).astype(np.float32)
                 bad = ~np.isfinite(bounds[:, g]).all(axis=(2, 3))
                 s = np.where(np.isnan(s) | bad, np.float32(np.inf), s)
                 out[:, t, g] = s.max(axis=0)

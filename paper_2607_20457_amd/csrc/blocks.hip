@@ -51,20 +51,74 @@ __global__ __launch_bounds__(256) void key_bounds_kernel(const uint16_t* __restr
 // ---------------------------------------------------------------------------
 // Scores: score[shard][t][kvh][b] = max over the heads of the group of
 // sum_i max(q_i lo_i, q_i hi_i) = sum_i max(q_i, 0) hi_i + min(q_i, 0) lo_i, in
-// fp64 (the products are exact, so that equal sums come out equal whatever the
-// order) and rounded once to fp32.  A score that is not a number, and that of a block
-// with any bound that is not finite, ranks above all: +inf.
+// fp64 (the products are exact) and rounded once to fp32.  A score that is not a
+// number, and that of a block with any bound that is not finite, ranks above all: +inf.
 
-// Whether any of the bf16 is an infinity or NaN (one step above their exponent carries
-// into the sign bit).
-template <typename T>
-__device__ __forceinline__ bool any_not_finite(T x) {
-  typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) / 4)));
-  const words w = (__builtin_bit_cast(words, x) & 0x7f807f80u) + 0x00800080u;
-  uint32_t all = 0;
+// Magnitudes as their bits: without their signs bf16 rank as integers, what is not finite
+// from kInfinite on.
+constexpr int kInfinite = 0x7f80;
+struct Magnitudes {
+  int most = 0, least = 0xffff;  // of those that are not 0
+  template <typename T>
+  __device__ __forceinline__ void add(T x) {
+    constexpr int W = sizeof(T) / 4;
+    typedef uint32_t words __attribute__((ext_vector_type(W)));
+    typedef uint16_t halves __attribute__((ext_vector_type(2 * W)));
+    const halves y = __builtin_bit_cast(halves, __builtin_bit_cast(words, x) & 0x7fff7fffu);
 #pragma unroll
-  for (int i = 0; i < (int)(sizeof(T) / 4); ++i) all |= w[i];
-  return (all & 0x80008000u) != 0;
+    for (int i = 0; i < 2 * W; ++i) {
+      most = max(most, (int)y[i]);
+      least = min(least, (int)(uint16_t)(y[i] - 1));  // (a 0 is passed over)
+    }
+  }
+  // over the lanes r, r + 16, r + 32, r + 48
+  __device__ __forceinline__ void join_rows() {
+#pragma unroll
+    for (int lanes = 16; lanes < 64; lanes <<= 1) {
+      most = max(most, __shfl_xor(most, lanes, 64));
+      least = min(least, __shfl_xor(least, lanes, 64));
+    }
+  }
+  __device__ __forceinline__ double size() const { return (double)__int_as_float(most << 16); }
+  // the exponent of a unit that all of them are multiples of
+  __device__ __forceinline__ int unit() const { return max((least + 1) >> 7, 1) - 134; }
+};
+
+// The score's sum of D products is that of sixteen parts of consecutive channels, added
+// two by two: as sixteen lanes form it for the selection, or one lane here.
+template <int D>
+__device__ __forceinline__ double sum_in_order(const uint16_t* q, const uint16_t* b) {
+  double half[4];  // sums of 1, 2, 4 and 8 parts that wait for as many more
+#pragma unroll 1
+  for (int part = 0;; ++part) {
+    double s = 0.;
+    for (int i = part * (D / 16); i < (part + 1) * (D / 16); ++i) {
+      const float y = __uint_as_float((uint32_t)q[i] << 16);
+      const float x = __uint_as_float((uint32_t)b[y < 0.f ? i : D + i] << 16);
+      s = __builtin_fma((double)y, (double)x, s);
+    }
+    bool ends = true;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (!ends) continue;
+      ends = (part >> k) & 1;
+      if (ends) s = half[k] + s;
+      else half[k] = s;
+    }
+    if (ends) return s;
+  }
+}
+// Whether a sum s of the same products in another order gives the same fp32.  In any
+// order it is off by at most D 2^-52 of sum_i |q_i b_i|, which D times the largest factors
+// bound: either no fp32 ends within twice that of s, or all sums are multiples of the
+// factors' units that fp64 holds exactly (as nearly all of random values are, 6 to 22 %
+// of which end at the border between two fp32).
+template <int D>
+__device__ __forceinline__ bool any_order(double s, const Magnitudes& q, const Magnitudes& b) {
+  const double size = D * (q.size() * b.size());
+  const double off = size * (D * 0x1p-51);
+  return (float)(s - off) == (float)(s + off) || s - s != 0. ||
+         size <= __builtin_ldexp(1., 53 + q.unit() + b.unit());
 }
 
 // Where the caller wants the scores: a wave takes 16 blocks as the rows of 16x16x4
@@ -72,7 +126,7 @@ __device__ __forceinline__ bool any_not_finite(T x) {
 // g) holds channels g D/4 .. of its block, so that it loads whole 16-byte pieces;
 // the channels of a product are then D/4 apart, the same for both operands.
 template <int D>
-__global__ __launch_bounds__(256) void block_scores_kernel(
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void block_scores_kernel(
     const uint16_t* __restrict__ q, const uint16_t* __restrict__ bounds, int Tq, int Hq, int Hkv,
     int blocks, int tiles, int tiles_per_wg, float* __restrict__ scores) {
   constexpr int N = D / 4;  // channels per lane
@@ -93,11 +147,19 @@ __global__ __launch_bounds__(256) void block_scores_kernel(
       hi[i] = reinterpret_cast<const bf16x8*>(p + D)[i];
     }
   }
-  bool bad = false;
+  // the bounds of row r, then of the rows whose products a lane gets, 4v + g
+  Magnitudes mine, block[4];
 #pragma unroll
-  for (int i = 0; i < N / 8; ++i) bad |= any_not_finite(lo[i]) || any_not_finite(hi[i]);
-  const uint64_t vote = __ballot(bad);  // bit r of each 16: row r
-  const uint32_t infinite = (uint32_t)(vote | vote >> 16 | vote >> 32 | vote >> 48);
+  for (int i = 0; i < N / 8; ++i) {
+    mine.add(lo[i]);
+    mine.add(hi[i]);
+  }
+  mine.join_rows();
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    block[v].most = __shfl(mine.most, 4 * v + g, 64);
+    block[v].least = __shfl(mine.least, 4 * v + g, 64);
+  }
   // columns: 16 / group tokens of `group` heads, or 16 heads of one token at a time
   const int tokens = max(16 / group, 1);
   const int passes = (group + 15) / 16;
@@ -125,10 +187,31 @@ __global__ __launch_bounds__(256) void block_scores_kernel(
         down = __builtin_amdgcn_mfma_f64_16x16x4f64((double)(float)lo[i / 8][i % 8],
                                                     (double)(qi < 0.f ? qi : 0.f), down, 0, 0, 0);
       }
+      Magnitudes head;
+#pragma unroll
+      for (int i = 0; i < N / 8; ++i) head.add(x[i]);
+      head.join_rows();
+      double sum[4];
+      int open = 0;  // sums to be formed in order
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        float s = (float)(up[v] + down[v]);
-        s = s != s || (infinite >> (4 * v + g)) & 1 ? INFINITY : s;
+        sum[v] = up[v] + down[v];
+        if (live && !any_order<D>(sum[v], head, block[v])) open |= 1 << v;
+      }
+      if (open != 0)
+#pragma unroll 1
+        for (int v = 0; v < 4; ++v) {
+          if (!((open >> v) & 1)) continue;
+          const int64_t b = (int64_t)blockIdx.y * blocks + min(b0 + 4 * v + g, blocks - 1);
+          const double x = sum_in_order<D>(q + ((int64_t)t * Hq + kvh * group + h) * D,
+                                           bounds + b * 2 * D);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) sum[k] = k == v ? x : sum[k];
+        }
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        float s = (float)sum[v];
+        s = s != s || block[v].most >= kInfinite ? INFINITY : s;
         best[v] = fmaxf(best[v], live ? s : -INFINITY);
       }
     }
@@ -149,7 +232,7 @@ __global__ __launch_bounds__(256) void block_scores_kernel(
 // ---------------------------------------------------------------------------
 // Near scores, for the selection alone: the same sums by bf16 matrix products
 // (16x16x32, exact products, fp32 sums).  The fp64 products bound the exact form (64
-// tokens, 4096 blocks of 8 KV heads: 112 us at 69 TFLOP/s); the selection needs them
+// tokens, 4096 blocks of 8 KV heads: 125 us with the pick); the selection needs them
 // only for the few blocks whose near scores lie within their errors of the last one
 // that it keeps.
 //
@@ -842,8 +925,10 @@ void block_pick_kernel(const uint16_t* __restrict__ q, const uint16_t* __restric
         }
         const auto lo = __builtin_convertvector(lo16, f64xN);
         const auto hi = __builtin_convertvector(hi16, f64xN);
-        const uint64_t bad = __ballot(any_not_finite(lo16) || any_not_finite(hi16));
-        float best = (bad >> (lane & 48)) & 0xffff ? INFINITY : -INFINITY;
+        Magnitudes m;
+        m.add(lo16);
+        m.add(hi16);
+        float best = over_row(m.most, Most{}) >= kInfinite ? INFINITY : -INFINITY;
         constexpr int HU = 4;  // heads at a time
         for (int h0 = 0; h0 < group; h0 += HU) {
           bf16xN y[HU];

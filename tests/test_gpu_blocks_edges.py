@@ -53,3 +53,24 @@ def test_more_infinite_scores_than_are_selected(blocks):
         sel, scores = _both_selections(q, b, topk, "infinite scores")
         assert np.array_equal(scores, want)
         assert np.array_equal(sel, ob.block_select(want, topk)), topk
+
+
+@pytest.mark.parametrize("blocks,Tq", [(90, 8), (240, 9), (700, 64), (5000, 12)])
+@pytest.mark.parametrize("Hq,d", [(4, 128), (24, 64)])
+def test_large_channels_that_cancel(blocks, Tq, Hq, d):
+    # two channels whose products cancel at 2^44, 2^20 and not at all beside those of N(0, 1):
+    # the sums of fp64 depend on their order, the scores and the selection do not
+    q, k = f64(normal(220, (Tq, Hq, d))), f64(normal(221, (1, 1, blocks, 1, d)))
+    a, b = 5, d - 9
+    for size in (22, 10):
+        x, y = q.copy(), k.copy()
+        x[..., a] = x[..., b] = 2.0 ** size * (1 + np.arange(Tq)[:, None] % 7 / 8)
+        y[..., a] = 2.0 ** size * (1 + np.arange(blocks)[None, None, :, None] % 5 / 8)
+        y[..., b] = -y[..., a]
+        y = torch.from_numpy(np.repeat(y, 2, axis=3)).to(torch.bfloat16)
+        words = torch.from_numpy(x).to(torch.bfloat16).view(torch.int16).numpy().view(np.uint16)
+        want = ob.block_scores(f64(words), host(y))
+        for topk in (3, blocks // 3):
+            sel, scores = _both_selections(words, y, topk, f"cancelling at 2^{2 * size}")
+            assert np.array_equal(scores, want)
+            assert np.array_equal(sel, ob.block_select(want, topk)), topk
