@@ -422,6 +422,8 @@ def phase2_tree(q, Kg, Vg, G: int, mask, K=None, V=None, softmax_scale: float | 
     _generation_shape(Kg, Vg, G, Tq, Hkv, d)
     _mask_shape(mask, Tq)
     n_shards, S, k_ptr, v_ptr = 0, 0, None, None
+    if (K is None) != (V is None):
+        raise ValueError("K and V go together")
     if K is not None:
         _check(dev, _BF16, ((K, "K"), (V, "V")))
         n_shards, S = K.shape[:2]

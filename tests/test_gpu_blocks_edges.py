@@ -6,7 +6,7 @@ import torch
 
 import paper_2607_20457_amd as P
 from oracle import blocks as ob
-from tests._blocks import f64, host, normal, to_dev_bf16
+from tests._blocks import dev_mask, f64, host, normal, to_dev_bf16
 
 pytestmark = pytest.mark.gpu
 
@@ -74,3 +74,12 @@ def test_large_channels_that_cancel(blocks, Tq, Hq, d):
             sel, scores = _both_selections(words, y, topk, f"cancelling at 2^{2 * size}")
             assert np.array_equal(scores, want)
             assert np.array_equal(sel, ob.block_select(want, topk)), topk
+
+
+def test_shards_of_drafts_go_together():
+    q, kg, k = (to_dev_bf16(normal(230 + i, s)) for i, s in enumerate(
+        ((2, 8, 64), (6, 4, 64), (1, 40, 4, 64))))
+    mask = dev_mask(np.eye(2, dtype=bool))
+    for kw in (dict(K=k), dict(V=k)):
+        with pytest.raises(ValueError):
+            P.phase2_tree(q, kg, kg, 4, mask, **kw)
