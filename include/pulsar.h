@@ -458,7 +458,8 @@ int pulsar_tree_mask(const int32_t* parent, int T, uint32_t* mask, int32_t* dept
  *           pulsar_phase2_query the size never drops when n_shards, Tq, S or G
  *           grows.
  * Errors: as pulsar_phase2_query, plus EINVAL for an unknown o_dtype or a NULL
- *         mask when Tq > 0, and EUNSUPPORTED for Tq * Hq >= 2^24.
+ *         mask when Tq > 0, and EUNSUPPORTED for Tq * Hq >= 2^24 or a row of K of
+ *         256 MiB or more.
  */
 size_t pulsar_phase2_tree_workspace_bytes(int n_shards, int Tq, int64_t S, int64_t G, int Hq,
                                           int Hkv, int d);

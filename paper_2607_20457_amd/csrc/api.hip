@@ -850,6 +850,7 @@ int pulsar_phase2_tree(const void* q, const void* Kg, const void* Vg, int64_t G,
   if (mask == nullptr) return PULSAR_EINVAL;
   if (n_shards > 0 && S > 0 && (!aligned16(K) || !aligned16(V))) return PULSAR_EINVAL;
   if (!grid_fits((int64_t)Tq * Hq, 256)) return PULSAR_EUNSUPPORTED;
+  if ((int64_t)Hkv * d * 2 >= 1 << 28) return PULSAR_EUNSUPPORTED;  // (16 rows of a tile)
   if (S == 0) n_shards = 0;
   const QueryPlan plan = tree_plan(n_shards, Tq, S, G, Hq, Hkv, d);
   if (plan.parts > 0 && (workspace == nullptr || !aligned16(workspace) ||
