@@ -497,7 +497,8 @@ int pulsar_kv_compact(void* K, void* V, int layers, int64_t capacity, int Hkv, i
  *         block's keys; NaN where a key's is NaN.
  * EINVAL: negative sizes, Hkv < 1, d < 1, block < 1, NULL or misaligned pointers
  *         when there is work.
- * EUNSUPPORTED: d not in {64, 128}, another block, S >= 2^31.
+ * EUNSUPPORTED: d not in {64, 128}, another block, S or Hkv * d >= 2^31,
+ *         n_shards * ceil(S / block) * Hkv * d / 8 > 2^32 - 256.
  */
 int pulsar_key_bounds(const void* K, int n_shards, int64_t S, int Hkv, int d, int block,
                       void* bounds, void* stream);

@@ -47,7 +47,7 @@ int pulsar_key_bounds(const void* K, int n_shards, int64_t S, int Hkv, int d, in
                       void* bounds, void* stream) {
   if (n_shards < 0 || S < 0 || Hkv < 1 || d < 1 || block < 1) return PULSAR_EINVAL;
   if ((d != 64 && d != 128) || !block_supported(block)) return PULSAR_EUNSUPPORTED;
-  if (S > kMaxInt) return PULSAR_EUNSUPPORTED;
+  if (S > kMaxInt || (int64_t)Hkv * d > kMaxInt) return PULSAR_EUNSUPPORTED;
   if (n_shards == 0 || S == 0) return PULSAR_OK;
   if (K == nullptr || bounds == nullptr || !aligned16(K) || !aligned16(bounds))
     return PULSAR_EINVAL;

@@ -18,3 +18,13 @@ def test_tree_rows_that_a_tile_cannot_address():
         assert call(Hq=heads, Hkv=heads, d=d) == EUNSUP
         if not GPU:
             assert call(Hq=heads - 1, Hkv=heads - 1, d=d) != EUNSUP
+
+
+def test_key_bounds_of_the_widest_rows():
+    # a row's channels are counted in 32 bits
+    call = caller("pulsar_key_bounds", "K n_shards S Hkv d block bounds stream", K=FAKE,
+                  n_shards=1, S=1, block=16, bounds=FAKE)
+    for heads, d in ((1 << 24, 128), (1 << 25, 64)):
+        assert call(Hkv=heads, d=d) == EUNSUP
+        if not GPU:
+            assert call(Hkv=heads - 1, d=d) != EUNSUP
