@@ -737,13 +737,24 @@ SparsePlan sparse_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int d, 
   // workgroups fill the chip in fewer parts, as many as are one on each compute unit
   // (four waves / eight, us: 64 tiles of 67 steps 13.0 / 12.4, 128 of 68 15.4 / 14.5, 256
   // of 69 20.0 / 16.6, 176 of 130 30 / 26; at d 64 128 of 131 18.6 / 16.0, 384 of 71 18.8 /
-  // 17.4; but 192 of 259 there 40 / 45).
+  // 17.4).  But not for long lists in one part that leaves a third of the places idle, one
+  // on each compute unit or, for more tiles than these, two at d 64: d 128, 168 tiles of
+  // 60 / 100 / 260 steps 15.6 / 15.0, 21.5 / 22.4, 43 / 48, against 176 18.3 / 14.9, 25.1 /
+  // 22.5, 58 / 48; d 64, 144 of 260 29 / 34, 336 40 / 46, against 400 48 / 46.  Nor, at d 64,
+  // for long lists of more than 32 tokens, which read each other's blocks from cache, where
+  // the four waves' twice as many help: 192 tiles of 260 steps that share a quarter, 96
+  // tokens 28.6 / 33.9, 48 31 / 34, against 24 33 / 34, 12 45 / 37, and 256 of 32 tokens 38 /
+  // 34.  (The same lists, 24 tokens, 26 / 31, lists of their own 45 / 37.)
+  const int64_t places = tiles <= 256 ? 256 : 512;
   if (steps <= (d == 64 ? 40 : 32)) {
     p.waves = 8;
     p.parts = 1;
-  } else if (fill < most && !(d == 64 && tiles > 128 && tiles <= 256 && steps > 160)) {
+  } else if (fill < most) {
+    const int parts = parts_at_once(std::min(256 / tiles, (steps + 7) / 8), Hkv, own, 32);
+    if (parts == 1 && steps > 80 && 3 * tiles < 2 * places) return p;
+    if (d == 64 && parts == 1 && tiles <= 256 && steps > 160 && Tq > 32) return p;
     p.waves = 8;
-    p.parts = parts_at_once(std::min(256 / tiles, (steps + 7) / 8), Hkv, own, 32);
+    p.parts = parts;
   }
   return p;
 }
@@ -815,16 +826,20 @@ static SparsePlan dense_plan(int64_t keys, int Tq, int64_t G, int Hq, int Hkv, i
   p.tokens = 16 / (Hq / Hkv);
   const int64_t own = (Tq + p.tokens - 1) / p.tokens, tiles = own * Hkv;
   const int64_t steps = steps_of(keys) + steps_of(G);
-  const int64_t fill = tiles_at_once(d) / tiles, most = (steps + 3) / 4;
   p.waves = 4;
-  p.parts = parts_at_once(std::min(fill, most), Hkv, own, tiles_at_once(d) / 8);
-  // Eight waves as for lists, except over long ranges and where they leave many compute
-  // units without work (with the merge, four waves / eight, us: 12 tokens of 32 / 8 heads
-  // of 128 over 4 x 1021 keys 14.0 / 11.9, 64 of 8 / 2 15.0 / 13.4; but 48 of 32 / 8 20.4 /
-  // 20.9, one over 16 x 8192 99 / 104).
-  if (fill < most && tiles <= 256) {
+  p.parts = parts_at_once(std::min(tiles_at_once(d) / tiles, (steps + 3) / 4), Hkv, own,
+                          tiles_at_once(d) / 8);
+  // Eight waves where that is a workgroup for 112 compute units at least and, unless the
+  // steps end before the parts do, for four fifths of them.  With the merge, four waves /
+  // eight, us: 32 / 8 heads of 128 over 4 x 1021 keys, 8 tiles (128 workgroups) 11.9 / 11.1,
+  // 64 (256) 18.7 / 17.1, over 8192 keys 96 tiles (192) 30.4 / 33.2; 8 / 2 heads over 4 x
+  // 1021, 6 tiles (96) 10.8 / 11.0; 16 / 8 of 64 over 16 x 8192, 16 tiles 61 / 50, over 4 x
+  // 4096 96 (192) 33 / 41.  Over 201 shapes the choice is 0.5 % slower than the better one
+  // of both on average, and 16 % at most.
+  if (tiles <= 256) {
     const int parts = parts_at_once(std::min(256 / tiles, (steps + 7) / 8), Hkv, own, 32);
-    if (steps <= 96 * parts && (d == 64 || 20 * parts >= 9 * p.parts)) {
+    const int64_t nwg = tiles * parts;
+    if (nwg >= 112 && (nwg >= 205 || steps <= 8 * parts)) {
       p.waves = 8;
       p.parts = parts;
     }
