@@ -700,10 +700,16 @@ int parts_at_once(int64_t parts, int Hkv, int64_t tiles, int64_t held) {
 // 64 these do not fit the registers of four waves), a block's byte and the union's map
 // and list.  Tokens that draw a quarter of the same blocks each, us, one by one / 16
 // columns / 32: 32 heads of 128 over 8, 256 tiles 558 MB 27.6 / 31.7 / 34.6, 288 of 326 MB
-// 25.7 / 22.4 / 25.3, 512 of 587 MB 27.5 / 27.0 / 29.0, 384 of 837 MB 45.0 / 36.9 / 35.8,
-// 1024 of 2.2 GB 84 / 65 / 58; 16 over 2, 512 tiles 638 MB 28.6 / 30.7 / 33.6; 16 of 64
-// over 16, 384 tiles 223 MB 17.9 / 18.9, 640 of 372 MB 24.0 / 20.7; 4 over 2, 512 of 319 MB
-// 17.4 / 19.8.  (The more they share the more it gives.)
+// 25.7 / 22.4 / 25.3, 512 of 587 MB 27.5 / 27.0 / 29.0, 512 of 1074 MB 44.9 / 41.0 / 40.3,
+// 640 of 1342 MB 75 / 48 / 44, 1024 of 2.2 GB 84 / 65 / 58; 16 over 2, 512 tiles 638 MB
+// 28.6 / 30.7 / 33.6, 400 of 839 MB 43.1 / 42.0 / 44.4; 16 of 64 over 16, 384 tiles 223 MB
+// 17.9 / 18.9, 640 of 372 MB 24.0 / 20.7; 4 over 2, 512 of 319 MB 17.4 / 19.8.
+// What they share the host does not see.  With the same lists: 264 tiles of 554 MB 42.8 /
+// 19.9 / 23.0, 512 of 1074 MB 44.7 / 22.6 / 25.2, 1024 of 2.1 GB 84 / 31 / 31.  With lists
+// that share nothing, whose blocks each tile reads for one column in eight: 264 of 554 MB
+// 100 / 88 / 98, 512 of 1074 MB 123 / 136 / 148, 640 of 1342 MB 170 / 162 / 175, 1024 of 2.1
+// GB 250 / 191 / 238; 16 over 2, 400 of 839 MB 48 / 59 / 77; 16 of 64 over 16, 640 of 336 MB
+// 55 / 59, 1280 of 671 MB 96 / 108.
 static int tile_tokens_most(int group, int d) {
   return std::min(16 / group * (d == 128 ? 2 : 1), 8);
 }
@@ -711,7 +717,7 @@ static int union_tokens(int Tq, int Hkv, int group, int d, int64_t blocks, int64
                         int64_t steps) {
   const int64_t mb = (int64_t)Tq * Hkv * steps * (SP_KEYS * d * 4) / 1000000;
   if (blocks > sp_map(d) || (int64_t)Tq * Hkv <= 256 || mb < (group <= 4 ? 320 : 800)) return 1;
-  for (const int most : {mb < 800 ? 1 : tile_tokens_most(group, d), std::min(16 / group, 8)}) {
+  for (const int most : {mb < 1200 ? 1 : tile_tokens_most(group, d), std::min(16 / group, 8)}) {
     const int fit = std::min(most, Tq);
     if (fit > 1 && std::min(entries * fit, blocks) <= sp_list(d)) return fit;
   }

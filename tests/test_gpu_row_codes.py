@@ -258,3 +258,24 @@ def test_eight_waves_in_several_parts(Hq, Hkv, d, Tq, ns, blocks, topk):
     o, lse = P.phase2_sparse(q, K, V, sel, block)
     ref = _device_reference(q, K, V, sel, block, 1 / math.sqrt(d))
     check(o, lse, ref, ns * topk * block, "eight waves")
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,Tq,ns,S,block,topk", [
+    (32, 8, 128, 100, 2, 1600, 32, 48),   # two groups of 16 columns: eight tokens of four heads
+    (12, 4, 128, 203, 1, 3301, 64, 50),   # eight of three heads
+    (16, 2, 128, 301, 1, 5100, 64, 66),   # four of eight heads
+    (20, 4, 128, 202, 1, 4800, 64, 50),   # six of five heads, four in the last
+])
+def test_two_groups_of_columns(Hq, Hkv, d, Tq, ns, S, block, topk):
+    # scores and values of any size, lists that share half, against 64 bits
+    gen = torch.Generator(device="cuda").manual_seed(Tq + S)
+    q, K, V = (torch.randn(s, generator=gen, **BF) for s in
+               ((Tq, Hq, d), (ns, S, Hkv, d), (ns, S, Hkv, d)))
+    assert Tq * Hkv * ns * topk * block * d * 4 >= 1200000000  # from here on two groups
+    u = torch.rand((ns, Tq, Hkv, -(-S // block)), generator=gen, device="cuda")
+    u += torch.rand((ns, 1, Hkv, -(-S // block)), generator=gen, device="cuda")
+    sel = torch.topk(u, topk, dim=3).indices.to(torch.int32)
+    for x in (q, q * 4):
+        o, lse = P.phase2_sparse(x, K, V, sel, block, o_dtype=P.OUT_BF16)
+        ref = _device_reference(x, K, V, sel, block, 1 / math.sqrt(d))
+        check(o, lse, ref, ns * topk * block, "two groups", bf16_out=True)
