@@ -444,7 +444,9 @@ int pulsar_tree_mask(const int32_t* parent, int T, uint32_t* mask, int32_t* dept
  *
  * The shards and the G rows give partials by the kernels of pulsar_phase2_query, or
  * by 16-row tiles of (token, head) rows where these are faster; the merge folds each
- * token's own branch in, in fp32.
+ * token's own branch in, in fp32.  As there, the softmax and its sums are fp32 and the
+ * weights of the partials enter the product with V rounded to bf16 (by 2^-8 of each at
+ * most, divided by the sum of the rounded ones), whatever o_dtype is.
  *
  * q, Kg, Vg, G, K, V, lse  as for pulsar_phase2_query (row G + t of Kg and Vg
  *           is token t's own); K and V 16-byte aligned.
@@ -539,15 +541,16 @@ int pulsar_block_select(const void* q, const void* bounds, int n_shards, int Tq,
  * Phase-2 attention of new tokens over selected blocks of the retained shards:
  * as pulsar_phase2_query, but of each shard token t reads, for KV head g, the
  * topk blocks listed in sel alone.  With every block listed it computes what
- * pulsar_phase2_query does.
+ * pulsar_phase2_query does.  The weights of all keys enter the product with V rounded
+ * to bf16, as for pulsar_phase2_tree.
  *
  * q         bf16 [Tq, Hq, d].
  * K, V      bf16 [n_shards, S, Hkv, d] (nullable when n_shards, S or topk is 0);
  *           a shard may exceed 2 GiB.
  * sel       int32 [n_shards, Tq, Hkv, topk], as written by pulsar_block_select,
  *           in any order.  An entry outside [0, ceil(S / block)) lists no block
- *           (a list filled up with -1); a block that is listed twice counts
- *           twice.
+ *           (a list filled up with -1, which takes most of the time of a full one);
+ *           a block that is listed twice counts twice.
  * block     as for pulsar_key_bounds.
  * Kg, Vg, G the generation shard, as for pulsar_phase2_query; both NULL (and
  *           G = 0) where another host has it: then the result is the partial

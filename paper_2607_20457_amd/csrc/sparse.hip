@@ -31,11 +31,14 @@
 // once PV has: each has the time of a step to arrive, with one stage per wave, and
 // two waves per SIMD (four at d 64) hide each other's waits.
 //
-// What must not be seen.  A row that no column sees is loaded as a copy of one that
-// some column does, and a step without any such row is left out.  Of the rows that
-// only some columns see, weights of zero keep the others clear of them unless they
-// hold a NaN or an infinity: a pass that ends with a NaN is repeated key by key, each
-// key's product taken over only into the columns that see it.
+// What must not be seen.  A row that no column sees is replaced by a copy of one of its
+// half, or of the other half, that some column does.  A step without any such row (of a
+// list filled up with -1, or of unseen drafts) is loaded from some row of the tensor and
+// scored like others, all its scores -inf, and PV is left out: it costs most of the time of
+// a step, and the plan counts it as one.  Of the rows that only some columns see, weights of
+// zero keep the others clear of them unless they hold a NaN or an infinity: a pass that
+// ends with a NaN is repeated key by key, each key's product taken over only into the
+// columns that see it.
 #include <algorithm>
 #include <type_traits>
 
