@@ -549,8 +549,8 @@ int pulsar_block_select(const void* q, const void* bounds, int n_shards, int Tq,
  *           a shard may exceed 2 GiB.
  * sel       int32 [n_shards, Tq, Hkv, topk], as written by pulsar_block_select,
  *           in any order.  An entry outside [0, ceil(S / block)) lists no block
- *           (a list filled up with -1, which takes most of the time of a full one);
- *           a block that is listed twice counts twice.
+ *           (a list filled up with -1; where tokens are read one by one it takes the
+ *           time of a full one); a block that is listed twice counts twice.
  * block     as for pulsar_key_bounds.
  * Kg, Vg, G the generation shard, as for pulsar_phase2_query; both NULL (and
  *           G = 0) where another host has it: then the result is the partial

@@ -32,13 +32,13 @@
 // two waves per SIMD (four at d 64) hide each other's waits.
 //
 // What must not be seen.  A row that no column sees is replaced by a copy of one of its
-// half, or of the other half, that some column does.  A step without any such row (of a
-// list filled up with -1, or of unseen drafts) is loaded from some row of the tensor and
-// scored like others, all its scores -inf, and PV is left out: it costs most of the time of
-// a step, and the plan counts it as one.  Of the rows that only some columns see, weights of
-// zero keep the others clear of them unless they hold a NaN or an infinity: a pass that
-// ends with a NaN is repeated key by key, each key's product taken over only into the
-// columns that see it.
+// half, or of the other half, that some column does.  A step without any such row (LISTED:
+// of entries that are no block; of unseen drafts) is loaded from some row of the tensor and
+// scored as others are, all -inf, and PV is left out: it takes the time of a step, and the
+// plan counts it as one (a token with 16 x 4 entries of 64 keys 10.2 us, all of them -1
+// 10.1).  Of the rows that only some columns see, weights of zero keep the others clear of
+// them unless they hold a NaN or an infinity: a pass that ends with a NaN is repeated key by
+// key, each key's product taken over only into the columns that see it.
 #include <algorithm>
 #include <type_traits>
 
