@@ -57,19 +57,25 @@ __global__ __launch_bounds__(256) void key_bounds_kernel(const uint16_t* __restr
 // Magnitudes as their bits: without their signs bf16 rank as integers, what is not finite
 // from kInfinite on.
 constexpr int kInfinite = 0x7f80;
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 struct Magnitudes {
   int most = 0, least = 0xffff;  // of those that are not 0
-  template <typename T>
-  __device__ __forceinline__ void add(T x) {
-    constexpr int W = sizeof(T) / 4;
-    typedef uint32_t words __attribute__((ext_vector_type(W)));
-    typedef uint16_t halves __attribute__((ext_vector_type(2 * W)));
-    const halves y = __builtin_bit_cast(halves, __builtin_bit_cast(words, x) & 0x7fff7fffu);
+  template <typename T, int N>
+  __device__ __forceinline__ void add(const T (&x)[N]) {
+    u16x2 top = {0, 0}, low = {0xffff, 0xffff};
 #pragma unroll
-    for (int i = 0; i < 2 * W; ++i) {
-      most = max(most, (int)y[i]);
-      least = min(least, (int)(uint16_t)(y[i] - 1));  // (a 0 is passed over)
+    for (int i = 0; i < N; ++i) {
+      typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) / 4)));
+      const words w = __builtin_bit_cast(words, x[i]) & 0x7fff7fffu;
+#pragma unroll
+      for (int k = 0; k < (int)(sizeof(T) / 4); ++k) {
+        const u16x2 y = __builtin_bit_cast(u16x2, (uint32_t)w[k]);
+        top = __builtin_elementwise_max(top, y);
+        low = __builtin_elementwise_min(low, y - (u16x2){1, 1});  // (a 0 is passed over)
+      }
     }
+    most = max(most, max((int)top[0], (int)top[1]));
+    least = min(least, min((int)low[0], (int)low[1]));
   }
   // over the lanes r, r + 16, r + 32, r + 48
   __device__ __forceinline__ void join_rows() {
@@ -149,11 +155,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void b
   }
   // the bounds of row r, then of the rows whose products a lane gets, 4v + g
   Magnitudes mine, block[4];
-#pragma unroll
-  for (int i = 0; i < N / 8; ++i) {
-    mine.add(lo[i]);
-    mine.add(hi[i]);
-  }
+  mine.add(lo);
+  mine.add(hi);
   mine.join_rows();
 #pragma unroll
   for (int v = 0; v < 4; ++v) {
@@ -188,8 +191,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void b
                                                     (double)(qi < 0.f ? qi : 0.f), down, 0, 0, 0);
       }
       Magnitudes head;
-#pragma unroll
-      for (int i = 0; i < N / 8; ++i) head.add(x[i]);
+      head.add(x);
       head.join_rows();
       double sum[4];
       int open = 0;  // sums to be formed in order
@@ -232,7 +234,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void b
 // ---------------------------------------------------------------------------
 // Near scores, for the selection alone: the same sums by bf16 matrix products
 // (16x16x32, exact products, fp32 sums).  The fp64 products bound the exact form (64
-// tokens, 4096 blocks of 8 KV heads: 125 us with the pick); the selection needs them
+// tokens, 4096 blocks of 8 KV heads: 123 us with the pick); the selection needs them
 // only for the few blocks whose near scores lie within their errors of the last one
 // that it keeps.
 //
@@ -926,8 +928,7 @@ void block_pick_kernel(const uint16_t* __restrict__ q, const uint16_t* __restric
         const auto lo = __builtin_convertvector(lo16, f64xN);
         const auto hi = __builtin_convertvector(hi16, f64xN);
         Magnitudes m;
-        m.add(lo16);
-        m.add(hi16);
+        m.add({lo16, hi16});
         float best = over_row(m.most, Most{}) >= kInfinite ? INFINITY : -INFINITY;
         constexpr int HU = 4;  // heads at a time
         for (int h0 = 0; h0 < group; h0 += HU) {
