@@ -6,6 +6,7 @@ import torch
 
 import paper_2607_20457_amd as P
 from oracle import blocks as ob
+from tests import test_gpu_blocks as lists
 from tests._blocks import dev_mask, f64, host, normal, to_dev_bf16
 
 pytestmark = pytest.mark.gpu
@@ -83,3 +84,20 @@ def test_shards_of_drafts_go_together():
     for kw in (dict(K=k), dict(V=k)):
         with pytest.raises(ValueError):
             P.phase2_tree(q, kg, kg, 4, mask, **kw)
+
+
+# heads and lists whose tokens fill two groups of 16 columns from 1200 MB of listed keys on
+TWO_GROUPS = [shape[:8] + (1300,) for shape in lists.TOGETHER
+              if shape[2] == 128 and shape[0] // shape[1] > 2 and shape[8] == 800]
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,Tq,ns,S,block,topk,mb", TWO_GROUPS)
+def test_two_groups_of_tokens_read_together(Hq, Hkv, d, Tq, ns, S, block, topk, mb):
+    lists.test_tokens_read_together(Hq, Hkv, d, Tq, ns, S, block, topk, mb)
+
+
+# (the one before the last block is to be token 3's alone: not among the first topk - 1)
+@pytest.mark.parametrize("Hq,Hkv,d,Tq,ns,S,block,topk,mb",
+                         [x for x in TWO_GROUPS if -(-x[5] // x[6]) - 2 >= x[7] - 1])
+def test_two_groups_of_tokens_keep_their_rows(Hq, Hkv, d, Tq, ns, S, block, topk, mb):
+    lists.test_tokens_read_together_keep_their_rows(Hq, Hkv, d, Tq, ns, S, block, topk, mb)
