@@ -839,16 +839,16 @@ static SparsePlan dense_plan(int64_t keys, int Tq, int64_t G, int Hq, int Hkv, i
   p.parts = parts_at_once(std::min(tiles_at_once(d) / tiles, (steps + 3) / 4), Hkv, own,
                           tiles_at_once(d) / 8);
   // Eight waves where that is a workgroup for 112 compute units at least and, unless the
-  // steps end before the parts do, for four fifths of them.  With the merge, four waves /
-  // eight, us: 32 / 8 heads of 128 over 4 x 1021 keys, 8 tiles (128 workgroups) 11.9 / 11.1,
-  // 64 (256) 18.7 / 17.1, over 8192 keys 96 tiles (192) 30.4 / 33.2; 8 / 2 heads over 4 x
-  // 1021, 6 tiles (96) 10.8 / 11.0; 16 / 8 of 64 over 16 x 8192, 16 tiles 61 / 50, over 4 x
-  // 4096 96 (192) 33 / 41.  Over 201 shapes the choice is 0.5 % slower than the better one
-  // of both on average, and 16 % at most.
+  // steps end before the parts do, in long ranges for four fifths of them.  With the merge,
+  // four waves / eight, us: 32 / 8 heads of 128 over 4 x 1021 keys, 8 tiles (128 workgroups)
+  // 11.9 / 11.1, 64 (256) 18.7 / 17.1; 8 / 2 heads over 4 x 1021, 6 tiles (96) 10.8 / 11.0; 96
+  // tiles (192) of 32 / 8 over 2048 keys 19.7 / 18.5, 4 x 1021 22.8 / 22.7, 8192 30.9 / 33.5,
+  // 80 (240) over 8192 27.1 / 27.0; 16 / 8 of 64, 96 over 4 x 1021 19.6 / 18.7.  Over 145 shapes
+  // the choice is 0.1 % slower than the better one of both on average, and 4 % at most.
   if (tiles <= 256) {
     const int parts = parts_at_once(std::min(256 / tiles, (steps + 7) / 8), Hkv, own, 32);
     const int64_t nwg = tiles * parts;
-    if (nwg >= 112 && (nwg >= 205 || steps <= 8 * parts)) {
+    if (nwg >= 112 && (nwg >= 205 || steps <= std::max(160, 8 * parts))) {
       p.waves = 8;
       p.parts = parts;
     }
