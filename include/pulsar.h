@@ -79,6 +79,12 @@ typedef enum {
   PULSAR_SCORE_ENTROPY = 3  /* distinct tokens / chunk length (Eq. entropy) */
 } pulsar_scorer;
 
+/* Codes of a cache held in 8 bits (pulsar_kv_quantize). */
+typedef enum {
+  PULSAR_KV_E4M3 = 0,  /* 4 exponent bits, 3 of mantissa, largest value 448, no infinity */
+  PULSAR_KV_INT8 = 1   /* two's complement; -128 is not written */
+} pulsar_kv_format;
+
 /* Human-readable name of a status code (static storage; never NULL). */
 const char* pulsar_status_string(int status);
 
@@ -580,6 +586,87 @@ int pulsar_phase2_sparse(const void* q, const void* K, const void* V, const int3
                          const void* Vg, int64_t G, const uint32_t* mask, int Hq, int Hkv, int d,
                          float softmax_scale, void* o, int o_dtype, float* lse, void* workspace,
                          size_t workspace_bytes, void* stream);
+
+/*
+ * A cache held in 8 bits.  K and V are each codes and scales:
+ *   codes   e4m3 or int8 (a pulsar_kv_format), one byte each, [n, Hkv, capacity, d]: the
+ *           rows of one KV head of a shard (or layer) lie one after another;
+ *   scales  float [n, Hkv, ceil(capacity / block)]: of each block of `block` rows
+ *           [b * block, (b + 1) * block) and head.
+ * A code stands for code * scale.
+ *
+ * pulsar_kv_quantize writes rows [first, first + rows) of every shard of the cache from
+ * bf16 rows, whole blocks of them: first is a multiple of block, and the last block may
+ * be short (it is written again, from its first row, once it has more).  A block's scale
+ * is 2^e with the least e >= -100 for which its largest magnitude is at most 448 * 2^e
+ * (e4m3) or 127 * 2^e (int8); a code is the nearest to x / 2^e, ties to even, and at e = 120
+ * of e4m3 at most 240, at e = 122 of int8 at most 63 in magnitude, so that code * 2^e is
+ * finite.  A block with a NaN or an infinity gets the scale NaN and codes 0: all of it
+ * reads back as NaN.  Only the rows given count towards a scale; other rows and blocks of
+ * the cache stay as they are.
+ *
+ * pulsar_kv_dequantize writes rows [first, first + rows), from any row on, as bf16: code *
+ * scale in fp32, rounded once (not at all for scales that pulsar_kv_quantize wrote).
+ *
+ * K, V      bf16, 16-byte aligned: row r of shard i is Hkv * d consecutive values at
+ *           element i * shard_stride + r * row_stride, both multiples of 8 (quantising;
+ *           rows may lie inside longer ones, or in a larger cache).  Dequantising: out
+ *           [n, rows, Hkv, d], contiguous.
+ * codes     16-byte aligned; no memory in common with K and V.
+ * block     16, 32, 64, 128 or 256 rows.
+ * EINVAL: negative sizes, Hkv < 1, d < 1, block < 1, an unknown format, first or rows past
+ *         the capacity, first not a multiple of block (quantising), NULL or misaligned
+ *         pointers or strides when there is work.
+ * EUNSUPPORTED: d not in {64, 128}; another block; capacity >= 2^31 or Hkv * d >= 2^23;
+ *         more workgroups than a launch holds (none below n * ceil(rows / 64) * Hkv = 2^21).
+ */
+int pulsar_kv_quantize(const void* K, const void* V, int64_t shard_stride, int64_t row_stride,
+                       int n, int64_t rows, int Hkv, int d, int block, int format, int64_t first,
+                       int64_t capacity, void* k_codes, void* v_codes, float* k_scales,
+                       float* v_scales, void* stream);
+int pulsar_kv_dequantize(const void* k_codes, const void* v_codes, const float* k_scales,
+                         const float* v_scales, int n, int64_t capacity, int Hkv, int d, int block,
+                         int format, int64_t first, int64_t rows, void* K, void* V, void* stream);
+
+/*
+ * Phase-2 attention of new tokens over shards held in 8 bits: as pulsar_phase2_query (or,
+ * with a mask, pulsar_phase2_tree), with a retained key or value standing for code * scale.
+ * The generation shard stays bf16; its closed blocks may be moved into the cache.  Scores
+ * and sums are fp32, with the codes and q multiplied exactly; the weights, times the scale
+ * of their block of V, enter the product with V's codes rounded to bf16 (by 2^-8 of each at
+ * most, divided by the sum of the rounded ones).
+ *
+ * q         bf16 [Tq, Hq, d].
+ * codes, scales  as for pulsar_kv_quantize, with n = n_shards and capacity = S (nullable
+ *           when n_shards or S is 0).  A scale that is NaN makes its block NaN; one below
+ *           2^-100 counts as 2^-100.
+ * rows      int32 [n_shards] on the device, nullable: shard i's live rows are [0, rows[i])
+ *           (clamped to [0, S]; NULL: S).  Nothing behind them is read, so a cache may grow
+ *           between two replays of a captured call.
+ * Kg, Vg, G, mask, o, o_dtype, lse  as for pulsar_phase2_sparse (Kg and Vg both NULL where
+ *           another host has the generation shard).  A token that sees no key gives 0, -inf;
+ *           rows that a token does not see cannot reach its output.
+ * workspace device buffer of at least pulsar_phase2_quant_workspace_bytes bytes, 16-byte
+ *           aligned (may be NULL when that is 0); contents on entry do not matter.  The size
+ *           holds for any number of tokens up to Tq and for any shards and appended rows.
+ *           pulsar_phase2_quant_call_bytes is what a call of just these sizes takes
+ *           (gen_rows: G + Tq, or 0 without Kg), often nothing.
+ * EINVAL: negative sizes, Hq % Hkv != 0, NULL or misaligned pointers when there is work,
+ *         only one of Kg and Vg, a mask or G > 0 without them, scale not finite and > 0,
+ *         unknown o_dtype or format.  EWORKSPACE: workspace too small.
+ * EUNSUPPORTED: d not in {64, 128}; another block; n_shards * S >= 2^31; rows with
+ *         n_shards > 1024; G + Tq >= 2^24; a row of Kg of 16 MiB or more; more workgroups
+ *         than a launch holds (none below Tq * Hkv * ceil(Hq / Hkv / 16) = 2^23).
+ */
+size_t pulsar_phase2_quant_workspace_bytes(int Tq, int Hq, int Hkv, int d);
+size_t pulsar_phase2_quant_call_bytes(int n_shards, int Tq, int64_t S, int64_t gen_rows, int Hq,
+                                      int Hkv, int d);
+int pulsar_phase2_quant(const void* q, const void* k_codes, const void* v_codes,
+                        const float* k_scales, const float* v_scales, int n_shards, int Tq,
+                        int64_t S, int block, int format, const int32_t* rows, const void* Kg,
+                        const void* Vg, int64_t G, const uint32_t* mask, int Hq, int Hkv, int d,
+                        float softmax_scale, void* o, int o_dtype, float* lse, void* workspace,
+                        size_t workspace_bytes, void* stream);
 
 /*
  * Rotary position embedding of query or key rows at given positions

@@ -35,8 +35,10 @@ Modules, each following the paper's definitions in its own notation:
 * ``blocks``    -- drafted tokens and block-sparse reads in Phase 2: visibility of a
                    tree, attention with key multiplicities, block bounds,
                    scores and selection, compaction of kept rows.
+* ``quant``     -- a cache held in 8 bits: scales and codes of blocks of rows, and
+                   the values that they stand for.
 
 Readings of points the paper leaves open are listed in each function's
 docstring.
 """
-from . import assembly, attention, blocks, cost, maxidf, rope, scorers  # noqa: F401
+from . import assembly, attention, blocks, cost, maxidf, quant, rope, scorers  # noqa: F401

@@ -62,6 +62,16 @@ SIGNATURES = {
     "pulsar_phase2_sparse": (_c_int, [_vp, _vp, _vp, _vp, _c_int, _c_int, _c_i64, _c_int, _c_int,
                                       _vp, _vp, _c_i64, _vp, _c_int, _c_int, _c_int, _c_float,
                                       _vp, _c_int, _vp, _vp, _c_size, _vp]),
+    "pulsar_kv_quantize": (_c_int, [_vp, _vp, _c_i64, _c_i64, _c_int, _c_i64, _c_int, _c_int,
+                                    _c_int, _c_int, _c_i64, _c_i64, _vp, _vp, _vp, _vp, _vp]),
+    "pulsar_kv_dequantize": (_c_int, [_vp, _vp, _vp, _vp, _c_int, _c_i64, _c_int, _c_int, _c_int,
+                                      _c_int, _c_i64, _c_i64, _vp, _vp, _vp]),
+    "pulsar_phase2_quant_workspace_bytes": (_c_size, [_c_int, _c_int, _c_int, _c_int]),
+    "pulsar_phase2_quant_call_bytes": (_c_size, [_c_int, _c_int, _c_i64, _c_i64, _c_int, _c_int,
+                                                 _c_int]),
+    "pulsar_phase2_quant": (_c_int, [_vp, _vp, _vp, _vp, _vp, _c_int, _c_int, _c_i64, _c_int,
+                                     _c_int, _vp, _vp, _vp, _c_i64, _vp, _c_int, _c_int, _c_int,
+                                     _c_float, _vp, _c_int, _vp, _vp, _c_size, _vp]),
     "pulsar_rope": (_c_int, [_vp, _c_int, _c_i64, _c_int, _c_int, _vp, _c_i64, _vp,
                              ctypes.c_double, _vp]),
 }

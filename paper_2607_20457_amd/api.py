@@ -559,3 +559,159 @@ def phase2_sparse(q, K, V, sel, block: int, Kg=None, Vg=None, G: int = 0, mask=N
         lse.data_ptr(), ws_ptr, need, _raw_stream(dev))
     _lib.check(st, "pulsar_phase2_sparse")
     return o, lse
+
+
+_FORMATS = {torch.float8_e4m3fn: 0, torch.int8: 1}
+
+
+def _cache_of(Kc, Vc, k_scale, v_scale, block, dev):
+    """The shape [n, Hkv, capacity, d] of a cache in 8 bits, and its format."""
+    _int32(block, "block")
+    if Kc.dtype not in _FORMATS:
+        raise ValueError(f"codes must be torch.float8_e4m3fn or torch.int8, got {Kc.dtype}")
+    _check(dev, Kc.dtype, ((Kc, "Kc"), (Vc, "Vc")))
+    _check(dev, torch.float32, ((k_scale, "k_scale"), (v_scale, "v_scale")))
+    if Kc.dim() != 4 or Vc.shape != Kc.shape:
+        raise ValueError("Kc/Vc must be [n, Hkv, capacity, d]")
+    n, Hkv, capacity, _ = Kc.shape
+    blocks = -(-capacity // block) if block > 0 else 0
+    if k_scale.shape != (n, Hkv, blocks) or v_scale.shape != k_scale.shape:
+        raise ValueError("k_scale/v_scale must be [n, Hkv, ceil(capacity / block)]")
+    return Kc.shape, _FORMATS[Kc.dtype]
+
+
+def _apart(a, b):
+    """Whether two tensors' memory, from the first element to the last, has none in common."""
+    def span(t):
+        last = sum((s - 1) * st for s, st in zip(t.shape, t.stride()))
+        return t.data_ptr(), t.data_ptr() + (last + 1) * t.element_size()
+    (a0, a1), (b0, b1) = span(a), span(b)
+    return not a.numel() or not b.numel() or a1 <= b0 or b1 <= a0
+
+
+def kv_quantize_(K, V, Kc, Vc, k_scale, v_scale, block: int, first: int = 0):
+    """Rows [first, first + rows) of a cache in 8 bits written from K/V bf16 [n, rows,
+    Hkv, d] (the rows of any longer tensors: strides of a multiple of 8 elements), whole
+    blocks of them: first is a multiple of block (16, 32, 64, 128 or 256), the last block may
+    be short.  Kc/Vc float8_e4m3fn or int8 [n, Hkv, capacity, d], k_scale/v_scale f32 [n, Hkv,
+    ceil(capacity / block)]: a code stands for code * scale, the scale a power of two for each
+    block and head, NaN (and codes 0) where the block holds a NaN or an infinity.
+    Returns the cache: Kc, Vc, k_scale, v_scale."""
+    dev = torch.cuda.current_device() if K.is_cuda else None
+    for t, name in ((K, "K"), (V, "V")):
+        if t.get_device() != dev or t.dtype is not _BF16:
+            _need(t, _BF16, name)
+            raise ValueError(f"{name} must be on the current device")
+    (n, Hkv, capacity, d), form = _cache_of(Kc, Vc, k_scale, v_scale, block, dev)
+    if K.dim() != 4 or V.shape != K.shape or K.shape[0] != n or K.shape[2:] != (Hkv, d):
+        raise ValueError("K/V must be [n, rows, Hkv, d]")
+    rows = K.shape[1]
+    if not 0 <= first <= capacity - rows:
+        raise ValueError("first and the rows must lie within the cache")
+    strides = [(x.stride(0) if n > 1 else 0, x.stride(1) if rows > 1 else 0) for x in (K, V)]
+    if strides[0] != strides[1] or K.numel() and any(
+            x.stride(3) != 1 or Hkv > 1 and x.stride(2) != d for x in (K, V)):
+        raise ValueError("K and V must have the same strides, each row [Hkv, d] contiguous")
+    for out, name in ((Kc, "Kc"), (Vc, "Vc"), (k_scale, "k_scale"), (v_scale, "v_scale")):
+        if not _apart(out, K) or not _apart(out, V):
+            raise ValueError(f"{name} must not share memory with K or V")
+    if not (_apart(Kc, Vc) and _apart(k_scale, v_scale)):
+        raise ValueError("the caches of K and V must not share memory")
+    st = _lib.lib().pulsar_kv_quantize(K.data_ptr(), V.data_ptr(), *strides[0], n, rows, Hkv, d,
+                                       block, form, first, capacity, Kc.data_ptr(),
+                                       Vc.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+                                       _raw_stream(dev))
+    _lib.check(st, "pulsar_kv_quantize")
+    return Kc, Vc, k_scale, v_scale
+
+
+def kv_quantize(K, V, block: int = 64, dtype=torch.float8_e4m3fn, capacity: int | None = None):
+    """K/V bf16 [n, rows, Hkv, d] as a new cache in 8 bits (``kv_quantize_``), with room for
+    `capacity` rows (None: rows); what lies behind the rows is undefined
+    -> Kc, Vc, k_scale, v_scale."""
+    if dtype not in _FORMATS:
+        raise ValueError("dtype must be torch.float8_e4m3fn or torch.int8")
+    if K.dim() != 4:
+        raise ValueError("K/V must be [n, rows, Hkv, d]")
+    n, rows, Hkv, d = K.shape
+    _int32(block, "block")
+    capacity = rows if capacity is None else capacity
+    if block < 1 or capacity < rows:
+        raise ValueError("block must be positive, capacity at least the rows")
+    codes = [K.new_empty((n, Hkv, capacity, d), dtype=dtype) for _ in range(2)]
+    scales = [K.new_empty((n, Hkv, -(-capacity // block)), dtype=torch.float32) for _ in range(2)]
+    return kv_quantize_(K, V, *codes, *scales, block)
+
+
+def kv_dequantize(Kc, Vc, k_scale, v_scale, block: int, first: int = 0, rows: int | None = None):
+    """Rows [first, first + rows) (None: all from first on) of a cache in 8 bits
+    -> K, V bf16 [n, rows, Hkv, d]."""
+    dev = torch.cuda.current_device() if Kc.is_cuda else None
+    (n, Hkv, capacity, d), form = _cache_of(Kc, Vc, k_scale, v_scale, block, dev)
+    rows = capacity - first if rows is None else rows
+    if first < 0 or rows < 0 or first + rows > capacity:
+        raise ValueError("first and rows must lie within the cache")
+    K, V = (Kc.new_empty((n, rows, Hkv, d), dtype=_BF16) for _ in range(2))
+    st = _lib.lib().pulsar_kv_dequantize(Kc.data_ptr(), Vc.data_ptr(), k_scale.data_ptr(),
+                                         v_scale.data_ptr(), n, capacity, Hkv, d, block, form,
+                                         first, rows, K.data_ptr(), V.data_ptr(),
+                                         _raw_stream(dev))
+    _lib.check(st, "pulsar_kv_dequantize")
+    return K, V
+
+
+@functools.lru_cache(maxsize=4096)
+def phase2_quant_workspace_bytes(Tq: int, Hq: int, Hkv: int, d: int) -> int:
+    return int(_lib.lib().pulsar_phase2_quant_workspace_bytes(Tq, Hq, Hkv, d))
+
+
+@functools.lru_cache(maxsize=4096)
+def _quant_call_bytes(n_shards, Tq, S, gen_rows, Hq, Hkv, d):
+    return int(_lib.lib().pulsar_phase2_quant_call_bytes(n_shards, Tq, S, gen_rows, Hq, Hkv, d))
+
+
+def phase2_quant(q, Kc, Vc, k_scale, v_scale, block: int, rows=None, Kg=None, Vg=None, G: int = 0,
+                 mask=None, softmax_scale: float | None = None, o_dtype: int = OUT_F32,
+                 workspace=None):
+    """Attention of Tq new tokens over shards held in 8 bits (``kv_quantize``) and over the
+    generation shard: q bf16 [Tq, Hq, d], Kc/Vc [n_shards, Hkv, S, d], rows int32 [n_shards]
+    the shards' live rows (None: all S), Kg/Vg bf16 [G + Tq, Hkv, d] (None: the shards alone)
+    up to each token itself, or by a tree's mask -> (o [Tq, Hq, d] per o_dtype, lse f32
+    [Hq, Tq])."""
+    dev = torch.cuda.current_device() if q.is_cuda else None
+    _check(dev, _BF16, ((q, "q"),))
+    (n_shards, Hkv, S, dk), form = _cache_of(Kc, Vc, k_scale, v_scale, block, dev)
+    Tq, Hq, d = q.shape
+    if dk != d:
+        raise ValueError("Kc/Vc must be [n_shards, Hkv, S, d]")
+    rows_ptr = kg_ptr = vg_ptr = mask_ptr = None
+    if rows is not None:
+        _check(dev, torch.int32, ((rows, "rows"),))
+        if rows.shape != (n_shards,):
+            raise ValueError("rows must be [n_shards]")
+        rows_ptr = rows.data_ptr()
+    if Kg is not None or Vg is not None:
+        if Kg is None or Vg is None:
+            raise ValueError("Kg and Vg go together")
+        _check(dev, _BF16, ((Kg, "Kg"), (Vg, "Vg")))
+        _generation_shape(Kg, Vg, G, Tq, Hkv, d)
+        kg_ptr, vg_ptr = Kg.data_ptr(), Vg.data_ptr()
+    elif G != 0 or mask is not None:
+        raise ValueError("G and mask belong to Kg and Vg")
+    if mask is not None:
+        _check(dev, torch.int32, ((mask, "mask"),))
+        _mask_shape(mask, Tq)
+        mask_ptr = mask.data_ptr()
+    o = _out(q, o_dtype)
+    lse = q.new_empty((Hq, Tq), dtype=torch.float32)
+    # (the plan takes the appended rows 32 at a time: few sizes to remember)
+    gen_rows = (G + Tq + 31 & ~31) if kg_ptr else 0
+    need = _quant_call_bytes(n_shards, Tq, S, gen_rows, Hq, Hkv, d)
+    workspace, ws_ptr = _scratch(workspace, need, dev, q)
+    st = _lib.lib().pulsar_phase2_quant(
+        q.data_ptr(), Kc.data_ptr(), Vc.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+        n_shards, Tq, S, block, form, rows_ptr, kg_ptr, vg_ptr, G, mask_ptr, Hq, Hkv, d,
+        1.0 / math.sqrt(d) if softmax_scale is None else softmax_scale, o.data_ptr(), o_dtype,
+        lse.data_ptr(), ws_ptr, need, _raw_stream(dev))
+    _lib.check(st, "pulsar_phase2_quant")
+    return o, lse

@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "../../include/pulsar.h"
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -282,6 +284,24 @@ int launch_tree_merge(const float* o_parts, const float* lse_parts, int H, int T
 int launch_kv_compact(void* K, void* V, int layers, int64_t capacity, int64_t row_bytes, int64_t G,
                       const int32_t* keep, int n, hipStream_t stream);
 
+// XCDs over which the `tiles` of each of `units` (KV head, part) pairs are spread: few
+// pairs that are no multiple of eight, so that all XCDs are at work.
+inline int tile_slices(int64_t units, int64_t tiles) {
+  int slices = 1;
+  if (units < 32)
+    while (units * slices % 8 != 0 && slices * 2 <= tiles) slices *= 2;
+  return slices;
+}
+// The most parts, up to `parts`, whose workgroups an XCD holds at once.
+inline int parts_at_once(int64_t parts, int Hkv, int64_t tiles, int64_t held) {
+  while (parts > 1) {
+    const int slices = tile_slices(Hkv * parts, tiles);
+    if ((Hkv * parts * slices + 7) / 8 * ((tiles + slices - 1) / slices) <= held) break;
+    --parts;
+  }
+  return (int)std::max<int64_t>(parts, 1);
+}
+
 // Block-sparse reads of the retained shards (blocks.hip, sparse.hip).
 int launch_key_bounds(const uint16_t* K, int n_shards, int64_t S, int Hkv, int d, int block,
                       uint16_t* bounds, hipStream_t stream);
@@ -330,6 +350,43 @@ bool dense_tiles_apply(int Hq, int Hkv);
 int dense_parts(int n_shards, int Tq, int64_t S, int64_t G, int Hq, int Hkv, int d);
 int64_t dense_part_rows_most(int Tq, int Hq, int Hkv, int d);
 int launch_dense(const SparseLaunch& a, int parts, float* o, float* lse, hipStream_t stream);
+
+// A cache in 8 bits (quant.hip, quant_attn.hip): codes [n, Hkv, capacity, d] and scales
+// [n, Hkv, ceil(capacity / block)] of K and of V.
+struct KvQuantLaunch {
+  const uint16_t* X[2];  // bf16 rows at these strides, in elements (quantising)
+  int64_t shard_stride, row_stride;
+  uint8_t* codes[2];
+  float* scales[2];
+  int n, Hkv, d, block, format;
+  int64_t rows, first, capacity;
+};
+int launch_quantize(const KvQuantLaunch& a, hipStream_t stream);
+int launch_dequantize(const KvQuantLaunch& a, uint16_t* const (&out)[2], hipStream_t stream);
+struct QuantAttnLaunch {
+  const uint16_t* q;    // bf16 [Tq, Hq, d]
+  const uint8_t* K;
+  const uint8_t* V;
+  const float* ks;
+  const float* vs;
+  const int32_t* rows;  // [n_shards], or NULL
+  const uint16_t* Kg;   // bf16 [G + Tq, Hkv, d], or NULL
+  const uint16_t* Vg;
+  const uint32_t* mask; // [Tq, ceil(Tq / 32)], or NULL for index-causal
+  int n_shards, Tq, Hq, Hkv, d, block, format;
+  int64_t S, G;
+  float scale;
+};
+constexpr int kMaxQuantShards = 1024;  // with lengths of their own
+struct QuantPlan {
+  int groups;  // of 16 columns in a tile
+  int tokens;  // per tile
+  int parts;   // of a tile's keys
+};
+QuantPlan quant_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int64_t gen_rows);
+int64_t quant_part_rows_most(int Tq, int Hq, int Hkv);
+int launch_quant_attn(const QuantAttnLaunch& a, const QuantPlan& plan, void* o, int o_bf16,
+                      float* lse, hipStream_t stream);
 
 // Rows of an assembled Phase-1 input gathered from a per-position tensor and
 // rotated per pos_mode (a pulsar_pos_mode).

@@ -1,0 +1,749 @@
+// Phase-2 attention of new tokens over shards held in 8 bits and over the generation
+// shard, which is bf16.
+//
+// Work.  A tile is 16, 32 or 64 columns of one KV head: column n is head n % group of
+// the tile's token n / group (or, of a larger group, 16 CG of one token's heads).  Its
+// keys are steps of 64 rows of a shard, or of 32 rows of the generation shard: 64 D bytes
+// of K and of V either way.  A workgroup takes one part of a tile's steps, wave w of NW
+// the steps w, w + NW, ... of it on its own; then the waves' states are merged through
+// LDS, and the parts by the log-sum-exp merge.  A step of a wave:
+//   K, V  into the wave's LDS stage by loads that write LDS directly: a head's rows
+//       are contiguous, so a step is 64 D consecutive bytes;
+//   S^T = K Q^T (16x16x32), K's codes widened to bf16, which holds them exactly, as
+//       they are read: lane (r, g) takes channels D/4 * g .. of row r, so that 16 bytes
+//       are two operands; the queries lie in the same order.  Then O^T += V^T P^T, V read
+//       transposed in 8 bits and widened;
+//   softmax  online, log2 domain, the reference raised when a step's maximum exceeds
+//       it by more than 2^8.  A score is (q . code) * (scale * ks log2 e), one product of
+//       the block; the weight that enters PV is exp2(score - reference + log2 vs): V's
+//       scale is in it before it is rounded to bf16 (2^-8 of each at most), and sums of
+//       weights are taken times 1 / vs.  O is divided by the sum of the rounded weights, the
+//       log-sum-exp uses the fp32 sum.
+// The next step's K is sent for once the scores have consumed this one's, its V once PV
+// has.
+//
+// What must not be seen.  Rows from a shard's live length on are not loaded (a copy of
+// the step's last live row is) and score -inf; their scales are not read.  Of the new
+// tokens' own rows, which only some columns see, unseen ones score -inf; where V holds a
+// NaN or an infinity among them, the product is taken key by key, each key's only into the
+// columns that see it.
+#include <algorithm>
+#include <type_traits>
+
+#include "tiles.hpp"
+
+namespace {
+
+constexpr int QA_KEYS = 64;           // codes' rows per step
+constexpr int QA_GEN = 32;            // generation shard's rows per step
+constexpr float QA_SLACK = 8.0f;      // log2 slack before the reference is raised
+constexpr float QA_LEAST = 0x1p-100f; // a smaller scale counts as this
+constexpr int QA_SHARDS = 1024;       // shards with lengths of their own
+
+struct QuantAttnArgs {
+  const uint16_t* q;
+  const uint8_t *K, *V;    // [n_shards, Hkv, S, D]
+  const float *ks, *vs;    // [n_shards, Hkv, blocks]
+  const int32_t* rows;     // [n_shards] live rows, or NULL: S
+  const uint16_t *Kg, *Vg; // bf16 [G + Tq, Hkv, D], or NULL
+  const uint32_t* mask;    // [Tq, ceil(Tq / 32)], or NULL for index-causal
+  int Tq, Hq, Hkv, group;
+  int tile_tokens, token_tiles, col_tiles, slices;
+  int n_shards, S, blocks, block_log2;
+  int gen_rows;            // G + Tq, or 0
+  int G;
+  int shard_steps;         // of a shard of S rows
+  int parts;
+  float scale_log2;
+  int o_bf16;
+  void* O;                 // parts > 1: float [parts, Tq, Hq, D]; else the output
+  float* lse;              // [parts, Hq, Tq]; nullable for the output
+};
+
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+
+template <int D, int NW>
+struct QaLds {
+  static constexpr int STAGE = QA_KEYS * D;  // a K or V step
+  static constexpr int LOOP = NW * 2 * STAGE;
+  static constexpr int PITCH = D + 4;        // floats of a state's column
+  static constexpr int MERGE = NW * 16 * (PITCH + 3) * 4;
+  static constexpr int REUSED = LOOP > MERGE ? LOOP : MERGE;
+  // with lengths: the steps before each shard
+  static constexpr int STEPS = (QA_SHARDS + 1) * 4 + NW * 4;
+};
+
+// Eight codes (two dwords) as bf16, exactly.
+template <int FORMAT>
+__device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi) {
+  if constexpr (FORMAT == PULSAR_KV_E4M3) {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
+    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false);
+    const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+  } else {
+    f32x8 y;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      y[b] = (float)((int)(lo << (24 - 8 * b)) >> 24);
+      y[4 + b] = (float)((int)(hi << (24 - 8 * b)) >> 24);
+    }
+    return __builtin_convertvector(y, bf16x8);
+  }
+}
+
+template <int D, int FORMAT, int NW, int CG>
+__global__ __launch_bounds__(64 * NW)
+__attribute__((amdgpu_waves_per_eu(CG > 2 ? 1 : 2, CG > 2 ? 1 : 2)))
+void quant_attn_kernel(QuantAttnArgs a) {
+  using L = QaLds<D, NW>;
+  constexpr int CPR = D / 16;             // 16-byte chunks of a row of codes
+  constexpr int GCPR = D / 8;             // of a bf16 row
+  constexpr int DS = D / 32;              // k-steps of S
+  constexpr int DT = D / 16;              // 16-row tiles of O^T
+  constexpr int SEGS = L::STAGE / 1024;   // 1 KiB segments: one 16-byte load per lane each
+  constexpr int NH = CG == 1 ? 4 : 2;     // halves (of 16 keys) multiplied at a time
+  extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r = lane & 15, g = lane >> 4;
+  // Workgroup -> tile of a (KV head, part): all tiles of one head's part, which read the
+  // same keys, go to one XCD, one after another (few such parts: to `slices` of them).
+  const int tiles = a.token_tiles * a.col_tiles, deep = (tiles + a.slices - 1) / a.slices;
+  int64_t wg = blockIdx.x >> 3;
+  const int in = (int)(wg % deep);
+  wg = wg / deep * 8 + (blockIdx.x & 7);
+  const int tile = in * a.slices + (int)(wg % a.slices);
+  wg /= a.slices;
+  if (wg >= (int64_t)a.Hkv * a.parts || tile >= tiles) return;
+  const int kvh = (int)(wg % a.Hkv), part = (int)(wg / a.Hkv);
+  const int t0 = tile % a.token_tiles * a.tile_tokens;
+  const int heads0 = tile / a.token_tiles * (16 * CG);
+  const int tokens = min(a.tile_tokens, a.Tq - t0);
+  const int cols = a.col_tiles > 1 ? min(16 * CG, a.group - heads0) : tokens * a.group;
+  const float c2 = a.scale_log2;
+
+  // ---- Q fragments (B operand): column 16 c + r, channels D/4 * g + 8 s .. --------
+  int t[CG];
+  bf16x8 qf[CG][DS];
+#pragma unroll
+  for (int c = 0; c < CG; ++c) {
+    const int n = 16 * c + r;
+    const bool live = n < cols;
+    const int tl = live && a.col_tiles == 1 ? n / a.group : 0;
+    t[c] = t0 + tl;
+    const int head = kvh * a.group + heads0 + (live ? n - tl * a.group : 0);
+    const bf16x8* src =
+        reinterpret_cast<const bf16x8*>(a.q + ((int64_t)t[c] * a.Hq + head) * D) + DS * g;
+#pragma unroll
+    for (int s = 0; s < DS; ++s) qf[c][s] = live ? src[s] : bf16x8{};
+  }
+
+  // ---- the tile's steps: those of the shards' live rows, then the generation shard's --
+  int* const before = reinterpret_cast<int*>(smem + L::REUSED);  // [n_shards + 1]
+  int list_steps = a.n_shards * a.shard_steps;
+  auto live_rows = [&](int shard) { return min(max(a.rows[shard], 0), a.S); };
+  if (a.rows != nullptr) {
+    int* const sums = before + QA_SHARDS + 1;
+    int total = 0;
+    for (int i0 = 0; i0 < a.n_shards; i0 += 64 * NW) {
+      const int i = i0 + tid;
+      const int steps = i < a.n_shards ? (live_rows(i) + QA_KEYS - 1) / QA_KEYS : 0;
+      const int excl = wave_excl_scan(steps);
+      if (lane == 63) sums[wave] = excl + steps;
+      __syncthreads();
+      int at = total + excl;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        at += w < wave ? sums[w] : 0;
+        total += sums[w];
+      }
+      if (i < a.n_shards) before[i] = at;
+      __syncthreads();
+    }
+    list_steps = __builtin_amdgcn_readfirstlane(total);
+  }
+  const int gen_end = a.gen_rows == 0 ? 0 : a.mask != nullptr ? a.gen_rows : a.G + t0 + tokens;
+  const int total = list_steps + (gen_end + QA_GEN - 1) / QA_GEN;
+  const int per_part = (total + a.parts - 1) / a.parts;
+  const int step0 = __builtin_amdgcn_readfirstlane(part * per_part);
+  const int step1 = __builtin_amdgcn_readfirstlane(min(step0 + per_part, total));
+  const int nsteps = max(0, (step1 - step0 - wave + NW - 1) / NW);
+
+  // The rows at .. at + 31 of the generation shard that token `token` sees.
+  auto gen_sees = [&](int at, int token) -> uint32_t {
+    const int end = a.mask != nullptr ? a.gen_rows : a.G + token + 1;
+    const int rows = end - at;
+    if (rows <= 0) return 0u;
+    uint32_t sees = rows >= 32 ? 0xffffffffu : (1u << rows) - 1;
+    if (a.mask != nullptr && at + 32 > a.G) {
+      // drafts at - G .. are visible by the token's bits
+      const int words = (a.Tq + 31) / 32;
+      const uint32_t* bits = a.mask + (int64_t)token * words;
+      const int from = at - a.G;
+      uint64_t w;
+      if (from < 0) {
+        w = ((uint64_t)bits[0] << -from) | ((1u << -from) - 1);
+      } else {
+        const int i = from >> 5;
+        w = (bits[i] | (i + 1 < words ? (uint64_t)bits[i + 1] << 32 : 0)) >> (from & 31);
+      }
+      sees &= (uint32_t)w;
+    }
+    return sees;
+  };
+
+  // ---- where the steps lie: lane 4 i + h, half h of the wave's step base + i ---------
+  // Byte offset of the step's first row in K (or Kg), its rows, and what the half's
+  // scales come to: the factor of its scores, log2 vs and 1 / vs.
+  uint32_t tab_lo = 0, tab_hi = 0;
+  int tab_rows = 0;
+  float tab_ck = c2, tab_lv = 0.f, tab_iv = 1.f;
+  uint64_t nan_v = 0;  // halves whose vs is not a number
+  auto fill_rows = [&](int base) {
+    const int st = step0 + wave + NW * (base + (lane >> 2));
+    uint64_t off = 0;
+    tab_rows = 0;
+    int64_t scale_at = -1;
+    if (st < step1 && st < list_steps) {
+      int shard, first, end = a.S;
+      if (a.rows == nullptr) {
+        shard = st / a.shard_steps;
+        first = st - shard * a.shard_steps;
+      } else {
+        // the last shard with no more than st steps before it
+        int lo = 0, hi = a.n_shards;
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (before[mid] <= st) lo = mid;
+          else hi = mid;
+        }
+        shard = lo;
+        first = st - before[lo];
+        end = live_rows(shard);
+      }
+      const int row = first * QA_KEYS;
+      tab_rows = min(QA_KEYS, end - row);
+      const int64_t plane = (int64_t)shard * a.Hkv + kvh;
+      off = (uint64_t)(plane * a.S + row) * D;
+      scale_at = plane * a.blocks + ((row + min(16 * (lane & 3), tab_rows - 1)) >> a.block_log2);
+    } else if (st < step1) {
+      const int row = (st - list_steps) * QA_GEN;
+      tab_rows = min(QA_GEN, gen_end - row);
+      off = ((uint64_t)row * a.Hkv + kvh) * (2 * D);
+    }
+    tab_lo = (uint32_t)off;
+    tab_hi = (uint32_t)(off >> 32);
+    return scale_at;
+  };
+  auto fill_scales = [&](int64_t at) {
+    tab_ck = c2;
+    tab_lv = 0.f;
+    tab_iv = 1.f;
+    bool bad = false;
+    if (at >= 0) {
+      float k = a.ks[at], v = a.vs[at];
+      k = k < QA_LEAST ? QA_LEAST : k;
+      v = v < QA_LEAST ? QA_LEAST : v;
+      bad = v != v;
+      // (a factor of zero would make -inf a NaN)
+      k *= c2;
+      tab_ck = k < 0x1p-126f ? 0x1p-126f : k;
+      tab_lv = bad ? 0.f : __log2f(v);
+      tab_iv = bad ? 1.f : 1.f / v;
+    }
+    nan_v = __ballot(bad);
+  };
+  struct Step {
+    int64_t off;
+    int rows;
+    int st;
+  };
+  auto step_at = [&](int j) {
+    const int at = 4 * (j & 15);
+    return Step{(int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)tab_hi, at) << 32 |
+                          (uint32_t)__builtin_amdgcn_readlane((int)tab_lo, at)),
+                __builtin_amdgcn_readlane(tab_rows, at), step0 + wave + NW * j};
+  };
+  auto is_gen = [&](const Step& x) {
+    return __builtin_amdgcn_readfirstlane(x.st >= list_steps) != 0;
+  };
+  auto lane_f = [&](float x, int at) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), at));
+  };
+
+  // ---- loads of one step ------------------------------------------------------------
+  // Lane l of segment i fills the 16-byte chunk position (64 i + l) % CPR of row
+  // (64 i + l) / CPR with the chunk that its swizzle puts there: for K, so that 16 rows'
+  // chunks of one column lie in different banks; for V, so that the 16 bytes that a
+  // transposing read takes of each of 16 rows do.
+  auto k_swizzle = [](int row) { return CPR == 8 ? (row >> 1) & 7 : (row >> 2) & 3; };
+  auto v_swizzle = [](int row) {
+    return CPR == 8 ? ((row >> 1) & 3) | ((row >> 2) & 4) : ((row >> 2) & 1) | ((row >> 3) & 2);
+  };
+  auto gk_swizzle = [](int row) { return GCPR == 16 ? row & 15 : (row >> 1) & 7; };
+  auto gv_swizzle = [](int row) { return GCPR == 16 ? 2 * (row & 7) : 2 * ((row >> 1) & 3); };
+  lds_u8* const k_lds = (lds_u8*)smem + wave * 2 * L::STAGE;
+  lds_u8* const v_lds = k_lds + L::STAGE;
+  const uint32_t gen_row = (uint32_t)(a.Hkv * D * 2);
+  const uint32_t k_off = (lane / CPR) * D + ((lane % CPR) ^ k_swizzle(lane / CPR)) * 16;
+  const uint32_t v_off = (lane / CPR) * D + ((lane % CPR) ^ v_swizzle(lane / CPR)) * 16;
+  auto issue = [&](const Step& step, bool is_v) {
+    Step x = step;
+    x.off = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane(
+                          (int)(uint32_t)((uint64_t)step.off >> 32)) << 32 |
+                      (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)step.off));
+    x.rows = __builtin_amdgcn_readfirstlane(step.rows);
+    const uint32_t st =
+        __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(is_v ? v_lds : k_lds));
+    int l = lane;  // (computed anew at each step: kept, the offsets do not fit the registers)
+    if (!is_gen(x)) {
+      const uint8_t* base = (is_v ? a.V : a.K) + x.off;
+      const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<uint8_t*>(base), (short)0, x.rows * D, kBufferFlags);
+      if (x.rows == QA_KEYS) {
+        // the swizzles of rows 64 / CPR apart differ in one bit
+#pragma unroll
+        for (int i = 0; i < SEGS; ++i) {
+          constexpr int kRows = 64 / CPR;
+          const int flip = is_v ? v_swizzle(i * kRows & 31) : k_swizzle(i * kRows & 15);
+          lds_dma16(rsrc, (is_v ? v_off : k_off) ^ (16 * flip), i * 1024, st + i * 1024);
+        }
+      } else {
+        asm volatile("" : "+v"(l));
+#pragma unroll
+        for (int i = 0; i < SEGS; ++i) {
+          const int row = i * (64 / CPR) + l / CPR;
+          const int chunk = (l % CPR) ^ (is_v ? v_swizzle(row & 31) : k_swizzle(row & 15));
+          lds_dma16(rsrc, (uint32_t)(min(row, x.rows - 1) * D + chunk * 16), st + i * 1024);
+        }
+      }
+    } else {
+      const uint8_t* base = reinterpret_cast<const uint8_t*>(is_v ? a.Vg : a.Kg) + x.off;
+      const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<uint8_t*>(base), (short)0, (int)((x.rows - 1) * gen_row + 2 * D),
+          kBufferFlags);
+      asm volatile("" : "+v"(l));
+#pragma unroll
+      for (int i = 0; i < SEGS; ++i) {
+        const int row = i * (64 / GCPR) + l / GCPR;
+        const int chunk = (l % GCPR) ^ (is_v ? gv_swizzle(row & 15) : gk_swizzle(row & 15));
+        lds_dma16(rsrc, (uint32_t)min(row, x.rows - 1) * gen_row + chunk * 16, st + i * 1024);
+      }
+    }
+  };
+
+  // ---- operands out of LDS ------------------------------------------------------------
+  // K: channels D/4 * g .. of row r of a half; V^T: keys 16 h + 4 g + v (slot 4 h + v) of a
+  // 32-row tile, at head_dim 16 e + r.  A transposing read of 8 bits hands lane i of 16, for
+  // slot j, byte i % 8 of the eight that lane 2 j + i / 8 addressed.
+  auto k_codes = [&](int h, int i) -> u32x4 {  // 16 of them
+    const int chunk = (CPR == 8 ? 2 * g + i : g) ^ k_swizzle(r);
+    return *reinterpret_cast<const lds_u32x4*>(k_lds + (16 * h + r) * D + chunk * 16);
+  };
+  auto k_gen = [&](int h, int s) -> bf16x8 {
+    const int chunk = (DS * g + s) ^ gk_swizzle(r);
+    return *reinterpret_cast<const lds_bf16x8*>(k_lds + (16 * h + r) * (2 * D) + chunk * 16);
+  };
+  auto v_codes = [&](int u, int e) -> bf16x8 {
+    const int j = r >> 1, row = 16 * (j >> 2) + 4 * g + (j & 3);
+    const i32x2 x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+        (lds_i32x2*)(v_lds + (32 * u + row) * D + (e ^ v_swizzle(row)) * 16 + 8 * (r & 1)));
+    return widen<FORMAT>((uint32_t)x[0], (uint32_t)x[1]);
+  };
+  auto v_gen = [&](int e) -> bf16x8 {
+    const int row = 4 * g + (r >> 2), q4 = r & 3;
+    const lds_u8* at =
+        v_lds + row * (2 * D) + 16 * ((2 * e + (q4 >> 1)) ^ gv_swizzle(row)) + 8 * (q4 & 1);
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * (2 * D)));
+    return __builtin_bit_cast(bf16x8,
+                              (s16x8){lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+  };
+
+  f32x4 acc[CG][DT];
+  float m_run[CG], l_run[CG], lr_run[CG];
+#pragma unroll
+  for (int c = 0; c < CG; ++c) {
+#pragma unroll
+    for (int e = 0; e < DT; ++e) acc[c][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m_run[c] = -INFINITY;
+    l_run[c] = lr_run[c] = 0.f;
+  }
+  // Weights of H halves of scores S of group c, as PV takes them in.
+  auto weigh = [&](auto halves, int c, const f32x4* S, const float* ck, const float* lv,
+                   const float* iv, bf16x8* P) {
+    constexpr int H = decltype(halves)::value;
+    float mx = -INFINITY;
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+      mx = fmaxf(mx, fmaxf(fmaxf(S[h][0], S[h][1]), fmaxf(S[h][2], S[h][3])) * ck[h]);
+    mx = max_of_rows(mx);
+    if (__any(mx > m_run[c] + QA_SLACK)) {
+      const float m_new = mx > m_run[c] + QA_SLACK ? mx : m_run[c];
+      const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[c] - m_new);
+#pragma unroll
+      for (int e = 0; e < DT; ++e) acc[c][e] *= alpha;
+      l_run[c] *= alpha;
+      lr_run[c] *= alpha;
+      m_run[c] = m_new;
+    }
+    // a column that has seen no key takes its weights against 0: they come out 0
+    const float m_use = m_run[c] == -INFINITY ? 0.f : m_run[c];
+    f32x8 p[H / 2];
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      float sum = 0.f;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const float y =
+            __builtin_amdgcn_exp2f(__builtin_fmaf(S[h][v], ck[h], lv[h] - m_use));
+        p[h >> 1][4 * (h & 1) + v] = y;
+        sum += y;
+      }
+      l_run[c] = __builtin_fmaf(sum, iv[h], l_run[c]);
+    }
+#pragma unroll
+    for (int u = 0; u < H / 2; ++u) {
+      P[u] = __builtin_convertvector(p[u], bf16x8);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{P[u][4 * h], P[u][4 * h + 1]}, kOnes2,
+                                                    0.f, false);
+        sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{P[u][4 * h + 2], P[u][4 * h + 3]}, kOnes2,
+                                              sum, false);
+        lr_run[c] = __builtin_fmaf(sum, iv[2 * u + h], lr_run[c]);
+      }
+    }
+  };
+
+  Step next{};
+  int64_t scale_at = -1;
+  if (nsteps > 0) {
+    scale_at = fill_rows(0);
+    next = step_at(0);
+    issue(next, false);
+    issue(next, true);
+    fill_scales(scale_at);
+  }
+  for (int j = 0; j < nsteps; ++j) {
+    const Step now = next;
+    const bool more = j + 1 < nsteps;
+    const int at = 4 * (j & 15);
+    float ck[4], lv[4], iv[4];
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      ck[h] = lane_f(tab_ck, at + h);
+      lv[h] = lane_f(tab_lv, at + h);
+      iv[h] = lane_f(tab_iv, at + h);
+    }
+    const uint32_t bad_v = (uint32_t)(nan_v >> at) & 15u;
+    auto send_k = [&]() {
+      __builtin_amdgcn_sched_barrier(0);
+      if (more) {
+        const bool refill = ((j + 1) & 15) == 0;
+        if (refill) scale_at = fill_rows(j + 1);
+        next = step_at(j + 1);
+        issue(next, false);
+        if (refill) fill_scales(scale_at);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    // V(j) is in LDS once only K(j + 1)'s loads are outstanding
+    auto wait_v = [&](bool sent) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (sent && more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(SEGS) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    // K(j) is in LDS once only V(j)'s loads are outstanding
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(SEGS) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    if (!is_gen(now)) {
+#pragma unroll
+      for (int u = 0; u < 4; u += NH) {
+        f32x4 S[CG][NH];
+#pragma unroll
+        for (int h = 0; h < NH; ++h) {
+          if (CG > 1) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int c = 0; c < CG; ++c) S[c][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < DS / 2; ++i) {
+            const u32x4 w = k_codes(u + h, i);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+              const bf16x8 k = widen<FORMAT>(w[2 * s], w[2 * s + 1]);
+#pragma unroll
+              for (int c = 0; c < CG; ++c)
+                S[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[c][2 * i + s], S[c][h],
+                                                                  0, 0, 0);
+            }
+          }
+        }
+        if (u + NH == 4) send_k();
+        if (now.rows < 16 * (u + NH)) {
+#pragma unroll
+          for (int c = 0; c < CG; ++c)
+#pragma unroll
+            for (int h = 0; h < NH; ++h)
+#pragma unroll
+              for (int v = 0; v < 4; ++v)
+                if (16 * (u + h) + 4 * g + v >= now.rows) S[c][h][v] = -INFINITY;
+        }
+        bf16x8 P[CG][NH / 2];
+#pragma unroll
+        for (int c = 0; c < CG; ++c)
+          weigh(std::integral_constant<int, NH>{}, c, S[c], ck + u, lv + u, iv + u, P[c]);
+        if (bad_v != 0) {
+          // a block whose values are not numbers
+#pragma unroll
+          for (int c = 0; c < CG; ++c)
+#pragma unroll
+            for (int h = 0; h < NH; ++h)
+              if ((bad_v >> (u + h)) & 1) {
+#pragma unroll
+                for (int v = 0; v < 4; ++v) P[c][h >> 1][4 * (h & 1) + v] = (__bf16)__builtin_nanf("");
+              }
+        }
+        if (u == 0) wait_v(NH == 4);
+#pragma unroll
+        for (int i = 0; i < NH / 2; ++i)
+#pragma unroll
+          for (int e = 0; e < DT; ++e) {
+            if (CG > 1 && e % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+            const bf16x8 v = v_codes(u / 2 + i, e);
+#pragma unroll
+            for (int c = 0; c < CG; ++c)
+              acc[c][e] =
+                  __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P[c][i], acc[c][e], 0, 0, 0);
+          }
+      }
+    } else {
+      f32x4 S[CG][2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int c = 0; c < CG; ++c) S[c][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < DS; ++s) {
+          const bf16x8 k = k_gen(h, s);
+#pragma unroll
+          for (int c = 0; c < CG; ++c)
+            S[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[c][s], S[c][h], 0, 0, 0);
+        }
+      }
+      send_k();
+      const int row0 = (now.st - list_steps) * QA_GEN;
+      const bool some = row0 + QA_GEN > a.G;  // rows that only some columns see
+      uint32_t vis[CG];
+      bf16x8 P[CG][1];
+#pragma unroll
+      for (int c = 0; c < CG; ++c) {
+        vis[c] = some ? gen_sees(row0, t[c]) : 0xffffffffu;
+        if (some) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+              if (!((vis[c] >> (16 * h + 4 * g + v)) & 1)) S[c][h][v] = -INFINITY;
+        }
+        const float one[2] = {1.f, 1.f}, zero[2] = {0.f, 0.f}, cc[2] = {c2, c2};
+        weigh(std::integral_constant<int, 2>{}, c, S[c], cc, zero, one, P[c]);
+      }
+      wait_v(true);
+      bool odd = false;  // a value that is not finite
+      if (some) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < DT; ++e) {
+          const u32x4 v = __builtin_bit_cast(u32x4, v_gen(e));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            top |= (v[k] & 0x7f80u) == 0x7f80u;
+            top |= (v[k] & 0x7f800000u) == 0x7f800000u;
+          }
+        }
+        odd = __any(top != 0);
+      }
+      if (!odd) {
+#pragma unroll
+        for (int e = 0; e < DT; ++e) {
+          const bf16x8 v = v_gen(e);
+#pragma unroll
+          for (int c = 0; c < CG; ++c)
+            acc[c][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P[c][0], acc[c][e], 0, 0, 0);
+        }
+      } else {
+        for (int k = 0; k < QA_GEN; ++k) {
+          // key k sits in a slot of lane group (k % 16) / 4
+          const int slot = (k & 3) + (k >> 4) * 4;
+          u32x4 keep = {0u, 0u, 0u, 0u};
+          if (g == ((k >> 2) & 3)) {
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+              keep[x] = slot >> 1 == x ? (slot & 1 ? 0xffff0000u : 0xffffu) : 0u;
+          }
+#pragma unroll
+          for (int e = 0; e < DT; ++e) {
+            const bf16x8 v =
+                __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, v_gen(e)) & keep);
+#pragma unroll
+            for (int c = 0; c < CG; ++c) {
+              const f32x4 x =
+                  __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P[c][0], acc[c][e], 0, 0, 0);
+              if ((vis[c] >> k) & 1) acc[c][e] = x;
+            }
+          }
+        }
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) issue(next, true);
+  }
+
+  // ---- the waves' states, merged through LDS --------------------------------------
+  float* const states = reinterpret_cast<float*>(smem);
+  float* const sums = states + NW * 16 * L::PITCH;
+  constexpr int DL = D / 4;
+  const int dv = tid % DL;
+#pragma unroll
+  for (int c = 0; c < CG; ++c) {
+    l_run[c] += __shfl_xor(l_run[c], 16, 64);
+    l_run[c] += __shfl_xor(l_run[c], 32, 64);
+    lr_run[c] += __shfl_xor(lr_run[c], 16, 64);
+    lr_run[c] += __shfl_xor(lr_run[c], 32, 64);
+    __syncthreads();  // every wave is done with its stages, or the states before
+    {
+      float* const mine = states + (wave * 16 + r) * L::PITCH;
+#pragma unroll
+      for (int e = 0; e < DT; ++e) *reinterpret_cast<f32x4*>(mine + 16 * e + 4 * g) = acc[c][e];
+      if (g == 0) {
+        sums[(wave * 16 + r) * 3] = m_run[c];
+        sums[(wave * 16 + r) * 3 + 1] = l_run[c];
+        sums[(wave * 16 + r) * 3 + 2] = lr_run[c];
+      }
+    }
+    __syncthreads();
+    // thread -> (column, four consecutive values), a row of D / 4 threads at a time
+    for (int x = tid / DL; x < min(16, cols - 16 * c); x += 64 * NW / DL) {
+      float m = -INFINITY, l = 0.f, lr = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) m = fmaxf(m, sums[(w * 16 + x) * 3]);
+      const float use = m == -INFINITY ? 0.f : m;
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const float* y = sums + (w * 16 + x) * 3;
+        const float e = __builtin_amdgcn_exp2f(y[0] - use);
+        l += e * y[1];
+        lr += e * y[2];
+        o += e * *reinterpret_cast<const f32x4*>(states + (w * 16 + x) * L::PITCH + 4 * dv);
+      }
+      o *= lr != 0.f ? 1.f / lr : 0.f;  // (a NaN score leaves a NaN sum)
+      const int n = 16 * c + x, nth = a.col_tiles > 1 ? 0 : n / a.group;
+      const int hd = kvh * a.group + heads0 + n - nth * a.group;
+      const int64_t at = ((int64_t)part * a.Tq + t0 + nth) * a.Hq + hd;
+      if (a.o_bf16)
+        static_cast<bf16x4*>(a.O)[at * DL + dv] = __builtin_convertvector(o, bf16x4);
+      else
+        static_cast<f32x4*>(a.O)[at * DL + dv] = o;
+      if (dv == 0 && a.lse != nullptr)
+        a.lse[((int64_t)part * a.Hq + hd) * a.Tq + t0 + nth] =
+            l != 0.f ? (m + __log2f(l)) * 0.69314718055994531f : -INFINITY;
+    }
+  }
+}
+
+template <int D, int FORMAT, int NW, int CG>
+int launch_one(const QuantAttnArgs& a, hipStream_t stream) {
+  using L = QaLds<D, NW>;
+  const size_t lds = L::REUSED + (a.rows != nullptr ? L::STEPS : 0);
+  const int64_t tiles = (int64_t)a.token_tiles * a.col_tiles;
+  const int64_t nwg = ((int64_t)a.Hkv * a.parts * a.slices + 7) / 8 * 8 *
+                      ((tiles + a.slices - 1) / a.slices);
+  if (!grid_fits(nwg, 64 * NW)) return PULSAR_EUNSUPPORTED;
+  const auto kern = quant_attn_kernel<D, FORMAT, NW, CG>;
+  if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize,
+                          (int)lds) != hipSuccess)
+    return PULSAR_EHIP;
+  hipLaunchKernelGGL(kern, dim3((unsigned)nwg), dim3(64 * NW), lds, stream, a);
+  return hipGetLastError() == hipSuccess ? PULSAR_OK : PULSAR_EHIP;
+}
+
+template <int D, int FORMAT>
+int launch_groups(const QuantAttnArgs& a, hipStream_t stream) {
+  return launch_one<D, FORMAT, 4, 1>(a, stream);
+}
+
+// Workgroups that the chip holds at once: two on each compute unit.
+constexpr int QA_AT_ONCE = 512;
+
+}  // namespace
+
+QuantPlan quant_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int64_t gen_rows) {
+  QuantPlan p{};
+  const int group = Hq / Hkv;
+  p.groups = 1;
+  const int most = 16 * p.groups;
+  p.tokens = std::max(1, most / group);
+  const int64_t own = (int64_t)((Tq + p.tokens - 1) / p.tokens) * ((group + most - 1) / most);
+  const int64_t steps = (int64_t)n_shards * ((S + QA_KEYS - 1) / QA_KEYS) +
+                        (gen_rows + QA_GEN - 1) / QA_GEN;
+  p.parts = parts_at_once(std::min(QA_AT_ONCE / std::max<int64_t>(own * Hkv, 1), (steps + 3) / 4),
+                          Hkv, own, QA_AT_ONCE / 8);
+  return p;
+}
+
+// Rows of partials (tokens times parts) of any call of up to Tq tokens: parts are
+// QA_AT_ONCE / (tiles * Hkv) at most, of tiles that hold 64 columns at most.
+int64_t quant_part_rows_most(int Tq, int Hq, int Hkv) {
+  if (Tq <= 0) return 0;
+  const int64_t tokens = std::min(std::max(64 / (Hq / Hkv), 1), Tq);
+  return (int64_t)QA_AT_ONCE / Hkv * tokens;
+}
+
+int launch_quant_attn(const QuantAttnLaunch& x, const QuantPlan& p, void* o, int o_bf16,
+                      float* lse, hipStream_t stream) {
+  QuantAttnArgs a{};
+  a.q = x.q;
+  a.K = x.K;
+  a.V = x.V;
+  a.ks = x.ks;
+  a.vs = x.vs;
+  a.rows = x.n_shards > 0 ? x.rows : nullptr;
+  a.Kg = x.Kg;
+  a.Vg = x.Vg;
+  a.mask = x.mask;
+  a.Tq = x.Tq;
+  a.Hq = x.Hq;
+  a.Hkv = x.Hkv;
+  a.group = x.Hq / x.Hkv;
+  const int most = 16 * p.groups;
+  a.tile_tokens = p.tokens;
+  a.token_tiles = (x.Tq + p.tokens - 1) / p.tokens;
+  a.col_tiles = (a.group + most - 1) / most;
+  a.slices = tile_slices((int64_t)x.Hkv * p.parts, (int64_t)a.token_tiles * a.col_tiles);
+  a.n_shards = x.n_shards;
+  a.S = (int)x.S;
+  a.block_log2 = __builtin_ctz(x.block);
+  a.blocks = (int)((x.S + x.block - 1) >> a.block_log2);
+  a.gen_rows = x.Kg != nullptr ? (int)(x.G + x.Tq) : 0;
+  a.G = (int)x.G;
+  a.shard_steps = (int)((x.S + QA_KEYS - 1) / QA_KEYS);
+  a.parts = p.parts;
+  a.scale_log2 = x.scale * 1.4426950408889634f;
+  a.O = o;
+  a.o_bf16 = o_bf16;
+  a.lse = lse;
+  const bool e4m3 = x.format == PULSAR_KV_E4M3;
+  if (x.d == 128)
+    return e4m3 ? launch_groups<128, PULSAR_KV_E4M3>(a, stream)
+                : launch_groups<128, PULSAR_KV_INT8>(a, stream);
+  return e4m3 ? launch_groups<64, PULSAR_KV_E4M3>(a, stream)
+              : launch_groups<64, PULSAR_KV_INT8>(a, stream);
+}

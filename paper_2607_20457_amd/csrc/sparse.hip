@@ -677,24 +677,6 @@ int tiles_at_once(int d) { return d == 64 ? 1024 : 512; }
 
 int64_t steps_of(int64_t keys) { return (keys + SP_KEYS - 1) / SP_KEYS; }
 
-// XCDs over which the `tiles` of each of `units` (KV head, part) pairs are spread: few
-// pairs that are no multiple of eight, so that all XCDs are at work.
-int tile_slices(int64_t units, int64_t tiles) {
-  int slices = 1;
-  if (units < 32)
-    while (units * slices % 8 != 0 && slices * 2 <= tiles) slices *= 2;
-  return slices;
-}
-// The most parts, up to `parts`, whose workgroups an XCD holds at once.
-int parts_at_once(int64_t parts, int Hkv, int64_t tiles, int64_t held) {
-  while (parts > 1) {
-    const int slices = tile_slices(Hkv * parts, tiles);
-    if ((Hkv * parts * slices + 7) / 8 * ((tiles + slices - 1) / slices) <= held) break;
-    --parts;
-  }
-  return (int)std::max<int64_t>(parts, 1);
-}
-
 }  // namespace
 
 // Tokens whose lists one tile reads together, where their own tiles are more than a
