@@ -75,6 +75,17 @@ struct QaLds {
   static constexpr int STEPS = (QA_SHARDS + 1) * 4 + NW * 4;
 };
 
+// lds_dma16, its scalars possibly fresh from a vector instruction (a lane read, or a spilled
+// register taken back): five wait states lie between those and a load, which the compiler
+// does not count before asm.
+__device__ __forceinline__ void lds_load16(__amdgpu_buffer_rsrc_t rsrc, uint32_t voffset,
+                                           uint32_t soffset, uint32_t lds_base) {
+  asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
+               :
+               : "v"(voffset), "s"(rsrc), "s"(soffset), "{m0}"(lds_base)
+               : "memory");
+}
+
 // Eight codes (two dwords) as bf16, exactly.
 template <int FORMAT>
 __device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi) {
@@ -311,7 +322,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
         for (int i = 0; i < SEGS; ++i) {
           constexpr int kRows = 64 / CPR;
           const int flip = is_v ? v_swizzle(i * kRows & 31) : k_swizzle(i * kRows & 15);
-          lds_dma16(rsrc, (is_v ? v_off : k_off) ^ (16 * flip), i * 1024, st + i * 1024);
+          lds_load16(rsrc, (is_v ? v_off : k_off) ^ (16 * flip), i * 1024, st + i * 1024);
         }
       } else {
         asm volatile("" : "+v"(l));
@@ -319,7 +330,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
         for (int i = 0; i < SEGS; ++i) {
           const int row = i * (64 / CPR) + l / CPR;
           const int chunk = (l % CPR) ^ (is_v ? v_swizzle(row & 31) : k_swizzle(row & 15));
-          lds_dma16(rsrc, (uint32_t)(min(row, x.rows - 1) * D + chunk * 16), st + i * 1024);
+          lds_load16(rsrc, (uint32_t)(min(row, x.rows - 1) * D + chunk * 16), 0, st + i * 1024);
         }
       }
     } else {
@@ -332,7 +343,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
       for (int i = 0; i < SEGS; ++i) {
         const int row = i * (64 / GCPR) + l / GCPR;
         const int chunk = (l % GCPR) ^ (is_v ? gv_swizzle(row & 15) : gk_swizzle(row & 15));
-        lds_dma16(rsrc, (uint32_t)min(row, x.rows - 1) * gen_row + chunk * 16, st + i * 1024);
+        lds_load16(rsrc, (uint32_t)min(row, x.rows - 1) * gen_row + chunk * 16, 0, st + i * 1024);
       }
     }
   };

@@ -271,6 +271,17 @@ def test_attention_over_many_steps(Hq, Hkv, d, Tq, fmt):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("Hq,Hkv,d,Tq,n,S", [
+    (64, 64, 128, 1, 2, 6000),   # six steps of every wave, most of them whole
+    (64, 64, 64, 1, 1, 12000),
+    (128, 64, 128, 20, 1, 2100),  # several tiles of a head
+    (32, 32, 64, 128, 1, 8300),  # more than a wave's table holds at a time
+])
+def test_attention_of_full_waves(Hq, Hkv, d, Tq, n, S, fmt):
+    _attn(Hq, Hkv, d, Tq, 70, n, S, 64, fmt, 135, what="full waves")
+
+
+@pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("block", [16, 64, 256])
 def test_attention_over_live_rows(block, fmt):
     # lengths of zero, one, past the shard and negative; behind them codes and scales of
