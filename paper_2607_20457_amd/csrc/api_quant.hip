@@ -96,7 +96,7 @@ size_t pulsar_phase2_quant_call_bytes(int n_shards, int Tq, int64_t S, int64_t g
   if (n_shards < 0 || Tq < 1 || S < 0 || S > kMaxInt || gen_rows < 0 || Hq < 1 || Hkv < 1 ||
       Hq % Hkv != 0 || (d != 64 && d != 128))
     return 0;
-  const int parts = quant_plan(n_shards, Tq, S, Hq, Hkv, gen_rows).parts;
+  const int parts = quant_plan(n_shards, Tq, S, Hq, Hkv, d, gen_rows).parts;
   return parts == 1 ? 0 : (size_t)parts * Tq * Hq * (d + 1) * 4;
 }
 
@@ -147,7 +147,7 @@ int pulsar_phase2_quant(const void* q, const void* k_codes, const void* v_codes,
   a.G = G;
   a.scale = softmax_scale;
   const QuantPlan plan =
-      quant_plan(a.n_shards, Tq, a.S, Hq, Hkv, Kg != nullptr ? G + Tq : 0);
+      quant_plan(a.n_shards, Tq, a.S, Hq, Hkv, d, Kg != nullptr ? G + Tq : 0);
   const int parts = plan.parts;
   const bool bf16 = o_dtype == PULSAR_OUT_BF16;
   if (parts == 1) return launch_quant_attn(a, plan, o, bf16, lse, (hipStream_t)stream);

@@ -379,11 +379,11 @@ struct QuantAttnLaunch {
 };
 constexpr int kMaxQuantShards = 1024;  // with lengths of their own
 struct QuantPlan {
-  int groups;  // of 16 columns in a tile
-  int tokens;  // per tile
-  int parts;   // of a tile's keys
+  int columns;  // of a tile
+  int tokens;   // per tile
+  int parts;    // of a tile's keys
 };
-QuantPlan quant_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int64_t gen_rows);
+QuantPlan quant_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int d, int64_t gen_rows);
 int64_t quant_part_rows_most(int Tq, int Hq, int Hkv);
 int launch_quant_attn(const QuantAttnLaunch& a, const QuantPlan& plan, void* o, int o_bf16,
                       float* lse, hipStream_t stream);

@@ -1,8 +1,8 @@
 // Phase-2 attention of new tokens over shards held in 8 bits and over the generation
 // shard, which is bf16.
 //
-// Work.  A tile is 16, 32 or 64 columns of one KV head: column n is head n % group of
-// the tile's token n / group (or, of a larger group, 16 CG of one token's heads).  Its
+// Work.  A tile is 16 CG columns of one KV head: column n is head n % group of the
+// tile's token n / group (or, of a larger group, 16 CG of one token's heads).  Its
 // keys are steps of 64 rows of a shard, or of 32 rows of the generation shard: 64 D bytes
 // of K and of V either way.  A workgroup takes one part of a tile's steps, wave w of NW
 // the steps w, w + NW, ... of it on its own; then the waves' states are merged through
@@ -34,8 +34,6 @@
 
 namespace {
 
-constexpr int QA_KEYS = 64;           // codes' rows per step
-constexpr int QA_GEN = 32;            // generation shard's rows per step
 constexpr float QA_SLACK = 8.0f;      // log2 slack before the reference is raised
 constexpr float QA_LEAST = 0x1p-100f; // a smaller scale counts as this
 constexpr int QA_SHARDS = 1024;       // shards with lengths of their own
@@ -64,9 +62,9 @@ typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
 typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 
-template <int D, int NW>
+template <int D, int NW, int KEYS>
 struct QaLds {
-  static constexpr int STAGE = QA_KEYS * D;  // a K or V step
+  static constexpr int STAGE = KEYS * D;     // a K or V step
   static constexpr int LOOP = NW * 2 * STAGE;
   static constexpr int PITCH = D + 4;        // floats of a state's column
   static constexpr int MERGE = NW * 16 * (PITCH + 3) * 4;
@@ -78,12 +76,19 @@ struct QaLds {
 // lds_dma16, its scalars possibly fresh from a vector instruction (a lane read, or a spilled
 // register taken back): five wait states lie between those and a load, which the compiler
 // does not count before asm.
+template <bool ONCE = false>  // (of what nobody reads again: kept out of the way in the caches)
 __device__ __forceinline__ void lds_load16(__amdgpu_buffer_rsrc_t rsrc, uint32_t voffset,
                                            uint32_t soffset, uint32_t lds_base) {
-  asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
-               :
-               : "v"(voffset), "s"(rsrc), "s"(soffset), "{m0}"(lds_base)
-               : "memory");
+  if constexpr (ONCE)
+    asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %0, %1, %2 offen nt lds"
+                 :
+                 : "v"(voffset), "s"(rsrc), "s"(soffset), "{m0}"(lds_base)
+                 : "memory");
+  else
+    asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
+                 :
+                 : "v"(voffset), "s"(rsrc), "s"(soffset), "{m0}"(lds_base)
+                 : "memory");
 }
 
 // Eight codes (two dwords) as bf16, exactly.
@@ -106,17 +111,20 @@ __device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi) {
   }
 }
 
-template <int D, int FORMAT, int NW, int CG>
+template <int D, int FORMAT, int NW, int KEYS, int CG>
 __global__ __launch_bounds__(64 * NW)
-__attribute__((amdgpu_waves_per_eu(CG > 2 ? 1 : 2, CG > 2 ? 1 : 2)))
+__attribute__((amdgpu_waves_per_eu(NW / 2, NW / 2)))
 void quant_attn_kernel(QuantAttnArgs a) {
-  using L = QaLds<D, NW>;
+  using L = QaLds<D, NW, KEYS>;
+  constexpr int HALVES = KEYS / 16;       // of a step, 16 rows each
+  constexpr int GEN = KEYS / 2;           // rows of the generation shard per step
+  constexpr int AT_A_TIME = 64 / HALVES;  // steps that a table of one entry per lane holds
+  constexpr int COLS = 16 * CG;           // of a tile
   constexpr int CPR = D / 16;             // 16-byte chunks of a row of codes
   constexpr int GCPR = D / 8;             // of a bf16 row
   constexpr int DS = D / 32;              // k-steps of S
   constexpr int DT = D / 16;              // 16-row tiles of O^T
   constexpr int SEGS = L::STAGE / 1024;   // 1 KiB segments: one 16-byte load per lane each
-  constexpr int NH = CG == 1 ? 4 : 2;     // halves (of 16 keys) multiplied at a time
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -133,26 +141,10 @@ void quant_attn_kernel(QuantAttnArgs a) {
   if (wg >= (int64_t)a.Hkv * a.parts || tile >= tiles) return;
   const int kvh = (int)(wg % a.Hkv), part = (int)(wg / a.Hkv);
   const int t0 = tile % a.token_tiles * a.tile_tokens;
-  const int heads0 = tile / a.token_tiles * (16 * CG);
+  const int heads0 = tile / a.token_tiles * COLS;
   const int tokens = min(a.tile_tokens, a.Tq - t0);
-  const int cols = a.col_tiles > 1 ? min(16 * CG, a.group - heads0) : tokens * a.group;
+  const int cols = a.col_tiles > 1 ? min(COLS, a.group - heads0) : tokens * a.group;
   const float c2 = a.scale_log2;
-
-  // ---- Q fragments (B operand): column 16 c + r, channels D/4 * g + 8 s .. --------
-  int t[CG];
-  bf16x8 qf[CG][DS];
-#pragma unroll
-  for (int c = 0; c < CG; ++c) {
-    const int n = 16 * c + r;
-    const bool live = n < cols;
-    const int tl = live && a.col_tiles == 1 ? n / a.group : 0;
-    t[c] = t0 + tl;
-    const int head = kvh * a.group + heads0 + (live ? n - tl * a.group : 0);
-    const bf16x8* src =
-        reinterpret_cast<const bf16x8*>(a.q + ((int64_t)t[c] * a.Hq + head) * D) + DS * g;
-#pragma unroll
-    for (int s = 0; s < DS; ++s) qf[c][s] = live ? src[s] : bf16x8{};
-  }
 
   // ---- the tile's steps: those of the shards' live rows, then the generation shard's --
   int* const before = reinterpret_cast<int*>(smem + L::REUSED);  // [n_shards + 1]
@@ -163,7 +155,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
     int total = 0;
     for (int i0 = 0; i0 < a.n_shards; i0 += 64 * NW) {
       const int i = i0 + tid;
-      const int steps = i < a.n_shards ? (live_rows(i) + QA_KEYS - 1) / QA_KEYS : 0;
+      const int steps = i < a.n_shards ? (live_rows(i) + KEYS - 1) / KEYS : 0;
       const int excl = wave_excl_scan(steps);
       if (lane == 63) sums[wave] = excl + steps;
       __syncthreads();
@@ -179,19 +171,23 @@ void quant_attn_kernel(QuantAttnArgs a) {
     list_steps = __builtin_amdgcn_readfirstlane(total);
   }
   const int gen_end = a.gen_rows == 0 ? 0 : a.mask != nullptr ? a.gen_rows : a.G + t0 + tokens;
-  const int total = list_steps + (gen_end + QA_GEN - 1) / QA_GEN;
-  const int per_part = (total + a.parts - 1) / a.parts;
-  const int step0 = __builtin_amdgcn_readfirstlane(part * per_part);
-  const int step1 = __builtin_amdgcn_readfirstlane(min(step0 + per_part, total));
-  const int nsteps = max(0, (step1 - step0 - wave + NW - 1) / NW);
+  const int total = list_steps + (gen_end + GEN - 1) / GEN;
+  // (the first `more` parts take one step more than the others)
+  const int per_part = total / a.parts, more = total - per_part * a.parts;
+  const int step0 = __builtin_amdgcn_readfirstlane(part * per_part + min(part, more));
+  const int step1 = __builtin_amdgcn_readfirstlane(step0 + per_part + (part < more ? 1 : 0));
+  // Wave w takes the steps w, w + NW, ... of them, its last ones of the generation shard.
+  auto of_wave = [&](int steps) { return max(0, (steps - wave + NW - 1) / NW); };
+  const int nsteps = of_wave(step1 - step0);
+  const int code_steps = of_wave(min(step1, list_steps) - step0);
 
-  // The rows at .. at + 31 of the generation shard that token `token` sees.
+  // The rows at .. at + GEN - 1 of the generation shard that token `token` sees.
   auto gen_sees = [&](int at, int token) -> uint32_t {
     const int end = a.mask != nullptr ? a.gen_rows : a.G + token + 1;
     const int rows = end - at;
     if (rows <= 0) return 0u;
     uint32_t sees = rows >= 32 ? 0xffffffffu : (1u << rows) - 1;
-    if (a.mask != nullptr && at + 32 > a.G) {
+    if (a.mask != nullptr && at + GEN > a.G) {
       // drafts at - G .. are visible by the token's bits
       const int words = (a.Tq + 31) / 32;
       const uint32_t* bits = a.mask + (int64_t)token * words;
@@ -208,18 +204,15 @@ void quant_attn_kernel(QuantAttnArgs a) {
     return sees;
   };
 
-  // ---- where the steps lie: lane 4 i + h, half h of the wave's step base + i ---------
-  // Byte offset of the step's first row in K (or Kg), its rows, and what the half's
-  // scales come to: the factor of its scores, log2 vs and 1 / vs.
-  uint32_t tab_lo = 0, tab_hi = 0;
-  int tab_rows = 0;
-  float tab_ck = c2, tab_lv = 0.f, tab_iv = 1.f;
-  uint64_t nan_v = 0;  // halves whose vs is not a number
-  auto fill_rows = [&](int base) {
-    const int st = step0 + wave + NW * (base + (lane >> 2));
-    uint64_t off = 0;
-    tab_rows = 0;
-    int64_t scale_at = -1;
+  // ---- where the steps lie: lane HALVES i + h, half h of the wave's step base + i --
+  struct Place {
+    uint64_t off;  // of the step's first row in K (or Kg), in bytes
+    int rows;      // of the step
+    int64_t scale; // where the half's scales are, or -1
+  };
+  auto place = [&](int base) {
+    const int st = step0 + wave + NW * (base + lane / HALVES);
+    Place x{0, 0, -1};
     if (st < step1 && st < list_steps) {
       int shard, first, end = a.S;
       if (a.rows == nullptr) {
@@ -237,27 +230,39 @@ void quant_attn_kernel(QuantAttnArgs a) {
         first = st - before[lo];
         end = live_rows(shard);
       }
-      const int row = first * QA_KEYS;
-      tab_rows = min(QA_KEYS, end - row);
+      const int row = first * KEYS;
       const int64_t plane = (int64_t)shard * a.Hkv + kvh;
-      off = (uint64_t)(plane * a.S + row) * D;
-      scale_at = plane * a.blocks + ((row + min(16 * (lane & 3), tab_rows - 1)) >> a.block_log2);
+      x.rows = min(KEYS, end - row);
+      x.off = (uint64_t)(plane * a.S + row) * D;
+      x.scale = plane * a.blocks + ((row + min(16 * (lane % HALVES), x.rows - 1)) >> a.block_log2);
     } else if (st < step1) {
-      const int row = (st - list_steps) * QA_GEN;
-      tab_rows = min(QA_GEN, gen_end - row);
-      off = ((uint64_t)row * a.Hkv + kvh) * (2 * D);
+      const int row = (st - list_steps) * GEN;
+      x.rows = min(GEN, gen_end - row);
+      x.off = ((uint64_t)row * a.Hkv + kvh) * (2 * D);
     }
-    tab_lo = (uint32_t)off;
-    tab_hi = (uint32_t)(off >> 32);
-    return scale_at;
+    return x;
   };
-  auto fill_scales = [&](int64_t at) {
+  // What is needed to send for a step ...
+  uint32_t tab_lo = 0, tab_hi = 0;
+  int tab_send = 0;
+  auto fill_send = [&](const Place& x) {
+    tab_lo = (uint32_t)x.off;
+    tab_hi = (uint32_t)(x.off >> 32);
+    tab_send = x.rows;
+  };
+  // ... and to multiply it: its rows and what the half's scales come to, the factor of its
+  // scores, log2 vs and 1 / vs.
+  int tab_rows = 0;
+  float tab_ck = c2, tab_lv = 0.f, tab_iv = 1.f;
+  uint64_t nan_v = 0;  // halves whose vs is not a number
+  auto fill_use = [&](const Place& x) {
+    tab_rows = x.rows;
     tab_ck = c2;
     tab_lv = 0.f;
     tab_iv = 1.f;
     bool bad = false;
-    if (at >= 0) {
-      float k = a.ks[at], v = a.vs[at];
+    if (x.scale >= 0) {
+      float k = a.ks[x.scale], v = a.vs[x.scale];
       k = k < QA_LEAST ? QA_LEAST : k;
       v = v < QA_LEAST ? QA_LEAST : v;
       bad = v != v;
@@ -268,20 +273,6 @@ void quant_attn_kernel(QuantAttnArgs a) {
       tab_iv = bad ? 1.f : 1.f / v;
     }
     nan_v = __ballot(bad);
-  };
-  struct Step {
-    int64_t off;
-    int rows;
-    int st;
-  };
-  auto step_at = [&](int j) {
-    const int at = 4 * (j & 15);
-    return Step{(int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)tab_hi, at) << 32 |
-                          (uint32_t)__builtin_amdgcn_readlane((int)tab_lo, at)),
-                __builtin_amdgcn_readlane(tab_rows, at), step0 + wave + NW * j};
-  };
-  auto is_gen = [&](const Step& x) {
-    return __builtin_amdgcn_readfirstlane(x.st >= list_steps) != 0;
   };
   auto lane_f = [&](float x, int at) {
     return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), at));
@@ -301,49 +292,59 @@ void quant_attn_kernel(QuantAttnArgs a) {
   lds_u8* const k_lds = (lds_u8*)smem + wave * 2 * L::STAGE;
   lds_u8* const v_lds = k_lds + L::STAGE;
   const uint32_t gen_row = (uint32_t)(a.Hkv * D * 2);
+  // byte offsets of a lane from a whole step's segment 0
   const uint32_t k_off = (lane / CPR) * D + ((lane % CPR) ^ k_swizzle(lane / CPR)) * 16;
   const uint32_t v_off = (lane / CPR) * D + ((lane % CPR) ^ v_swizzle(lane / CPR)) * 16;
-  auto issue = [&](const Step& step, bool is_v) {
-    Step x = step;
-    x.off = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane(
-                          (int)(uint32_t)((uint64_t)step.off >> 32)) << 32 |
-                      (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)step.off));
-    x.rows = __builtin_amdgcn_readfirstlane(step.rows);
-    const uint32_t st =
-        __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(is_v ? v_lds : k_lds));
+  // K (or V) of the wave's step j into its stage.
+  auto send = [&](int j, bool is_v) {
+    const int at = HALVES * (j % AT_A_TIME);
+    const uint32_t off_lo = (uint32_t)__builtin_amdgcn_readlane((int)tab_lo, at);
+    const uint32_t off_hi = (uint32_t)__builtin_amdgcn_readlane((int)tab_hi, at);
+    const int rows = __builtin_amdgcn_readlane(tab_send, at);
+    const int64_t off = (int64_t)((uint64_t)off_hi << 32 | off_lo);
+    const uint32_t st = __builtin_amdgcn_readfirstlane(
+        (uint32_t)(uintptr_t)(is_v ? v_lds : k_lds));
     int l = lane;  // (computed anew at each step: kept, the offsets do not fit the registers)
-    if (!is_gen(x)) {
-      const uint8_t* base = (is_v ? a.V : a.K) + x.off;
+    if (__builtin_amdgcn_readfirstlane(step0 + wave + NW * j < list_steps)) {
+      const uint8_t* base = (is_v ? a.V : a.K) + off;
       const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
-          const_cast<uint8_t*>(base), (short)0, x.rows * D, kBufferFlags);
-      if (x.rows == QA_KEYS) {
-        // the swizzles of rows 64 / CPR apart differ in one bit
+          const_cast<uint8_t*>(base), (short)0, rows * D, kBufferFlags);
+      constexpr int kRows = 64 / CPR;
+      // a whole step: the swizzles of rows 64 / CPR apart differ in one bit
+      auto whole = [&](auto once) {
 #pragma unroll
         for (int i = 0; i < SEGS; ++i) {
-          constexpr int kRows = 64 / CPR;
-          const int flip = is_v ? v_swizzle(i * kRows & 31) : k_swizzle(i * kRows & 15);
-          lds_load16(rsrc, (is_v ? v_off : k_off) ^ (16 * flip), i * 1024, st + i * 1024);
+          const int row = i * kRows;
+          const uint32_t flip = 16 * (is_v ? v_swizzle(row & 31) : k_swizzle(row & 15));
+          lds_load16<decltype(once)::value>(rsrc, (is_v ? v_off : k_off) ^ flip, i * 1024,
+                                            st + i * 1024);
         }
+      };
+      if (rows == KEYS && tiles == 1) {
+        whole(std::true_type{});
+      } else if (rows == KEYS) {
+        whole(std::false_type{});
       } else {
         asm volatile("" : "+v"(l));
 #pragma unroll
         for (int i = 0; i < SEGS; ++i) {
-          const int row = i * (64 / CPR) + l / CPR;
+          const int row = i * kRows + l / CPR;
           const int chunk = (l % CPR) ^ (is_v ? v_swizzle(row & 31) : k_swizzle(row & 15));
-          lds_load16(rsrc, (uint32_t)(min(row, x.rows - 1) * D + chunk * 16), 0, st + i * 1024);
+          lds_load16(rsrc, (uint32_t)(min(row, rows - 1) * D + chunk * 16), 0,
+                     st + i * 1024);
         }
       }
     } else {
-      const uint8_t* base = reinterpret_cast<const uint8_t*>(is_v ? a.Vg : a.Kg) + x.off;
+      const uint8_t* base = reinterpret_cast<const uint8_t*>(is_v ? a.Vg : a.Kg) + off;
       const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
-          const_cast<uint8_t*>(base), (short)0, (int)((x.rows - 1) * gen_row + 2 * D),
-          kBufferFlags);
+          const_cast<uint8_t*>(base), (short)0, (int)((rows - 1) * gen_row + 2 * D), kBufferFlags);
       asm volatile("" : "+v"(l));
 #pragma unroll
       for (int i = 0; i < SEGS; ++i) {
         const int row = i * (64 / GCPR) + l / GCPR;
         const int chunk = (l % GCPR) ^ (is_v ? gv_swizzle(row & 15) : gk_swizzle(row & 15));
-        lds_load16(rsrc, (uint32_t)min(row, x.rows - 1) * gen_row + chunk * 16, 0, st + i * 1024);
+        lds_load16(rsrc, (uint32_t)min(row, rows - 1) * gen_row + chunk * 16, 0,
+                   st + i * 1024);
       }
     }
   };
@@ -352,26 +353,36 @@ void quant_attn_kernel(QuantAttnArgs a) {
   // K: channels D/4 * g .. of row r of a half; V^T: keys 16 h + 4 g + v (slot 4 h + v) of a
   // 32-row tile, at head_dim 16 e + r.  A transposing read of 8 bits hands lane i of 16, for
   // slot j, byte i % 8 of the eight that lane 2 j + i / 8 addressed.
-  auto k_codes = [&](int h, int i) -> u32x4 {  // 16 of them
-    const int chunk = (CPR == 8 ? 2 * g + i : g) ^ k_swizzle(r);
-    return *reinterpret_cast<const lds_u32x4*>(k_lds + (16 * h + r) * D + chunk * 16);
+  // (Their addresses are computed anew from `at`, a lane's number that the compiler does not
+  // know to be the same in each step: kept, they do not fit the registers.)
+  auto fresh_lane = [&]() {
+    int l = lane;
+    asm volatile("" : "+v"(l));
+    return l;
   };
-  auto k_gen = [&](int h, int s) -> bf16x8 {
-    const int chunk = (DS * g + s) ^ gk_swizzle(r);
-    return *reinterpret_cast<const lds_bf16x8*>(k_lds + (16 * h + r) * (2 * D) + chunk * 16);
+  auto k_codes = [&](int at, int h, int i) -> u32x4 {  // 16 of them
+    const int row = at & 15, chunk = (CPR == 8 ? 2 * (at >> 4) + i : at >> 4) ^ k_swizzle(row);
+    return *reinterpret_cast<const lds_u32x4*>(k_lds + row * D + chunk * 16 + 16 * h * D);
   };
-  auto v_codes = [&](int u, int e) -> bf16x8 {
-    const int j = r >> 1, row = 16 * (j >> 2) + 4 * g + (j & 3);
+  auto k_gen = [&](int at, int h, int s) -> bf16x8 {
+    const int row = at & 15, chunk = (DS * (at >> 4) + s) ^ gk_swizzle(row);
+    return *reinterpret_cast<const lds_bf16x8*>(k_lds + row * (2 * D) + chunk * 16 +
+                                                16 * h * (2 * D));
+  };
+  auto v_codes = [&](int at, int u, int e) -> bf16x8 {
+    const int j = (at >> 1) & 7, row = 16 * (j >> 2) + 4 * (at >> 4) + (j & 3);
     const i32x2 x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-        (lds_i32x2*)(v_lds + (32 * u + row) * D + (e ^ v_swizzle(row)) * 16 + 8 * (r & 1)));
+        (lds_i32x2*)(v_lds + row * D + (e ^ v_swizzle(row)) * 16 + 8 * (at & 1) + 32 * u * D));
     return widen<FORMAT>((uint32_t)x[0], (uint32_t)x[1]);
   };
-  auto v_gen = [&](int e) -> bf16x8 {
-    const int row = 4 * g + (r >> 2), q4 = r & 3;
-    const lds_u8* at =
+  auto v_gen = [&](int at, int e) -> bf16x8 {
+    const int row = 4 * (at >> 4) + ((at >> 2) & 3), q4 = at & 3;
+    const lds_u8* from =
         v_lds + row * (2 * D) + 16 * ((2 * e + (q4 >> 1)) ^ gv_swizzle(row)) + 8 * (q4 & 1);
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * (2 * D)));
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)from);
+    const s16x4 hi =
+        GEN == 32 ? __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(from + 16 * (2 * D)))
+                  : s16x4{0, 0, 0, 0};
     return __builtin_bit_cast(bf16x8,
                               (s16x8){lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
   };
@@ -385,17 +396,17 @@ void quant_attn_kernel(QuantAttnArgs a) {
     m_run[c] = -INFINITY;
     l_run[c] = lr_run[c] = 0.f;
   }
-  // Weights of H halves of scores S of group c, as PV takes them in.
-  auto weigh = [&](auto halves, int c, const f32x4* S, const float* ck, const float* lv,
-                   const float* iv, bf16x8* P) {
-    constexpr int H = decltype(halves)::value;
-    float mx = -INFINITY;
+  // The reference of every group against mx, the largest of a lane's scores of it: raised
+  // where it has to be, O and the sums rescaled.
+  auto raise = [&](const float* mx) {
+    bool any = false;
 #pragma unroll
-    for (int h = 0; h < H; ++h)
-      mx = fmaxf(mx, fmaxf(fmaxf(S[h][0], S[h][1]), fmaxf(S[h][2], S[h][3])) * ck[h]);
-    mx = max_of_rows(mx);
-    if (__any(mx > m_run[c] + QA_SLACK)) {
-      const float m_new = mx > m_run[c] + QA_SLACK ? mx : m_run[c];
+    for (int c = 0; c < CG; ++c) any |= mx[c] > m_run[c] + QA_SLACK;
+    if (!__any(any)) return;
+#pragma unroll
+    for (int c = 0; c < CG; ++c) {
+      const float top = max_of_rows(mx[c]);
+      const float m_new = top > m_run[c] + QA_SLACK ? top : m_run[c];
       const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[c] - m_new);
 #pragma unroll
       for (int e = 0; e < DT; ++e) acc[c][e] *= alpha;
@@ -403,218 +414,243 @@ void quant_attn_kernel(QuantAttnArgs a) {
       lr_run[c] *= alpha;
       m_run[c] = m_new;
     }
+  };
+  // Weights of two halves of group c as PV takes them in, and their sums.
+  auto weigh = [&](int c, const f32x4* S, const float* ck, const float* lv, const float* iv) {
     // a column that has seen no key takes its weights against 0: they come out 0
     const float m_use = m_run[c] == -INFINITY ? 0.f : m_run[c];
-    f32x8 p[H / 2];
+    f32x8 p;
 #pragma unroll
-    for (int h = 0; h < H; ++h) {
-      float sum = 0.f;
+    for (int h = 0; h < 2; ++h) {
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const float y =
-            __builtin_amdgcn_exp2f(__builtin_fmaf(S[h][v], ck[h], lv[h] - m_use));
-        p[h >> 1][4 * (h & 1) + v] = y;
-        sum += y;
-      }
+      for (int v = 0; v < 4; ++v)
+        p[4 * h + v] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[h][v], ck[h], lv[h] - m_use));
+      const float sum = (p[4 * h] + p[4 * h + 1]) + (p[4 * h + 2] + p[4 * h + 3]);
       l_run[c] = __builtin_fmaf(sum, iv[h], l_run[c]);
     }
+    const bf16x8 P = __builtin_convertvector(p, bf16x8);
 #pragma unroll
-    for (int u = 0; u < H / 2; ++u) {
-      P[u] = __builtin_convertvector(p[u], bf16x8);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{P[u][4 * h], P[u][4 * h + 1]}, kOnes2,
-                                                    0.f, false);
-        sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{P[u][4 * h + 2], P[u][4 * h + 3]}, kOnes2,
-                                              sum, false);
-        lr_run[c] = __builtin_fmaf(sum, iv[2 * u + h], lr_run[c]);
-      }
+    for (int h = 0; h < 2; ++h) {
+      float sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{P[4 * h], P[4 * h + 1]}, kOnes2, 0.f,
+                                                  false);
+      sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{P[4 * h + 2], P[4 * h + 3]}, kOnes2, sum,
+                                            false);
+      lr_run[c] = __builtin_fmaf(sum, iv[h], lr_run[c]);
     }
+    return P;
+  };
+  auto largest = [](f32x4 x) { return fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])); };
+
+  const Place first = place(0);
+  fill_send(first);
+  if (nsteps > 0) {
+    send(0, false);
+    send(0, true);
+  }
+
+  // ---- Q fragments (B operand): column 16 c + r, channels D/4 * g + 8 s .. ----
+  int t[CG];
+  bf16x8 qf[CG][DS];
+  {
+#pragma unroll
+    for (int c = 0; c < CG; ++c) {
+      const int n = 16 * c + r;
+      const bool live = n < cols;
+      const int tl = live && a.col_tiles == 1 ? n / a.group : 0;
+      t[c] = t0 + tl;
+      const int head = kvh * a.group + heads0 + (live ? n - tl * a.group : 0);
+      const bf16x8* src =
+          reinterpret_cast<const bf16x8*>(a.q + ((int64_t)t[c] * a.Hq + head) * D) + DS * g;
+#pragma unroll
+      for (int s = 0; s < DS; ++s) qf[c][s] = live ? src[s] : bf16x8{};
+    }
+  }
+  fill_use(first);
+
+  // A wave has one stage: K of step j + 1 is sent for once the scores have consumed this
+  // one's, its V once PV has.
+  auto need_k = [&]() {
+    // K(j) is in LDS once only V(j)'s loads are outstanding
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(SEGS) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto scored = [&](int j) {
+    __builtin_amdgcn_sched_barrier(0);
+    if (j + 1 < nsteps) {
+      if ((j + 1) % AT_A_TIME == 0) fill_send(place(j + 1));
+      send(j + 1, false);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // V(j) is in LDS once only K(j + 1)'s loads are outstanding, if these have been sent for
+  auto need_v = [&](bool sent) {
+    __builtin_amdgcn_sched_barrier(0);
+    if (sent) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(SEGS) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto done = [&](int j) {
+    __builtin_amdgcn_sched_barrier(0);
+    if (j + 1 < nsteps) send(j + 1, true);
   };
 
-  Step next{};
-  int64_t scale_at = -1;
-  if (nsteps > 0) {
-    scale_at = fill_rows(0);
-    next = step_at(0);
-    issue(next, false);
-    issue(next, true);
-    fill_scales(scale_at);
-  }
-  for (int j = 0; j < nsteps; ++j) {
-    const Step now = next;
-    const bool more = j + 1 < nsteps;
-    const int at = 4 * (j & 15);
-    float ck[4], lv[4], iv[4];
+  // ---- the wave's steps of codes ----------------------------------------------------
+  int j = 0;
+  for (; j < code_steps; ++j) {
+    if (j > 0 && j % AT_A_TIME == 0) fill_use(place(j));
+    const int at = HALVES * (j % AT_A_TIME);
+    const int rows = __builtin_amdgcn_readlane(tab_rows, at);
+    float ck[HALVES], lv[HALVES], iv[HALVES];
 #pragma unroll
-    for (int h = 0; h < 4; ++h) {
+    for (int h = 0; h < HALVES; ++h) {
       ck[h] = lane_f(tab_ck, at + h);
       lv[h] = lane_f(tab_lv, at + h);
       iv[h] = lane_f(tab_iv, at + h);
     }
-    const uint32_t bad_v = (uint32_t)(nan_v >> at) & 15u;
-    auto send_k = [&]() {
-      __builtin_amdgcn_sched_barrier(0);
-      if (more) {
-        const bool refill = ((j + 1) & 15) == 0;
-        if (refill) scale_at = fill_rows(j + 1);
-        next = step_at(j + 1);
-        issue(next, false);
-        if (refill) fill_scales(scale_at);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    };
-    // V(j) is in LDS once only K(j + 1)'s loads are outstanding
-    auto wait_v = [&](bool sent) {
-      __builtin_amdgcn_sched_barrier(0);
-      if (sent && more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(SEGS) : "memory");
-      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __builtin_amdgcn_sched_barrier(0);
-    };
-    // K(j) is in LDS once only V(j)'s loads are outstanding
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(SEGS) : "memory");
-    __builtin_amdgcn_sched_barrier(0);
-    if (!is_gen(now)) {
+    const uint32_t bad_v = (uint32_t)(nan_v >> at) & ((1u << HALVES) - 1);
+    need_k();
+    f32x4 S[CG][HALVES];
 #pragma unroll
-      for (int u = 0; u < 4; u += NH) {
-        f32x4 S[CG][NH];
+    for (int h = 0; h < HALVES; ++h) {
 #pragma unroll
-        for (int h = 0; h < NH; ++h) {
-          if (CG > 1) __builtin_amdgcn_sched_barrier(0);
+      for (int c = 0; c < CG; ++c) S[c][h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int c = 0; c < CG; ++c) S[c][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < DS / 2; ++i) {
+        const u32x4 w = k_codes(lane, h, i);
 #pragma unroll
-          for (int i = 0; i < DS / 2; ++i) {
-            const u32x4 w = k_codes(u + h, i);
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-              const bf16x8 k = widen<FORMAT>(w[2 * s], w[2 * s + 1]);
-#pragma unroll
-              for (int c = 0; c < CG; ++c)
-                S[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[c][2 * i + s], S[c][h],
-                                                                  0, 0, 0);
-            }
-          }
-        }
-        if (u + NH == 4) send_k();
-        if (now.rows < 16 * (u + NH)) {
+        for (int s = 0; s < 2; ++s) {
+          const bf16x8 k = widen<FORMAT>(w[2 * s], w[2 * s + 1]);
 #pragma unroll
           for (int c = 0; c < CG; ++c)
-#pragma unroll
-            for (int h = 0; h < NH; ++h)
-#pragma unroll
-              for (int v = 0; v < 4; ++v)
-                if (16 * (u + h) + 4 * g + v >= now.rows) S[c][h][v] = -INFINITY;
-        }
-        bf16x8 P[CG][NH / 2];
-#pragma unroll
-        for (int c = 0; c < CG; ++c)
-          weigh(std::integral_constant<int, NH>{}, c, S[c], ck + u, lv + u, iv + u, P[c]);
-        if (bad_v != 0) {
-          // a block whose values are not numbers
-#pragma unroll
-          for (int c = 0; c < CG; ++c)
-#pragma unroll
-            for (int h = 0; h < NH; ++h)
-              if ((bad_v >> (u + h)) & 1) {
-#pragma unroll
-                for (int v = 0; v < 4; ++v) P[c][h >> 1][4 * (h & 1) + v] = (__bf16)__builtin_nanf("");
-              }
-        }
-        if (u == 0) wait_v(NH == 4);
-#pragma unroll
-        for (int i = 0; i < NH / 2; ++i)
-#pragma unroll
-          for (int e = 0; e < DT; ++e) {
-            if (CG > 1 && e % 2 == 0) __builtin_amdgcn_sched_barrier(0);
-            const bf16x8 v = v_codes(u / 2 + i, e);
-#pragma unroll
-            for (int c = 0; c < CG; ++c)
-              acc[c][e] =
-                  __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P[c][i], acc[c][e], 0, 0, 0);
-          }
-      }
-    } else {
-      f32x4 S[CG][2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int c = 0; c < CG; ++c) S[c][h] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int s = 0; s < DS; ++s) {
-          const bf16x8 k = k_gen(h, s);
-#pragma unroll
-          for (int c = 0; c < CG; ++c)
-            S[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[c][s], S[c][h], 0, 0, 0);
-        }
-      }
-      send_k();
-      const int row0 = (now.st - list_steps) * QA_GEN;
-      const bool some = row0 + QA_GEN > a.G;  // rows that only some columns see
-      uint32_t vis[CG];
-      bf16x8 P[CG][1];
-#pragma unroll
-      for (int c = 0; c < CG; ++c) {
-        vis[c] = some ? gen_sees(row0, t[c]) : 0xffffffffu;
-        if (some) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int v = 0; v < 4; ++v)
-              if (!((vis[c] >> (16 * h + 4 * g + v)) & 1)) S[c][h][v] = -INFINITY;
-        }
-        const float one[2] = {1.f, 1.f}, zero[2] = {0.f, 0.f}, cc[2] = {c2, c2};
-        weigh(std::integral_constant<int, 2>{}, c, S[c], cc, zero, one, P[c]);
-      }
-      wait_v(true);
-      bool odd = false;  // a value that is not finite
-      if (some) {
-        uint32_t top = 0;
-#pragma unroll
-        for (int e = 0; e < DT; ++e) {
-          const u32x4 v = __builtin_bit_cast(u32x4, v_gen(e));
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            top |= (v[k] & 0x7f80u) == 0x7f80u;
-            top |= (v[k] & 0x7f800000u) == 0x7f800000u;
-          }
-        }
-        odd = __any(top != 0);
-      }
-      if (!odd) {
-#pragma unroll
-        for (int e = 0; e < DT; ++e) {
-          const bf16x8 v = v_gen(e);
-#pragma unroll
-          for (int c = 0; c < CG; ++c)
-            acc[c][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P[c][0], acc[c][e], 0, 0, 0);
-        }
-      } else {
-        for (int k = 0; k < QA_GEN; ++k) {
-          // key k sits in a slot of lane group (k % 16) / 4
-          const int slot = (k & 3) + (k >> 4) * 4;
-          u32x4 keep = {0u, 0u, 0u, 0u};
-          if (g == ((k >> 2) & 3)) {
-#pragma unroll
-            for (int x = 0; x < 4; ++x)
-              keep[x] = slot >> 1 == x ? (slot & 1 ? 0xffff0000u : 0xffffu) : 0u;
-          }
-#pragma unroll
-          for (int e = 0; e < DT; ++e) {
-            const bf16x8 v =
-                __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, v_gen(e)) & keep);
-#pragma unroll
-            for (int c = 0; c < CG; ++c) {
-              const f32x4 x =
-                  __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P[c][0], acc[c][e], 0, 0, 0);
-              if ((vis[c] >> k) & 1) acc[c][e] = x;
-            }
-          }
+            S[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[c][2 * i + s], S[c][h], 0, 0,
+                                                              0);
         }
       }
     }
-    __builtin_amdgcn_sched_barrier(0);
-    if (more) issue(next, true);
+    scored(j);
+    if (rows < KEYS) {
+#pragma unroll
+      for (int c = 0; c < CG; ++c)
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+            if (16 * h + 4 * g + v >= rows) S[c][h][v] = -INFINITY;
+    }
+    float mx[CG];
+#pragma unroll
+    for (int c = 0; c < CG; ++c) {
+      mx[c] = -INFINITY;
+#pragma unroll
+      for (int h = 0; h < HALVES; ++h) mx[c] = fmaxf(mx[c], largest(S[c][h]) * ck[h]);
+    }
+    raise(mx);
+    need_v(j + 1 < nsteps);
+#pragma unroll
+    for (int u = 0; u < HALVES / 2; ++u) {
+      const int h = 2 * u;
+      bf16x8 P[CG];
+#pragma unroll
+      for (int c = 0; c < CG; ++c) P[c] = weigh(c, S[c] + h, ck + h, lv + h, iv + h);
+#pragma unroll
+      for (int e = 0; e < DT; ++e) {
+        const bf16x8 v = v_codes(lane, u, e);
+#pragma unroll
+        for (int c = 0; c < CG; ++c)
+          acc[c][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P[c], acc[c][e], 0, 0, 0);
+      }
+    }
+    if (bad_v != 0) {
+      // values that are not numbers, in blocks that every column sees
+#pragma unroll
+      for (int c = 0; c < CG; ++c)
+#pragma unroll
+        for (int e = 0; e < DT; ++e) acc[c][e] = f32x4{} + __builtin_nanf("");
+    }
+    done(j);
+  }
+
+  // ---- those of the generation shard --------------------------------------------------
+  for (; j < nsteps; ++j) {
+    const int st = step0 + wave + NW * j;
+    const int row0 = (st - list_steps) * GEN;
+    const int la = fresh_lane();
+    need_k();
+    f32x4 S[CG][2];
+#pragma unroll
+    for (int c = 0; c < CG; ++c)
+      S[c][0] = f32x4{0.f, 0.f, 0.f, 0.f},
+      S[c][1] = f32x4{} + (GEN == 32 ? 0.f : -INFINITY);
+#pragma unroll
+    for (int h = 0; h < GEN / 16; ++h)
+#pragma unroll
+      for (int s = 0; s < DS; ++s) {
+        const bf16x8 k = k_gen(la, h, s);
+#pragma unroll
+        for (int c = 0; c < CG; ++c)
+          S[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[c][s], S[c][h], 0, 0, 0);
+      }
+    scored(j);
+    const bool some = row0 + GEN > a.G;  // rows that only some columns see
+    uint32_t vis[CG];
+    float mx[CG];
+#pragma unroll
+    for (int c = 0; c < CG; ++c) {
+      vis[c] = some ? gen_sees(row0, t[c]) : 0xffffffffu;
+      if (some) {
+#pragma unroll
+        for (int h = 0; h < GEN / 16; ++h)
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+            if (!((vis[c] >> (16 * h + 4 * g + v)) & 1)) S[c][h][v] = -INFINITY;
+      }
+      mx[c] = fmaxf(largest(S[c][0]), largest(S[c][1])) * c2;
+    }
+    raise(mx);
+    bf16x8 P[CG];
+#pragma unroll
+    for (int c = 0; c < CG; ++c) {
+      const float one[2] = {1.f, 1.f}, zero[2] = {0.f, 0.f}, cc[2] = {c2, c2};
+      P[c] = weigh(c, S[c], cc, zero, one);
+    }
+    need_v(j + 1 < nsteps);
+    bool odd = false;  // a value that is not finite
+    if (some) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int e = 0; e < DT; ++e) {
+        const u32x4 v = __builtin_bit_cast(u32x4, v_gen(la, e));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          top |= (v[k] & 0x7f80u) == 0x7f80u;
+          top |= (v[k] & 0x7f800000u) == 0x7f800000u;
+        }
+      }
+      odd = __any(top != 0);
+    }
+    // all keys at once, or key by key
+    for (int k = 0; k < (odd ? GEN : 1); ++k) {
+      u32x4 keep;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        // key k sits in slot (k % 4) + 4 (k / 16) of lane group (k % 16) / 4
+        const bool here = g == ((k >> 2) & 3) && ((k & 3) + (k >> 4) * 4) >> 1 == x;
+        keep[x] = !odd ? 0xffffffffu : here ? (k & 1 ? 0xffff0000u : 0xffffu) : 0u;
+      }
+#pragma unroll
+      for (int e = 0; e < DT; ++e) {
+        if (CG > 1) __builtin_amdgcn_sched_barrier(0);
+        const bf16x8 v =
+            __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, v_gen(la, e)) & keep);
+#pragma unroll
+        for (int c = 0; c < CG; ++c) {
+          const f32x4 x =
+              __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P[c], acc[c][e], 0, 0, 0);
+          if (!odd || ((vis[c] >> k) & 1)) acc[c][e] = x;
+        }
+      }
+    }
+    done(j);
   }
 
   // ---- the waves' states, merged through LDS --------------------------------------
@@ -670,16 +706,17 @@ void quant_attn_kernel(QuantAttnArgs a) {
   }
 }
 
-template <int D, int FORMAT, int NW, int CG>
+template <int D, int FORMAT, int NW, int KEYS, int CG>
 int launch_one(const QuantAttnArgs& a, hipStream_t stream) {
-  using L = QaLds<D, NW>;
+  using L = QaLds<D, NW, KEYS>;
   const size_t lds = L::REUSED + (a.rows != nullptr ? L::STEPS : 0);
   const int64_t tiles = (int64_t)a.token_tiles * a.col_tiles;
   const int64_t nwg = ((int64_t)a.Hkv * a.parts * a.slices + 7) / 8 * 8 *
                       ((tiles + a.slices - 1) / a.slices);
   if (!grid_fits(nwg, 64 * NW)) return PULSAR_EUNSUPPORTED;
-  const auto kern = quant_attn_kernel<D, FORMAT, NW, CG>;
-  if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize,
+  const auto kern = quant_attn_kernel<D, FORMAT, NW, KEYS, CG>;
+  if (lds > 65536 &&
+      hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize,
                           (int)lds) != hipSuccess)
     return PULSAR_EHIP;
   hipLaunchKernelGGL(kern, dim3((unsigned)nwg), dim3(64 * NW), lds, stream, a);
@@ -687,34 +724,63 @@ int launch_one(const QuantAttnArgs& a, hipStream_t stream) {
 }
 
 template <int D, int FORMAT>
-int launch_groups(const QuantAttnArgs& a, hipStream_t stream) {
-  return launch_one<D, FORMAT, 4, 1>(a, stream);
+int launch_tile(const QuantAttnArgs& a, int columns, hipStream_t stream) {
+  return columns == 16 ? launch_one<D, FORMAT, 8, 32, 1>(a, stream)
+                       : launch_one<D, FORMAT, 4, 64, 2>(a, stream);
 }
 
 // Workgroups that the chip holds at once: two on each compute unit.
 constexpr int QA_AT_ONCE = 512;
 
+// Tiles of 16 columns in steps of 32 rows by eight waves, four to a SIMD; or of 32 columns in
+// steps of 64 by four waves, two to a SIMD.
+int step_keys(int columns) { return columns == 16 ? 32 : 64; }
+
 }  // namespace
 
-QuantPlan quant_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int64_t gen_rows) {
+// Tiles of 32 columns widen a code for twice the columns and read it half as often, tiles of
+// 16 have less to wait for: the former from three steps of a wave on.  16 / 32 columns, us with
+// the merge: 32 / 8 heads of 128, 5 tokens over 16384 keys (1 step) 15.9 / 19.3, 65536 (4) 35.5 /
+// 33.7, 131072 (8) 59 / 55; 24 tokens over 16384 (3) 26.1 / 25.6; 8 / 2 heads, 12 tokens over
+// 65536 (2) 20.3 / 22.4, 24 (3) 26.2 / 26.3, 64 (8) 47 / 41; 16 / 16 of 64, 24 tokens over 16384
+// (2) 17.1 / 16.9, 65536 (8) 37 / 31.
+// Parts: of 16 columns, as many as give each compute unit one workgroup, or two where waves
+// would have eight steps or more and d is 64 or tiles share their keys (one / two: 32 / 8 heads
+// of 128, 1 token over 131072 keys 46.8 / 48.5, 16384 13.4 / 14.4; 16 / 16 of 64, 1 token over
+// 131072 50.7 / 48.4, 4 x 1021 9.4 / 10.4; 8 / 2 of 128, 5 tokens over 65536 15.9 / 17.7; 32 / 8,
+// 24 tokens over 16384 27.1 / 26.1).
+QuantPlan quant_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int d, int64_t gen_rows) {
   QuantPlan p{};
   const int group = Hq / Hkv;
-  p.groups = 1;
-  const int most = 16 * p.groups;
-  p.tokens = std::max(1, most / group);
-  const int64_t own = (int64_t)((Tq + p.tokens - 1) / p.tokens) * ((group + most - 1) / most);
-  const int64_t steps = (int64_t)n_shards * ((S + QA_KEYS - 1) / QA_KEYS) +
-                        (gen_rows + QA_GEN - 1) / QA_GEN;
-  p.parts = parts_at_once(std::min(QA_AT_ONCE / std::max<int64_t>(own * Hkv, 1), (steps + 3) / 4),
-                          Hkv, own, QA_AT_ONCE / 8);
+  const int64_t gen = (gen_rows + 31) / 32;  // (whole 32 rows, for few sizes to ask for)
+  int64_t own = 0, steps = 0;
+  auto take = [&](int columns) {
+    p.columns = columns;
+    p.tokens = std::max(1, columns / group);
+    own = (int64_t)((Tq + p.tokens - 1) / p.tokens) * ((group + columns - 1) / columns);
+    const int keys = step_keys(columns);
+    steps = n_shards * ((S + keys - 1) / keys) + gen * (64 / keys);
+  };
+  auto parts = [&](int at_once, int waves) {
+    const int64_t fill = at_once / std::max<int64_t>(own * Hkv, 1);
+    return parts_at_once(std::min(fill, (steps + waves - 1) / waves), Hkv, own, at_once / 8);
+  };
+  if ((int64_t)Tq * group > 16) {
+    take(32);
+    p.parts = parts(QA_AT_ONCE, 4);
+    if (own * Hkv * steps >= 3 * 4 * QA_AT_ONCE) return p;
+  }
+  take(16);
+  p.parts = parts(QA_AT_ONCE / 2, 8);
+  if (steps >= 8 * 8 * (int64_t)p.parts && (d == 64 || own > 1)) p.parts = parts(QA_AT_ONCE, 8);
   return p;
 }
 
 // Rows of partials (tokens times parts) of any call of up to Tq tokens: parts are
-// QA_AT_ONCE / (tiles * Hkv) at most, of tiles that hold 64 columns at most.
+// QA_AT_ONCE / (tiles * Hkv) at most, of tiles that hold 32 columns at most.
 int64_t quant_part_rows_most(int Tq, int Hq, int Hkv) {
   if (Tq <= 0) return 0;
-  const int64_t tokens = std::min(std::max(64 / (Hq / Hkv), 1), Tq);
+  const int64_t tokens = std::min(std::max(32 / (Hq / Hkv), 1), Tq);
   return (int64_t)QA_AT_ONCE / Hkv * tokens;
 }
 
@@ -734,7 +800,7 @@ int launch_quant_attn(const QuantAttnLaunch& x, const QuantPlan& p, void* o, int
   a.Hq = x.Hq;
   a.Hkv = x.Hkv;
   a.group = x.Hq / x.Hkv;
-  const int most = 16 * p.groups;
+  const int most = p.columns;
   a.tile_tokens = p.tokens;
   a.token_tiles = (x.Tq + p.tokens - 1) / p.tokens;
   a.col_tiles = (a.group + most - 1) / most;
@@ -745,7 +811,8 @@ int launch_quant_attn(const QuantAttnLaunch& x, const QuantPlan& p, void* o, int
   a.blocks = (int)((x.S + x.block - 1) >> a.block_log2);
   a.gen_rows = x.Kg != nullptr ? (int)(x.G + x.Tq) : 0;
   a.G = (int)x.G;
-  a.shard_steps = (int)((x.S + QA_KEYS - 1) / QA_KEYS);
+  const int keys = step_keys(p.columns);
+  a.shard_steps = (int)((x.S + keys - 1) / keys);
   a.parts = p.parts;
   a.scale_log2 = x.scale * 1.4426950408889634f;
   a.O = o;
@@ -753,8 +820,8 @@ int launch_quant_attn(const QuantAttnLaunch& x, const QuantPlan& p, void* o, int
   a.lse = lse;
   const bool e4m3 = x.format == PULSAR_KV_E4M3;
   if (x.d == 128)
-    return e4m3 ? launch_groups<128, PULSAR_KV_E4M3>(a, stream)
-                : launch_groups<128, PULSAR_KV_INT8>(a, stream);
-  return e4m3 ? launch_groups<64, PULSAR_KV_E4M3>(a, stream)
-              : launch_groups<64, PULSAR_KV_INT8>(a, stream);
+    return e4m3 ? launch_tile<128, PULSAR_KV_E4M3>(a, p.columns, stream)
+                : launch_tile<128, PULSAR_KV_INT8>(a, p.columns, stream);
+  return e4m3 ? launch_tile<64, PULSAR_KV_E4M3>(a, p.columns, stream)
+              : launch_tile<64, PULSAR_KV_INT8>(a, p.columns, stream);
 }

@@ -74,7 +74,7 @@ def test_phase2_quant():
     for kw in (dict(d=96), dict(block=24), dict(block=8), dict(S=1 << 31), dict(G=1 << 24),
                dict(G=1 << 62), dict(n_shards=1 << 20, S=1 << 11), dict(n_shards=1025, rows=FAKE),
                dict(Hkv=1 << 17, Hq=1 << 17), dict(Tq=1 << 23, Hq=128),
-               dict(Tq=1 << 23, Hkv=1, Hq=32)):
+               dict(Tq=1 << 23, Hkv=1, Hq=128)):
         assert call(**kw) == EUNSUP, kw
     size = P.phase2_quant_workspace_bytes(3, 32, 8, 128)
     assert size > 0

@@ -414,6 +414,48 @@ def test_attention_of_flat_and_peaked_scores(q_scale):
     _attn(8, 8, 64, 20, 50, 2, 500, 64, "int8", 201, q_scale=q_scale, what=f"q times {q_scale}")
 
 
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_of_queries_with_outliers(d, fmt):
+    # channels of one query that differ by up to 2^30, columns that differ by up to 2^60 and
+    # one that is zero; the keys' large channels are small where the queries' are large
+    Hq, Hkv, Tq, n, S, block = 8, 2, 5, 2, 300, 32
+    rng = np.random.default_rng(205)
+    size = 2.0 ** rng.integers(-30, 1, (Tq, Hq, d))
+    size *= 2.0 ** -(np.arange(Tq * Hq).reshape(Tq, Hq, 1) % 60)
+    x = f64(normal(206, (Tq, Hq, d))) * size
+    x[2, 3] = 0
+    q = torch.from_numpy(x).to(torch.bfloat16).view(torch.int16).numpy().view(np.uint16)
+    k, v = (spread(s, (n, S, Hkv, d)) for s in (207, 208))
+    k[:, :, :, ::7] = 0
+    cache, vals = dev_cache(k, v, block, fmt)
+    for scale in (1.0, 2.0 ** 20):
+        o, lse = P.phase2_quant(to_dev_bf16(q), *cache, block, softmax_scale=scale)
+        ref, keys = reference(q, *vals, None, None, None, 0, None, scale)
+        check(o, lse, ref, keys, f"outliers, scale {scale}")
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_queries_that_are_not_finite(fmt):
+    Hq, Hkv, d, Tq, S, block = 8, 2, 64, 3, 200, 32
+    q = normal(209, (Tq, Hq, d))
+    good = f64(q).copy()
+    q[0, 1, 5], q[1, 6, 63], q[2, 0, 0] = 0x7fc0, 0x7f80, 0xff80
+    k, v = (spread(s, (1, S, Hkv, d)) for s in (215, 216))
+    cache, vals = dev_cache(k, v, block, fmt)
+    o, lse = P.phase2_quant(to_dev_bf16(q), *cache, block)
+    bad = np.zeros((Tq, Hq), dtype=bool)
+    bad[0, 1] = bad[1, 6] = bad[2, 0] = True
+    assert np.isnan(host(o)[bad]).all() and np.isnan(host(lse).T[bad]).all()
+    assert np.isfinite(host(o)[~bad]).all() and np.isfinite(host(lse).T[~bad]).all()
+    ref, keys = ob.counted_attention(good, vals[0][0], vals[1][0], np.ones((Tq, 1, S)),
+                                     softmax_scale(d)), S
+    keep = torch.from_numpy(~bad).cuda()
+    check(torch.where(keep[..., None], o, 0), torch.where(keep.t(), lse, 0),
+          (np.where(bad[..., None], 0, ref[0]), np.where(bad.T, 0, ref[1]), ref[2], ref[3]), keys,
+          "the other columns")
+
+
 def test_attention_scale_and_refusals():
     q = torch.zeros((2, 8, 64), dtype=torch.bfloat16, device="cuda")
     kg = torch.zeros((5, 2, 64), dtype=torch.bfloat16, device="cuda")
