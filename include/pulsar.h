@@ -612,11 +612,12 @@ int pulsar_phase2_sparse(const void* q, const void* K, const void* V, const int3
  *           element i * shard_stride + r * row_stride, both multiples of 8 (quantising;
  *           rows may lie inside longer ones, or in a larger cache).  Dequantising: out
  *           [n, rows, Hkv, d], contiguous.
- * codes     16-byte aligned; no memory in common with K and V.
+ * codes     16-byte aligned.  Quantising, codes and scales have no memory in common with
+ *           each other or with K and V.
  * block     16, 32, 64, 128 or 256 rows.
  * EINVAL: negative sizes, Hkv < 1, d < 1, block < 1, an unknown format, first or rows past
  *         the capacity, first not a multiple of block (quantising), NULL or misaligned
- *         pointers or strides when there is work.
+ *         pointers or strides when there is work, or memory in common.
  * EUNSUPPORTED: d not in {64, 128}; another block; capacity >= 2^31 or Hkv * d >= 2^23;
  *         more workgroups than a launch holds (none below n * ceil(rows / 64) * Hkv = 2^21).
  */

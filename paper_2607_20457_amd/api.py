@@ -567,26 +567,31 @@ _FORMATS = {torch.float8_e4m3fn: 0, torch.int8: 1}
 def _cache_of(Kc, Vc, k_scale, v_scale, block, dev):
     """The shape [n, Hkv, capacity, d] of a cache in 8 bits, and its format."""
     _int32(block, "block")
-    if Kc.dtype not in _FORMATS:
-        raise ValueError(f"codes must be torch.float8_e4m3fn or torch.int8, got {Kc.dtype}")
-    _check(dev, Kc.dtype, ((Kc, "Kc"), (Vc, "Vc")))
+    dtype, shape = Kc.dtype, Kc.shape
+    if dtype not in _FORMATS:
+        raise ValueError(f"codes must be torch.float8_e4m3fn or torch.int8, got {dtype}")
+    _check(dev, dtype, ((Kc, "Kc"), (Vc, "Vc")))
     _check(dev, torch.float32, ((k_scale, "k_scale"), (v_scale, "v_scale")))
-    if Kc.dim() != 4 or Vc.shape != Kc.shape:
+    if len(shape) != 4 or Vc.shape != shape:
         raise ValueError("Kc/Vc must be [n, Hkv, capacity, d]")
-    n, Hkv, capacity, _ = Kc.shape
-    blocks = -(-capacity // block) if block > 0 else 0
-    if k_scale.shape != (n, Hkv, blocks) or v_scale.shape != k_scale.shape:
+    scales = (shape[0], shape[1], -(-shape[2] // block) if block > 0 else 0)
+    if k_scale.shape != scales or v_scale.shape != scales:
         raise ValueError("k_scale/v_scale must be [n, Hkv, ceil(capacity / block)]")
-    return Kc.shape, _FORMATS[Kc.dtype]
+    return shape, _FORMATS[dtype]
 
 
-def _apart(a, b):
-    """Whether two tensors' memory, from the first element to the last, has none in common."""
-    def span(t):
-        last = sum((s - 1) * st for s, st in zip(t.shape, t.stride()))
-        return t.data_ptr(), t.data_ptr() + (last + 1) * t.element_size()
-    (a0, a1), (b0, b1) = span(a), span(b)
-    return not a.numel() or not b.numel() or a1 <= b0 or b1 <= a0
+def _row_strides(K, V):
+    """Elements from shard to shard and from row to row of K and V [n, rows, Hkv, d]."""
+    n, rows, Hkv, d = K.shape
+    a = K.stride()
+    if a != V.stride() or a[3] != 1 or a[2] != d:
+        # (a dimension of one has any stride)
+        sizes = (n, rows, Hkv, d)
+        if K.numel() and any(
+                size > 1 and (x != y or i == 3 and x != 1 or i == 2 and x != d)
+                for i, (size, x, y) in enumerate(zip(sizes, a, V.stride()))):
+            raise ValueError("K and V must have the same strides, each row [Hkv, d] contiguous")
+    return a[0] if n > 1 else 0, a[1] if rows > 1 else 0
 
 
 def kv_quantize_(K, V, Kc, Vc, k_scale, v_scale, block: int, first: int = 0):
@@ -595,30 +600,25 @@ def kv_quantize_(K, V, Kc, Vc, k_scale, v_scale, block: int, first: int = 0):
     blocks of them: first is a multiple of block (16, 32, 64, 128 or 256), the last block may
     be short.  Kc/Vc float8_e4m3fn or int8 [n, Hkv, capacity, d], k_scale/v_scale f32 [n, Hkv,
     ceil(capacity / block)]: a code stands for code * scale, the scale a power of two for each
-    block and head, NaN (and codes 0) where the block holds a NaN or an infinity.
+    block and head, NaN (and codes 0) where the block holds a NaN or an infinity.  None of
+    the cache's tensors shares memory with another, or with K and V.
     Returns the cache: Kc, Vc, k_scale, v_scale."""
     dev = torch.cuda.current_device() if K.is_cuda else None
     for t, name in ((K, "K"), (V, "V")):
         if t.get_device() != dev or t.dtype is not _BF16:
-            _need(t, _BF16, name)
-            raise ValueError(f"{name} must be on the current device")
+            if t.is_cuda and t.dtype is _BF16:
+                raise ValueError(f"{name} must be on the current device")
+            raise ValueError(f"{name} must be a device tensor of {_BF16}")
     (n, Hkv, capacity, d), form = _cache_of(Kc, Vc, k_scale, v_scale, block, dev)
-    if K.dim() != 4 or V.shape != K.shape or K.shape[0] != n or K.shape[2:] != (Hkv, d):
+    shape = K.shape
+    if len(shape) != 4 or V.shape != shape or shape != (n, shape[1], Hkv, d):
         raise ValueError("K/V must be [n, rows, Hkv, d]")
-    rows = K.shape[1]
+    rows = shape[1]
     if not 0 <= first <= capacity - rows:
         raise ValueError("first and the rows must lie within the cache")
-    strides = [(x.stride(0) if n > 1 else 0, x.stride(1) if rows > 1 else 0) for x in (K, V)]
-    if strides[0] != strides[1] or K.numel() and any(
-            x.stride(3) != 1 or Hkv > 1 and x.stride(2) != d for x in (K, V)):
-        raise ValueError("K and V must have the same strides, each row [Hkv, d] contiguous")
-    for out, name in ((Kc, "Kc"), (Vc, "Vc"), (k_scale, "k_scale"), (v_scale, "v_scale")):
-        if not _apart(out, K) or not _apart(out, V):
-            raise ValueError(f"{name} must not share memory with K or V")
-    if not (_apart(Kc, Vc) and _apart(k_scale, v_scale)):
-        raise ValueError("the caches of K and V must not share memory")
-    st = _lib.lib().pulsar_kv_quantize(K.data_ptr(), V.data_ptr(), *strides[0], n, rows, Hkv, d,
-                                       block, form, first, capacity, Kc.data_ptr(),
+    shard_stride, row_stride = _row_strides(K, V)
+    st = _lib.lib().pulsar_kv_quantize(K.data_ptr(), V.data_ptr(), shard_stride, row_stride, n,
+                                       rows, Hkv, d, block, form, first, capacity, Kc.data_ptr(),
                                        Vc.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
                                        _raw_stream(dev))
     _lib.check(st, "pulsar_kv_quantize")
@@ -638,9 +638,9 @@ def kv_quantize(K, V, block: int = 64, dtype=torch.float8_e4m3fn, capacity: int 
     capacity = rows if capacity is None else capacity
     if block < 1 or capacity < rows:
         raise ValueError("block must be positive, capacity at least the rows")
-    codes = [K.new_empty((n, Hkv, capacity, d), dtype=dtype) for _ in range(2)]
-    scales = [K.new_empty((n, Hkv, -(-capacity // block)), dtype=torch.float32) for _ in range(2)]
-    return kv_quantize_(K, V, *codes, *scales, block)
+    Kc = K.new_empty((n, Hkv, capacity, d), dtype=dtype)
+    k_scale = K.new_empty((n, Hkv, -(-capacity // block)), dtype=torch.float32)
+    return kv_quantize_(K, V, Kc, torch.empty_like(Kc), k_scale, torch.empty_like(k_scale), block)
 
 
 def kv_dequantize(Kc, Vc, k_scale, v_scale, block: int, first: int = 0, rows: int | None = None):
@@ -651,7 +651,8 @@ def kv_dequantize(Kc, Vc, k_scale, v_scale, block: int, first: int = 0, rows: in
     rows = capacity - first if rows is None else rows
     if first < 0 or rows < 0 or first + rows > capacity:
         raise ValueError("first and rows must lie within the cache")
-    K, V = (Kc.new_empty((n, rows, Hkv, d), dtype=_BF16) for _ in range(2))
+    K = Kc.new_empty((n, rows, Hkv, d), dtype=_BF16)
+    V = torch.empty_like(K)
     st = _lib.lib().pulsar_kv_dequantize(Kc.data_ptr(), Vc.data_ptr(), k_scale.data_ptr(),
                                          v_scale.data_ptr(), n, capacity, Hkv, d, block, form,
                                          first, rows, K.data_ptr(), V.data_ptr(),

@@ -2,6 +2,8 @@
 // launches.
 #include <math.h>
 
+#include <initializer_list>
+
 #include "common.hpp"
 
 namespace {
@@ -21,6 +23,25 @@ int check_rows(int n, int64_t rows, int Hkv, int d, int block, int format, int64
   if ((d != 64 && d != 128) || !quant_block(block)) return PULSAR_EUNSUPPORTED;
   if (capacity > kMaxInt || (int64_t)Hkv * d >= 1 << 23) return PULSAR_EUNSUPPORTED;
   return PULSAR_OK;
+}
+
+// Memory [from, to), and whether two pieces of it have any in common.
+struct Span {
+  __int128 from, to;
+};
+bool meet(const Span& a, const Span& b) { return a.from < b.to && b.from < a.to; }
+Span span(const void* p, __int128 bytes) {
+  const __int128 at = (__int128) reinterpret_cast<uintptr_t>(p);
+  return Span{at, at + bytes};
+}
+// bf16 rows of `width` values at these strides.
+Span rows_span(const void* p, int n, int64_t rows, int64_t width, int64_t shard_stride,
+               int64_t row_stride) {
+  Span s = span(p, (__int128)width * 2);
+  for (const __int128 far : {(__int128)(n - 1) * shard_stride * 2,
+                             (__int128)(rows - 1) * row_stride * 2})
+    (far < 0 ? s.from : s.to) += far;
+  return s;
 }
 
 KvQuantLaunch cache_of(const void* k_codes, const void* v_codes, const float* k_scales,
@@ -60,6 +81,17 @@ int pulsar_kv_quantize(const void* K, const void* V, int64_t shard_stride, int64
   if (!aligned16(K) || !aligned16(V) || !aligned16(k_codes) || !aligned16(v_codes) ||
       shard_stride % 8 != 0 || row_stride % 8 != 0)
     return PULSAR_EINVAL;
+  const __int128 codes = (__int128)n * Hkv * capacity * d;
+  const __int128 scales = (__int128)n * Hkv * ((capacity + block - 1) / block) * 4;
+  const Span all[6] = {span(k_codes, codes),
+                       span(v_codes, codes),
+                       span(k_scales, scales),
+                       span(v_scales, scales),
+                       rows_span(K, n, rows, (int64_t)Hkv * d, shard_stride, row_stride),
+                       rows_span(V, n, rows, (int64_t)Hkv * d, shard_stride, row_stride)};
+  for (int i = 0; i < 4; ++i)
+    for (int j = i + 1; j < 6; ++j)
+      if (meet(all[i], all[j])) return PULSAR_EINVAL;
   KvQuantLaunch a = cache_of(k_codes, v_codes, k_scales, v_scales, n, rows, Hkv, d, block, format,
                              first, capacity);
   a.X[0] = static_cast<const uint16_t*>(K);

@@ -9,6 +9,7 @@ import paper_2607_20457_amd as P
 from paper_2607_20457_amd import _lib
 from tests.test_abi_blocks import BIG, EINVAL, EUNSUP, EWS, FAKE, caller
 
+EHIP = -3  # (without a GPU: what a call that is not refused ends with)
 QUANTIZE = ("K V shard_stride row_stride n rows Hkv d block format first capacity kc vc ks vs "
             "stream")
 DEQUANTIZE = "kc vc ks vs n capacity Hkv d block format first rows K V stream"
@@ -16,9 +17,13 @@ ATTN = ("q kc vc ks vs n_shards Tq S block format rows Kg Vg G mask Hq Hkv d sca
         "ws wsb stream")
 
 
+# apart from each other: rows of K and V, codes of 2 x 8 x 200 x 64, scales of 2 x 8 x 7
+KC, VC, KS, VS = 2 * FAKE, 3 * FAKE, 4 * FAKE, 5 * FAKE
+
+
 def quantizer(**kw):
     ok = dict(K=FAKE, V=FAKE, shard_stride=800, row_stride=512, n=2, rows=50, Hkv=8, d=64,
-              block=32, format=0, first=64, capacity=200, kc=FAKE, vc=FAKE, ks=FAKE, vs=FAKE)
+              block=32, format=0, first=64, capacity=200, kc=KC, vc=VC, ks=KS, vs=VS)
     return caller("pulsar_kv_quantize", QUANTIZE, **{**ok, **kw})
 
 
@@ -38,9 +43,22 @@ def test_kv_quantize():
                dict(vs=None), dict(K=FAKE + 8), dict(V=FAKE + 2), dict(kc=FAKE + 8),
                dict(vc=FAKE + 1), dict(shard_stride=801), dict(row_stride=516)):
         assert call(**kw) == EINVAL, kw
+    # memory in common
+    rows = ((800 + 49 * 512) + 8 * 64) * 2
+    codes, scales = 2 * 8 * 200 * 64, 2 * 8 * 7 * 4
+    for kw in (dict(vc=KC), dict(vs=KS), dict(kc=FAKE), dict(vc=KC + codes - 16), dict(ks=KC),
+               dict(ks=KC + codes - 4), dict(vs=KS - scales + 4), dict(kc=FAKE + rows - 16),
+               dict(V=KC + codes - 16), dict(K=VC - rows + 16),
+               dict(K=VC + codes + 800 * 2 - 16, shard_stride=-800),
+               dict(V=VS + 49 * 512 * 2, row_stride=-512), dict(K=FAKE, shard_stride=1 << 61)):
+        assert call(**kw) == EINVAL, kw
+    for kw in (dict(vc=KC + codes), dict(vs=KS + scales), dict(kc=FAKE + rows),
+               dict(K=VC + codes + 800 * 2, shard_stride=-800), dict(V=FAKE + 16)):
+        if not torch.cuda.is_available():
+            assert call(**kw) == EHIP, kw
     for kw in (dict(d=96), dict(block=8, first=0), dict(block=48, first=48),
                dict(block=512, first=0), dict(capacity=1 << 31), dict(Hkv=1 << 17),
-               dict(n=1 << 30, rows=64)):
+               dict(n=1 << 24, kc=1 << 50, vc=1 << 51, ks=1 << 52, vs=1 << 53, K=1 << 54, V=1 << 54)):
         assert call(**kw) == EUNSUP, kw
     assert call(n=0, K=None, V=None) == 0 and call(rows=0, K=None, kc=None) == 0
     assert call(capacity=0, first=0, rows=0) == 0

@@ -150,7 +150,6 @@ def test_quantize_refusals():
         lambda: P.kv_quantize_(K, V, *cache, 16, -16),
         lambda: P.kv_quantize_(K, V, Kc, Vc.view(torch.int8), ks, vs, 16),
         lambda: P.kv_quantize_(K, V, Kc.view(torch.uint8), Vc.view(torch.uint8), ks, vs, 16),
-        lambda: P.kv_quantize_(K, V, Kc, Kc, ks, vs, 16), lambda: P.kv_quantize_(K, V, Kc, Vc, ks, ks, 16),
         lambda: P.kv_quantize_(K, V, Kc, Vc, ks.double(), vs.double(), 16),
         lambda: P.kv_quantize_(K, V, Kc, Vc, ks[:, :, :3], vs[:, :, :3], 16),
         lambda: P.kv_quantize_(K[..., ::2], V[..., ::2], *cache, 16),
@@ -167,12 +166,13 @@ def test_quantize_refusals():
     # a source that begins inside the cache, and rows whose strides are no multiple of 8
     raw = torch.zeros(2 * 4 * 64 * 64 * 3, dtype=torch.uint8, device="cuda")
     inside = raw.view(torch.bfloat16)[4096:4096 + 2 * 40 * 256].view(2, 40, 4, 64)
-    with pytest.raises(ValueError):
-        P.kv_quantize_(inside, inside, raw[:32768].view(torch.int8).view(2, 4, 64, 64),
-                       torch.zeros_like(Kc).view(torch.int8), ks, vs, 16)
+    outer = raw[:32768].view(torch.int8).view(2, 4, 64, 64), torch.zeros_like(Kc).view(torch.int8)
     odd = torch.zeros(2, 40, 260, **bf)[:, :, :256].unflatten(2, (4, 64))
     small = torch.zeros(1, 16, 1, 32, **bf)
-    for fn in (lambda: P.kv_quantize_(odd, odd, *cache, 16), lambda: P.kv_quantize_(K, V, *cache, 16, 8),
+    for fn in (lambda: P.kv_quantize_(inside, inside, *outer, ks, vs, 16),
+               lambda: P.kv_quantize_(K, V, Kc, Kc, ks, vs, 16),
+               lambda: P.kv_quantize_(K, V, Kc, Vc, ks, ks, 16),
+               lambda: P.kv_quantize_(odd, odd, *cache, 16), lambda: P.kv_quantize_(K, V, *cache, 16, 8),
                lambda: P.kv_quantize(K, V, 24), lambda: P.kv_quantize(small, small, 16)):
         with pytest.raises(RuntimeError):
             fn()
