@@ -33,6 +33,7 @@ struct QuantizeArgs {
   int row_groups;        // workgroups over the rows of a shard
   int head_groups;       // and over its heads
   int waves_log2;        // log2 of a block's waves
+  int once;              // more rows than the caches hold
 };
 
 // The largest 16-bit magnitude of both halves of x, over all lanes.
@@ -77,10 +78,13 @@ __device__ __forceinline__ u32x2 encode(u32x4 w, float s, float inv) {
   return out;
 }
 
-// Workgroup: 64 rows of four heads, or of fewer heads where a block has more rows.  A
-// wave holds its 64 rows of one head in registers, so that each value is read once;
-// blocks of more rows exchange their magnitudes through LDS.  Four heads side by side
-// are 1 KiB of a row of the source.
+// Bound by HBM.  Workgroup: 64 rows of four heads, or of fewer heads where a block has
+// more rows.  A wave holds its 64 rows of one head in registers, so that each value is
+// read once; blocks of more rows exchange their magnitudes through LDS.  Four heads side
+// by side are 1 KiB of a row of the source.  K and V of 16 x 8192 rows of 8 heads of 128
+// (805 MB): 141 us, 134 with stores that pass the caches by, 124 (6.5 TB/s) where from 256
+// MB on the loads do so too; below, where the rows may lie in the last-level cache, those
+// loads lose (5 x 3001 rows of 16 heads of 64, 61 MB of K and V: 16.3 / 18.4).
 template <int D, int FORMAT>
 __global__ __launch_bounds__(64 * QZ_WAVES) void quantize_kernel(QuantizeArgs a) {
   constexpr int CPR = D / 8;          // 16-byte chunks per row
@@ -103,12 +107,20 @@ __global__ __launch_bounds__(64 * QZ_WAVES) void quantize_kernel(QuantizeArgs a)
 
   u32x4 w[LOADS];
   const uint16_t* const x = a.X[which] + shard * a.shard_stride + (int64_t)head * D + 8 * at;
+  auto load = [&](auto once) {
 #pragma unroll
-  for (int i = 0; i < LOADS; ++i) {
-    const int64_t row = row0 + i * SEG + lane / CPR;
-    w[i] = live && row < a.rows ? *reinterpret_cast<const u32x4*>(x + row * a.row_stride)
-                                : u32x4{0u, 0u, 0u, 0u};
-  }
+    for (int i = 0; i < LOADS; ++i) {
+      const int64_t row = row0 + i * SEG + lane / CPR;
+      const u32x4* const from = reinterpret_cast<const u32x4*>(x + row * a.row_stride);
+      w[i] = u32x4{0u, 0u, 0u, 0u};
+      if (live && row < a.rows) {
+        if constexpr (decltype(once)::value) w[i] = __builtin_nontemporal_load(from);
+        else w[i] = *from;
+      }
+    }
+  };
+  if (a.once) load(std::true_type{});
+  else load(std::false_type{});
   const int64_t plane = shard * a.Hkv + head;
   uint8_t* const out = a.codes[which] + (plane * a.capacity + a.first + row0) * D + 8 * at;
   float* const scales =
@@ -141,7 +153,8 @@ __global__ __launch_bounds__(64 * QZ_WAVES) void quantize_kernel(QuantizeArgs a)
       u32x2 c = encode<FORMAT>(y, s, inv);
       if (bad) c = u32x2{0u, 0u};
       if (live && row0 + i * SEG + lane / CPR < a.rows)
-        *reinterpret_cast<u32x2*>(out + (i * SEG + lane / CPR) * D) = c;
+        __builtin_nontemporal_store(c,
+                                    reinterpret_cast<u32x2*>(out + (i * SEG + lane / CPR) * D));
     }
     if (writes && live && lane == 0) scales[nth] = bad ? __uint_as_float(0x7fc00000u) : s;
   };
@@ -196,7 +209,9 @@ struct DequantizeArgs {
 };
 
 // The quantiser's shape the other way: a wave reads 64 rows of one head, four heads side
-// by side write 1 KiB of a row.  A lane takes 8 codes, 16 bytes of output.
+// by side write 1 KiB of a row.  A lane takes 8 codes, 16 bytes of output.  16 x 8192 rows
+// of 8 heads of 128 (805 MB): 149 us, 5.4 TB/s (a copy: 5.0); with stores that pass the
+// caches by, 4 x 1021 rows 6.4 us against 8.5, 32768 rows 35.5 against 40.8.
 template <int D, int FORMAT>
 __global__ __launch_bounds__(64 * QZ_WAVES, 4) void dequantize_kernel(DequantizeArgs a) {
   constexpr int CPR = D / 8;
@@ -247,8 +262,9 @@ __global__ __launch_bounds__(64 * QZ_WAVES, 4) void dequantize_kernel(Dequantize
 #pragma unroll
     for (int k = 0; k < 8; ++k) y[k] *= s[i];
     if (row0 + r < a.rows)
-      *reinterpret_cast<bf16x8*>(out + (int64_t)r * a.Hkv * D) =
-          __builtin_convertvector(y, bf16x8);
+      __builtin_nontemporal_store(
+          __builtin_bit_cast(u32x4, __builtin_convertvector(y, bf16x8)),
+          reinterpret_cast<u32x4*>(out + (int64_t)r * a.Hkv * D));
   }
 }
 
@@ -273,6 +289,7 @@ int launch_quantize(const KvQuantLaunch& x, hipStream_t stream) {
   const int heads = QZ_WAVES >> a.waves_log2, rows = QZ_ROWS << a.waves_log2;
   a.head_groups = (x.Hkv + heads - 1) / heads;
   a.row_groups = (int)((x.rows + rows - 1) / rows);
+  a.once = (int64_t)x.n * x.rows * x.Hkv * x.d * 4 >= 256 << 20;
   const int64_t nwg = 2 * (int64_t)x.n * a.row_groups * a.head_groups;
   if (!grid_fits(nwg, 64 * QZ_WAVES)) return PULSAR_EUNSUPPORTED;
   const bool e4m3 = x.format == PULSAR_KV_E4M3;
