@@ -380,6 +380,7 @@ struct QuantAttnLaunch {
 constexpr int kMaxQuantShards = 1024;  // with lengths of their own
 struct QuantPlan {
   int columns;  // of a tile
+  int keys;     // rows of a step
   int tokens;   // per tile
   int parts;    // of a tile's keys
 };

@@ -113,7 +113,7 @@ __device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi) {
 
 template <int D, int FORMAT, int NW, int KEYS, int CG>
 __global__ __launch_bounds__(64 * NW)
-__attribute__((amdgpu_waves_per_eu(NW / 2, NW / 2)))
+__attribute__((amdgpu_waves_per_eu(CG == 1 ? 4 : 2, CG == 1 ? 4 : 2)))
 void quant_attn_kernel(QuantAttnArgs a) {
   using L = QaLds<D, NW, KEYS>;
   constexpr int HALVES = KEYS / 16;       // of a step, 16 rows each
@@ -724,60 +724,71 @@ int launch_one(const QuantAttnArgs& a, hipStream_t stream) {
 }
 
 template <int D, int FORMAT>
-int launch_tile(const QuantAttnArgs& a, int columns, hipStream_t stream) {
-  return columns == 16 ? launch_one<D, FORMAT, 8, 32, 1>(a, stream)
-                       : launch_one<D, FORMAT, 4, 64, 2>(a, stream);
+int launch_tile(const QuantAttnArgs& a, const QuantPlan& p, hipStream_t stream) {
+  if (p.keys == 64) return launch_one<D, FORMAT, 4, 64, 2>(a, stream);
+  if constexpr (D == 128) {
+    if (p.columns == 48) return launch_one<D, FORMAT, 8, 32, 3>(a, stream);
+    if (p.columns == 32) return launch_one<D, FORMAT, 8, 32, 2>(a, stream);
+  }
+  return launch_one<D, FORMAT, 8, 32, 1>(a, stream);
 }
 
-// Workgroups that the chip holds at once: two on each compute unit.
-constexpr int QA_AT_ONCE = 512;
-
-// Tiles of 16 columns in steps of 32 rows by eight waves, four to a SIMD; or of 32 columns in
-// steps of 64 by four waves, two to a SIMD.
-int step_keys(int columns) { return columns == 16 ? 32 : 64; }
+// Workgroups that give each compute unit one, and two, as many as it holds.
+constexpr int QA_ONE_EACH = 256, QA_AT_ONCE = 512;
 
 }  // namespace
 
-// Tiles of 32 columns widen a code for twice the columns and read it half as often, tiles of
-// 16 have less to wait for: the former from three steps of a wave on.  16 / 32 columns, us with
-// the merge: 32 / 8 heads of 128, 5 tokens over 16384 keys (1 step) 15.9 / 19.3, 65536 (4) 35.5 /
-// 33.7, 131072 (8) 59 / 55; 24 tokens over 16384 (3) 26.1 / 25.6; 8 / 2 heads, 12 tokens over
-// 65536 (2) 20.3 / 22.4, 24 (3) 26.2 / 26.3, 64 (8) 47 / 41; 16 / 16 of 64, 24 tokens over 16384
-// (2) 17.1 / 16.9, 65536 (8) 37 / 31.
-// Parts: of 16 columns, as many as give each compute unit one workgroup, or two where waves
-// would have eight steps or more and d is 64 or tiles share their keys (one / two: 32 / 8 heads
-// of 128, 1 token over 131072 keys 46.8 / 48.5, 16384 13.4 / 14.4; 16 / 16 of 64, 1 token over
-// 131072 50.7 / 48.4, 4 x 1021 9.4 / 10.4; 8 / 2 of 128, 5 tokens over 65536 15.9 / 17.7; 32 / 8,
-// 24 tokens over 16384 27.1 / 26.1).
+// Four shapes of tiles.  Each code is widened and read once for all columns of a tile, so wide
+// tiles do less, but narrow ones wait less: 16 columns have four waves to a SIMD, the others
+// two.
+//   16 columns, steps of 32 rows, eight waves: up to 12 steps of a wave with all compute units
+//   at work.  Us with the merge, 16 columns / the best of the others: 32 / 8 heads of 128, 8
+//   tokens over 32768 keys 20.9 / 22.9, 49152 28.6 / 27.5; 12 tokens 24.3 / 26.0, 33.3 / 31.4; 24
+//   tokens over 16384 24.7 / 23.0; 16 / 16 of 64, 24 tokens over 16384 16.7 / 16.7, 32768 21.8 /
+//   21.0.
+//   48 columns, as above (d 128; d 64 has the registers for no more than it gains), where that
+//   is a third fewer tiles than of 32: 12 tokens over 131072 keys 55 / 67, 24 tokens 87 / 95, 36
+//   122 / 139; but 64 (6 tiles against 8) 218 / 200.
+//   32 columns, as above (d 128): one tile, bound by its keys: 8 tokens over 131072 52 against
+//   55 of the next shape, 49152 27.5 / 30.7; but two tiles (16 tokens) 72 / 69, 8 tiles 224 / 200.
+//   32 columns, steps of 64 rows, four waves: the rest.
+// Parts: as many as give each compute unit one workgroup; two for the last shape, and for 16
+// columns where waves would have ten steps or more and d is 64 or tiles share their keys (one /
+// two: 32 / 8 heads of 128, 1 token over 131072 keys 46.8 / 48.5, 16384 13.4 / 14.4, 12 tokens
+// over 32768 26.5 / 24.3; 16 / 16 of 64, 1 token over 131072 50.7 / 48.4, 4 x 1021 9.4 / 10.4).
 QuantPlan quant_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int d, int64_t gen_rows) {
   QuantPlan p{};
   const int group = Hq / Hkv;
   const int64_t gen = (gen_rows + 31) / 32;  // (whole 32 rows, for few sizes to ask for)
-  int64_t own = 0, steps = 0;
-  auto take = [&](int columns) {
+  auto tiles = [&](int columns) {
+    const int tokens = std::max(1, columns / group);
+    return (int64_t)((Tq + tokens - 1) / tokens) * ((group + columns - 1) / columns);
+  };
+  auto steps = [&](int keys) { return n_shards * ((S + keys - 1) / keys) + gen * (64 / keys); };
+  auto take = [&](int columns, int keys, int at_once) {
+    const int waves = keys == 32 ? 8 : 4;
+    const int64_t own = tiles(columns), fill = at_once / std::max<int64_t>(own * Hkv, 1);
     p.columns = columns;
+    p.keys = keys;
     p.tokens = std::max(1, columns / group);
-    own = (int64_t)((Tq + p.tokens - 1) / p.tokens) * ((group + columns - 1) / columns);
-    const int keys = step_keys(columns);
-    steps = n_shards * ((S + keys - 1) / keys) + gen * (64 / keys);
+    p.parts = parts_at_once(std::min(fill, (steps(keys) + waves - 1) / waves), Hkv, own,
+                            at_once / 8);
+    return p;
   };
-  auto parts = [&](int at_once, int waves) {
-    const int64_t fill = at_once / std::max<int64_t>(own * Hkv, 1);
-    return parts_at_once(std::min(fill, (steps + waves - 1) / waves), Hkv, own, at_once / 8);
-  };
-  if ((int64_t)Tq * group > 16) {
-    take(32);
-    p.parts = parts(QA_AT_ONCE, 4);
-    if (own * Hkv * steps >= 3 * 4 * QA_AT_ONCE) return p;
+  if ((int64_t)Tq * group > 16 && tiles(16) * Hkv * steps(32) >= 12 * 8 * QA_ONE_EACH) {
+    const int64_t of32 = tiles(32);
+    if (d == 128 && 3 * tiles(48) <= 2 * of32) return take(48, 32, QA_ONE_EACH);
+    if (d == 128 && of32 == 1) return take(32, 32, QA_ONE_EACH);
+    return take(32, 64, QA_AT_ONCE);
   }
-  take(16);
-  p.parts = parts(QA_AT_ONCE / 2, 8);
-  if (steps >= 8 * 8 * (int64_t)p.parts && (d == 64 || own > 1)) p.parts = parts(QA_AT_ONCE, 8);
+  take(16, 32, QA_ONE_EACH);
+  if (steps(32) >= 10 * 8 * (int64_t)p.parts && (d == 64 || tiles(16) > 1))
+    take(16, 32, QA_AT_ONCE);
   return p;
 }
 
-// Rows of partials (tokens times parts) of any call of up to Tq tokens: parts are
-// QA_AT_ONCE / (tiles * Hkv) at most, of tiles that hold 32 columns at most.
+// Rows of partials (tokens times parts) of any call of up to Tq tokens: parts are QA_AT_ONCE /
+// (tiles * Hkv) at most, of tiles that hold 32 columns at most, or half as many of 48.
 int64_t quant_part_rows_most(int Tq, int Hq, int Hkv) {
   if (Tq <= 0) return 0;
   const int64_t tokens = std::min(std::max(32 / (Hq / Hkv), 1), Tq);
@@ -811,8 +822,7 @@ int launch_quant_attn(const QuantAttnLaunch& x, const QuantPlan& p, void* o, int
   a.blocks = (int)((x.S + x.block - 1) >> a.block_log2);
   a.gen_rows = x.Kg != nullptr ? (int)(x.G + x.Tq) : 0;
   a.G = (int)x.G;
-  const int keys = step_keys(p.columns);
-  a.shard_steps = (int)((x.S + keys - 1) / keys);
+  a.shard_steps = (int)((x.S + p.keys - 1) / p.keys);
   a.parts = p.parts;
   a.scale_log2 = x.scale * 1.4426950408889634f;
   a.O = o;
@@ -820,8 +830,8 @@ int launch_quant_attn(const QuantAttnLaunch& x, const QuantPlan& p, void* o, int
   a.lse = lse;
   const bool e4m3 = x.format == PULSAR_KV_E4M3;
   if (x.d == 128)
-    return e4m3 ? launch_tile<128, PULSAR_KV_E4M3>(a, p.columns, stream)
-                : launch_tile<128, PULSAR_KV_INT8>(a, p.columns, stream);
-  return e4m3 ? launch_tile<64, PULSAR_KV_E4M3>(a, p.columns, stream)
-              : launch_tile<64, PULSAR_KV_INT8>(a, p.columns, stream);
+    return e4m3 ? launch_tile<128, PULSAR_KV_E4M3>(a, p, stream)
+                : launch_tile<128, PULSAR_KV_INT8>(a, p, stream);
+  return e4m3 ? launch_tile<64, PULSAR_KV_E4M3>(a, p, stream)
+              : launch_tile<64, PULSAR_KV_INT8>(a, p, stream);
 }

@@ -42,10 +42,9 @@ def dev_cache(k, v, block, fmt):
     return (*codes, *scales), vals
 
 
-def reference(q, K, V, rows, kg, vg, G, sees, scale):
-    """The oracle's phase2_quant: q bf16 bits, K and V [n, S, H, d] the values of the codes,
-    rows the live ones of each shard (None: all), kg and vg bf16 bits or None, sees None is
-    causal -> what tests._blocks.check takes, and the number of keys."""
+def _seen(q, K, V, rows, kg, vg, G, sees):
+    """The keys and values that are live, one after another, and how often each token sees
+    them [Tq, 1, keys]."""
     n, S, Hkv, d = K.shape
     Tq = q.shape[0]
     live = np.full(n, S) if rows is None else np.clip(np.asarray(rows), 0, S).astype(int)
@@ -59,7 +58,53 @@ def reference(q, K, V, rows, kg, vg, G, sees, scale):
         Ks.append(f64(kg))
         Vs.append(f64(vg))
     K, V = (np.concatenate(x) if x else np.zeros((0, Hkv, d)) for x in (Ks, Vs))
+    return K, V, counts
+
+
+def reference(q, K, V, rows, kg, vg, G, sees, scale):
+    """The oracle's phase2_quant: q bf16 bits, K and V [n, S, Hkv, d] the values of the codes,
+    rows the live ones of each shard (None: all), kg and vg bf16 bits or None, sees None is
+    causal -> what tests._blocks.check takes, and the number of keys."""
+    K, V, counts = _seen(q, K, V, rows, kg, vg, G, sees)
     return ob.counted_attention(f64(q), K, V, counts, scale), counts.shape[2]
+
+
+def long_reference(q, cache, block, rows, kg, vg, G, sees, scale):
+    """`reference` of a cache on the device by matrix products in fp64 there, a KV head at a
+    time, for long shards."""
+    Kc, Vc, ks, vs = cache
+    n, Hkv, S, d = Kc.shape
+    Tq, Hq = q.shape[:2]
+    group = Hq // Hkv
+    live = np.full(n, S) if rows is None else np.clip(np.asarray(rows), 0, S).astype(int)
+    x = torch.from_numpy(f64(q)).cuda()
+    dead = torch.zeros((Tq, int(live.sum()) + (0 if kg is None else G + Tq)), dtype=torch.bool,
+                       device="cuda")
+    if kg is not None:
+        see = np.tri(Tq) if sees is None else np.asarray(sees)
+        dead[:, dead.shape[1] - Tq:] = torch.from_numpy(see == 0).cuda()
+    dead = torch.repeat_interleave(dead, group, dim=0)
+    o, size = (torch.zeros((Tq, Hq, d), dtype=torch.float64, device="cuda") for _ in range(2))
+    lse, most = torch.zeros((Hq, Tq), dtype=torch.float64, device="cuda"), 0.0
+    for g in range(Hkv):
+        both = []
+        for codes, scales, more in ((Kc, ks, kg), (Vc, vs, vg)):
+            s = torch.repeat_interleave(scales[:, g].double(), block, dim=1)[:, :S, None]
+            v = codes[:, g].double() * s
+            v = [v[i, :live[i]] for i in range(n)]
+            if more is not None:
+                v.append(torch.from_numpy(f64(more[:, g])).cuda())
+            both.append(torch.cat(v))
+        k, v = both[0].t().contiguous(), both[1]
+        y = x[:, g * group:(g + 1) * group].reshape(Tq * group, d)
+        s = ((y @ k) * scale).masked_fill_(dead, -np.inf)
+        most = max(most, float((y.abs() @ k.abs()).masked_fill_(dead, 0).max()) * scale)
+        ell = torch.logsumexp(s, dim=1)
+        p = torch.exp_(s - ell[:, None])
+        for out, w in ((o, v), (size, v.abs())):
+            out[:, g * group:(g + 1) * group] = (p @ w).view(Tq, group, d)
+        lse[g * group:(g + 1) * group] = ell.view(Tq, group).t()
+    return (o.cpu().numpy(), lse.cpu().numpy(), size.cpu().numpy(), most), dead.shape[1]
 
 
 def check(o, lse, ref, keys, what, bf16_out=False):
@@ -79,5 +124,5 @@ def softmax_scale(d):
     return 1.0 / math.sqrt(d)
 
 
-__all__ = ["DTYPES", "spread", "codes_of", "dev_codes", "dev_cache", "reference", "check", "host",
+__all__ = ["DTYPES", "spread", "codes_of", "dev_codes", "dev_cache", "reference", "long_reference", "check", "host",
            "normal", "f64", "to_dev_bf16", "softmax_scale", "oq"]

@@ -10,7 +10,7 @@ import paper_2607_20457_amd as P
 from tests._blocks import dev_i32, dev_mask, random_tree
 from oracle import blocks as ob
 from tests._quant import (DTYPES, check, codes_of, dev_cache, dev_codes, f64, host, normal, oq,
-                          reference, softmax_scale, spread, to_dev_bf16)
+                          long_reference, reference, softmax_scale, spread, to_dev_bf16)
 
 pytestmark = pytest.mark.gpu
 
@@ -218,19 +218,23 @@ def test_read_back_again(fmt):
 
 
 def _attn(Hq, Hkv, d, Tq, G, n, S, block, fmt, seed, sees=None, rows=None, gen=True,
-          bf16_out=False, q_scale=1.0, what=""):
+          bf16_out=False, q_scale=1.0, what="", long=False):
     print(f"phase2_quant parity: {what} Hq={Hq} Hkv={Hkv} d={d} Tq={Tq} G={G} {n}x{S} "
           f"block={block} {fmt}", flush=True)
     q = normal(seed, (Tq, Hq, d), q_scale)
     k, v = (spread(seed + i, (n, S, Hkv, d)) for i in (1, 2))
     kg, vg = (normal(seed + i, (G + Tq, Hkv, d)) for i in (3, 4)) if gen else (None, None)
-    cache, (K, V) = dev_cache(k, v, block, fmt)
+    if long:  # (the oracle quantises block by block)
+        cache = P.kv_quantize(to_dev_bf16(k), to_dev_bf16(v), block, DTYPES[fmt])
+    else:
+        cache, (K, V) = dev_cache(k, v, block, fmt)
     o, lse = P.phase2_quant(to_dev_bf16(q), *cache, block,
                             None if rows is None else dev_i32(rows),
                             *((to_dev_bf16(kg), to_dev_bf16(vg), G) if gen else ()),
                             mask=None if sees is None else dev_mask(sees),
                             o_dtype=P.OUT_BF16 if bf16_out else P.OUT_F32)
-    ref, keys = reference(q, K, V, rows, kg, vg, G, sees, softmax_scale(d))
+    rest = rows, kg, vg, G, sees, softmax_scale(d)
+    ref, keys = long_reference(q, cache, block, *rest) if long else reference(q, K, V, *rest)
     check(o, lse, ref, max(keys, 1), what, bf16_out)
 
 
@@ -272,13 +276,24 @@ def test_attention_over_many_steps(Hq, Hkv, d, Tq, fmt):
 
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("Hq,Hkv,d,Tq,n,S", [
-    (64, 64, 128, 1, 2, 6000),   # six steps of every wave, most of them whole
-    (64, 64, 64, 1, 1, 12000),
-    (128, 64, 128, 20, 1, 2100),  # several tiles of a head
-    (32, 32, 64, 128, 1, 8300),  # more than a wave's table holds at a time
+    (64, 64, 128, 1, 1, 3500),    # 16 columns: three steps of every wave, most of them whole
+    (128, 128, 128, 1, 1, 17600), # more steps than a wave's table holds at a time
+    (128, 64, 128, 20, 1, 4200),  # 48 columns, 40 of them in use
+    (64, 8, 128, 6, 3, 11000),    # 48, whole ones
+    (64, 64, 128, 192, 1, 8700),  # four tiles of 48, more than the table
+    (64, 64, 128, 30, 1, 6300),   # 32 columns in steps of 32 rows
+    (16, 16, 128, 64, 1, 12400),  # 32 columns in steps of 64 rows
+    (64, 64, 64, 128, 1, 8700),   # more than the table
+    (60, 4, 64, 20, 2, 8300),     # 15 heads per KV head
 ])
 def test_attention_of_full_waves(Hq, Hkv, d, Tq, n, S, fmt):
-    _attn(Hq, Hkv, d, Tq, 70, n, S, 64, fmt, 135, what="full waves")
+    _attn(Hq, Hkv, d, Tq, 70, n, S, 64, fmt, 135, what="full waves", long=True)
+    # a tree of drafts over shards that are filled to different lengths
+    rng = np.random.default_rng(136)
+    sees, _ = ob.tree_visible(random_tree(Tq, Tq))
+    rows = np.r_[S - rng.integers(0, 500, n - 1), S - 77]
+    _attn(Hq, Hkv, d, Tq, 13, n, S, 16, fmt, 137, sees=sees, rows=rows, bf16_out=True,
+          what="full waves, a tree, lengths", long=True)
 
 
 @pytest.mark.parametrize("fmt", FMTS)
