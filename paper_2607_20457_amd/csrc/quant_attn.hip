@@ -741,7 +741,7 @@ constexpr int QA_ONE_EACH = 256, QA_AT_ONCE = 512;
 // Four shapes of tiles.  Each code is widened and read once for all columns of a tile, so wide
 // tiles do less, but narrow ones wait less: 16 columns have four waves to a SIMD, the others
 // two.
-//   16 columns, steps of 32 rows, eight waves: up to 12 steps of a wave with all compute units
+//   16 columns, steps of 32 rows, eight waves: up to 13 steps of a wave with all compute units
 //   at work.  Us with the merge, 16 columns / the best of the others: 32 / 8 heads of 128, 8
 //   tokens over 32768 keys 20.9 / 22.9, 49152 28.6 / 27.5; 12 tokens 24.3 / 26.0, 33.3 / 31.4; 24
 //   tokens over 16384 24.7 / 23.0; 16 / 16 of 64, 24 tokens over 16384 16.7 / 16.7, 32768 21.8 /
@@ -775,7 +775,7 @@ QuantPlan quant_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int d, in
                             at_once / 8);
     return p;
   };
-  if ((int64_t)Tq * group > 16 && tiles(16) * Hkv * steps(32) >= 12 * 8 * QA_ONE_EACH) {
+  if ((int64_t)Tq * group > 16 && tiles(16) * Hkv * steps(32) >= 13 * 8 * QA_ONE_EACH) {
     const int64_t of32 = tiles(32);
     if (d == 128 && 3 * tiles(48) <= 2 * of32) return take(48, 32, QA_ONE_EACH);
     if (d == 128 && of32 == 1) return take(32, 32, QA_ONE_EACH);

@@ -278,11 +278,11 @@ def test_attention_over_many_steps(Hq, Hkv, d, Tq, fmt):
 @pytest.mark.parametrize("Hq,Hkv,d,Tq,n,S", [
     (64, 64, 128, 1, 1, 3500),    # 16 columns: three steps of every wave, most of them whole
     (128, 128, 128, 1, 1, 17600), # more steps than a wave's table holds at a time
-    (128, 64, 128, 20, 1, 4200),  # 48 columns, 40 of them in use
-    (64, 8, 128, 6, 3, 11000),    # 48, whole ones
+    (128, 64, 128, 20, 1, 4700),  # 48 columns, 40 of them in use
+    (64, 8, 128, 6, 3, 12500),    # 48, whole ones
     (64, 64, 128, 192, 1, 8700),  # four tiles of 48, more than the table
-    (64, 64, 128, 30, 1, 6300),   # 32 columns in steps of 32 rows
-    (16, 16, 128, 64, 1, 12400),  # 32 columns in steps of 64 rows
+    (64, 64, 128, 30, 1, 7100),   # 32 columns in steps of 32 rows
+    (16, 16, 128, 64, 1, 14000),  # 32 columns in steps of 64 rows
     (64, 64, 64, 128, 1, 8700),   # more than the table
     (60, 4, 64, 20, 2, 8300),     # 15 heads per KV head
 ])
