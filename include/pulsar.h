@@ -655,9 +655,10 @@ int pulsar_kv_dequantize(const void* k_codes, const void* v_codes, const float* 
  * EINVAL: negative sizes, Hq % Hkv != 0, NULL or misaligned pointers when there is work,
  *         only one of Kg and Vg, a mask or G > 0 without them, scale not finite and > 0,
  *         unknown o_dtype or format.  EWORKSPACE: workspace too small.
- * EUNSUPPORTED: d not in {64, 128}; another block; n_shards * S >= 2^31; rows with
- *         n_shards > 1024; G + Tq >= 2^24; a row of Kg of 16 MiB or more; more workgroups
- *         than a launch holds (none below Tq * Hkv * ceil(Hq / Hkv / 16) = 2^23).
+ * EUNSUPPORTED: d not in {64, 128}; another block; n_shards * S >= 2^31 or n_shards *
+ *         ceil(S / 32) >= 2^30; rows with n_shards > 1024; G + Tq >= 2^24; a row of Kg of 16
+ *         MiB or more; more workgroups than a launch holds (none below Tq * Hkv * ceil(Hq /
+ *         Hkv / 16) = 2^23).
  */
 size_t pulsar_phase2_quant_workspace_bytes(int Tq, int Hq, int Hkv, int d);
 size_t pulsar_phase2_quant_call_bytes(int n_shards, int Tq, int64_t S, int64_t gen_rows, int Hq,

@@ -147,7 +147,8 @@ int pulsar_phase2_quant(const void* q, const void* k_codes, const void* v_codes,
     return PULSAR_EINVAL;
   if ((d != 64 && d != 128) || !quant_block(block)) return PULSAR_EUNSUPPORTED;
   if (S > kMaxInt || Tq >= PULSAR_MAX_ROWS || G >= PULSAR_MAX_ROWS || G + Tq >= PULSAR_MAX_ROWS ||
-      (int64_t)Hkv * d * 2 >= 1 << 24 || (int64_t)n_shards * S > kMaxInt)
+      (int64_t)Hkv * d * 2 >= 1 << 24 || (int64_t)n_shards * S > kMaxInt ||
+      (int64_t)n_shards * ((S + 31) / 32) >= 1 << 30)
     return PULSAR_EUNSUPPORTED;
   const bool keys = n_shards > 0 && S > 0;
   if (keys && rows != nullptr && n_shards > kMaxQuantShards) return PULSAR_EUNSUPPORTED;

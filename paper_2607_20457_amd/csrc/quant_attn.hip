@@ -3,12 +3,12 @@
 //
 // Work.  A tile is 16 CG columns of one KV head: column n is head n % group of the
 // tile's token n / group (or, of a larger group, 16 CG of one token's heads).  Its
-// keys are steps of 64 rows of a shard, or of 32 rows of the generation shard: 64 D bytes
-// of K and of V either way.  A workgroup takes one part of a tile's steps, wave w of NW
-// the steps w, w + NW, ... of it on its own; then the waves' states are merged through
+// keys are steps of KEYS rows of a shard, or of KEYS / 2 rows of the generation shard: KEYS
+// * D bytes of K and of V either way.  A workgroup takes one part of a tile's steps, wave w
+// of NW the steps w, w + NW, ... of it on its own; then the waves' states are merged through
 // LDS, and the parts by the log-sum-exp merge.  A step of a wave:
 //   K, V  into the wave's LDS stage by loads that write LDS directly: a head's rows
-//       are contiguous, so a step is 64 D consecutive bytes;
+//       are contiguous, so a step is KEYS * D consecutive bytes;
 //   S^T = K Q^T (16x16x32), K's codes widened to bf16, which holds them exactly, as
 //       they are read: lane (r, g) takes channels D/4 * g .. of row r, so that 16 bytes
 //       are two operands; the queries lie in the same order.  Then O^T += V^T P^T, V read
@@ -21,6 +21,17 @@
 //       log-sum-exp uses the fp32 sum.
 // The next step's K is sent for once the scores have consumed this one's, its V once PV
 // has.
+//
+// What bounds it.  One token: HBM.  16 x 8192 keys of 8 heads of 128 (268 MB of codes) take
+// 41 to 44 us and the merge 4: 6.3 TB/s, where a read alone reaches 6.5.  Many tokens: vector
+// instructions.  64 tokens over the same keys take 200 to 214 us with the merge (0.67
+// PFLOP/s; vector issue 73 % and matrix units 31 % busy).  A step of 64 keys and 32 columns has
+// 64 matrix instructions, and beside them 128 that widen codes and some ten for each of a
+// lane's 32 scores; int8 codes take three to widen a pair, not one (257 us).  Tried there and
+// no faster: three waves to a SIMD (199 to 206 us), key and value stages shared by two or
+// four waves, 64 columns a wave with one wave to a SIMD (265).  e4m3 codes in the matrix unit
+// as they are, q in two e4m3 parts, leave the scores less than fp32's precision: a log-sum-exp
+// was 5e-3 off.
 //
 // What must not be seen.  Rows from a shard's live length on are not loaded (a copy of
 // the step's last live row is) and score -inf; their scales are not read.  Of the new

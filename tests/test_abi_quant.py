@@ -90,7 +90,8 @@ def test_phase2_quant():
                dict(vc=FAKE + 8), dict(Kg=FAKE + 8), dict(Vg=FAKE + 2), dict(o=FAKE + 8)):
         assert call(**kw) == EINVAL, kw
     for kw in (dict(d=96), dict(block=24), dict(block=8), dict(S=1 << 31), dict(G=1 << 24),
-               dict(G=1 << 62), dict(n_shards=1 << 20, S=1 << 11), dict(n_shards=1025, rows=FAKE),
+               dict(G=1 << 62), dict(n_shards=1 << 20, S=1 << 11), dict(n_shards=1 << 30, S=1),
+               dict(n_shards=1025, rows=FAKE),
                dict(Hkv=1 << 17, Hq=1 << 17), dict(Tq=1 << 23, Hq=128),
                dict(Tq=1 << 23, Hkv=1, Hq=128)):
         assert call(**kw) == EUNSUP, kw
