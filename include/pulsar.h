@@ -639,8 +639,8 @@ int pulsar_kv_dequantize(const void* k_codes, const void* v_codes, const float* 
  *
  * q         bf16 [Tq, Hq, d].
  * codes, scales  as for pulsar_kv_quantize, with n = n_shards and capacity = S (nullable
- *           when n_shards or S is 0).  A scale that is NaN makes its block NaN; one below
- *           2^-100 counts as 2^-100.
+ *           when n_shards or S is 0).  A scale that is NaN (of V: or above 2^124, which quantising
+ *           does not write) makes its block NaN; one below 2^-100 counts as 2^-100.
  * rows      int32 [n_shards] on the device, nullable: shard i's live rows are [0, rows[i])
  *           (clamped to [0, S]; NULL: S).  Nothing behind them is read, so a cache may grow
  *           between two replays of a captured call.

@@ -27,7 +27,7 @@
 // instructions.  64 tokens over the same keys take 200 to 214 us with the merge (0.67
 // PFLOP/s; vector issue 73 % and matrix units 31 % busy).  A step of 64 keys and 32 columns has
 // 64 matrix instructions, and beside them 128 that widen codes and some ten for each of a
-// lane's 32 scores; int8 codes take three to widen a pair, not one (257 us).  Tried there and
+// lane's 32 scores; int8 codes take three to widen a pair, not one (257 to 265 us).  Tried there and
 // no faster: three waves to a SIMD (199 to 206 us), key and value stages shared by two or
 // four waves, 64 columns a wave with one wave to a SIMD (265).  e4m3 codes in the matrix unit
 // as they are, q in two e4m3 parts, leave the scores less than fp32's precision: a log-sum-exp
@@ -47,6 +47,8 @@ namespace {
 
 constexpr float QA_SLACK = 8.0f;      // log2 slack before the reference is raised
 constexpr float QA_LEAST = 0x1p-100f; // a smaller scale counts as this
+constexpr float QA_BIG = 0x1p64f;     // scales of V whose weights get no slack ...
+constexpr float QA_MOST = 0x1p124f;   // ... and whose sums leave fp32 all the same
 constexpr int QA_SHARDS = 1024;       // shards with lengths of their own
 
 struct QuantAttnArgs {
@@ -265,25 +267,27 @@ void quant_attn_kernel(QuantAttnArgs a) {
   // scores, log2 vs and 1 / vs.
   int tab_rows = 0;
   float tab_ck = c2, tab_lv = 0.f, tab_iv = 1.f;
-  uint64_t nan_v = 0;  // halves whose vs is not a number
+  uint64_t nan_v = 0, big_v = 0;  // halves whose vs is no number or above QA_MOST, and above QA_BIG
   auto fill_use = [&](const Place& x) {
     tab_rows = x.rows;
     tab_ck = c2;
     tab_lv = 0.f;
     tab_iv = 1.f;
-    bool bad = false;
+    bool bad = false, big = false;
     if (x.scale >= 0) {
       float k = a.ks[x.scale], v = a.vs[x.scale];
       k = k < QA_LEAST ? QA_LEAST : k;
       v = v < QA_LEAST ? QA_LEAST : v;
-      bad = v != v;
+      bad = !(v <= QA_MOST);
       // (a factor of zero would make -inf a NaN)
       k *= c2;
       tab_ck = k < 0x1p-126f ? 0x1p-126f : k;
+      big = v > QA_BIG;
       tab_lv = bad ? 0.f : __log2f(v);
       tab_iv = bad ? 1.f : 1.f / v;
     }
     nan_v = __ballot(bad);
+    big_v = __ballot(big);
   };
   auto lane_f = [&](float x, int at) {
     return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), at));
@@ -409,15 +413,15 @@ void quant_attn_kernel(QuantAttnArgs a) {
   }
   // The reference of every group against mx, the largest of a lane's scores of it: raised
   // where it has to be, O and the sums rescaled.
-  auto raise = [&](const float* mx) {
+  auto raise = [&](const float* mx, float slack) {
     bool any = false;
 #pragma unroll
-    for (int c = 0; c < CG; ++c) any |= mx[c] > m_run[c] + QA_SLACK;
+    for (int c = 0; c < CG; ++c) any |= mx[c] > m_run[c] + slack;
     if (!__any(any)) return;
 #pragma unroll
     for (int c = 0; c < CG; ++c) {
       const float top = max_of_rows(mx[c]);
-      const float m_new = top > m_run[c] + QA_SLACK ? top : m_run[c];
+      const float m_new = top > m_run[c] + slack ? top : m_run[c];
       const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[c] - m_new);
 #pragma unroll
       for (int e = 0; e < DT; ++e) acc[c][e] *= alpha;
@@ -519,6 +523,8 @@ void quant_attn_kernel(QuantAttnArgs a) {
       iv[h] = lane_f(tab_iv, at + h);
     }
     const uint32_t bad_v = (uint32_t)(nan_v >> at) & ((1u << HALVES) - 1);
+    // (weights times a scale of up to 2^124 stay in fp32 if they are 1 at most)
+    const float slack = (big_v >> at & ((1u << HALVES) - 1)) != 0 ? 0.f : QA_SLACK;
     need_k();
     f32x4 S[CG][HALVES];
 #pragma unroll
@@ -555,7 +561,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
 #pragma unroll
       for (int h = 0; h < HALVES; ++h) mx[c] = fmaxf(mx[c], largest(S[c][h]) * ck[h]);
     }
-    raise(mx);
+    raise(mx, slack);
     need_v(j + 1 < nsteps);
 #pragma unroll
     for (int u = 0; u < HALVES / 2; ++u) {
@@ -617,7 +623,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
       }
       mx[c] = fmaxf(largest(S[c][0]), largest(S[c][1])) * c2;
     }
-    raise(mx);
+    raise(mx, QA_SLACK);
     bf16x8 P[CG];
 #pragma unroll
     for (int c = 0; c < CG; ++c) {

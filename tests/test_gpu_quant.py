@@ -423,6 +423,47 @@ def test_attention_with_any_scales(block, fmt):
     check(o, lse, (o_ref, lse_ref, size + 1e-25, most + extra * 2.0 ** 24 / (d + 4)), keys, fmt)
 
 
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("Hkv,d,Tq,S", [(32, 64, 1, 4096), (32, 128, 24, 1 << 14)])
+def test_values_near_the_largest(Hkv, d, Tq, S, fmt):
+    # Keys whose weights are 2^7.5 times those of the keys that a wave sees before them (32 or
+    # 64 rows each wave of four or eight) and whose values, 2^127 in one channel, times such a
+    # weight leave fp32: the log-sum-exp and the other channels stay what they are.
+    high = (np.arange(S) // 256 % 2 == 1)
+    q, k, v = (np.zeros(x) for x in ((Tq, Hkv, d), (1, S, Hkv, d), (1, S, Hkv, d)))
+    q[..., 0] = 1.0
+    k[0, high, :, 0] = 1.0
+    v[0, high, :, 3] = 2.0 ** 127
+    v[0, ~high, :, 5] = 1.0
+    q, k, v = (torch.from_numpy(x).to(torch.bfloat16).cuda() for x in (q, k, v))
+    o, lse = P.phase2_quant(q, *P.kv_quantize(k, v, 32, DTYPES[fmt]), 32,
+                            softmax_scale=7.5 * math.log(2.0))
+    total = S / 2 * (1 + 2 ** 7.5)
+    # (scores are exact but for the scale and the base change; sums as in tests._blocks.check)
+    off = 7.5 * 2.0 ** -22 + (S + 64) * 2.0 ** -23
+    assert np.abs(host(lse) - math.log(total)).max() <= off
+    o = host(o)
+    assert np.abs(o[..., 5] - S / 2 / total).max() <= (2.0 ** -7 + 2 * off) * S / 2 / total
+    assert (np.delete(o, [3, 5], axis=-1) == 0).all()
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_scales_of_v_out_of_range(fmt):
+    c = _small(310)
+    (Kc, Vc, ks, vs), vals = dev_cache(c["k"], c["v"], c["block"], fmt)
+    vs[0, 0, 0], vs[1, 0, 1] = math.inf, 2.0 ** 125
+    o, lse = P.phase2_quant(to_dev_bf16(c["q"]), Kc, Vc, ks, vs, c["block"], None,
+                            to_dev_bf16(c["kg"]), to_dev_bf16(c["vg"]), c["G"])
+    ref, keys = reference(c["q"], *vals, None, c["kg"], c["vg"], c["G"], None,
+                          softmax_scale(c["d"]))
+    half = c["q"].shape[1] // c["k"].shape[2]
+    assert np.isnan(host(o)[:, :half]).all()
+    check(o[:, half:], lse[half:], (ref[0][:, half:], ref[1][half:], ref[2][:, half:], ref[3]),
+          keys, "the other heads")
+    zero = np.zeros_like(ref[0])
+    check(torch.zeros_like(o), lse, (zero, ref[1], zero, ref[3]), keys, "lse")
+
+
 @pytest.mark.parametrize("q_scale", [1e-3, 30.0])
 def test_attention_of_flat_and_peaked_scores(q_scale):
     _attn(8, 2, 128, 3, 50, 2, 500, 64, "e4m3", 200, q_scale=q_scale, what=f"q times {q_scale}")
