@@ -618,8 +618,9 @@ int pulsar_phase2_sparse(const void* q, const void* K, const void* V, const int3
  * EINVAL: negative sizes, Hkv < 1, d < 1, block < 1, an unknown format, first or rows past
  *         the capacity, first not a multiple of block (quantising), NULL or misaligned
  *         pointers or strides when there is work, or memory in common.
- * EUNSUPPORTED: d not in {64, 128}; another block; capacity >= 2^31 or Hkv * d >= 2^23;
- *         more workgroups than a launch holds (none below n * ceil(rows / 64) * Hkv = 2^21).
+ * EUNSUPPORTED: d not in {64, 128}; another block; capacity >= 2^31, Hkv * d >= 2^23 or 2^48
+ *         codes and more; more workgroups than a launch holds (none below n * ceil(rows / 64)
+ *         * Hkv = 2^21).
  */
 int pulsar_kv_quantize(const void* K, const void* V, int64_t shard_stride, int64_t row_stride,
                        int n, int64_t rows, int Hkv, int d, int block, int format, int64_t first,

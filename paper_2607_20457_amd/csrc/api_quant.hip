@@ -21,7 +21,9 @@ int check_rows(int n, int64_t rows, int Hkv, int d, int block, int format, int64
     return PULSAR_EINVAL;
   if (first > capacity || rows > capacity - first) return PULSAR_EINVAL;
   if ((d != 64 && d != 128) || !quant_block(block)) return PULSAR_EUNSUPPORTED;
-  if (capacity > kMaxInt || (int64_t)Hkv * d >= 1 << 23) return PULSAR_EUNSUPPORTED;
+  if (capacity > kMaxInt || (int64_t)Hkv * d >= 1 << 23 ||
+      (__int128)n * capacity * Hkv * d >= (__int128)1 << 48)
+    return PULSAR_EUNSUPPORTED;
   return PULSAR_OK;
 }
 

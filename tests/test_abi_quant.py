@@ -58,6 +58,7 @@ def test_kv_quantize():
             assert call(**kw) == EHIP, kw
     for kw in (dict(d=96), dict(block=8, first=0), dict(block=48, first=48),
                dict(block=512, first=0), dict(capacity=1 << 31), dict(Hkv=1 << 17),
+               dict(n=1 << 22, capacity=1 << 20, Hkv=1),
                dict(n=1 << 24, kc=1 << 50, vc=1 << 51, ks=1 << 52, vs=1 << 53, K=1 << 54, V=1 << 54)):
         assert call(**kw) == EUNSUP, kw
     assert call(n=0, K=None, V=None) == 0 and call(rows=0, K=None, kc=None) == 0
@@ -74,7 +75,9 @@ def test_kv_dequantize():
                dict(kc=FAKE + 8), dict(vc=FAKE + 1)):
         assert call(**kw) == EINVAL, kw
     for kw in (dict(d=96), dict(block=8), dict(block=48), dict(block=512),
-               dict(capacity=1 << 31), dict(Hkv=1 << 17), dict(n=1 << 30)):
+               dict(capacity=1 << 31), dict(Hkv=1 << 17), dict(n=1 << 30),
+               dict(n=(1 << 31) - 1, capacity=(1 << 31) - 64, rows=(1 << 31) - 100, Hkv=1 << 16),
+               dict(n=1 << 22, capacity=1 << 20, Hkv=1)):
         assert call(**kw) == EUNSUP, kw
     assert call(n=0, K=None) == 0 and call(rows=0, K=None, kc=None) == 0
 

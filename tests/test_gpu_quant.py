@@ -296,6 +296,41 @@ def test_attention_of_full_waves(Hq, Hkv, d, Tq, n, S, fmt):
           what="full waves, a tree, lengths", long=True)
 
 
+@pytest.mark.parametrize("lengths", [False, True])
+@pytest.mark.parametrize("Hq,Hkv,d,Tq,n,S", [
+    (32, 8, 128, 1, 4, 1021), (16, 16, 64, 24, 5, 3001), (32, 8, 128, 12, 4, 8192),
+    (32, 8, 128, 12, 16, 8192), (64, 8, 128, 6, 3, 12500), (32, 8, 128, 8, 7, 9999),
+    (16, 16, 128, 64, 1, 14000), (64, 64, 64, 128, 1, 8700), (20, 1, 64, 3, 2, 77),
+])
+def test_every_row_counts_once(Hq, Hkv, d, Tq, n, S, lengths):
+    # Equal weights and a code in every row of V: a row that a plan drops, doubles or replaces
+    # shows as a whole 1 in a channel.  Scores are 0, weights and their sums whole numbers, so
+    # that only the log-sum-exps of the parts (log2 of at most 2^18, off by an ulp of it and
+    # of its product: 2^-18), the weights that merge them and a division are rounded.
+    G, rng = 45, np.random.default_rng(160)
+    rows = rng.integers(0, S + 1, n) if lengths else np.full(n, S)
+    rows[-1] = S - 13 * lengths
+    q = torch.zeros((Tq, Hq, d), dtype=torch.bfloat16, device="cuda")
+    k, kg = (torch.ones(x, dtype=torch.bfloat16, device="cuda")
+             for x in ((n, S, Hkv, d), (G + Tq, Hkv, d)))
+    nth = np.arange(n * S).reshape(n, S)
+    live = np.arange(S) < rows[:, None]
+    for code in (lambda i: i % d, lambda i: i // d % d):
+        vs, vg = (torch.nn.functional.one_hot(torch.from_numpy(code(i)).cuda(), d)
+                  .to(torch.bfloat16).unsqueeze(-2).expand(*i.shape, Hkv, d).contiguous()
+                  for i in (nth, n * S + np.arange(G + Tq)))
+        o, lse = P.phase2_quant(q, *P.kv_quantize(k, vs, 64), 64,
+                                dev_i32(rows) if lengths else None, kg, vg, G)
+        counts = np.bincount(code(nth)[live], minlength=d).astype(float)
+        for i in range(G):
+            counts[code(n * S + i)] += 1
+        for t in range(Tq):
+            counts[code(n * S + G + t)] += 1
+            total = counts.sum()
+            assert np.abs(host(o[t]) * total - counts).max() <= 2.0 ** -16 * counts.max(), t
+            assert np.abs(host(lse[:, t]) - math.log(total)).max() <= 2.0 ** -17, t
+
+
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("block", [16, 64, 256])
 def test_attention_over_live_rows(block, fmt):
