@@ -773,6 +773,11 @@ constexpr int QA_ONE_EACH = 256, QA_AT_ONCE = 512;
 // columns where waves would have ten steps or more and d is 64 or tiles share their keys (one /
 // two: 32 / 8 heads of 128, 1 token over 131072 keys 46.8 / 48.5, 16384 13.4 / 14.4, 12 tokens
 // over 32768 26.5 / 24.3; 16 / 16 of 64, 1 token over 131072 50.7 / 48.4, 4 x 1021 9.4 / 10.4).
+// But one part up to five steps of a wave: parts need the merge's launch and a workspace, 4 us
+// of the host's time.  Device / call from the host, several parts and one, 32 / 8 heads of 128,
+// 1 token over 480 keys 8.7 / 15.9 and 7.9 / 11.7, 1000 9.0 / 15.9 and 9.9 / 11.6, 1500 9.4 / 15.8
+// and 13.5 / 13.6 (a wave alone waits for each step's loads, 1.8 us a step); 16 / 16 of 64, 24
+// tokens over 1000 keys 8.7 / 15.8 and 8.6 / 11.4.
 QuantPlan quant_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int d, int64_t gen_rows) {
   QuantPlan p{};
   const int group = Hq / Hkv;
@@ -799,7 +804,8 @@ QuantPlan quant_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int d, in
     return take(32, 64, QA_AT_ONCE);
   }
   take(16, 32, QA_ONE_EACH);
-  if (steps(32) >= 10 * 8 * (int64_t)p.parts && (d == 64 || tiles(16) > 1))
+  if (steps(32) <= 5 * 8) p.parts = 1;
+  else if (steps(32) >= 10 * 8 * (int64_t)p.parts && (d == 64 || tiles(16) > 1))
     take(16, 32, QA_AT_ONCE);
   return p;
 }
