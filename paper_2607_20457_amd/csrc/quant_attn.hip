@@ -481,6 +481,11 @@ void quant_attn_kernel(QuantAttnArgs a) {
     }
   }
   fill_use(first);
+  // (Q is there: else the compiler waits for it in every step, and so for all loads before)
+#pragma unroll
+  for (int c = 0; c < CG; ++c)
+#pragma unroll
+    for (int s = 0; s < DS; ++s) asm volatile("" : "+v"(qf[c][s]));
 
   // A wave has one stage: K of step j + 1 is sent for once the scores have consumed this
   // one's, its V once PV has.
