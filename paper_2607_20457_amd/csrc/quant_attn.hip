@@ -13,8 +13,10 @@
 //       they are read: lane (r, g) takes channels D/4 * g .. of row r, so that 16 bytes
 //       are two operands; the queries lie in the same order.  Then O^T += V^T P^T, V read
 //       transposed in 8 bits and widened;
-//   softmax  online, log2 domain, the reference raised when a step's maximum exceeds
-//       it by more than 2^8.  A score is (q . code) * (scale * ks log2 e), one product of
+//   softmax  online, log2 domain.  A step's weights are formed against the reference as it
+//       is; only where their sums show a score more than 2^8 above it is the step's maximum
+//       looked for, the reference raised and the step weighed again (a maximum in every step:
+//       64 tokens over 16 x 8192 keys 203 us against 195, int8 259 / 245).  A score is (q . code) * (scale * ks log2 e), one product of
 //       the block; the weight that enters PV is exp2(score - reference + log2 vs): V's
 //       scale is in it before it is rounded to bf16 (2^-8 of each at most), and sums of
 //       weights are taken times 1 / vs.  O is divided by the sum of the rounded weights, the
@@ -24,14 +26,13 @@
 //
 // What bounds it.  One token: HBM.  16 x 8192 keys of 8 heads of 128 (268 MB of codes) take
 // 41 to 44 us and the merge 4: 6.3 TB/s, where a read alone reaches 6.5.  Many tokens: vector
-// instructions.  64 tokens over the same keys take 200 to 214 us with the merge (0.67
-// PFLOP/s; vector issue 73 % and matrix units 31 % busy).  A step of 64 keys and 32 columns has
-// 64 matrix instructions, and beside them 128 that widen codes and some ten for each of a
-// lane's 32 scores; int8 codes take three to widen a pair, not one (257 to 265 us).  Tried there and
-// no faster: three waves to a SIMD (199 to 206 us), key and value stages shared by two or
-// four waves, 64 columns a wave with one wave to a SIMD (265).  e4m3 codes in the matrix unit
-// as they are, q in two e4m3 parts, leave the scores less than fp32's precision: a log-sum-exp
-// was 5e-3 off.
+// instructions.  64 tokens over the same keys take 195 us with the merge (0.71 PFLOP/s).  A
+// step of 64 keys and 32 columns has 64 matrix instructions, and beside them 128 that widen
+// codes and seven or eight for each of a lane's 32 scores; int8 codes take three to widen a
+// pair, not one (245 us).  Tried there and no faster: key and value stages shared by two or
+// four waves, 64 columns a wave with one wave to a SIMD (265 us when this took 201).  e4m3
+// codes in the matrix unit as they are, q in two e4m3 parts, leave the scores less than fp32's
+// precision: a log-sum-exp was 5e-3 off.
 //
 // What must not be seen.  Rows from a shard's live length on are not loaded (a copy of
 // the step's last live row is) and score -inf; their scales are not read.  Of the new
@@ -46,6 +47,7 @@
 namespace {
 
 constexpr float QA_SLACK = 8.0f;      // log2 slack before the reference is raised
+constexpr float QA_OVER = 4 * 0x1p8f; // a lane's four weights of 2^QA_SLACK
 constexpr float QA_LEAST = 0x1p-100f; // a smaller scale counts as this
 constexpr float QA_BIG = 0x1p64f;     // scales of V whose weights get no slack ...
 constexpr float QA_MOST = 0x1p124f;   // ... and whose sums leave fp32 all the same
@@ -413,6 +415,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
   }
   // The reference of every group against mx, the largest of a lane's scores of it: raised
   // where it has to be, O and the sums rescaled.
+  bool unset = true;  // columns without a reference (the same in all lanes)
   auto raise = [&](const float* mx, float slack) {
     bool any = false;
 #pragma unroll
@@ -429,9 +432,14 @@ void quant_attn_kernel(QuantAttnArgs a) {
       lr_run[c] *= alpha;
       m_run[c] = m_new;
     }
+    bool still = false;
+#pragma unroll
+    for (int c = 0; c < CG; ++c) still |= m_run[c] == -INFINITY;
+    unset = __any(still);
   };
-  // Weights of two halves of group c as PV takes them in, and their sums.
-  auto weigh = [&](int c, const f32x4* S, const float* ck, const float* lv, const float* iv) {
+  // Weights of two halves of group c as PV takes them in; their sums are added to l and lr.
+  auto weigh = [&](int c, const f32x4* S, const float* ck, const float* lv, const float* iv,
+                   float& l, float& lr) {
     // a column that has seen no key takes its weights against 0: they come out 0
     const float m_use = m_run[c] == -INFINITY ? 0.f : m_run[c];
     f32x8 p;
@@ -441,7 +449,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
       for (int v = 0; v < 4; ++v)
         p[4 * h + v] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[h][v], ck[h], lv[h] - m_use));
       const float sum = (p[4 * h] + p[4 * h + 1]) + (p[4 * h + 2] + p[4 * h + 3]);
-      l_run[c] = __builtin_fmaf(sum, iv[h], l_run[c]);
+      l = __builtin_fmaf(sum, iv[h], l);
     }
     const bf16x8 P = __builtin_convertvector(p, bf16x8);
 #pragma unroll
@@ -450,7 +458,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
                                                   false);
       sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{P[4 * h + 2], P[4 * h + 3]}, kOnes2, sum,
                                             false);
-      lr_run[c] = __builtin_fmaf(sum, iv[h], lr_run[c]);
+      lr = __builtin_fmaf(sum, iv[h], lr);
     }
     return P;
   };
@@ -528,8 +536,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
       iv[h] = lane_f(tab_iv, at + h);
     }
     const uint32_t bad_v = (uint32_t)(nan_v >> at) & ((1u << HALVES) - 1);
-    // (weights times a scale of up to 2^124 stay in fp32 if they are 1 at most)
-    const float slack = (big_v >> at & ((1u << HALVES) - 1)) != 0 ? 0.f : QA_SLACK;
+    const bool big = (big_v >> at & ((1u << HALVES) - 1)) != 0;
     need_k();
     f32x4 S[CG][HALVES];
 #pragma unroll
@@ -559,29 +566,46 @@ void quant_attn_kernel(QuantAttnArgs a) {
           for (int v = 0; v < 4; ++v)
             if (16 * h + 4 * g + v >= rows) S[c][h][v] = -INFINITY;
     }
-    float mx[CG];
+    // The weights against the reference as it is; if a lane's sum shows that a score is above
+    // it by more than QA_SLACK (or where there is none yet), the step's maximum is looked for,
+    // the reference raised and they are formed again.
+    bf16x8 P[CG][HALVES / 2];
+    float l[CG], lr[CG];
+    for (bool raised = unset || big;; raised = true) {
+      if (raised) {
+        float mx[CG];
 #pragma unroll
-    for (int c = 0; c < CG; ++c) {
-      mx[c] = -INFINITY;
+        for (int c = 0; c < CG; ++c) {
+          mx[c] = -INFINITY;
 #pragma unroll
-      for (int h = 0; h < HALVES; ++h) mx[c] = fmaxf(mx[c], largest(S[c][h]) * ck[h]);
+          for (int h = 0; h < HALVES; ++h) mx[c] = fmaxf(mx[c], largest(S[c][h]) * ck[h]);
+        }
+        // (weights times a scale of up to 2^124 stay in fp32 if they are 1 at most)
+        raise(mx, big ? 0.f : QA_SLACK);
+      }
+      bool over = false;
+#pragma unroll
+      for (int c = 0; c < CG; ++c) {
+        l[c] = lr[c] = 0.f;
+#pragma unroll
+        for (int u = 0; u < HALVES / 2; ++u)
+          P[c][u] = weigh(c, S[c] + 2 * u, ck + 2 * u, lv + 2 * u, iv + 2 * u, l[c], lr[c]);
+        over |= l[c] > QA_OVER * HALVES;
+      }
+      if (raised || !__any(over)) break;
     }
-    raise(mx, slack);
+#pragma unroll
+    for (int c = 0; c < CG; ++c) l_run[c] += l[c], lr_run[c] += lr[c];
     need_v(j + 1 < nsteps);
 #pragma unroll
-    for (int u = 0; u < HALVES / 2; ++u) {
-      const int h = 2 * u;
-      bf16x8 P[CG];
-#pragma unroll
-      for (int c = 0; c < CG; ++c) P[c] = weigh(c, S[c] + h, ck + h, lv + h, iv + h);
+    for (int u = 0; u < HALVES / 2; ++u)
 #pragma unroll
       for (int e = 0; e < DT; ++e) {
         const bf16x8 v = v_codes(lane, u, e);
 #pragma unroll
         for (int c = 0; c < CG; ++c)
-          acc[c][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P[c], acc[c][e], 0, 0, 0);
+          acc[c][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P[c][u], acc[c][e], 0, 0, 0);
       }
-    }
     if (bad_v != 0) {
       // values that are not numbers, in blocks that every column sees
 #pragma unroll
@@ -633,7 +657,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
 #pragma unroll
     for (int c = 0; c < CG; ++c) {
       const float one[2] = {1.f, 1.f}, zero[2] = {0.f, 0.f}, cc[2] = {c2, c2};
-      P[c] = weigh(c, S[c], cc, zero, one);
+      P[c] = weigh(c, S[c], cc, zero, one, l_run[c], lr_run[c]);
     }
     need_v(j + 1 < nsteps);
     bool odd = false;  // a value that is not finite
