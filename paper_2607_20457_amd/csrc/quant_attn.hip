@@ -788,15 +788,16 @@ constexpr int QA_ONE_EACH = 256, QA_AT_ONCE = 512;
 // tiles do less, but narrow ones wait less: 16 columns have four waves to a SIMD, the others
 // two.
 //   16 columns, steps of 32 rows, eight waves: up to 13 steps of a wave with all compute units
-//   at work.  Us with the merge, 16 columns / the best of the others: 32 / 8 heads of 128, 8
-//   tokens over 32768 keys 20.9 / 22.9, 49152 28.6 / 27.5; 12 tokens 24.3 / 26.0, 33.3 / 31.4; 24
-//   tokens over 16384 24.7 / 23.0; 16 / 16 of 64, 24 tokens over 16384 16.7 / 16.7, 32768 21.8 /
-//   21.0.
-//   48 columns, as above (d 128; d 64 has the registers for no more than it gains), where that
-//   is a third fewer tiles than of 32: 12 tokens over 131072 keys 55 / 67, 24 tokens 87 / 95, 36
-//   122 / 139; but 64 (6 tiles against 8) 218 / 200.
-//   32 columns, as above (d 128): one tile, bound by its keys: 8 tokens over 131072 52 against
-//   55 of the next shape, 49152 27.5 / 30.7; but two tiles (16 tokens) 72 / 69, 8 tiles 224 / 200.
+//   at work (12 where the others are of 32 columns and d is 128).  Us with the merge, 16 columns
+//   / the best of the others, 32 / 8 heads of 128: 8 tokens over 40960 keys 21.6 / 24.2, 49152
+//   26.5 / 26.4, 57344 30.2 / 28.8; 12 tokens over 32768 23.0 / 25.1, 49152 33.5 / 30.8; 24 over
+//   16384 23.4 / 22.2; 16 / 16 of 64, 24 tokens over 16384 16.0 / 15.7, 32768 21.2 / 20.3.
+//   48 columns, as above (d 128), where that
+//   is a third fewer tiles than of 32: 12 tokens over 131072 keys 55 / 65, 24 tokens 82 / 90, 36
+//   116 / 136; but 64 (6 tiles against 8) 211 / 196.
+//   32 columns, as above (d 128): one tile, bound by its keys (8 tokens over 131072 50 against
+//   54 of the next shape), or up to 28 steps of a wave: 64 tokens over 16384 keys 36.6 / 38.6,
+//   32768 59.4 / 60.5, 49152 85.5 / 83.7, 131072 204 / 196.
 //   32 columns, steps of 64 rows, four waves: the rest.
 // Parts: as many as give each compute unit one workgroup; two for the last shape, and for 16
 // columns where waves would have ten steps or more and d is 64 or tiles share their keys (one /
@@ -826,10 +827,14 @@ QuantPlan quant_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int d, in
                             at_once / 8);
     return p;
   };
-  if ((int64_t)Tq * group > 16 && tiles(16) * Hkv * steps(32) >= 13 * 8 * QA_ONE_EACH) {
-    const int64_t of32 = tiles(32);
-    if (d == 128 && 3 * tiles(48) <= 2 * of32) return take(48, 32, QA_ONE_EACH);
-    if (d == 128 && of32 == 1) return take(32, 32, QA_ONE_EACH);
+  const int64_t of32 = tiles(32);
+  const bool of48 = d == 128 && 3 * tiles(48) <= 2 * of32;
+  const int64_t at_once = 8 * QA_ONE_EACH;  // waves
+  if ((int64_t)Tq * group > 16 &&
+      tiles(16) * Hkv * steps(32) >= (d == 64 || of48 ? 13 : 12) * at_once) {
+    if (of48) return take(48, 32, QA_ONE_EACH);
+    if (d == 128 && (of32 == 1 || of32 * Hkv * steps(32) <= 28 * at_once))
+      return take(32, 32, QA_ONE_EACH);
     return take(32, 64, QA_AT_ONCE);
   }
   take(16, 32, QA_ONE_EACH);

@@ -282,7 +282,8 @@ def test_attention_over_many_steps(Hq, Hkv, d, Tq, fmt):
     (64, 8, 128, 6, 3, 12500),    # 48, whole ones
     (64, 64, 128, 192, 1, 8700),  # four tiles of 48, more than the table
     (64, 64, 128, 30, 1, 7100),   # 32 columns in steps of 32 rows
-    (16, 16, 128, 64, 1, 14000),  # 32 columns in steps of 64 rows
+    (16, 16, 128, 64, 1, 14000),  # two tiles of 32
+    (16, 16, 128, 256, 1, 17600), # 32 columns in steps of 64 rows, more than the table
     (64, 64, 64, 128, 1, 8700),   # more than the table
     (60, 4, 64, 20, 2, 8300),     # 15 heads per KV head
 ])
@@ -301,6 +302,7 @@ def test_attention_of_full_waves(Hq, Hkv, d, Tq, n, S, fmt):
     (32, 8, 128, 1, 4, 1021), (16, 16, 64, 24, 5, 3001), (32, 8, 128, 12, 4, 8192),
     (32, 8, 128, 12, 16, 8192), (64, 8, 128, 6, 3, 12500), (32, 8, 128, 8, 7, 9999),
     (16, 16, 128, 64, 1, 14000), (64, 64, 64, 128, 1, 8700), (20, 1, 64, 3, 2, 77),
+    (16, 16, 128, 256, 1, 17600),
 ])
 def test_every_row_counts_once(Hq, Hkv, d, Tq, n, S, lengths):
     # Equal weights and a code in every row of V: a row that a plan drops, doubles or replaces
