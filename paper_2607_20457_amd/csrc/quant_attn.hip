@@ -26,13 +26,13 @@
 //
 // What bounds it.  One token: HBM.  16 x 8192 keys of 8 heads of 128 (268 MB of codes) take
 // 41 to 44 us and the merge 4: 6.3 TB/s, where a read alone reaches 6.5.  Many tokens: vector
-// instructions.  64 tokens over the same keys take 195 us with the merge (0.71 PFLOP/s).  A
+// instructions.  64 tokens over the same keys take 188 us with the merge (0.73 PFLOP/s).  A
 // step of 64 keys and 32 columns has 64 matrix instructions, and beside them 128 that widen
 // codes and seven or eight for each of a lane's 32 scores; int8 codes take three to widen a
-// pair, not one (245 us).  Tried there and no faster: key and value stages shared by two or
-// four waves, 64 columns a wave with one wave to a SIMD (265 us when this took 201).  e4m3
-// codes in the matrix unit as they are, q in two e4m3 parts, leave the scores less than fp32's
-// precision: a log-sum-exp was 5e-3 off.
+// pair, not one (229 us).  Tried there and no faster: three waves to a SIMD (188), key and
+// value stages shared by two or four waves, 64 columns a wave with one wave to a SIMD (265 us
+// when this took 201).  e4m3 codes in the matrix unit as they are, q in two e4m3 parts, leave
+// the scores less than fp32's precision: a log-sum-exp was 5e-3 off.
 //
 // What must not be seen.  Rows from a shard's live length on are not loaded (a copy of
 // the step's last live row is) and score -inf; their scales are not read.  Of the new
@@ -538,6 +538,9 @@ void quant_attn_kernel(QuantAttnArgs a) {
     const uint32_t bad_v = (uint32_t)(nan_v >> at) & ((1u << HALVES) - 1);
     const bool big = (big_v >> at & ((1u << HALVES) - 1)) != 0;
     need_k();
+    // (a wave at its matrix products goes before one at its weights: 64 tokens over 16 x 8192
+    // keys 196 -> 188 us, int8 246 -> 229)
+    __builtin_amdgcn_s_setprio(1);
     f32x4 S[CG][HALVES];
 #pragma unroll
     for (int h = 0; h < HALVES; ++h) {
@@ -556,6 +559,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
         }
       }
     }
+    __builtin_amdgcn_s_setprio(0);
     scored(j);
     if (rows < KEYS) {
 #pragma unroll
@@ -597,6 +601,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
 #pragma unroll
     for (int c = 0; c < CG; ++c) l_run[c] += l[c], lr_run[c] += lr[c];
     need_v(j + 1 < nsteps);
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int u = 0; u < HALVES / 2; ++u)
 #pragma unroll
@@ -606,6 +611,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
         for (int c = 0; c < CG; ++c)
           acc[c][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, P[c][u], acc[c][e], 0, 0, 0);
       }
+    __builtin_amdgcn_s_setprio(0);
     if (bad_v != 0) {
       // values that are not numbers, in blocks that every column sees
 #pragma unroll
