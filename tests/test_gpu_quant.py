@@ -507,6 +507,28 @@ def test_attention_of_flat_and_peaked_scores(q_scale):
     _attn(8, 8, 64, 20, 50, 2, 500, 64, "int8", 201, q_scale=q_scale, what=f"q times {q_scale}")
 
 
+@pytest.mark.parametrize("rise", [0.4, 2.0, 5.5, 5.6, 8.3, 9.5, 40.0, 95.0, -5.6, -40.0])
+@pytest.mark.parametrize("Hq,Hkv,d,Tq,S", [(8, 2, 64, 2, 2500), (4, 1, 128, 12, 1100),
+                                           (64, 64, 128, 30, 7100)])
+def test_scores_that_rise(Hq, Hkv, d, Tq, S, rise):
+    # The score of a wave's next step is `rise` nats (0.4 to 95: weights of 2^0.6 to 2^137)
+    # above the one before, of a few of its keys or of all of them
+    rng = np.random.default_rng(220)
+    q = normal(221, (Tq, Hq, d), 0.01)
+    k, v = f64(normal(222, (1, S, Hkv, d), 0.01)), normal(223, (1, S, Hkv, d))
+    q[..., 0] = 0x3f80
+    some = rng.random(S) < (0.2 if Tq == 2 else 1.0)
+    k[0, :, :, 0] = np.where(some, np.arange(S) // 256, 0)[:, None]
+    k = torch.from_numpy(k).to(torch.bfloat16).view(torch.int16).numpy().view(np.uint16)
+    q[1:, :, 0] = 0x3f00  # (half as steep for the other tokens)
+    if rise < 0:
+        q[..., 0] |= 0x8000
+    cache = P.kv_quantize(to_dev_bf16(k), to_dev_bf16(v), 32, torch.int8)
+    o, lse = P.phase2_quant(to_dev_bf16(q), *cache, 32, softmax_scale=abs(rise))
+    ref, keys = long_reference(q, cache, 32, None, None, None, 0, None, abs(rise))
+    check(o, lse, ref, keys, f"rising by {rise}")
+
+
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("d", [64, 128])
 def test_attention_of_queries_with_outliers(d, fmt):
