@@ -128,7 +128,7 @@ __device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi) {
 
 template <int D, int FORMAT, int NW, int KEYS, int CG>
 __global__ __launch_bounds__(64 * NW)
-__attribute__((amdgpu_waves_per_eu(CG == 1 ? 4 : 2, CG == 1 ? 4 : 2)))
+__attribute__((amdgpu_waves_per_eu(CG == 1 || D == 64 ? 4 : 2, CG == 1 || D == 64 ? 4 : 2)))
 void quant_attn_kernel(QuantAttnArgs a) {
   using L = QaLds<D, NW, KEYS>;
   constexpr int HALVES = KEYS / 16;       // of a step, 16 rows each
@@ -777,11 +777,11 @@ int launch_one(const QuantAttnArgs& a, hipStream_t stream) {
 
 template <int D, int FORMAT>
 int launch_tile(const QuantAttnArgs& a, const QuantPlan& p, hipStream_t stream) {
-  if (p.keys == 64) return launch_one<D, FORMAT, 4, 64, 2>(a, stream);
   if constexpr (D == 128) {
+    if (p.keys == 64) return launch_one<D, FORMAT, 4, 64, 2>(a, stream);
     if (p.columns == 48) return launch_one<D, FORMAT, 8, 32, 3>(a, stream);
-    if (p.columns == 32) return launch_one<D, FORMAT, 8, 32, 2>(a, stream);
   }
+  if (p.columns == 32) return launch_one<D, FORMAT, 8, 32, 2>(a, stream);
   return launch_one<D, FORMAT, 8, 32, 1>(a, stream);
 }
 
@@ -792,7 +792,7 @@ constexpr int QA_ONE_EACH = 256, QA_AT_ONCE = 512;
 
 // Four shapes of tiles.  Each code is widened and read once for all columns of a tile, so wide
 // tiles do less, but narrow ones wait less: 16 columns have four waves to a SIMD, the others
-// two.
+// two (of d 128).
 //   16 columns, steps of 32 rows, eight waves: up to 13 steps of a wave with all compute units
 //   at work (12 where the others are of 32 columns and d is 128).  Us with the merge, 16 columns
 //   / the best of the others, 32 / 8 heads of 128: 8 tokens over 40960 keys 21.6 / 24.2, 49152
@@ -804,15 +804,19 @@ constexpr int QA_ONE_EACH = 256, QA_AT_ONCE = 512;
 //   32 columns, as above (d 128): one tile, bound by its keys (8 tokens over 131072 50 against
 //   54 of the next shape), or up to 28 steps of a wave: 64 tokens over 16384 keys 36.6 / 38.6,
 //   32768 59.4 / 60.5, 49152 85.5 / 83.7, 131072 204 / 196.
-//   32 columns, steps of 64 rows, four waves: the rest.
-// Parts: as many as give each compute unit one workgroup; two for the last shape, and for 16
-// columns where waves would have ten steps or more and d is 64 or tiles share their keys (one /
-// two: 32 / 8 heads of 128, 1 token over 131072 keys 46.8 / 48.5, 16384 13.4 / 14.4, 12 tokens
-// over 32768 26.5 / 24.3; 16 / 16 of 64, 1 token over 131072 50.7 / 48.4, 4 x 1021 9.4 / 10.4).
+//   32 columns, steps of 64 rows, four waves: the rest of d 128.  Of d 64, whose 32 columns
+//   leave room for four waves to a SIMD: steps of 32 rows and eight waves (32 / 8 heads of 64,
+//   64 tokens over 131072 keys 126 us against 135, int8 148 / 157; over 16384 28.1 / 28.3).
+// Parts: as many as give each compute unit one workgroup; two for the last two shapes, but for
+// up to two tiles of d 64 (16 / 16 heads, 24 tokens over 131072 keys 48.8 one / 51.3 two; 64
+// tokens over 65536 47.9 / 44.1), and for 16 columns where waves would have ten steps or more
+// and tiles share their keys (32 / 8 heads of 128, 12 tokens over 32768 keys 23.8 one / 22.9 two;
+// 1 token over 131072 45.2 / 45.8, 16384 12.7 / 14.0; 16 / 16 of 64, 1 token over 131072 44.7 /
+// 47.0, 4 x 1021 9.4 / 10.2).
 // But one part up to five steps of a wave: parts need the merge's launch and a workspace, 4 us
 // of the host's time.  Device / call from the host, several parts and one, 32 / 8 heads of 128,
 // 1 token over 480 keys 8.7 / 15.9 and 7.9 / 11.7, 1000 9.0 / 15.9 and 9.9 / 11.6, 1500 9.4 / 15.8
-// and 13.5 / 13.6 (a wave alone waits for each step's loads, 1.8 us a step); 16 / 16 of 64, 24
+// and 13.5 / 13.6 (1.8 us a step of a wave); 16 / 16 of 64, 24
 // tokens over 1000 keys 8.7 / 15.8 and 8.6 / 11.4.
 QuantPlan quant_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int d, int64_t gen_rows) {
   QuantPlan p{};
@@ -841,11 +845,12 @@ QuantPlan quant_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int d, in
     if (of48) return take(48, 32, QA_ONE_EACH);
     if (d == 128 && (of32 == 1 || of32 * Hkv * steps(32) <= 28 * at_once))
       return take(32, 32, QA_ONE_EACH);
+    if (d == 64) return take(32, 32, of32 <= 2 ? QA_ONE_EACH : QA_AT_ONCE);
     return take(32, 64, QA_AT_ONCE);
   }
   take(16, 32, QA_ONE_EACH);
   if (steps(32) <= 5 * 8) p.parts = 1;
-  else if (steps(32) >= 10 * 8 * (int64_t)p.parts && (d == 64 || tiles(16) > 1))
+  else if (steps(32) >= 10 * 8 * (int64_t)p.parts && tiles(16) > 1)
     take(16, 32, QA_AT_ONCE);
   return p;
 }

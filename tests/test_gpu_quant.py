@@ -284,7 +284,8 @@ def test_attention_over_many_steps(Hq, Hkv, d, Tq, fmt):
     (64, 64, 128, 30, 1, 7100),   # 32 columns in steps of 32 rows
     (16, 16, 128, 64, 1, 14000),  # two tiles of 32
     (16, 16, 128, 256, 1, 17600), # 32 columns in steps of 64 rows, more than the table
-    (64, 64, 64, 128, 1, 8700),   # more than the table
+    (64, 64, 64, 128, 1, 8700),   # 32 columns of heads of 64
+    (32, 32, 64, 256, 1, 17000),  # more than the table
     (60, 4, 64, 20, 2, 8300),     # 15 heads per KV head
 ])
 def test_attention_of_full_waves(Hq, Hkv, d, Tq, n, S, fmt):
