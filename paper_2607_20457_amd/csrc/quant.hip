@@ -30,8 +30,8 @@ struct QuantizeArgs {
   int Hkv;
   int64_t rows, first, capacity, blocks;
   int block_log2;
-  int row_groups;        // workgroups over the rows of a shard
-  int head_groups;       // and over its heads
+  uint32_t row_groups;   // workgroups over the rows of a shard
+  uint32_t head_groups;  // and over its heads
   int waves_log2;        // log2 of a block's waves
   int once;              // more rows than the caches hold
 };
@@ -93,12 +93,10 @@ __global__ __launch_bounds__(64 * QZ_WAVES) void quantize_kernel(QuantizeArgs a)
   __shared__ uint32_t s_max[QZ_WAVES];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int64_t wg = blockIdx.x;
-  const int which = (int)(wg & 1);
-  wg >>= 1;
-  const int hg = (int)(wg % a.head_groups);
-  wg /= a.head_groups;
-  const int64_t rg = wg % a.row_groups, shard = wg / a.row_groups;
+  const int which = blockIdx.x & 1;
+  const uint32_t wg = blockIdx.x >> 1, groups = wg / a.head_groups;
+  const int hg = (int)(wg - groups * a.head_groups);
+  const int64_t shard = groups / a.row_groups, rg = groups - (uint32_t)shard * a.row_groups;
   const int per_head = 1 << a.waves_log2;
   const int head = hg * (QZ_WAVES >> a.waves_log2) + (wave >> a.waves_log2);
   const int64_t row0 = (rg * per_head + (wave & (per_head - 1))) * QZ_ROWS;
@@ -205,7 +203,7 @@ struct DequantizeArgs {
   int Hkv;
   int64_t rows, first, capacity, blocks;
   int block_log2;
-  int row_groups, head_groups;
+  uint32_t row_groups, head_groups;
 };
 
 // The quantiser's shape the other way: a wave reads 64 rows of one head, four heads side
@@ -219,12 +217,11 @@ __global__ __launch_bounds__(64 * QZ_WAVES, 4) void dequantize_kernel(Dequantize
   constexpr int LOADS = QZ_ROWS / SEG;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int64_t wg = blockIdx.x;
-  const int which = (int)(wg & 1);
-  wg >>= 1;
-  const int head = (int)(wg % a.head_groups) * QZ_WAVES + wave;
-  wg /= a.head_groups;
-  const int64_t row0 = wg % a.row_groups * QZ_ROWS, shard = wg / a.row_groups;
+  const int which = blockIdx.x & 1;
+  const uint32_t wg = blockIdx.x >> 1, groups = wg / a.head_groups;
+  const int head = (int)(wg - groups * a.head_groups) * QZ_WAVES + wave;
+  const int64_t shard = groups / a.row_groups;
+  const int64_t row0 = (int64_t)(groups - (uint32_t)shard * a.row_groups) * QZ_ROWS;
   if (head >= a.Hkv) return;
   const int at = lane % CPR;
   const int64_t plane = shard * a.Hkv + head;
@@ -288,7 +285,7 @@ int launch_quantize(const KvQuantLaunch& x, hipStream_t stream) {
   a.waves_log2 = a.block_log2 > 6 ? a.block_log2 - 6 : 0;
   const int heads = QZ_WAVES >> a.waves_log2, rows = QZ_ROWS << a.waves_log2;
   a.head_groups = (x.Hkv + heads - 1) / heads;
-  a.row_groups = (int)((x.rows + rows - 1) / rows);
+  a.row_groups = (uint32_t)((x.rows + rows - 1) / rows);
   a.once = (int64_t)x.n * x.rows * x.Hkv * x.d * 4 >= 256 << 20;
   const int64_t nwg = 2 * (int64_t)x.n * a.row_groups * a.head_groups;
   if (!grid_fits(nwg, 64 * QZ_WAVES)) return PULSAR_EUNSUPPORTED;
@@ -315,7 +312,7 @@ int launch_dequantize(const KvQuantLaunch& x, uint16_t* const (&out)[2], hipStre
   a.block_log2 = __builtin_ctz(x.block);
   a.blocks = (x.capacity + x.block - 1) >> a.block_log2;
   a.head_groups = (x.Hkv + QZ_WAVES - 1) / QZ_WAVES;
-  a.row_groups = (int)((x.rows + QZ_ROWS - 1) / QZ_ROWS);
+  a.row_groups = (uint32_t)((x.rows + QZ_ROWS - 1) / QZ_ROWS);
   const int64_t nwg = 2 * (int64_t)x.n * a.row_groups * a.head_groups;
   if (!grid_fits(nwg, 64 * QZ_WAVES)) return PULSAR_EUNSUPPORTED;
   const bool e4m3 = x.format == PULSAR_KV_E4M3;

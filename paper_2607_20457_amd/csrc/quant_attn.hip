@@ -147,14 +147,14 @@ void quant_attn_kernel(QuantAttnArgs a) {
   const int r = lane & 15, g = lane >> 4;
   // Workgroup -> tile of a (KV head, part): all tiles of one head's part, which read the
   // same keys, go to one XCD, one after another (few such parts: to `slices` of them).
-  const int tiles = a.token_tiles * a.col_tiles, deep = (tiles + a.slices - 1) / a.slices;
-  int64_t wg = blockIdx.x >> 3;
-  const int in = (int)(wg % deep);
-  wg = wg / deep * 8 + (blockIdx.x & 7);
-  const int tile = in * a.slices + (int)(wg % a.slices);
-  wg /= a.slices;
-  if (wg >= (int64_t)a.Hkv * a.parts || tile >= tiles) return;
-  const int kvh = (int)(wg % a.Hkv), part = (int)(wg / a.Hkv);
+  // (all of them fit 32 bits, as the workgroups of a launch do)
+  const uint32_t tiles = a.token_tiles * a.col_tiles, deep = (tiles + a.slices - 1) / a.slices;
+  const uint32_t wg = blockIdx.x >> 3;
+  const uint32_t row = wg / deep, unit = row * 8 + (blockIdx.x & 7);
+  const uint32_t pair = unit / a.slices;
+  const int tile = (int)((wg - row * deep) * a.slices + (unit - pair * a.slices));
+  if (pair >= (uint32_t)a.Hkv * a.parts || tile >= (int)tiles) return;
+  const int part = (int)(pair / a.Hkv), kvh = (int)(pair - part * a.Hkv);
   const int t0 = tile % a.token_tiles * a.tile_tokens;
   const int heads0 = tile / a.token_tiles * COLS;
   const int tokens = min(a.tile_tokens, a.Tq - t0);
