@@ -808,8 +808,8 @@ constexpr int QA_ONE_EACH = 256, QA_AT_ONCE = 512;
 //   leave room for four waves to a SIMD: steps of 32 rows and eight waves (32 / 8 heads of 64,
 //   64 tokens over 131072 keys 126 us against 135, int8 148 / 157; over 16384 28.1 / 28.3).
 // Parts: as many as give each compute unit one workgroup; two for the last two shapes, but for
-// up to two tiles of d 64 (16 / 16 heads, 24 tokens over 131072 keys 48.8 one / 51.3 two; 64
-// tokens over 65536 47.9 / 44.1), and for 16 columns where waves would have ten steps or more
+// one tile of d 64 (16 / 16 heads, 24 tokens over 131072 keys 48.8 one / 51.3 two; two tiles, 64
+// tokens over 65536, 48.4 / 44.5), and for 16 columns where waves would have ten steps or more
 // and tiles share their keys (32 / 8 heads of 128, 12 tokens over 32768 keys 23.8 one / 22.9 two;
 // 1 token over 131072 45.2 / 45.8, 16384 12.7 / 14.0; 16 / 16 of 64, 1 token over 131072 44.7 /
 // 47.0, 4 x 1021 9.4 / 10.2).
@@ -845,7 +845,7 @@ QuantPlan quant_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int d, in
     if (of48) return take(48, 32, QA_ONE_EACH);
     if (d == 128 && (of32 == 1 || of32 * Hkv * steps(32) <= 28 * at_once))
       return take(32, 32, QA_ONE_EACH);
-    if (d == 64) return take(32, 32, of32 <= 2 ? QA_ONE_EACH : QA_AT_ONCE);
+    if (d == 64) return take(32, 32, of32 == 1 ? QA_ONE_EACH : QA_AT_ONCE);
     return take(32, 64, QA_AT_ONCE);
   }
   take(16, 32, QA_ONE_EACH);
