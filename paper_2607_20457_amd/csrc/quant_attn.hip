@@ -247,7 +247,8 @@ void quant_attn_kernel(QuantAttnArgs a) {
       }
       const int row = first * KEYS;
       const int64_t plane = (int64_t)shard * a.Hkv + kvh;
-      x.rows = min(KEYS, end - row);
+      // (one at least, also of a shard that somebody shortens meanwhile: in its capacity still)
+      x.rows = max(1, min(KEYS, end - row));
       x.off = (uint64_t)(plane * a.S + row) * D;
       x.scale = plane * a.blocks + ((row + min(16 * (lane % HALVES), x.rows - 1)) >> a.block_log2);
     } else if (st < step1) {
