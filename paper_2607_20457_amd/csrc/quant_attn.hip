@@ -338,7 +338,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
                                             st + i * 1024);
         }
       };
-      if (rows == KEYS && tiles == 1) {
+      if (KEYS == 32 && rows == KEYS && tiles == 1) {  // (64 rows: more tiles than one)
         whole(std::true_type{});
       } else if (rows == KEYS) {
         whole(std::false_type{});
