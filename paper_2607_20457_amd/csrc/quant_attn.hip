@@ -19,8 +19,9 @@
 //       64 tokens over 16 x 8192 keys 203 us against 195, int8 259 / 245).  A score is (q . code) * (scale * ks log2 e), one product of
 //       the block; the weight that enters PV is exp2(score - reference + log2 vs): V's
 //       scale is in it before it is rounded to bf16 (2^-8 of each at most), and sums of
-//       weights are taken times 1 / vs.  O is divided by the sum of the rounded weights, the
-//       log-sum-exp uses the fp32 sum.
+//       weights are taken times 1 / vs.  (A scale below 2^-32 is multiplied to the rounded
+//       weights after their sums: exactly, if it is a power of two.)  O is divided by the sum
+//       of the rounded weights, the log-sum-exp uses the fp32 sum.
 // The next step's K is sent for once the scores have consumed this one's, its V once PV
 // has.
 //
@@ -49,6 +50,7 @@ namespace {
 constexpr float QA_SLACK = 8.0f;      // log2 slack before the reference is raised
 constexpr float QA_OVER = 4 * 0x1p8f; // a lane's four weights of 2^QA_SLACK
 constexpr float QA_LEAST = 0x1p-100f; // a smaller scale counts as this
+constexpr float QA_SMALL = 0x1p-32f;  // scales of V that weights get after their sums
 constexpr float QA_BIG = 0x1p64f;     // scales of V whose weights get no slack ...
 constexpr float QA_MOST = 0x1p124f;   // ... and whose sums leave fp32 all the same
 constexpr int QA_SHARDS = 1024;       // shards with lengths of their own
@@ -267,16 +269,20 @@ void quant_attn_kernel(QuantAttnArgs a) {
     tab_send = x.rows;
   };
   // ... and to multiply it: its rows and what the half's scales come to, the factor of its
-  // scores, log2 vs and 1 / vs.
+  // scores, log2 vs and 1 / vs.  A vs below QA_SMALL counts as 1 there, and weights are
+  // multiplied by it after their sums: with vs in it, 2^-100 in a block of zeros, a weight below
+  // 2^-26 would be 0 and its key missing from the sums.
   int tab_rows = 0;
-  float tab_ck = c2, tab_lv = 0.f, tab_iv = 1.f;
-  uint64_t nan_v = 0, big_v = 0;  // halves whose vs is no number or above QA_MOST, and above QA_BIG
+  float tab_ck = c2, tab_lv = 0.f, tab_iv = 1.f, tab_vs = 1.f;
+  // halves whose vs is no number or above QA_MOST, above QA_BIG, and below QA_SMALL
+  uint64_t nan_v = 0, big_v = 0, small_v = 0;
   auto fill_use = [&](const Place& x) {
     tab_rows = x.rows;
     tab_ck = c2;
     tab_lv = 0.f;
     tab_iv = 1.f;
-    bool bad = false, big = false;
+    tab_vs = 1.f;
+    bool bad = false, big = false, small = false;
     if (x.scale >= 0) {
       float k = a.ks[x.scale], v = a.vs[x.scale];
       k = k < QA_LEAST ? QA_LEAST : k;
@@ -286,11 +292,14 @@ void quant_attn_kernel(QuantAttnArgs a) {
       k *= c2;
       tab_ck = k < 0x1p-126f ? 0x1p-126f : k;
       big = v > QA_BIG;
-      tab_lv = bad ? 0.f : __log2f(v);
-      tab_iv = bad ? 1.f : 1.f / v;
+      small = v < QA_SMALL;
+      tab_lv = bad || small ? 0.f : __log2f(v);
+      tab_iv = bad || small ? 1.f : 1.f / v;
+      tab_vs = small ? v : 1.f;
     }
     nan_v = __ballot(bad);
     big_v = __ballot(big);
+    small_v = __ballot(small);
   };
   auto lane_f = [&](float x, int at) {
     return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), at));
@@ -538,6 +547,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
     }
     const uint32_t bad_v = (uint32_t)(nan_v >> at) & ((1u << HALVES) - 1);
     const bool big = (big_v >> at & ((1u << HALVES) - 1)) != 0;
+    const bool small = (small_v >> at & ((1u << HALVES) - 1)) != 0;
     need_k();
     // (a wave at its matrix products goes before one at its weights: 64 tokens over 16 x 8192
     // keys 196 -> 188 us, int8 246 -> 229)
@@ -601,6 +611,17 @@ void quant_attn_kernel(QuantAttnArgs a) {
     }
 #pragma unroll
     for (int c = 0; c < CG; ++c) l_run[c] += l[c], lr_run[c] += lr[c];
+    if (small) {
+#pragma unroll
+      for (int h = 0; h < HALVES; ++h) {
+        const float vs = lane_f(tab_vs, at + h);
+#pragma unroll
+        for (int c = 0; c < CG; ++c)
+#pragma unroll
+          for (int v = 4 * (h & 1); v < 4 * (h & 1) + 4; ++v)
+            P[c][h / 2][v] = (__bf16)((float)P[c][h / 2][v] * vs);
+      }
+    }
     need_v(j + 1 < nsteps);
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
