@@ -89,10 +89,11 @@ int launch_idf_fill(float* idf, int64_t n, int num_blocks, hipStream_t stream) {
 }
 
 // ---------------------------------------------------------------------------
-// (may also say so of opposite infinities)
-__device__ __forceinline__ bool is_nan(f32x4 x) {
-  const float s = (x[0] + x[1]) + (x[2] + x[3]);
-  return s != s;
+constexpr float LM_FAR = 0x1p90f;     // sums of this size may leave fp32 in those that follow ...
+constexpr float LM_DOWN = 0x1p-32f;   // ... and are taken times this, which 2^31 parts cannot make up for
+// Whether the sum of x's magnitudes is `most` or more, an infinity or a NaN.
+__device__ __forceinline__ bool is_far(f32x4 x, float most) {
+  return !((fabsf(x[0]) + fabsf(x[1])) + (fabsf(x[2]) + fabsf(x[3])) < most);
 }
 
 // Online-softmax merge (Appendix "Phase 2 Distributed Softmax Merge").
@@ -103,7 +104,8 @@ __device__ __forceinline__ bool is_nan(f32x4 x) {
 // rises; then l = m + ln s and o = a / s.  -inf partials weigh zero, and what
 // their o holds must not count either: where a zero weight has met a NaN or an
 // infinity there (so that a is NaN), the pass is repeated with such parts left
-// out.  (To leave them out at once costs every merge 3 to 6 %.)
+// out.  (To leave them out at once costs every merge 3 to 6 %.)  So it is where the
+// sum of large values has left fp32, which o does not: then a is taken times 2^-32.
 template <int CH, typename OUT>
 __global__ __launch_bounds__(256) void lse_merge_kernel(
     const float* __restrict__ o_parts, const float* __restrict__ lse_parts, int H, int Tq, int Hq,
@@ -123,7 +125,7 @@ __global__ __launch_bounds__(256) void lse_merge_kernel(
   const f32x4* op = reinterpret_cast<const f32x4*>(o_parts) + z * (int64_t)H * (part_ostride / 4);
   float m, sum;
   f32x4 acc;
-  auto fold = [&](auto leave_out) {
+  auto fold = [&](auto careful) {
     m = -INFINITY, sum = 0.f;
     acc = f32x4{0.f, 0.f, 0.f, 0.f};
     for (int p0 = 0; p0 < H; p0 += CH) {
@@ -151,19 +153,22 @@ __global__ __launch_bounds__(256) void lse_merge_kernel(
       for (int u = 0; u < CH; ++u) {
         const float w = p0 + u < H ? __expf(l[u] - nm_use) : 0.f;
         sum += w;
-        if (decltype(leave_out)::value && (p0 + u >= H || l[u] == -INFINITY)) continue;
+        if (decltype(careful)::value)
+          v[u] = p0 + u < H && l[u] != -INFINITY ? v[u] * LM_DOWN : f32x4{0.f, 0.f, 0.f, 0.f};
         acc += w * v[u];
       }
       m = nm;
     }
   };
   fold(std::false_type{});
-  if (is_nan(acc)) fold(std::true_type{});
+  const bool far = is_far(acc, INFINITY);
+  if (far) fold(std::true_type{});
   float ell = -INFINITY;
   if (m != -INFINITY) {
     ell = m + __logf(sum);
     acc *= 1.f / sum;
   }
+  if (far) acc *= 1.f / LM_DOWN;
   o[z * (int64_t)Tq * Hq * d4 + orow] = __builtin_convertvector(acc, OUT);
   if (lse && dv == 0) lse[z * (int64_t)Hq * Tq + (int64_t)h * Tq + q] = ell;
 }
@@ -200,7 +205,7 @@ __global__ __launch_bounds__(THREADS) void lse_merge_wide_kernel(
                     orow + min(dv, d4 - 1);
   float m, sum;
   f32x4 acc;
-  auto fold = [&](auto leave_out) {
+  auto fold = [&](auto careful) {
     m = -INFINITY, sum = 0.f;
     acc = f32x4{0.f, 0.f, 0.f, 0.f};
     for (int p0 = pg; p0 < H; p0 += CH * PG) {
@@ -224,14 +229,17 @@ __global__ __launch_bounds__(THREADS) void lse_merge_wide_kernel(
       for (int u = 0; u < CH; ++u) {
         const float w = p0 + u * PG < H ? __expf(l[u] - use) : 0.f;
         sum += w;
-        if (decltype(leave_out)::value && (p0 + u * PG >= H || l[u] == -INFINITY)) continue;
+        if (decltype(careful)::value)
+          v[u] = p0 + u * PG < H && l[u] != -INFINITY ? v[u] * LM_DOWN : f32x4{0.f, 0.f, 0.f, 0.f};
         acc += w * v[u];
       }
       m = nm;
     }
   };
   fold(std::false_type{});
-  if (is_nan(acc)) fold(std::true_type{});  // as in the per-output kernel
+  // as in the per-output kernel, but before sums of several lanes and waves leave fp32
+  const bool far = __any(is_far(acc, LM_FAR));
+  if (far) fold(std::true_type{});
   // lanes DL apart hold the same values' other parts
 #pragma unroll
   for (int off = DL; off < 64; off <<= 1) {
@@ -247,7 +255,7 @@ __global__ __launch_bounds__(THREADS) void lse_merge_wide_kernel(
   const int wave = tid >> 6, lane = tid & 63;
   if (lane == 0) {
     s_m[wave] = m;
-    s_s[wave] = sum;
+    s_s[wave] = far ? -sum : sum;  // (a sum is not negative: the sign says that acc is down)
   }
   if (lane < DL) s_a[wave][lane] = acc;
   __syncthreads();
@@ -258,17 +266,29 @@ __global__ __launch_bounds__(THREADS) void lse_merge_wide_kernel(
   const float use = m == -INFINITY ? 0.f : m;
   sum = 0.f;
   acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  float least = 0.f;
 #pragma unroll
   for (int w = 0; w < W; ++w) {
-    const float e = __expf(s_m[w] - use);
-    sum += s_s[w] * e;
+    const float e = __expf(s_m[w] - use), s = s_s[w];
+    least = fminf(least, s);
+    sum += fabsf(s) * e;
     acc += s_a[w][tid] * e;
+  }
+  const bool down = least < 0.f;
+  if (down) {
+    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const float e = __expf(s_m[w] - use);
+      acc += s_a[w][tid] * (s_s[w] < 0.f ? e : e * LM_DOWN);
+    }
   }
   float ell = -INFINITY;
   if (m != -INFINITY) {
     ell = m + __logf(sum);
     acc *= 1.f / sum;
   }
+  if (down) acc *= 1.f / LM_DOWN;
   o[z * (int64_t)Tq * Hq * d4 + orow + dv] = __builtin_convertvector(acc, OUT);
   if (lse && dv == 0) lse[z * (int64_t)Hq * Tq + (int64_t)h * Tq + q] = ell;
 }
