@@ -51,8 +51,13 @@ constexpr float QA_SLACK = 8.0f;      // log2 slack before the reference is rais
 constexpr float QA_OVER = 4 * 0x1p8f; // a lane's four weights of 2^QA_SLACK
 constexpr float QA_LEAST = 0x1p-100f; // a smaller scale counts as this
 constexpr float QA_SMALL = 0x1p-32f;  // scales of V that weights get after their sums
-constexpr float QA_BIG = 0x1p64f;     // scales of V whose weights get no slack ...
-constexpr float QA_MOST = 0x1p124f;   // ... and whose sums leave fp32 all the same
+constexpr float QA_BIG = 0x1p64f;     // from here on scales of V have weights with QA_ROOM
+constexpr float QA_MOST = 0x1p124f;   // larger ones make their block no number
+// Values near the largest number leave fp32 in a sum of theirs, though not in their average,
+// which O is.  Steps that may hold such values keep their weights at 2^-QA_ROOM or less, the
+// reference that far above the scores: 2^32 of them, more than a call has keys, sum to half a
+// value.  (Not so in all steps: a weight has 2^-126 to go down to, and log2 vs is in it.)
+constexpr float QA_ROOM = 33.0f;
 constexpr int QA_SHARDS = 1024;       // shards with lengths of their own
 
 struct QuantAttnArgs {
@@ -423,10 +428,11 @@ void quant_attn_kernel(QuantAttnArgs a) {
     m_run[c] = -INFINITY;
     l_run[c] = lr_run[c] = 0.f;
   }
-  // The reference of every group against mx, the largest of a lane's scores of it: raised
-  // where it has to be, O and the sums rescaled.
+  // The reference of every group against mx, the largest of a lane's scores of it: where these
+  // are above it by more than `slack`, it is raised to `above` more than they are, O and the sums
+  // rescaled.
   bool unset = true;  // columns without a reference (the same in all lanes)
-  auto raise = [&](const float* mx, float slack) {
+  auto raise = [&](const float* mx, float slack, float above) {
     bool any = false;
 #pragma unroll
     for (int c = 0; c < CG; ++c) any |= mx[c] > m_run[c] + slack;
@@ -434,7 +440,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
 #pragma unroll
     for (int c = 0; c < CG; ++c) {
       const float top = max_of_rows(mx[c]);
-      const float m_new = top > m_run[c] + slack ? top : m_run[c];
+      const float m_new = top > m_run[c] + slack ? top + above : m_run[c];
       const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[c] - m_new);
 #pragma unroll
       for (int e = 0; e < DT; ++e) acc[c][e] *= alpha;
@@ -595,8 +601,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
 #pragma unroll
           for (int h = 0; h < HALVES; ++h) mx[c] = fmaxf(mx[c], largest(S[c][h]) * ck[h]);
         }
-        // (weights times a scale of up to 2^124 stay in fp32 if they are 1 at most)
-        raise(mx, big ? 0.f : QA_SLACK);
+        raise(mx, big ? -QA_ROOM : QA_SLACK, big ? QA_ROOM + QA_SLACK : 0.f);
       }
       bool over = false;
 #pragma unroll
@@ -680,7 +685,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
       }
       mx[c] = fmaxf(largest(S[c][0]), largest(S[c][1])) * c2;
     }
-    raise(mx, QA_SLACK);
+    raise(mx, -QA_ROOM, QA_ROOM + QA_SLACK);  // (whatever the values are)
     bf16x8 P[CG];
 #pragma unroll
     for (int c = 0; c < CG; ++c) {
@@ -773,9 +778,14 @@ void quant_attn_kernel(QuantAttnArgs a) {
         static_cast<bf16x4*>(a.O)[at * DL + dv] = __builtin_convertvector(o, bf16x4);
       else
         static_cast<f32x4*>(a.O)[at * DL + dv] = o;
-      if (dv == 0 && a.lse != nullptr)
+      if (dv == 0 && a.lse != nullptr) {
+        // (l's exponent, which QA_ROOM makes large, goes to m: no bits of its logarithm)
+        const float log2_l = __log2f(__builtin_amdgcn_frexp_mantf(l));
         a.lse[((int64_t)part * a.Hq + hd) * a.Tq + t0 + nth] =
-            l != 0.f ? (m + __log2f(l)) * 0.69314718055994531f : -INFINITY;
+            l != 0.f ? ((m + (float)__builtin_amdgcn_frexp_expf(l)) + log2_l) *
+                           0.69314718055994531f
+                     : -INFINITY;
+      }
     }
   }
 }

@@ -7,8 +7,9 @@ import pytest
 import torch
 
 import paper_2607_20457_amd as P
-from tests._blocks import host
-from tests._plan import plan
+from tests._blocks import dev_i32, dev_mask, host
+from tests._plan import SHAPES, plan
+from tests._quant import DTYPES, check, long_reference, softmax_scale
 
 pytestmark = pytest.mark.gpu
 
@@ -61,3 +62,91 @@ def test_low_scores_in_blocks_of_the_least_scale(Hq, Hkv, d, Tq, S, shape, ordin
     else:
         # low weights times 2^-100 are lost or not
         assert np.abs(host(o) * 2.0 ** 100 - 1).max() <= 2.0 ** -8 + tail
+
+
+# ---- every shape of tile ------------------------------------------------------------
+
+
+def _bits(x):
+    return x.contiguous().view(torch.int16).cpu().numpy().view(np.uint16)
+
+
+def _normal(gen, shape, size=1.0):
+    return (size * torch.randn(shape, generator=gen, device="cuda")).to(torch.bfloat16)
+
+
+class Case:
+    """Sizes that take one shape of tile, its inputs on the device, and a cache of 32-row
+    blocks."""
+
+    def __init__(self, shape, fmt, seed, G=70):
+        (self.Hq, self.Hkv, self.d, self.Tq, self.n, self.S), want = SHAPES[shape]
+        p = plan(self.n, self.Tq, self.S, self.Hq, self.Hkv, self.d, G + self.Tq)
+        assert (p.columns, p.keys) == want
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        rows = (self.n, self.S, self.Hkv, self.d)
+        self.group, self.G, self.fmt, self.block = self.Hq // self.Hkv, G, fmt, 32
+        self.q = _normal(gen, (self.Tq, self.Hq, self.d))
+        self.k, self.v = _normal(gen, rows), _normal(gen, rows)
+        self.kg, self.vg = (_normal(gen, (G + self.Tq, self.Hkv, self.d)) for _ in range(2))
+        self.scale = softmax_scale(self.d)
+        print(f"phase2_quant edges: {shape} {fmt} seed {seed} {self.n}x{self.S}", flush=True)
+
+    def quantize(self):
+        self.cache = P.kv_quantize(self.k, self.v, self.block, DTYPES[self.fmt])
+
+    def call(self, rows=None, mask=None, **kw):
+        return P.phase2_quant(self.q, *self.cache, self.block,
+                              None if rows is None else dev_i32(rows), self.kg, self.vg, self.G,
+                              mask, softmax_scale=self.scale, **kw)
+
+    def reference(self, rows=None, sees=None, cache=None, **kw):
+        x = {**dict(q=self.q, kg=self.kg, vg=self.vg), **kw}
+        return long_reference(_bits(x["q"]), cache or self.cache, self.block, rows,
+                              _bits(x["kg"]), _bits(x["vg"]), self.G, sees, self.scale)
+
+
+def _compare(out, ref, keys, bad_o, bad_lse, what, bf16_out=False):
+    """`check`, but for what has to be NaN: outputs bad_o [Tq, Hq] and sums bad_lse [Hq, Tq]."""
+    o, lse = out
+    assert np.array_equal(np.isnan(host(o)), np.broadcast_to(bad_o[..., None], o.shape)), what
+    assert np.array_equal(np.isnan(host(lse)), bad_lse), what
+    o = torch.where(torch.from_numpy(bad_o).cuda()[..., None], 0, o)
+    lse = torch.where(torch.from_numpy(bad_lse).cuda(), 0, lse)
+    check(o, lse, (np.where(bad_o[..., None], 0, ref[0]), np.where(bad_lse, 0, ref[1]), ref[2],
+                   ref[3]), keys, what, bf16_out)
+
+
+ALL = pytest.mark.parametrize("shape", list(SHAPES))
+FMTS = pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+
+
+@FMTS
+@ALL
+@pytest.mark.parametrize("where", ["codes", "generation", "both"])
+def test_average_of_values_near_the_largest(shape, fmt, where):
+    # The largest bf16 number in some channels of every second block, of all kinds of scores: a
+    # few of them leave fp32 in a sum, none in the average.  Other channels, and other blocks,
+    # are ordinary.
+    c = Case(shape, fmt, 400)
+    top = torch.finfo(torch.bfloat16).max
+    second = (torch.arange(c.S, device="cuda") // 64 % 2 == 1).nonzero().view(-1)
+    if where != "generation":
+        c.v[:, second[:, None], :, 3] = top
+        c.v[:, second[:, None], 0, 5] = -top
+    if where != "codes":
+        c.vg[..., 3] = top
+        c.vg[::2, :, 7] = -top
+    c.quantize()
+    for bf16_out in (False, True):
+        o, lse = c.call(o_dtype=P.OUT_BF16 if bf16_out else P.OUT_F32)
+        assert torch.isfinite(o).all()
+        # (the bound goes by the weighted |v| of each channel, so ordinary ones count as such)
+        check(o, lse, *c.reference(), where, bf16_out)
+    # all keys alike and all values the largest: their average is one of them
+    c.q.zero_()
+    c.v.fill_(top)
+    c.vg.fill_(top)
+    c.quantize()
+    o, lse = c.call()
+    check(o, lse, *c.reference(), "all of them")
