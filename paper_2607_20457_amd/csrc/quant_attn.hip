@@ -58,7 +58,6 @@ constexpr float QA_MOST = 0x1p124f;   // larger ones make their block no number
 // reference that far above the scores: 2^32 of them, more than a call has keys, sum to half a
 // value.  (Not so in all steps: a weight has 2^-126 to go down to, and log2 vs is in it.)
 constexpr float QA_ROOM = 33.0f;
-constexpr int QA_SHARDS = 1024;       // shards with lengths of their own
 
 struct QuantAttnArgs {
   const uint16_t* q;
@@ -92,7 +91,7 @@ struct QaLds {
   static constexpr int MERGE = NW * 16 * (PITCH + 3) * 4;
   static constexpr int REUSED = LOOP > MERGE ? LOOP : MERGE;
   // with lengths: the steps before each shard
-  static constexpr int STEPS = (QA_SHARDS + 1) * 4 + NW * 4;
+  static constexpr int STEPS = (kMaxQuantShards + 1) * 4 + NW * 4;
 };
 
 // lds_dma16, its scalars possibly fresh from a vector instruction (a lane read, or a spilled
@@ -173,7 +172,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
   int list_steps = a.n_shards * a.shard_steps;
   auto live_rows = [&](int shard) { return min(max(a.rows[shard], 0), a.S); };
   if (a.rows != nullptr) {
-    int* const sums = before + QA_SHARDS + 1;
+    int* const sums = before + kMaxQuantShards + 1;
     int total = 0;
     for (int i0 = 0; i0 < a.n_shards; i0 += 64 * NW) {
       const int i = i0 + tid;
