@@ -164,7 +164,7 @@ __global__ __launch_bounds__(256) void lse_merge_kernel(
   const bool far = is_far(acc, INFINITY);
   if (far) fold(std::true_type{});
   float ell = -INFINITY;
-  if (m != -INFINITY) {
+  if (sum != 0.f) {  // (a NaN, if every part is one: m is -inf then too)
     ell = m + __logf(sum);
     acc *= 1.f / sum;
   }
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(THREADS) void lse_merge_wide_kernel(
     }
   }
   float ell = -INFINITY;
-  if (m != -INFINITY) {
+  if (sum != 0.f) {  // (a NaN, if every part is one: m is -inf then too)
     ell = m + __logf(sum);
     acc *= 1.f / sum;
   }

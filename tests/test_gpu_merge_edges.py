@@ -54,3 +54,22 @@ def test_merge_near_the_largest_beside_what_is_missing(H, Tq, Hq, d):
     big[-1, 0, 2] = 0
     small[-1, 0, 2] = 0
     assert torch.equal(big, small * 2.0 ** 126)
+
+
+@pytest.mark.parametrize("H,Tq,Hq,d", SIZES)
+def test_merge_of_parts_that_are_all_no_number(H, Tq, Hq, d):
+    # (not a row that saw no key: a merge of its result would leave it out)
+    o, lse = _parts(3, H, Tq, Hq, d)
+    small, ell = P.lse_merge(o, lse)
+    lse[:, 0, 0] = torch.nan
+    lse[:, Hq - 1, Tq - 1] = -torch.inf
+    o[:, 0, 0] = torch.nan
+    for some in (False, True):
+        if some:  # one part that saw no key, or a key
+            lse[0, 0, 0] = -torch.inf
+        got, sums = P.lse_merge(o, lse)
+        assert torch.isnan(got[0, 0]).all() and torch.isnan(sums[0, 0]), some
+        assert (got[-1, -1] == 0).all() and torch.isneginf(sums[-1, -1])
+        got[0, 0], sums[0, 0], got[-1, -1], sums[-1, -1] = (
+            small[0, 0], ell[0, 0], small[-1, -1], ell[-1, -1])
+        assert torch.equal(got, small) and torch.equal(sums, ell)
