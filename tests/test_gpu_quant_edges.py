@@ -150,3 +150,108 @@ def test_average_of_values_near_the_largest(shape, fmt, where):
     c.quantize()
     o, lse = c.call()
     check(o, lse, *c.reference(), "all of them")
+
+
+@FMTS
+@ALL
+def test_scales_of_every_kind(shape, fmt):
+    # head 0: blocks of V whose scale is none (NaN, infinity, past the largest); the last head:
+    # K's too; in all of them scales of V from 2^-90 to 2^110, and blocks of zeros
+    c = Case(shape, fmt, 410)
+    rng = np.random.default_rng(411)
+    blocks = -(-c.S // c.block)
+    size = 2.0 ** rng.integers(-90, 111, (c.n, blocks, c.Hkv))
+    size[:, ::2] = rng.integers(0, 2, size[:, ::2].shape)
+    size = torch.from_numpy(size.repeat(c.block, axis=1)[:, :c.S, :, None]).cuda()
+    c.v = (c.v.double() * size).to(torch.bfloat16)
+    c.quantize()
+    ref, keys = c.reference()
+    none = np.zeros((c.Tq, c.Hq), dtype=bool)
+    _compare(c.call(), ref, keys, none, none.T, "scales of any size")
+    bad = none.copy()
+    bad[:, :c.group] = True
+    vs = c.cache[3]
+    at = blocks // 3
+    for x in (math.nan, math.inf, 2.0 ** 125):
+        was = vs[0, 0, at].clone()
+        vs[0, 0, at] = x
+        _compare(c.call(), ref, keys, bad, none.T, f"a scale of {x}")
+        vs[0, 0, at] = was
+    last = none.copy()
+    last[:, -c.group:] = True
+    c.cache[2][-1, -1, -1] = math.nan
+    _compare(c.call(), ref, keys, last, last.T, "a scale of K that is none")
+
+
+@FMTS
+@ALL
+def test_nothing_behind_live_rows_is_seen(shape, fmt):
+    # lengths that end inside steps and blocks, of zero and one; codes and scales of anything
+    # behind them
+    c = Case(shape, fmt, 420, G=7)
+    c.quantize()
+    for most in (c.S - 5, c.S // 2 + 17, 33, 1, 0):
+        rows = np.minimum(c.S - 5, most + 100 * np.arange(c.n))
+        ref, keys = c.reference(rows)
+        was = [x.clone() for x in c.cache]
+        for i, live in enumerate(rows):
+            for x, s in ((c.cache[0], c.cache[2]), (c.cache[1], c.cache[3])):
+                x.view(torch.uint8)[i, :, live:] = 0x7f
+                s[i, :, -(-live // c.block):] = math.nan
+        check(*c.call(rows), ref, keys, f"{most} rows")
+        c.cache = was
+
+
+@FMTS
+@ALL
+def test_unseen_generation_rows_that_are_not_finite(shape, fmt):
+    # drafts that hold NaN and infinities reach only those that see them, by a mask and by
+    # order; G ends inside a step of 16 or 32 rows
+    c = Case(shape, fmt, 430, G=21)
+    c.quantize()
+    Tq = c.Tq
+    sees = np.tri(Tq, dtype=bool)
+    odd = {1: math.nan, Tq // 2 + 1: -math.inf, Tq - 1: math.inf}
+    for row in odd:
+        sees[row + 1:, row] = False
+    clean = c.kg.clone(), c.vg.clone()
+    for row, x in odd.items():
+        c.kg[c.G + row, :, ::5] = x
+        c.vg[c.G + row] = x
+    for see, mask in ((sees, dev_mask(sees)), (np.tri(Tq, dtype=bool), None)):
+        bad = np.repeat(see[:, list(odd)].any(axis=1)[:, None], c.Hq, axis=1)
+        assert bad.any() and not bad.all()
+        ref, keys = c.reference(None, see, kg=clean[0], vg=clean[1])
+        _compare(c.call(None, mask), ref, keys, bad, bad.T, f"mask {mask is not None}")
+
+
+@FMTS
+@ALL
+def test_queries_that_are_not_finite_in_every_tile(shape, fmt):
+    c = Case(shape, fmt, 440)
+    c.quantize()
+    bad = np.zeros((c.Tq, c.Hq), dtype=bool)
+    ref, keys = c.reference()
+    for t, h, ch, x in ((0, c.Hq - 1, 5, math.nan), (c.Tq - 1, 0, c.d - 1, math.inf),
+                        (c.Tq // 2, c.Hq // 2, 0, -math.inf)):
+        c.q[t, h, ch] = x
+        bad[t, h] = True
+    _compare(c.call(), ref, keys, bad, bad.T, "queries")
+
+
+@ALL
+@pytest.mark.parametrize("rise", [0.4, 5.6, 8.3, 40.0, 95.0, -5.6, -40.0])
+def test_scores_that_rise_in_every_tile(shape, rise):
+    # The score of a wave's next step (256 rows on, in all shapes) is `rise` nats above the one
+    # before, for the first token twice as steeply
+    c = Case(shape, "int8", 450)
+    c.q *= 0.01
+    c.k *= 0.01
+    c.q[..., 0] = math.copysign(0.5, rise)
+    c.q[0, :, 0] = math.copysign(1.0, rise)
+    some = torch.rand((1, c.S, 1), generator=torch.Generator("cuda").manual_seed(451),
+                      device="cuda") < 0.3
+    c.k[..., 0] = torch.where(some, torch.arange(c.S, device="cuda")[None, :, None] // 256, 0)
+    c.scale = abs(rise)
+    c.quantize()
+    check(*c.call(), *c.reference(), f"rising by {rise}")
