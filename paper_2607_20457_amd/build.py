@@ -32,8 +32,7 @@ FLAGS = [
 # registers, from which each score is copied back.  (An option of this compiler
 # alone: with one that does not know it the source is compiled without, 4 % slower
 # on average over 140 calls and 12 % at most.)
-SOURCE_FLAGS = {"packed.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-                "quant_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+SOURCE_FLAGS = {"packed.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def sources():
