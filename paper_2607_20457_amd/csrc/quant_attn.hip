@@ -487,6 +487,8 @@ void quant_attn_kernel(QuantAttnArgs a) {
   }
 
   // ---- Q fragments (B operand): column 16 c + r, channels D/4 * g + 8 s .. ----
+  // (columns past the tile's are its first one again: loads without a branch around each, where
+  // the compiler waits for all before; 1 token over 4 x 1021 keys 0.3 us)
   int t[CG];
   bf16x8 qf[CG][DS];
   {
@@ -500,7 +502,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
       const bf16x8* src =
           reinterpret_cast<const bf16x8*>(a.q + ((int64_t)t[c] * a.Hq + head) * D) + DS * g;
 #pragma unroll
-      for (int s = 0; s < DS; ++s) qf[c][s] = live ? src[s] : bf16x8{};
+      for (int s = 0; s < DS; ++s) qf[c][s] = src[s];
     }
   }
   fill_use(first);
