@@ -15,25 +15,29 @@
 //       transposed in 8 bits and widened;
 //   softmax  online, log2 domain.  A step's weights are formed against the reference as it
 //       is; only where their sums show a score more than 2^8 above it is the step's maximum
-//       looked for, the reference raised and the step weighed again (a maximum in every step:
-//       64 tokens over 16 x 8192 keys 203 us against 195, int8 259 / 245).  A score is (q . code) * (scale * ks log2 e), one product of
-//       the block; the weight that enters PV is exp2(score - reference + log2 vs): V's
-//       scale is in it before it is rounded to bf16 (2^-8 of each at most), and sums of
-//       weights are taken times 1 / vs.  (A scale below 2^-32 is multiplied to the rounded
-//       weights after their sums: exactly, if it is a power of two.)  O is divided by the sum
-//       of the rounded weights, the log-sum-exp uses the fp32 sum.
+//       looked for, the reference raised and the step weighed again (a maximum in every step
+//       made 64 tokens over 16 x 8192 keys 4 % slower, in int8 6 %).  A score is
+//       (q . code) * (scale * ks log2 e), one product of the block; the weight that enters PV
+//       is exp2(score - reference + log2 vs): V's scale is in it before it is rounded to bf16
+//       (2^-8 of each at most), and sums of weights are taken times 1 / vs.  (A scale below
+//       2^-32 is multiplied to the rounded weights after their sums: exactly, if it is a power
+//       of two.)  O is divided by the sum of the rounded weights, the log-sum-exp uses the fp32
+//       sum.
 // The next step's K is sent for once the scores have consumed this one's, its V once PV
 // has.
 //
 // What bounds it.  One token: HBM.  16 x 8192 keys of 8 heads of 128 (268 MB of codes) take
-// 41 to 44 us and the merge 4: 6.3 TB/s, where a read alone reaches 6.5.  Many tokens: vector
-// instructions.  64 tokens over the same keys take 188 us with the merge (0.73 PFLOP/s).  A
-// step of 64 keys and 32 columns has 64 matrix instructions, and beside them 128 that widen
-// codes and seven or eight for each of a lane's 32 scores; int8 codes take three to widen a
-// pair, not one (229 us).  Tried there and no faster: three waves to a SIMD (188), key and
-// value stages shared by two or four waves, 64 columns a wave with one wave to a SIMD (265 us
-// when this took 201).  e4m3 codes in the matrix unit as they are, q in two e4m3 parts, leave
-// the scores less than fp32's precision: a log-sum-exp was 5e-3 off.
+// 41 to 44 us and the merge 4: 6.3 TB/s, where a read alone reaches 6.5.  Many tokens: the
+// issue of instructions, one kind after another.  64 tokens over the same keys take 180 to 188
+// us with the merge (0.73 to 0.76 PFLOP/s).  A step of 64 keys and 32 columns has 64 matrix
+// instructions, and beside them 128 that widen codes and five for each of a lane's 32 scores, one
+// of them an exponential of four times the others' length.  Counted over the call, of a SIMD's
+// cycles matrix instructions take 31 %, vector ones 47 % and scalar ones 13 %: the two waves of a
+// SIMD hardly overlap them.  int8 codes take three instructions to widen a pair, not one: vector
+// ones take 60 % of the cycles and matrix ones 24 (236 us).  Tried there and no faster: three
+// waves to a SIMD, key and value stages shared by two or four waves, 64 columns a wave with one
+// wave to a SIMD (a third slower).  e4m3 codes in the matrix unit as they are, q in two e4m3
+// parts, leave the scores less than fp32's precision: a log-sum-exp was 5e-3 off.
 //
 // What must not be seen.  Rows from a shard's live length on are not loaded (a copy of
 // the step's last live row is) and score -inf; their scales are not read.  Of the new
@@ -384,8 +388,9 @@ void quant_attn_kernel(QuantAttnArgs a) {
   // K: channels D/4 * g .. of row r of a half; V^T: keys 16 h + 4 g + v (slot 4 h + v) of a
   // 32-row tile, at head_dim 16 e + r.  A transposing read of 8 bits hands lane i of 16, for
   // slot j, byte i % 8 of the eight that lane 2 j + i / 8 addressed.
-  // (Their addresses are computed anew from `at`, a lane's number that the compiler does not
-  // know to be the same in each step: kept, they do not fit the registers.)
+  // (In the generation shard's steps their addresses are computed anew from `at`, a lane's number
+  // that the compiler does not know to be the same in each step: kept beside those of the steps of
+  // codes, they do not fit the registers.)
   auto fresh_lane = [&]() {
     int l = lane;
     asm volatile("" : "+v"(l));
@@ -557,7 +562,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
     const bool small = (small_v >> at & ((1u << HALVES) - 1)) != 0;
     need_k();
     // (a wave at its matrix products goes before one at its weights: 64 tokens over 16 x 8192
-    // keys 196 -> 188 us, int8 246 -> 229)
+    // keys 4 % faster, in int8 7 %)
     __builtin_amdgcn_s_setprio(1);
     f32x4 S[CG][HALVES];
 #pragma unroll
@@ -825,32 +830,37 @@ constexpr int QA_ONE_EACH = 256, QA_AT_ONCE = 512;
 
 // Four shapes of tiles.  Each code is widened and read once for all columns of a tile, so wide
 // tiles do less, but narrow ones wait less: 16 columns have four waves to a SIMD, the others
-// two (of d 128).
+// two (of d 128).  Us in replayed graphs, with the merge and 100 rows of the generation shard;
+// 32 / 8 heads of 128 in e4m3 where nothing else is said.
 //   16 columns, steps of 32 rows, eight waves: up to 13 steps of a wave with all compute units
-//   at work (12 where the others are of 32 columns and d is 128).  Us with the merge, 16 columns
-//   / the best of the others, 32 / 8 heads of 128: 8 tokens over 40960 keys 21.6 / 24.2, 49152
-//   26.5 / 26.4, 57344 30.2 / 28.8; 12 tokens over 32768 23.0 / 25.1, 49152 33.5 / 30.8; 24 over
-//   16384 23.4 / 22.2; 16 / 16 of 64, 24 tokens over 16384 16.0 / 15.7, 32768 21.2 / 20.3.
-//   48 columns, as above (d 128), where that
-//   is a third fewer tiles than of 32: 12 tokens over 131072 keys 55 / 65, 24 tokens 82 / 90, 36
-//   116 / 136; but 64 (6 tiles against 8) 211 / 196.
-//   32 columns, as above (d 128): one tile, bound by its keys (8 tokens over 131072 50 against
-//   54 of the next shape), or up to 28 steps of a wave: 64 tokens over 16384 keys 36.6 / 38.6,
-//   32768 59.4 / 60.5, 49152 85.5 / 83.7, 131072 204 / 196.
+//   at work (12 where the others are of 32 columns and d is 128).  16 columns / 32 in steps of 32
+//   rows: 8 tokens over 32768 keys 21.0 / 23.1, 40960 24.8 / 25.2, 49152 27.9 / 27.5, 65536 33.8
+//   / 32.1; of d 64, 16 / 16 heads, 24 tokens over 8192 13.2 / 14.0, 16384 16.6 / 16.5, 32768
+//   21.5 / 21.6.  16 columns / 48: 12 tokens over 32768 25.4 / 27.3, 49152 34.6 / 31.5, 24 tokens
+//   over 8192 18.3 / 22.7, 16384 25.0 / 25.0 (32 columns 22.7), 24576 31.1 / 28.3.
+//   48 columns, as above (d 128), where that is a third fewer tiles than of 32.  48 / the best of
+//   32: 12 tokens over 49152 keys 31.5 / 31.5, 131072 55 / 62, 24 tokens 72 / 84, 36 tokens 105 /
+//   128; but 64 (6 tiles against 8) 188 / 180.
+//   32 columns, as above (d 128): one tile, bound by its keys (8 tokens over 131072 51 against
+//   57 of the next shape), or up to 28 steps of a wave.  Steps of 32 / of 64 rows, 64 tokens over
+//   8192 keys 26.6 / 29.0, 16384 36.1 / 36.7, 24576 46.4 / 46.4, 32768 57.6 / 57.7, 49152 79.9 /
+//   78.4, 131072 189 / 180.  (int8, which the rule does not ask for: 16384 41.5 / 43.9, 32768
+//   68.9 / 72.0, 131072 234 / 236.)
 //   32 columns, steps of 64 rows, four waves: the rest of d 128.  Of d 64, whose 32 columns
-//   leave room for four waves to a SIMD: steps of 32 rows and eight waves (32 / 8 heads of 64,
-//   64 tokens over 131072 keys 126 us against 135, int8 148 / 157; over 16384 28.1 / 28.3).
-// Parts: as many as give each compute unit one workgroup; two for the last two shapes, but for
-// one tile of d 64 (16 / 16 heads, 24 tokens over 131072 keys 48.8 one / 51.3 two; two tiles, 64
-// tokens over 65536, 48.4 / 44.5), and for 16 columns where waves would have ten steps or more
-// and tiles share their keys (32 / 8 heads of 128, 12 tokens over 32768 keys 23.8 one / 22.9 two;
-// 1 token over 131072 45.2 / 45.8, 16384 12.7 / 14.0; 16 / 16 of 64, 1 token over 131072 44.7 /
-// 47.0, 4 x 1021 9.4 / 10.2).
+//   leave room for four waves to a SIMD: steps of 32 rows and eight waves (64 rows, when they were
+//   built for d 64, took 64 tokens of 32 / 8 heads over 131072 keys 7 % longer, in int8 6 %).
+// Parts: as many as give each compute unit one workgroup.  Two for the last two shapes, but for
+// one tile of d 64 (one / two: 16 / 16 heads, 24 tokens over 131072 keys 50.1 / 52.3; of two tiles,
+// 64 tokens over 16384 20.7 / 21.6, 65536 48.5 / 43.2, and 32 / 8 heads, 64 tokens over 16384 29.8
+// / 28.8, 131072 160 / 130).  Two too for 16 columns where waves would have ten steps or more and
+// tiles share their keys (12 tokens over 16384 17.4 / 18.6, 32768 25.4 / 24.2; 1 token over 16384
+// 13.1 / 14.2, 131072 47.9 / 48.3; 16 / 16 of 64, 1 token over 4084 9.8 / 10.3, 131072 48.8 /
+// 49.2).
 // But one part up to five steps of a wave: parts need the merge's launch and a workspace, 4 us
-// of the host's time.  Device / call from the host, several parts and one, 32 / 8 heads of 128,
-// 1 token over 480 keys 8.7 / 15.9 and 7.9 / 11.7, 1000 9.0 / 15.9 and 9.9 / 11.6, 1500 9.4 / 15.8
-// and 13.5 / 13.6 (1.8 us a step of a wave); 16 / 16 of 64, 24
-// tokens over 1000 keys 8.7 / 15.8 and 8.6 / 11.4.
+// of the host's time, for which calls from the host wait and replayed ones do not.  A replayed
+// graph / calls from the host, several parts and one: 1 token over 480 keys 9.1 / 15.4 and 9.5 /
+// 11.3, 1000 9.6 / 15.5 and 11.9 / 11.8, 1500 9.8 / 15.4 and 14.1 / 14.0; 16 / 16 of 64, 24 tokens
+// over 1000 keys 8.9 / 15.4 and 9.9 / 11.3.
 QuantPlan quant_plan(int n_shards, int Tq, int64_t S, int Hq, int Hkv, int d, int64_t gen_rows) {
   QuantPlan p{};
   const int group = Hq / Hkv;
