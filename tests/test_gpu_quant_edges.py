@@ -255,3 +255,27 @@ def test_scores_that_rise_in_every_tile(shape, rise):
     c.scale = abs(rise)
     c.quantize()
     check(*c.call(), *c.reference(), f"rising by {rise}")
+
+
+@FMTS
+def test_the_last_shard_of_a_cache_grows(fmt):
+    # retained shards and one that takes the generation shard's closed blocks, in one cache
+    Hq, Hkv, d, n, S, block = 8, 2, 128, 4, 100, 16
+    gen = torch.Generator(device="cuda").manual_seed(460)
+    k, v, more_k, more_v = (_normal(gen, (m, S, Hkv, d)) for m in (n, n, 1, 1))
+    cache = P.kv_quantize(*(torch.cat([x, torch.zeros_like(x[:1])]) for x in (k, v)), block,
+                          DTYPES[fmt])
+    last = [x[-1:] for x in cache]
+    rows = dev_i32([S] * n + [0])
+    q = _normal(gen, (1, Hq, d))
+    for step in range(0, 2 * block + 3):
+        moved = step // block * block
+        if step == moved > 0:
+            new = slice(moved - block, moved)
+            P.kv_quantize_(more_k[:, new], more_v[:, new], *last, block, moved - block)
+            rows[-1] = moved
+        kg, vg = more_k[0, moved:step + 1], more_v[0, moved:step + 1]
+        o, lse = P.phase2_quant(q, *cache, block, rows, kg, vg, step - moved)
+        check(o, lse, *long_reference(_bits(q), cache, block, [S] * n + [moved], _bits(kg),
+                                      _bits(vg), step - moved, None, softmax_scale(d)),
+              f"step {step}")
