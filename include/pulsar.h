@@ -603,7 +603,9 @@ int pulsar_phase2_sparse(const void* q, const void* K, const void* V, const int3
  * of e4m3 at most 240, at e = 122 of int8 at most 63 in magnitude, so that code * 2^e is
  * finite.  A block with a NaN or an infinity gets the scale NaN and codes 0: all of it
  * reads back as NaN.  Only the rows given count towards a scale; other rows and blocks of
- * the cache stay as they are.
+ * the cache stay as they are.  first is an argument on the host, for all shards: a captured
+ * write goes to the same rows in each replay, and shards that are filled to different rows
+ * take a call each.
  *
  * pulsar_kv_dequantize writes rows [first, first + rows), from any row on, as bf16: code *
  * scale in fp32, rounded once (not at all for scales that pulsar_kv_quantize wrote).
@@ -636,7 +638,8 @@ int pulsar_kv_dequantize(const void* k_codes, const void* v_codes, const float* 
  * The generation shard stays bf16; its closed blocks may be moved into the cache.  Scores
  * and sums are fp32, with the codes and q multiplied exactly; the weights, times the scale
  * of their block of V, enter the product with V's codes rounded to bf16 (by 2^-8 of each at
- * most, divided by the sum of the rounded ones).
+ * most, divided by the sum of the rounded ones).  An average of values near the largest numbers
+ * is finite as they are (of scores below 2^29).
  *
  * q         bf16 [Tq, Hq, d].
  * codes, scales  as for pulsar_kv_quantize, with n = n_shards and capacity = S (nullable
@@ -644,7 +647,7 @@ int pulsar_kv_dequantize(const void* k_codes, const void* v_codes, const float* 
  *           does not write) makes its block NaN; one below 2^-100 counts as 2^-100.
  * rows      int32 [n_shards] on the device, nullable: shard i's live rows are [0, rows[i])
  *           (clamped to [0, S]; NULL: S).  Nothing behind them is read, so a cache may grow
- *           between two replays of a captured call.
+ *           between two replays of a captured call (its writes are calls of their own).
  * Kg, Vg, G, mask, o, o_dtype, lse  as for pulsar_phase2_sparse (Kg and Vg both NULL where
  *           another host has the generation shard).  A token that sees no key gives 0, -inf;
  *           rows that a token does not see cannot reach its output.

@@ -32,12 +32,12 @@
 // us with the merge (0.73 to 0.76 PFLOP/s).  A step of 64 keys and 32 columns has 64 matrix
 // instructions, and beside them 128 that widen codes and five for each of a lane's 32 scores, one
 // of them an exponential of four times the others' length.  Counted over the call, of a SIMD's
-// cycles matrix instructions take 31 %, vector ones 47 % and scalar ones 13 %: the two waves of a
-// SIMD hardly overlap them.  int8 codes take three instructions to widen a pair, not one: vector
-// ones take 60 % of the cycles and matrix ones 24 (236 us).  Tried there and no faster: three
-// waves to a SIMD, key and value stages shared by two or four waves, 64 columns a wave with one
-// wave to a SIMD (a third slower).  e4m3 codes in the matrix unit as they are, q in two e4m3
-// parts, leave the scores less than fp32's precision: a log-sum-exp was 5e-3 off.
+// cycles matrix instructions take 31 %, vector ones 47 %, scalar ones 13 %; a vector one runs
+// beside 29 % of the matrix cycles only.  int8 codes take three instructions to widen a pair, not
+// one: vector ones take 58 % of the cycles and matrix ones 23 (236 us).  Tried there and no
+// faster: three waves to a SIMD, key and value stages shared by two or four waves, 64 columns a
+// wave with one wave to a SIMD (a third slower).  e4m3 codes in the matrix unit as they are, q in
+// two e4m3 parts, leave the scores less than fp32's precision: a log-sum-exp was 5e-3 off.
 //
 // What must not be seen.  Rows from a shard's live length on are not loaded (a copy of
 // the step's last live row is) and score -inf; their scales are not read.  Of the new
