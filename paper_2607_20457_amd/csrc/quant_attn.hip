@@ -55,12 +55,12 @@ constexpr float QA_SLACK = 8.0f;      // log2 slack before the reference is rais
 constexpr float QA_OVER = 4 * 0x1p8f; // a lane's four weights of 2^QA_SLACK
 constexpr float QA_LEAST = 0x1p-100f; // a smaller scale counts as this
 constexpr float QA_SMALL = 0x1p-32f;  // scales of V that weights get after their sums
-constexpr float QA_BIG = 0x1p64f;     // from here on scales of V have weights with QA_ROOM
+constexpr float QA_BIG = 0x1p64f;     // above it scales of V have weights with QA_ROOM
 constexpr float QA_MOST = 0x1p124f;   // larger ones make their block no number
 // Values near the largest number leave fp32 in a sum of theirs, though not in their average,
-// which O is.  Steps that may hold such values keep their weights at 2^-QA_ROOM or less, the
-// reference that far above the scores: 2^32 of them, more than a call has keys, sum to half a
-// value.  (Not so in all steps: a weight has 2^-126 to go down to, and log2 vs is in it.)
+// which O is.  Steps with such values keep their weights at 2^-QA_ROOM or less, the reference
+// that far above the scores: 2^32 of them, more than a call has keys, sum to half a value.
+// (Not so in all steps: products of small values would fall below 2^-126.)
 constexpr float QA_ROOM = 33.0f;
 
 struct QuantAttnArgs {
@@ -691,28 +691,40 @@ void quant_attn_kernel(QuantAttnArgs a) {
       }
       mx[c] = fmaxf(largest(S[c][0]), largest(S[c][1])) * c2;
     }
-    raise(mx, -QA_ROOM, QA_ROOM + QA_SLACK);  // (whatever the values are)
+    raise(mx, QA_SLACK, 0.f);
     bf16x8 P[CG];
-#pragma unroll
-    for (int c = 0; c < CG; ++c) {
+    float l[CG], lr[CG];
+    auto weigh_all = [&]() {
       const float one[2] = {1.f, 1.f}, zero[2] = {0.f, 0.f}, cc[2] = {c2, c2};
-      P[c] = weigh(c, S[c], cc, zero, one, l_run[c], lr_run[c]);
-    }
-    need_v(j + 1 < nsteps);
-    bool odd = false;  // a value that is not finite
-    if (some) {
-      uint32_t top = 0;
 #pragma unroll
-      for (int e = 0; e < DT; ++e) {
-        const u32x4 v = __builtin_bit_cast(u32x4, v_gen(la, e));
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          top |= (v[k] & 0x7f80u) == 0x7f80u;
-          top |= (v[k] & 0x7f800000u) == 0x7f800000u;
-        }
+      for (int c = 0; c < CG; ++c) {
+        l[c] = lr[c] = 0.f;
+        P[c] = weigh(c, S[c], cc, zero, one, l[c], lr[c]);
       }
-      odd = __any(top != 0);
+    };
+    weigh_all();
+    need_v(j + 1 < nsteps);
+    // A step whose squares sum to 2^120 or more has values of 2^57 and more, or ones that are not
+    // finite: its weights get room, and rows that only some columns see are taken one by one.
+    bf16x8 vt[DT];
+    float squares = 0.f;
+#pragma unroll
+    for (int e = 0; e < DT; ++e) {
+      vt[e] = v_gen(la, e);
+#pragma unroll
+      for (int k = 0; k < GEN / 4; k += 2) {
+        const bf16x2 x = {vt[e][k], vt[e][k + 1]};
+        squares = __builtin_amdgcn_fdot2_f32_bf16(x, x, squares, false);
+      }
     }
+    const bool huge = __any(!(squares < 0x1p120f));
+    if (huge) {
+      raise(mx, -QA_ROOM, QA_ROOM + QA_SLACK);
+      weigh_all();
+    }
+    const bool odd = some && huge;  // (of which some may not be finite)
+#pragma unroll
+    for (int c = 0; c < CG; ++c) l_run[c] += l[c], lr_run[c] += lr[c];
     // all keys at once, or key by key
     for (int k = 0; k < (odd ? GEN : 1); ++k) {
       u32x4 keep;
@@ -726,7 +738,7 @@ void quant_attn_kernel(QuantAttnArgs a) {
       for (int e = 0; e < DT; ++e) {
         if (CG > 1) __builtin_amdgcn_sched_barrier(0);
         const bf16x8 v =
-            __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, v_gen(la, e)) & keep);
+            __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, vt[e]) & keep);
 #pragma unroll
         for (int c = 0; c < CG; ++c) {
           const f32x4 x =

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 import paper_2607_20457_amd as P
+from tests import _blocks
 from tests._blocks import dev_i32, dev_mask, host
 from tests._plan import SHAPES, plan
 from tests._quant import DTYPES, check, long_reference, softmax_scale
@@ -279,3 +280,18 @@ def test_the_last_shard_of_a_cache_grows(fmt):
         check(o, lse, *long_reference(_bits(q), cache, block, [S] * n + [moved], _bits(kg),
                                       _bits(vg), step - moved, None, softmax_scale(d)),
               f"step {step}")
+
+
+@FMTS
+@ALL
+@pytest.mark.parametrize("size", [-60, -105])
+def test_values_that_are_all_tiny(shape, fmt, size):
+    # The codes' and the generation rows'.  Scores within 2^12 of each other leave weights of
+    # 2^-20 and more against any reference that trails by 2^8: products of 2^-125 and more, so
+    # that nothing but the weights' rounding is off (tests._blocks.check).
+    c = Case(shape, fmt, 470)
+    c.v *= 2.0 ** size
+    c.vg *= 2.0 ** size
+    c.quantize()
+    ref, keys = c.reference()
+    _blocks.check(*c.call(), ref, keys, "tiny values")
